@@ -197,7 +197,7 @@ def _own_ffn(s, train):
     if not train:
         return sds.gated_ffn(s["x"], s["wg"], s["wu"], s["wd"], act)
     y, kept = sds.gated_ffn(s["x"], s["wg"], s["wu"], s["wd"], act, keep=True)
-    dx, dwg, dwu, dwd = sds.gated_ffn_backward(s["dy"], s["x"], s["wg"], s["wu"], s["wd"], kept, act)
+    dx, dwg, dwu, dwd = sds.gated_ffn_backward(s["dy"], s["x"], s["wg"], s["wu"], s["wd"], kept)
     return y, dx, dwg, dwu, dwd
 
 
