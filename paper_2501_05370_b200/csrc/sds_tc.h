@@ -1,6 +1,7 @@
 // Tensor-core GEMM launcher and the helper kernels of the bf16 denoisers (sds_tc.cu).
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -49,6 +50,11 @@ struct TcGemmArgs {
   int nseg_short;
   uint8_t a_short[8], b_short[8];
 };
+
+// tensor map of a 16-bit matrix [rows, cols], rows ld elements apart: boxes of box_rows x 64 elements with the
+// 128-byte swizzle, zeros outside. base 16-byte aligned, ld a multiple of 8.
+bool make_tmap_2d(CUtensorMap* tm, const void* base, bool f16, uint64_t rows, uint64_t cols, uint64_t ld,
+                  uint32_t box_rows);
 
 bool tc_shape_ok(int N, int K);
 cudaError_t launch_gemm_tc(int epi, const TcGemmArgs& g, const void* A_bf16, const void* B_bf16, cudaStream_t st);
