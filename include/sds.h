@@ -59,6 +59,7 @@ extern "C" {
 
 #define SDS_F32           0
 #define SDS_BF16          1
+#define SDS_F16           2     /* layer operators only */
 
 #define SDS_FROZEN_PREV   0     /* drafter reuses the newest target output on the accepted path (no extra call;
                                    the fallback the "efficient frozen draft strategy" paragraph offers, used always) */
@@ -386,6 +387,71 @@ int sds_profile_read(sds_ctx* ctx, double* ms, int64_t* launches, int32_t reset)
 int sds_gmm_denoise_static(const float* x_dev, const int32_t* k_dev, int64_t rows, int32_t d, int32_t ncomp,
                            const float* means_dev, const float* logw_dev, const double* tcond_dev, int32_t K,
                            float* out_dev, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Layer operators: the parts of a gated denoiser, forward and backward, for programs that train one or run
+ * one outside a context. Like sds_gmm_denoise_static they need no context: device pointers and a stream in, work
+ * enqueued on cuda_stream (cudaStream_t, NULL = default stream) of the current device, no wait, no allocation.
+ * Outputs must not overlap inputs or workspaces. rows = 0 is allowed. Two calls that can run at the same time
+ * (other streams, or two captured graphs) need workspaces of their own. The calls can be captured into a graph.
+ *
+ * Layer norm over rows of d elements:
+ *   y = (x - mean) / sqrt(var + eps) * w + b,   var = sum (x - mean)^2 / d
+ * x_dev [rows, d] of x_dtype (SDS_F32, SDS_BF16, SDS_F16), rows ldx >= d elements apart. y_dev likewise of y_dtype:
+ * x_dtype, or for float x any of the three. w_dev, b_dev [d] of w_dtype (any of the three; NULL = ones, zeros). mean_dev,
+ * rstd_dev [rows] float: the row's mean and 1 / sqrt(var + eps), kept for the backward pass (NULL = not kept).
+ * eps >= 0 and finite. Sums are held in float, and the rounding of the mean is taken back out of the differences. */
+int sds_layer_norm(const void* x_dev, int64_t ldx, int32_t x_dtype, const void* w_dev, const void* b_dev,
+                   int32_t w_dtype, int64_t rows, int32_t d, float eps, void* y_dev, int64_t ldy, int32_t y_dtype,
+                   float* mean_dev, float* rstd_dev, void* cuda_stream);
+
+/* Its gradients, from dy_dev [rows, d] of y_dtype and the forward call's x, w, mean and rstd:
+ *   dx = rstd (w dy - <w dy> - xhat <w dy xhat>) of x_dtype,   dw = sum_rows dy xhat,   db = sum_rows dy of w_dtype
+ * (<.> the mean over a row, xhat = (x - mean) rstd). Any of dx_dev, dw_dev, db_dev may be NULL. Sums over rows are
+ * held in float and added in a fixed order: same bits on every run. workspace_dev: 256-byte aligned, at least
+ * sds_layer_norm_workspace_bytes. With rows = 0, dw and db are zeros. */
+int sds_layer_norm_workspace_bytes(int64_t rows, int32_t d, size_t* bytes);
+int sds_layer_norm_backward(const void* dy_dev, int64_t lddy, int32_t y_dtype, const void* x_dev, int64_t ldx,
+                            int32_t x_dtype, const void* w_dev, int32_t w_dtype, const float* mean_dev,
+                            const float* rstd_dev, int64_t rows, int32_t d, void* dx_dev, int64_t lddx, void* dw_dev,
+                            void* db_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* Gated feed-forward block:
+ *   y = (act(x Wg^T) * (x Wu^T)) Wd^T
+ * x_dev, y_dev [rows, d], rows ldx / ldy elements apart; wg_dev, wu_dev [f, d], wd_dev [d, f] dense; all of one
+ * dtype, SDS_BF16 or SDS_F16. d, f, ldx and ldy multiples of 8 and every pointer 16-byte aligned (else
+ * SDS_EUNSUPPORTED). Products are accumulated in float; the hidden rows h = act(x Wg^T) * (x Wu^T) are rounded to
+ * dtype, as operands of the second product. keep_dev: what the backward pass needs of the forward one, opaque, 256-byte
+ * aligned, keep_bytes of sds_gated_ffn_bytes (NULL = no backward pass will follow). workspace_dev: 256-byte
+ * aligned, forward_bytes (smaller with keep_dev: the hidden rows then live there).
+ * The result of a row may differ in the last bit with the number of rows of the call. */
+#define SDS_ACT_SILU      0     /* g / (1 + exp(-g)) */
+#define SDS_ACT_GELU      1     /* g Phi(g), Phi the normal distribution function */
+#define SDS_ACT_GELU_TANH 2     /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+typedef struct {
+  size_t keep_bytes;            /* keep_dev */
+  size_t forward_bytes;         /* workspace of sds_gated_ffn without keep_dev */
+  size_t forward_keep_bytes;    /* workspace of sds_gated_ffn with keep_dev */
+  size_t backward_bytes;        /* workspace of sds_gated_ffn_backward */
+} sds_gated_ffn_sizes;
+int sds_gated_ffn_bytes(int64_t rows, int32_t d, int32_t f, sds_gated_ffn_sizes* sizes);
+int sds_gated_ffn(const void* x_dev, int64_t ldx, int32_t dtype, int64_t rows, int32_t d, int32_t f,
+                  const void* wg_dev, const void* wu_dev, const void* wd_dev, int32_t act, void* y_dev, int64_t ldy,
+                  void* keep_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* Its gradients, from dy_dev [rows, d] (rows lddy elements apart) and the forward call's x, weights and keep_dev,
+ * all of dtype: dx_dev [rows, d] (rows lddx apart), dwg_dev, dwu_dev [f, d], dwd_dev [d, f] dense; any may be NULL.
+ * With rows = 0 the weights' gradients are zeros. The gradients of the two pre-activations are rounded to dtype,
+ * as operands of the products that follow. */
+int sds_gated_ffn_backward(const void* dy_dev, int64_t lddy, const void* x_dev, int64_t ldx, int32_t dtype,
+                           int64_t rows, int32_t d, int32_t f, const void* wg_dev, const void* wu_dev,
+                           const void* wd_dev, const void* keep_dev, void* dx_dev, int64_t lddx, void* dwg_dev,
+                           void* dwu_dev, void* dwd_dev, void* workspace_dev, size_t workspace_bytes,
+                           void* cuda_stream);
+
+/* The feed-forward kernels' waits are bounded. Waits for cuda_stream and returns SDS_ETIMEOUT if a wait of the last
+ * call that used workspace_dev gave up (its outputs are then invalid), else SDS_OK. */
+int sds_gated_ffn_status(const void* workspace_dev, void* cuda_stream);
 
 const char* sds_strerror(int code);
 int sds_last_cuda_error(const sds_ctx* ctx);

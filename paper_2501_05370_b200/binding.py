@@ -19,7 +19,8 @@ SDS_OK = 0
 SDS_EINVAL, SDS_ESTATE, SDS_ENOMEM, SDS_EUNSUPPORTED = -1, -2, -3, -4
 SDS_ECUDA, SDS_ETIMEOUT, SDS_ENONFINITE, SDS_ECALLBACK = -5, -6, -7, -8
 SDS_DEN_GMM, SDS_DEN_MLP, SDS_DEN_CALLBACK, SDS_DEN_PHI4 = 1, 2, 3, 4
-SDS_F32, SDS_BF16 = 0, 1
+SDS_F32, SDS_BF16, SDS_F16 = 0, 1, 2
+SDS_ACT_SILU, SDS_ACT_GELU, SDS_ACT_GELU_TANH = 0, 1, 2
 SDS_FROZEN_PREV, SDS_FROZEN_EXACT, SDS_INDEPENDENT, SDS_PICARD = 0, 1, 2, 3
 (GET_X, GET_TAIL, GET_DQ, GET_DC, GET_Y, GET_N, GET_ACT, GET_ROWOFF, GET_S1, GET_S2, GET_ELL, GET_LOGU,
  GET_ACCMASK, GET_JSTAR, GET_NFE_CALLS, GET_NFE_ROWS, GET_CTL, GET_ROWK, GET_DP) = range(1, 20)
@@ -37,6 +38,11 @@ class SdsDenoiser(C.Structure):
                 ("means_dtype", C.c_int32), ("nlayer", C.c_int32), ("W_dev", C.c_void_p), ("bias_dev", C.c_void_p),
                 ("temb_dev", C.c_void_p), ("dims", C.c_void_p), ("fn", DENOISE_FN), ("user", C.c_void_p),
                 ("grid_side", C.c_int32), ("coupling", C.c_float), ("periodic", C.c_int32)]
+
+
+class SdsGatedFfnSizes(C.Structure):
+    _fields_ = [("keep_bytes", C.c_size_t), ("forward_bytes", C.c_size_t), ("forward_keep_bytes", C.c_size_t),
+                ("backward_bytes", C.c_size_t)]
 
 
 EXPORTS = {
@@ -71,6 +77,20 @@ EXPORTS = {
     "sds_profile_read": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]),
     "sds_gmm_denoise_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "sds_layer_norm": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32,
+                                 C.c_float, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sds_layer_norm_workspace_bytes": (C.c_int, [C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]),
+    "sds_layer_norm_backward": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                                          C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "sds_gated_ffn_bytes": (C.c_int, [C.c_int64, C.c_int32, C.c_int32, C.POINTER(SdsGatedFfnSizes)]),
+    "sds_gated_ffn": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t,
+                                C.c_void_p]),
+    "sds_gated_ffn_backward": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int32,
+                                         C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "sds_gated_ffn_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "sds_strerror": (C.c_char_p, [C.c_int]),
     "sds_last_cuda_error": (C.c_int, [C.c_void_p]),
     "sds_destroy": (None, [C.c_void_p]),

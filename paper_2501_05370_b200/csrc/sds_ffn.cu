@@ -1,0 +1,949 @@
+// Gated feed-forward block, forward and backward, on the tensor cores.
+//
+//   forward   G = x Wg^T, U = x Wu^T, h = act(G) * U, y = h Wd^T
+//   backward  dH = dy Wd, dG = dH * U act'(G), dU = dH * act(G)
+//             dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x, dWd = dy^T h
+//
+// Both projections, the activation and the product are one kernel: a tile holds the same columns of G and of U in
+// one accumulator, and its epilogue writes h only. For the backward pass it also keeps the two factors
+// U act'(G) and act(G) as floats (16 bits there would add an error to every gradient as large as its own rounding,
+// and the activation would have to be evaluated again); they lie in the order in which the epilogue's threads
+// hold them, so that every access is 512 contiguous bytes of a warp. h and dG, dU are rounded to the operand type:
+// they are operands of the products that follow.
+//
+// Two forms of the products:
+//   - k_ffn_tile: persistent CTA pairs on 256 x 256 tiles (single CTAs on 128 x 128 tiles where there are few), for
+//     batches. Operands arrive by TMA in either order (K contiguous, or M / N contiguous for the transposed
+//     operands of the gradients: the matrix descriptors and the instruction descriptor say which, nothing is
+//     transposed in memory). Two accumulators: the epilogue of a tile runs under the next tile's products.
+//   - k_ffn_split: few rows. The time is that of reading the weights once, so the weights are the 128 rows of the
+//     instruction and the tokens its 16 to 128 columns; K is split over a cluster of CTAs so that all SMs
+//     read, and the partial sums are added through distributed shared memory in the order of K.
+// Sums are held in 32 bits (tensor memory) throughout.
+#include <atomic>
+#include <algorithm>
+
+#include <cuda_fp16.h>
+
+#include "../../include/sds.h"
+#include "sds_device.cuh"
+#include "sds_layers.h"
+#include "sds_tc.h"
+#include "sds_umma.cuh"
+
+namespace sds {
+
+namespace {
+
+enum FfnEpi : int {
+  kFfnGlu = 0,     // accumulator holds G | U: h and the kept factors
+  kFfnOut = 1,     // out (16 bit) = acc
+  kFfnAdd = 2,     // out (float) += acc
+  kFfnDGlu = 3,    // accumulator holds dH: dG, dU
+};
+
+constexpr int kBM = 128;                          // rows of one CTA's accumulator
+constexpr int kBK = 64;                           // elements of K per stage: one 128-byte swizzle row
+constexpr int kChunkBytes = 64 * kBK * 2;         // 64 x 64 elements
+constexpr int kEpiWarps = 16;
+constexpr int kTileThreads = 64 + 32 * kEpiWarps; // warp 0: TMA, warp 1: MMA and tensor memory, then the epilogue
+constexpr int kWarpStage = 2048;                  // staging bytes of an epilogue warp: 32 rows of 64 bytes
+
+// one product C[M, N] = sum over segments A_s B_s, with every operand K-major ([M or N, K]) or MN-major ([K, M or N])
+struct FfnProduct {
+  CUtensorMap a[2], b[2];                         // kFfnGlu: b[0] = Wg, b[1] = Wu, one segment
+  int M, N, K;                                    // K of one segment
+  int nseg, a_mn, b_mn;
+  void* out;
+  int64_t ldo;
+};
+
+constexpr int kMaxProducts = 4;
+struct FfnTileArgs {
+  FfnProduct p[kMaxProducts];
+  int np;
+  int f16, act;
+  const int* nrows_dev;                           // row count of p[0] on the device (NULL: p[0].M)
+  float* keep;
+  void* out2;                                     // kFfnDGlu: dU (out is dG)
+  int* err;
+};
+
+// ---------------------------------------------------------------------------------------------
+// the epilogues' arithmetic
+// ---------------------------------------------------------------------------------------------
+
+// a = act(g), da = act'(g). The fast exponential and division are accurate to a few units of the 24-bit
+// significand, far inside the 16-bit operands' rounding.
+__device__ __forceinline__ void activation(int act, float g, float& a, float& da) {
+  if (act == SDS_ACT_SILU) {
+    const float p = __fdividef(1.0f, 1.0f + __expf(-g));
+    a = g * p;
+    da = p * fmaf(g, 1.0f - p, 1.0f);
+  } else if (act == SDS_ACT_GELU) {
+    const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+    a = g * p;
+    da = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
+  } else {
+    const float k2 = 1.5957691216057308f, c = 0.044715f;      // 2 sqrt(2 / pi)
+    const float g2 = g * g;
+    const float p = __fdividef(1.0f, 1.0f + __expf(-k2 * g * fmaf(c, g2, 1.0f)));
+    const float t = p * (1.0f - p);
+    a = g * p;
+    da = t > 0.f ? fmaf(g * t * k2, fmaf(3.0f * c, g2, 1.0f), p) : p;   // (t = 0 where g^2 might overflow)
+  }
+}
+
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, int f16) {
+  if (f16) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  return pack_bf16x2(lo, hi);
+}
+
+// the kept factors of 32 x 32 blocks of (row, column of f): [row block][column block][factor][column quad][row] quads
+__device__ __forceinline__ size_t keep_index(int row, int col, int ncc, int which) {
+  return ((((size_t)(row >> 5) * ncc + (col >> 5)) * 2 + which) * 8 + ((col & 31) >> 2)) * 128 + (size_t)(row & 31) * 4;
+}
+
+// 32 rows of 64 bytes, one per lane as 16 words, to global memory: turned through shared memory so that four lanes
+// write the 64 bytes of a row. Piece p of row r lies at p ^ (r / 2 % 4): 128-bit accesses free of bank conflicts both ways.
+__device__ __forceinline__ void store_rows64(uint4* stg, const uint32_t (&w)[16], char* out, size_t ld_bytes, int nrows,
+                                             int npieces, int lane) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p)
+    stg[lane * 4 + (p ^ ((lane >> 1) & 3))] = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+  __syncwarp();
+  const int pc = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 8 * i + (lane >> 2);
+    const uint4 v = stg[r * 4 + (pc ^ ((r >> 1) & 3))];
+    if (r < nrows && pc < npieces) *reinterpret_cast<uint4*>(out + (size_t)r * ld_bytes + pc * 16) = v;
+  }
+  __syncwarp();
+}
+
+// the same for an accumulation in place: out (float) += the 16 floats of every row
+__device__ __forceinline__ void add_rows64(uint4* stg, const uint32_t* w, float* out, size_t ld, int nrows, int npieces,
+                                           int lane) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p)
+    stg[lane * 4 + (p ^ ((lane >> 1) & 3))] = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+  __syncwarp();
+  const int pc = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 8 * i + (lane >> 2);
+    const uint4 v = stg[r * 4 + (pc ^ ((r >> 1) & 3))];
+    if (r < nrows && pc < npieces) {
+      float4* o = reinterpret_cast<float4*>(out + (size_t)r * ld + pc * 4);
+      float4 c = *o;
+      c.x += __uint_as_float(v.x); c.y += __uint_as_float(v.y); c.z += __uint_as_float(v.z); c.w += __uint_as_float(v.w);
+      *o = c;
+    }
+  }
+  __syncwarp();
+}
+
+// ---------------------------------------------------------------------------------------------
+// batches: persistent tiles
+// ---------------------------------------------------------------------------------------------
+
+template <int BN, bool PAIR> struct FfnTile {
+  static constexpr int kTM = PAIR ? 2 * kBM : kBM;                 // rows of a tile
+  static constexpr int kBRows = PAIR ? BN / 2 : BN;                // rows of B that one CTA stages
+  static constexpr int kABytes = kBM * kBK * 2;
+  static constexpr int kBBytes = kBRows * kBK * 2;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kFixedBytes = 1024 /*align*/ + 256 /*barriers*/ + kEpiWarps * kWarpStage;
+  static constexpr int kStages = (227 * 1024 - kFixedBytes) / kStageBytes;
+  static constexpr int kSmemBytes = kStages * kStageBytes + kFixedBytes;
+  static constexpr int kTmemCols = 2 * BN;
+  static_assert(kStages >= 3 && kStages <= 12 && kTmemCols <= 512, "stages and tensor memory");
+};
+
+struct TileAt {
+  int prod, m, n;                                 // product, tile row, tile column
+};
+
+// Tiles of all products in one sequence. Within a product, bands of eight tile rows are walked column by column:
+// the tiles that run at the same time then share few rows of A and of B, which stay in L2.
+template <int TM, int TN>
+__device__ __forceinline__ bool tile_at(const FfnTileArgs& g, int m0_rows, int t, TileAt* at) {
+  for (int p = 0; p < g.np; ++p) {
+    const int M = p == 0 ? m0_rows : g.p[p].M;
+    const int mt = (M + TM - 1) / TM, nt = (g.p[p].N + TN - 1) / TN;
+    const int n = mt * nt;
+    if (t < n) {
+      const int band = t / (8 * nt), in = t - band * 8 * nt;
+      const int rows = min(8, mt - band * 8);
+      at->prod = p;
+      at->m = band * 8 + in % rows;
+      at->n = in / rows;
+      return true;
+    }
+    t -= n;
+  }
+  return false;
+}
+
+template <int BN, int EPI, bool PAIR>
+__global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
+  using C = FfnTile<BN, PAIR>;
+  constexpr int TM = C::kTM, TN = EPI == kFfnGlu ? BN / 2 : BN;    // output columns of a tile
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(stages + C::kStages * C::kStageBytes);
+  uint64_t* empty_bar = full_bar + C::kStages;
+  uint64_t* tfull_bar = empty_bar + C::kStages;
+  uint64_t* tempty_bar = tfull_bar + 2;
+  uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(tempty_bar + 2);
+  volatile int* abort_s = reinterpret_cast<volatile int*>(tmem_base_s + 1);
+  uint8_t* epi_stage = reinterpret_cast<uint8_t*>(full_bar) + 256;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+  const int worker = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+  const int nworkers = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  const int M0 = g.nrows_dev ? min(*g.nrows_dev, g.p[0].M) : g.p[0].M;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar + s, 1); mbar_init(empty_bar + s, 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(tfull_bar + s, 1); mbar_init(tempty_bar + s, PAIR ? 2 * kEpiWarps : kEpiWarps); }
+    *abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_base_s)),
+                   "r"((uint32_t)C::kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_base_s)),
+                   "r"((uint32_t)C::kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_base_s;
+
+  TileAt at;
+  if (warp == 0) {
+    // ---------------- TMA producer ----------------
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const uint32_t leader_full0 = PAIR ? map_to_cta(smem_u32(full_bar), 0u) : 0u;
+      for (int t = worker; ok && tile_at<TM, TN>(g, M0, t, &at); t += nworkers) {
+        const FfnProduct& p = g.p[at.prod];
+        const int m0 = at.m * TM + (int)rank * kBM;
+        const int n0 = at.n * TN + (EPI == kFfnGlu ? 0 : (int)rank * C::kBRows);
+        const int kb_seg = (p.K + kBK - 1) / kBK, nkb = kb_seg * p.nseg;
+        for (int kb = 0; kb < nkb; ++kb) {
+          if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
+          uint8_t* sa = stages + stage * C::kStageBytes;
+          uint8_t* sb = sa + C::kABytes;
+          const int seg = kb / kb_seg, kk = (kb - seg * kb_seg) * kBK;
+          const uint32_t fb = PAIR ? leader_full0 + (uint32_t)stage * 8u : 0u;
+          if (PAIR) {
+            if (rank == 0) mbar_expect_tx(full_bar + stage, 2u * (uint32_t)C::kStageBytes);
+          } else {
+            mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
+          }
+          auto load = [&](uint8_t* dst, const CUtensorMap* tm, int c0, int c1) {
+            if (PAIR) tma_load_2d_pair(dst, tm, c0, c1, fb);
+            else tma_load_2d(dst, tm, c0, c1, full_bar + stage);
+          };
+          if (p.a_mn) {
+#pragma unroll
+            for (int j = 0; j < kBM / 64; ++j) load(sa + j * kChunkBytes, &p.a[seg], m0 + 64 * j, kk);
+          } else {
+            load(sa, &p.a[seg], kk, m0);
+          }
+          if (EPI == kFfnGlu) {                   // the tile's columns of Wg, then those of Wu (one CTA of a pair each)
+            if (PAIR) load(sb, rank == 0 ? &p.b[0] : &p.b[1], kk, n0);
+            else { load(sb, &p.b[0], kk, n0); load(sb + C::kBBytes / 2, &p.b[1], kk, n0); }
+          } else if (p.b_mn) {
+#pragma unroll
+            for (int j = 0; j < C::kBRows / 64; ++j) load(sb + j * kChunkBytes, &p.b[seg], n0 + 64 * j, kk);
+          } else {
+            load(sb, &p.b[seg], kk, n0);
+          }
+          if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) {
+        raise_abort(abort_s, PAIR);
+        atomicExch(g.err, 1);
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (lane == 0 && rank == 0) {
+      int stage = 0, it = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = worker; ok && tile_at<TM, TN>(g, M0, t, &at); t += nworkers, ++it) {
+        const FfnProduct& p = g.p[at.prod];
+        const uint32_t idesc = make_idesc(TM, BN, g.f16 != 0, p.a_mn != 0, p.b_mn != 0);
+        const int nkb = (p.K + kBK - 1) / kBK * p.nseg;
+        const uint32_t a_chunk = p.a_mn ? (uint32_t)kChunkBytes : 0u, b_chunk = p.b_mn ? (uint32_t)kChunkBytes : 0u;
+        const uint64_t a_step = p.a_mn ? 128u : 2u, b_step = p.b_mn ? 128u : 2u;    // 16 elements of K, in 16 bytes
+        const int buf = it & 1;
+        if (!mbar_wait(tempty_bar + buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_s)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
+        for (int kb = 0; kb < nkb; ++kb) {
+          if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sa = smem_u32(stages + stage * C::kStageBytes);
+          const uint64_t adesc = make_sdesc(sa, a_chunk), bdesc = make_sdesc(sa + C::kABytes, b_chunk);
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k) {
+            if (PAIR) umma_f16_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
+            else umma_f16(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
+          }
+          if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
+          if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) { if (PAIR) umma_commit_pair(tfull_bar + buf); else umma_commit(tfull_bar + buf); }
+      }
+      if (!ok) {
+        raise_abort(abort_s, PAIR);
+        atomicExch(g.err, 2);
+      }
+    }
+  } else {
+    // ---------------- epilogue: a warp reaches the 32 tensor-memory lanes of quarter warp % 4 ----------------
+    const int q = warp & 3, share = (warp - 2) >> 2;
+    constexpr int kChunks = TN / 32;              // chunks of 32 output columns, dealt to the four warps of a quarter
+    constexpr int kLast = (kChunks + 3) / 4 - 1;  // a warp's last round
+    uint4* stg = reinterpret_cast<uint4*>(epi_stage + (warp - 2) * kWarpStage);
+    const uint32_t drained0 = (PAIR && rank != 0) ? map_to_cta(smem_u32(tempty_bar), 0u) : 0u;
+    const int f16 = g.f16;
+    int it = 0;
+    bool ok = true;
+    for (int t = worker; ok && tile_at<TM, TN>(g, M0, t, &at); t += nworkers, ++it) {
+      const FfnProduct& p = g.p[at.prod];
+      const int M = at.prod == 0 ? M0 : p.M, N = p.N;
+      const int buf = it & 1;
+      const int row0 = at.m * TM + (int)rank * kBM + q * 32, n0 = at.n * TN;
+      const int nlive = min(32, M - row0);        // (may be negative)
+      const uint32_t tbase = tmem_base + (uint32_t)(buf * BN) + ((uint32_t)(q * 32) << 16);
+      const int ncc = (N + 31) >> 5;
+      // the kept factors do not depend on this product: requested before its accumulator is waited for
+      float4 kp[8], kq[8];
+      auto keep_fetch = [&](int col) {
+        const bool in = nlive > 0 && col < N;
+        const float4* kp0 = reinterpret_cast<const float4*>(g.keep + (in ? keep_index(row0 + lane, col, ncc, 0) : 0));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          kp[i] = in ? __ldg(kp0 + i * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+          kq[i] = in ? __ldg(kp0 + (8 + i) * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      };
+      if (EPI == kFfnDGlu && share < kChunks) keep_fetch(n0 + share * 32);
+      if (!mbar_wait_warp(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s)) { ok = false; break; }
+      tc_fence_after();
+#pragma unroll
+      for (int rnd = 0; rnd <= kLast; ++rnd) {
+        const int c = (share + 4 * rnd) * 32, col = n0 + c;
+        const bool have = share + 4 * rnd < kChunks;
+        uint32_t acc[32], up[EPI == kFfnGlu ? 32 : 1];
+        if (have) {
+          tmem_ld32(tbase + (uint32_t)c, acc);
+          if (EPI == kFfnGlu) tmem_ld32(tbase + (uint32_t)(BN / 2 + c), reinterpret_cast<uint32_t(&)[32]>(up));
+        }
+        if (rnd == kLast) {                       // accumulator read: hand the buffer back
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (PAIR && rank != 0) mbar_arrive_cluster(drained0 + (uint32_t)buf * 8u);
+            else mbar_arrive(tempty_bar + buf);
+          }
+        }
+        if (!have || nlive <= 0 || col >= N) continue;            // (uniform over the warp)
+        const int npieces = min(4, (N - col) >> 3);               // pieces of eight 16-bit columns
+        if (EPI == kFfnGlu) {
+          uint32_t w[16];
+          float4* keep = g.keep ? reinterpret_cast<float4*>(g.keep + keep_index(row0 + lane, col, ncc, 0)) : nullptr;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float pg[4], pu[4], hh[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float uu = __uint_as_float(up[(4 * i + u) % (EPI == kFfnGlu ? 32 : 1)]);
+              float a, da;
+              activation(g.act, __uint_as_float(acc[4 * i + u]), a, da);
+              hh[u] = a * uu;
+              pg[u] = da * uu;
+              pu[u] = a;
+            }
+            w[2 * i] = pack16(hh[0], hh[1], f16);
+            w[2 * i + 1] = pack16(hh[2], hh[3], f16);
+            if (keep) {
+              keep[i * 32] = make_float4(pg[0], pg[1], pg[2], pg[3]);
+              keep[(8 + i) * 32] = make_float4(pu[0], pu[1], pu[2], pu[3]);
+            }
+          }
+          store_rows64(stg, w, static_cast<char*>(p.out) + ((size_t)row0 * p.ldo + col) * 2, (size_t)p.ldo * 2, nlive,
+                       npieces, lane);
+        } else if (EPI == kFfnOut) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = pack16(__uint_as_float(acc[2 * i]), __uint_as_float(acc[2 * i + 1]), f16);
+          store_rows64(stg, w, static_cast<char*>(p.out) + ((size_t)row0 * p.ldo + col) * 2, (size_t)p.ldo * 2, nlive,
+                       npieces, lane);
+        } else if (EPI == kFfnAdd) {
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+            if (col + 16 * hf < N)
+              add_rows64(stg, acc + 16 * hf, static_cast<float*>(p.out) + (size_t)row0 * p.ldo + col + 16 * hf,
+                         (size_t)p.ldo, nlive, min(4, (N - col - 16 * hf) >> 2), lane);
+        } else {
+          uint32_t wgr[16], wur[16];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float a0 = __uint_as_float(acc[4 * i]), a1 = __uint_as_float(acc[4 * i + 1]);
+            const float a2 = __uint_as_float(acc[4 * i + 2]), a3 = __uint_as_float(acc[4 * i + 3]);
+            wgr[2 * i] = pack16(a0 * kp[i].x, a1 * kp[i].y, f16);
+            wgr[2 * i + 1] = pack16(a2 * kp[i].z, a3 * kp[i].w, f16);
+            wur[2 * i] = pack16(a0 * kq[i].x, a1 * kq[i].y, f16);
+            wur[2 * i + 1] = pack16(a2 * kq[i].z, a3 * kq[i].w, f16);
+          }
+          if (rnd < kLast) keep_fetch(n0 + (share + 4 * (rnd + 1)) * 32);
+          const size_t off = ((size_t)row0 * p.ldo + col) * 2;
+          store_rows64(stg, wgr, static_cast<char*>(p.out) + off, (size_t)p.ldo * 2, nlive, npieces, lane);
+          store_rows64(stg, wur, static_cast<char*>(g.out2) + off, (size_t)p.ldo * 2, nlive, npieces, lane);
+        }
+      }
+    }
+    if (!ok && lane == 0) {
+      raise_abort(abort_s, PAIR);
+      atomicExch(g.err, 3);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_s && threadIdx.x == 0) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies still in flight land before the memory is released
+  }
+  __syncthreads();
+  if (PAIR) cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    if (PAIR)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+    else
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// few rows: weights as the 128 rows of the instruction, K split over a cluster
+// ---------------------------------------------------------------------------------------------
+
+struct FfnSplitArgs {
+  CUtensorMap w[2], t[2];                         // weights and tokens per segment (kFfnGlu: w = Wg, Wu, one t)
+  int rows, N, K;                                 // tokens, output columns, K of one segment
+  int nseg, w_mn;                                 // w_mn: weights lie [K, N]
+  int f16, act;
+  float* keep;
+  void* out;
+  void* out2;
+  int64_t ldo;
+  int* err;
+};
+
+constexpr int kSplitThreads = 256;
+
+template <int BN> struct FfnSplit {
+  static constexpr int kABytes = kBM * kBK * 2, kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
+  static constexpr int kFixedBytes = 1024 + 512;
+  static constexpr int kFit = (227 * 1024 - kFixedBytes) / kStageBytes;
+  static constexpr int kStages = kFit > 12 ? 12 : kFit;
+  static constexpr int kSmemBytes = kStages * kStageBytes + kFixedBytes;
+  static constexpr int kTmemCols = BN < 32 ? 32 : BN;
+  static_assert(kStages * kStageBytes >= BN * kBM * 4, "the partial sums fit where the stages were");
+};
+
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int BN, int EPI>
+__global__ void __launch_bounds__(kSplitThreads, 1) k_ffn_split(const __grid_constant__ FfnSplitArgs g) {
+  using C = FfnSplit<BN>;
+  constexpr int TN = EPI == kFfnGlu ? 64 : 128;   // output columns of a CTA
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(stages + C::kStages * C::kStageBytes);
+  uint64_t* empty_bar = full_bar + C::kStages;
+  uint64_t* tfull_bar = empty_bar + C::kStages;
+  uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(tfull_bar + 1);
+  volatile int* abort_s = reinterpret_cast<volatile int*>(tmem_base_s + 1);
+  float* part = reinterpret_cast<float*>(stages); // [BN][128], once the products are done
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t nsplit;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(nsplit));
+  const uint32_t rank = cluster_ctarank();
+  const int n0 = (int)(blockIdx.x / nsplit) * TN, tok0 = (int)blockIdx.y * BN;
+  const int kb_seg = (g.K + kBK - 1) / kBK, nkb = kb_seg * g.nseg;
+  const int kb0 = (int)((int64_t)nkb * rank / nsplit), kb1 = (int)((int64_t)nkb * (rank + 1) / nsplit);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar + s, 1); mbar_init(empty_bar + s, 1); }
+    mbar_init(tfull_bar, 1);
+    *abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_base_s)),
+                 "r"((uint32_t)C::kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_base_s;
+
+  if (warp == 0 && lane == 0) {
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
+      uint8_t* sa = stages + stage * C::kStageBytes;
+      const int seg = kb / kb_seg, kk = (kb - seg * kb_seg) * kBK;
+      mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
+      if (EPI == kFfnGlu) {                       // rows 0..63 of the instruction: Wg, rows 64..127: Wu
+        tma_load_2d(sa, &g.w[0], kk, n0, full_bar + stage);
+        tma_load_2d(sa + C::kABytes / 2, &g.w[1], kk, n0, full_bar + stage);
+      } else if (g.w_mn) {
+        tma_load_2d(sa, &g.w[seg], n0, kk, full_bar + stage);
+        tma_load_2d(sa + kChunkBytes, &g.w[seg], n0 + 64, kk, full_bar + stage);
+      } else {
+        tma_load_2d(sa, &g.w[seg], kk, n0, full_bar + stage);
+      }
+      tma_load_2d(sa + C::kABytes, &g.t[EPI == kFfnGlu ? 0 : seg], kk, tok0, full_bar + stage);
+      if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+    }
+    if (!ok) {
+      *abort_s = 1;
+      atomicExch(g.err, 1);
+    }
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t idesc = make_idesc(kBM, BN, g.f16 != 0, g.w_mn != 0, false);
+    const uint32_t a_chunk = g.w_mn ? (uint32_t)kChunkBytes : 0u;
+    const uint64_t a_step = g.w_mn ? 128u : 2u;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t sa = smem_u32(stages + stage * C::kStageBytes);
+      const uint64_t adesc = make_sdesc(sa, a_chunk), bdesc = make_sdesc(sa + C::kABytes);
+#pragma unroll
+      for (int k = 0; k < kBK / 16; ++k)
+        umma_f16(tmem_base, adesc + a_step * k, bdesc + (uint64_t)(2 * k), idesc, (kb > kb0 || k) ? 1u : 0u);
+      umma_commit(empty_bar + stage);
+      if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+    }
+    if (ok) {
+      umma_commit(tfull_bar);
+    } else {
+      *abort_s = 1;
+      atomicExch(g.err, 2);
+    }
+  }
+  __syncwarp();
+
+  // the accumulator to shared memory, [token][row of the instruction]
+  const bool ok = mbar_wait_warp(tfull_bar, 0u, abort_s);
+  if (ok) {
+    tc_fence_after();
+    const int q = warp & 3, half = warp >> 2;
+    uint32_t acc[BN / 2];
+#pragma unroll
+    for (int c = 0; c < BN / 2; c += 8)
+      tmem_ld8(tmem_base + (uint32_t)(half * (BN / 2) + c) + ((uint32_t)(q * 32) << 16), acc + c);
+    tmem_ld_wait();
+#pragma unroll
+    for (int c = 0; c < BN / 2; ++c) part[(half * (BN / 2) + c) * kBM + q * 32 + lane] = __uint_as_float(acc[c]);
+  } else if (lane == 0) {
+    *abort_s = 1;
+    atomicExch(g.err, 3);
+  }
+  tc_fence_before();
+  if (nsplit > 1) cluster_sync_all(); else __syncthreads();
+
+  // this CTA's share of the tokens: partial sums added in the order of K, then the epilogue; a lane holds four columns
+  const int share = BN / (int)nsplit;
+  const uint32_t part_a = smem_u32(part);
+  const int ncc = (g.N + 31) >> 5;
+  for (int i = warp; i < share; i += kSplitThreads / 32) {
+    const int tk = (int)rank * share + i, tok = tok0 + tk;
+    if (tok >= g.rows) break;
+    const uint32_t off = (uint32_t)(tk * kBM + lane * 4) * 4u;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (nsplit == 1) {
+      s = *reinterpret_cast<const float4*>(part + tk * kBM + lane * 4);
+    } else {
+      for (uint32_t r = 0; r < nsplit; ++r) {
+        const float4 v = ld_cluster4(map_to_cta(part_a + off, r));
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+    }
+    if (EPI == kFfnGlu) {
+      float4 u;
+      u.x = __shfl_down_sync(0xffffffffu, s.x, 16); u.y = __shfl_down_sync(0xffffffffu, s.y, 16);
+      u.z = __shfl_down_sync(0xffffffffu, s.z, 16); u.w = __shfl_down_sync(0xffffffffu, s.w, 16);
+      const int col = n0 + 4 * lane;
+      if (lane < 16 && col < g.N) {
+        float4 a, da;
+        activation(g.act, s.x, a.x, da.x); activation(g.act, s.y, a.y, da.y);
+        activation(g.act, s.z, a.z, da.z); activation(g.act, s.w, a.w, da.w);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.out) + (size_t)tok * g.ldo + col) =
+            make_uint2(pack16(a.x * u.x, a.y * u.y, g.f16), pack16(a.z * u.z, a.w * u.w, g.f16));
+        if (g.keep) {
+          *reinterpret_cast<float4*>(g.keep + keep_index(tok, col, ncc, 0)) = make_float4(da.x * u.x, da.y * u.y, da.z * u.z, da.w * u.w);
+          *reinterpret_cast<float4*>(g.keep + keep_index(tok, col, ncc, 1)) = a;
+        }
+      }
+    } else {
+      const int col = n0 + 4 * lane;
+      if (col < g.N) {
+        if (EPI == kFfnOut) {
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.out) + (size_t)tok * g.ldo + col) =
+              make_uint2(pack16(s.x, s.y, g.f16), pack16(s.z, s.w, g.f16));
+        } else {
+          const float4 p = *reinterpret_cast<const float4*>(g.keep + keep_index(tok, col, ncc, 0));
+          const float4 w = *reinterpret_cast<const float4*>(g.keep + keep_index(tok, col, ncc, 1));
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.out) + (size_t)tok * g.ldo + col) =
+              make_uint2(pack16(s.x * p.x, s.y * p.y, g.f16), pack16(s.z * p.z, s.w * p.w, g.f16));
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.out2) + (size_t)tok * g.ldo + col) =
+              make_uint2(pack16(s.x * w.x, s.y * w.y, g.f16), pack16(s.z * w.z, s.w * w.w, g.f16));
+        }
+      }
+    }
+  }
+  if (*abort_s && threadIdx.x == 0) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies still in flight land before the memory is released
+  }
+  __syncthreads();
+  if (nsplit > 1) cluster_sync_all();             // no CTA leaves while a peer may still read its sums
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------------
+
+constexpr int kMaxDevices = 64;
+
+int current_device() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : -1;
+}
+
+// a kernel's shared-memory limit and the number of its clusters that are resident at once, per device, looked up once
+struct KernelInfo {
+  std::atomic<int> resident[kMaxDevices];         // 0: not looked up; else 1 + resident CTAs (clusters of a pair)
+};
+
+template <int BN, int EPI, bool PAIR>
+cudaError_t tile_resident(int* n) {
+  static KernelInfo info;                         // zero-initialised
+  using C = FfnTile<BN, PAIR>;
+  const int dev = current_device();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  int r = info.resident[dev].load(std::memory_order_acquire);
+  if (r == 0) {
+    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    if (e != cudaSuccess) return e;
+    int sms = 0, got = 0;
+    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    got = sms;
+    if (PAIR) {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3(sms / 2 * 2);
+      cfg.blockDim = dim3(kTileThreads);
+      cfg.dynamicSmemBytes = C::kSmemBytes;
+      cudaLaunchAttribute attr{};
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR>, &cfg)) != cudaSuccess) return e;
+      got = std::min(got, sms / 2);
+    }
+    if (got < 1) return cudaErrorLaunchOutOfResources;
+    r = got + 1;
+    info.resident[dev].store(r, std::memory_order_release);
+  }
+  *n = r - 1;
+  return cudaSuccess;
+}
+
+template <int BN, int EPI, bool PAIR>
+cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) {
+  using C = FfnTile<BN, PAIR>;
+  int resident = 0;
+  const cudaError_t e = tile_resident<BN, EPI, PAIR>(&resident);
+  if (e != cudaSuccess) return e;
+  const int workers = (int)std::min<int64_t>(tiles, resident);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(PAIR ? 2 * workers : workers);
+  cfg.blockDim = dim3(kTileThreads);
+  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = PAIR ? 2 : 1; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR>, g);
+}
+
+// where an operand lies: [rows, cols] with rows ld elements apart; K-major if K runs along the columns
+struct Mat {
+  const void* p;
+  int64_t ld;
+};
+
+// one product's tensor maps: operand rows (M or N) by K elements, box of `box` rows (K-major) or 64 k (MN-major)
+bool map_operand(CUtensorMap* tm, const Mat& m, bool f16, int64_t mn, int64_t k, bool mn_major, int box) {
+  return mn_major ? make_tmap_2d(tm, m.p, f16, (uint64_t)k, (uint64_t)mn, (uint64_t)m.ld, 64)
+                  : make_tmap_2d(tm, m.p, f16, (uint64_t)mn, (uint64_t)k, (uint64_t)m.ld, (uint32_t)box);
+}
+
+struct ProductSpec {
+  Mat a[2], b[2];
+  int nseg;
+  bool a_mn, b_mn;
+  int M, N, K;
+  void* out;
+  int64_t ldo;
+};
+
+// Tile shape: single CTAs on 128 x 128 tiles while these are at most one per SM (each has an SM of its own), pairs on
+// 256 x 256 tiles above that.
+template <int EPI>
+cudaError_t launch_tiles(const FfnArgs& a, const ProductSpec* specs, int n, cudaStream_t st, float* keep = nullptr,
+                         void* out2 = nullptr) {
+  constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
+  int64_t small = 0, wide = 0;
+  for (int i = 0; i < n; ++i) {
+    small += (int64_t)((specs[i].M + 127) / 128) * ((specs[i].N + kNarrow - 1) / kNarrow);
+    wide += (int64_t)((specs[i].M + 255) / 256) * ((specs[i].N + kWide - 1) / kWide);
+  }
+  const bool pair = small > 148;
+  FfnTileArgs g;
+  g.np = n;
+  g.f16 = a.f16;
+  g.act = a.act;
+  g.nrows_dev = a.nrows_dev;
+  g.keep = keep;
+  g.out2 = out2;
+  g.err = a.err;
+  for (int i = 0; i < n; ++i) {
+    const ProductSpec& s = specs[i];
+    FfnProduct& p = g.p[i];
+    p.M = s.M; p.N = s.N; p.K = s.K;
+    p.nseg = s.nseg; p.a_mn = s.a_mn; p.b_mn = s.b_mn;
+    p.out = s.out; p.ldo = s.ldo;
+    const int box_b = EPI == kFfnGlu && !pair ? 64 : 128;
+    for (int k = 0; k < (EPI == kFfnGlu ? 2 : s.nseg); ++k) {
+      if (k < s.nseg && !map_operand(&p.a[k], s.a[k], a.f16 != 0, s.M, s.K, s.a_mn, 128)) return cudaErrorInvalidValue;
+      if (!map_operand(&p.b[k], s.b[k], a.f16 != 0, s.N, s.K, s.b_mn, box_b)) return cudaErrorInvalidValue;
+    }
+  }
+  if (pair) {
+    const cudaError_t e = launch_tile_t<256, EPI, true>(g, wide, st);
+    if (e != cudaErrorLaunchOutOfResources) return e;
+    // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
+    for (int i = 0; EPI == kFfnGlu && i < n; ++i)
+      for (int k = 0; k < 2; ++k)
+        if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, specs[i].b_mn, 64))
+          return cudaErrorInvalidValue;
+  }
+  return launch_tile_t<128, EPI, false>(g, small, st);
+}
+
+template <int BN, int EPI>
+cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, cudaStream_t st) {
+  using C = FfnSplit<BN>;
+  static KernelInfo info;
+  const int dev = current_device();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  if (info.resident[dev].load(std::memory_order_acquire) == 0) {
+    const cudaError_t e = cudaFuncSetAttribute(k_ffn_split<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    if (e != cudaSuccess) return e;
+    info.resident[dev].store(1, std::memory_order_release);
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(tiles * splits, (g.rows + BN - 1) / BN);
+  cfg.blockDim = dim3(kSplitThreads);
+  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)splits; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_ffn_split<BN, EPI>, g);
+}
+
+// weights [N, K] (or [K, N]: w_mn) times tokens [rows, K]
+struct SplitSpec {
+  Mat w[2], t[2];
+  int nseg;
+  bool w_mn;
+  int N, K;
+  void* out;
+  void* out2;
+  int64_t ldo;
+};
+
+template <int EPI>
+cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, cudaStream_t st) {
+  constexpr int TN = EPI == kFfnGlu ? 64 : 128;
+  const int bn = a.rows <= 16 ? 16 : a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
+  FfnSplitArgs g;
+  g.rows = a.rows; g.N = s.N; g.K = s.K;
+  g.nseg = s.nseg; g.w_mn = s.w_mn;
+  g.f16 = a.f16; g.act = a.act;
+  g.keep = keep;
+  g.out = s.out; g.out2 = s.out2; g.ldo = s.ldo;
+  g.err = a.err;
+  const int nw = EPI == kFfnGlu ? 2 : s.nseg;
+  for (int k = 0; k < nw; ++k)
+    if (!map_operand(&g.w[k], s.w[k], a.f16 != 0, s.N, s.K, s.w_mn, EPI == kFfnGlu ? 64 : 128)) return cudaErrorInvalidValue;
+  for (int k = 0; k < s.nseg; ++k)
+    if (!map_operand(&g.t[k], s.t[k], a.f16 != 0, a.rows, s.K, false, bn)) return cudaErrorInvalidValue;
+  const int tiles = (s.N + TN - 1) / TN, tok = (a.rows + bn - 1) / bn;
+  const int nkb = (s.K + kBK - 1) / kBK * s.nseg;
+  // enough CTAs that nearly every SM reads weights, with at least four steps of K each
+  int splits = 1;
+  while (splits < 8 && (int64_t)tiles * tok * splits < 120 && nkb / (2 * splits) >= 4) splits *= 2;
+  switch (bn) {
+    case 16: return launch_split_t<16, EPI>(g, tiles, splits, st);
+    case 32: return launch_split_t<32, EPI>(g, tiles, splits, st);
+    case 64: return launch_split_t<64, EPI>(g, tiles, splits, st);
+    default: return launch_split_t<128, EPI>(g, tiles, splits, st);
+  }
+}
+
+// rows up to which the products take the form that reads the weights as the instruction's rows
+constexpr int kSplitRows = 128;
+
+}  // namespace
+
+size_t ffn_keep_floats(int64_t rows, int64_t f) {
+  return (size_t)((rows + 31) / 32 * 32) * (size_t)((f + 31) / 32 * 32) * 2;
+}
+
+cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
+  cudaError_t e = cudaMemsetAsync(a.err, 0, sizeof(int), st);
+  if (e != cudaSuccess || a.rows <= 0) return e;
+  if (a.rows <= kSplitRows) {
+    SplitSpec s{};
+    s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.x, a.ldx};
+    s.nseg = 1; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
+    if ((e = launch_split<kFfnGlu>(a, s, a.keep, st)) != cudaSuccess) return e;
+    SplitSpec o{};
+    o.w[0] = {a.wd, a.f}; o.t[0] = {a.h, a.f};
+    o.nseg = 1; o.N = a.d; o.K = a.f; o.out = a.y; o.ldo = a.ldy;
+    return launch_split<kFfnOut>(a, o, nullptr, st);
+  }
+  ProductSpec s{};
+  s.a[0] = {a.x, a.ldx}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
+  s.nseg = 1; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
+  if ((e = launch_tiles<kFfnGlu>(a, &s, 1, st, a.keep)) != cudaSuccess) return e;
+  ProductSpec o{};
+  o.a[0] = {a.h, a.f}; o.b[0] = {a.wd, a.f};
+  o.nseg = 1; o.M = a.rows; o.N = a.d; o.K = a.f; o.out = a.y; o.ldo = a.ldy;
+  return launch_tiles<kFfnOut>(a, &o, 1, st);
+}
+
+cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st) {
+  if (a.rows <= 0) return cudaSuccess;
+  ProductSpec s{};
+  s.a[0] = {a.x, a.ldx}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
+  s.nseg = 1; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
+  const cudaError_t e = launch_tiles<kFfnGlu>(a, &s, 1, st);
+  if (e != cudaSuccess) return e;
+  ProductSpec o{};
+  o.a[0] = {a.h, a.f}; o.b[0] = {a.wd, a.f};
+  o.nseg = 1; o.M = a.rows; o.N = a.d; o.K = a.f; o.out = a.res; o.ldo = a.d;
+  return launch_tiles<kFfnAdd>(a, &o, 1, st);
+}
+
+cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
+  const size_t wbytes = (size_t)a.d * a.f * 2;
+  cudaError_t e = cudaMemsetAsync(a.err, 0, sizeof(int), st);
+  if (e != cudaSuccess) return e;
+  if (a.rows <= 0) {                              // an empty sum: the weights' gradients are zeros
+    for (void* w : {a.dwg, a.dwu, a.dwd})
+      if (w && (e = cudaMemsetAsync(w, 0, wbytes, st)) != cudaSuccess) return e;
+    return cudaSuccess;
+  }
+  const bool few = a.rows <= kSplitRows;
+  if (a.dx || a.dwg || a.dwu) {                   // dH = dy Wd, dG and dU
+    if (few) {
+      SplitSpec s{};
+      s.w[0] = {a.wd, a.f}; s.t[0] = {a.dy, a.lddy};
+      s.nseg = 1; s.w_mn = true; s.N = a.f; s.K = a.d; s.out = a.dg; s.out2 = a.du; s.ldo = a.f;
+      e = launch_split<kFfnDGlu>(a, s, a.keep, st);
+    } else {
+      ProductSpec s{};
+      s.a[0] = {a.dy, a.lddy}; s.b[0] = {a.wd, a.f};
+      s.nseg = 1; s.b_mn = true; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.dg; s.ldo = a.f;
+      e = launch_tiles<kFfnDGlu>(a, &s, 1, st, a.keep, a.du);
+    }
+    if (e != cudaSuccess) return e;
+  }
+  if (a.dx) {
+    if (few) {
+      SplitSpec s{};
+      s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.dg, a.f}; s.t[1] = {a.du, a.f};
+      s.nseg = 2; s.w_mn = true; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
+      e = launch_split<kFfnOut>(a, s, nullptr, st);
+    } else {
+      ProductSpec s{};
+      s.a[0] = {a.dg, a.f}; s.a[1] = {a.du, a.f}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
+      s.nseg = 2; s.b_mn = true; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
+      e = launch_tiles<kFfnOut>(a, &s, 1, st);
+    }
+    if (e != cudaSuccess) return e;
+  }
+  ProductSpec w[3];
+  int n = 0;
+  const auto gradient = [&](const Mat& left, const Mat& right, int M, int N, void* out) {
+    ProductSpec s{};
+    s.a[0] = left; s.b[0] = right;
+    s.nseg = 1; s.a_mn = s.b_mn = true; s.M = M; s.N = N; s.K = a.rows; s.out = out; s.ldo = N;
+    w[n++] = s;
+  };
+  if (a.dwg) gradient({a.dg, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwg);
+  if (a.dwu) gradient({a.du, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwu);
+  if (a.dwd) gradient({a.dy, a.lddy}, {a.h, a.f}, a.d, a.f, a.dwd);
+  return n > 0 ? launch_tiles<kFfnOut>(a, w, n, st) : cudaSuccess;
+}
+
+}  // namespace sds
