@@ -45,7 +45,11 @@ enum FfnEpi : int {
 constexpr int kBM = 128;                          // rows of one CTA's accumulator
 constexpr int kBK = 64;                           // elements of K per stage: one 128-byte swizzle row
 constexpr int kChunkBytes = 64 * kBK * 2;         // 64 x 64 elements
-constexpr int kEpiWarps = 16;
+// Epilogue warps: one per quarter of the lanes. The main loop takes up shared memory (operand tiles written and read:
+// 128 bytes per cycle), and every warp that stages and polls beside it costs; four finish a tile well within the next
+// one's products. Measured at 16384 rows, d = 2048, f = 8192 in a long run: forward projections 806 us with 4 warps, 896
+// with 8; dH 550 and 566; second product 430 and 447.
+constexpr int kEpiWarps = 4;
 constexpr int kTileThreads = 64 + 32 * kEpiWarps; // warp 0: TMA, warp 1: MMA and tensor memory, then the epilogue
 constexpr int kWarpStage = 2048;                  // staging bytes of an epilogue warp: 32 rows of 64 bytes
 
@@ -54,6 +58,7 @@ struct FfnProduct {
   CUtensorMap a[2], b[2];                         // kFfnGlu: b[0] = Wg, b[1] = Wu, one segment
   int M, N, K;                                    // K of one segment
   int nseg, a_mn, b_mn;
+  int band;                                       // tile rows of a band (see tile_at)
   void* out;
   int64_t ldo;
 };
@@ -62,6 +67,7 @@ constexpr int kMaxProducts = 4;
 struct FfnTileArgs {
   FfnProduct p[kMaxProducts];
   int np;
+  int na, give;                                   // order of the tiles (see tile_index)
   int f16, act;
   const int* nrows_dev;                           // row count of p[0] on the device (NULL: p[0].M)
   float* keep;
@@ -75,12 +81,13 @@ struct FfnTileArgs {
 
 // a = act(g), da = act'(g). The fast exponential and division are accurate to a few units of the 24-bit
 // significand, far inside the 16-bit operands' rounding.
-__device__ __forceinline__ void activation(int act, float g, float& a, float& da) {
-  if (act == SDS_ACT_SILU) {
+template <int ACT>
+__device__ __forceinline__ void activation(float g, float& a, float& da) {
+  if (ACT == SDS_ACT_SILU) {
     const float p = __fdividef(1.0f, 1.0f + __expf(-g));
     a = g * p;
     da = p * fmaf(g, 1.0f - p, 1.0f);
-  } else if (act == SDS_ACT_GELU) {
+  } else if (ACT == SDS_ACT_GELU) {
     const float p = 0.5f * erfcf(-0.70710678118654752f * g);
     a = g * p;
     da = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
@@ -92,6 +99,15 @@ __device__ __forceinline__ void activation(int act, float g, float& a, float& da
     a = g * p;
     da = t > 0.f ? fmaf(g * t * k2, fmaf(3.0f * c, g2, 1.0f), p) : p;   // (t = 0 where g^2 might overflow)
   }
+}
+
+template <int N> struct Act { static constexpr int value = N; };
+// f(Act<act>): the choice is made once per tile or row and not per element
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+  if (act == SDS_ACT_SILU) f(Act<SDS_ACT_SILU>());
+  else if (act == SDS_ACT_GELU) f(Act<SDS_ACT_GELU>());
+  else f(Act<SDS_ACT_GELU_TANH>());
 }
 
 __device__ __forceinline__ uint32_t pack16(float lo, float hi, int f16) {
@@ -168,8 +184,8 @@ struct TileAt {
   int prod, m, n;                                 // product, tile row, tile column
 };
 
-// Tiles of all products in one sequence. Within a product, bands of eight tile rows are walked column by column:
-// the tiles that run at the same time then share few rows of A and of B, which stay in L2.
+// Tiles of all products in one sequence. Within a product, bands of `band` tile rows are walked column by column: the
+// band's rows of A stay in L2 while B passes by.
 template <int TM, int TN>
 __device__ __forceinline__ bool tile_at(const FfnTileArgs& g, int m0_rows, int t, TileAt* at) {
   for (int p = 0; p < g.np; ++p) {
@@ -177,16 +193,35 @@ __device__ __forceinline__ bool tile_at(const FfnTileArgs& g, int m0_rows, int t
     const int mt = (M + TM - 1) / TM, nt = (g.p[p].N + TN - 1) / TN;
     const int n = mt * nt;
     if (t < n) {
-      const int band = t / (8 * nt), in = t - band * 8 * nt;
-      const int rows = min(8, mt - band * 8);
+      const int height = g.p[p].band, band = t / (height * nt), in = t - band * height * nt;
+      const int rows = min(height, mt - band * height);
       at->prod = p;
-      at->m = band * 8 + in % rows;
+      at->m = band * height + in % rows;
       at->n = in / rows;
       return true;
     }
     t -= n;
   }
   return false;
+}
+
+// The i-th tile of a worker. One class of tiles: dealt round robin. Two (the first `na` tiles take about `give` times as
+// long as the others): the long ones round robin, then `give` short ones to every worker that got one long tile
+// less, then the rest round robin. Known in advance, so no role has to ask another.
+__device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int nworkers, int i) {
+  if (g.give == 0) return worker + i * nworkers;
+  const int rest = g.na % nworkers, mine = g.na / nworkers + (worker < rest ? 1 : 0);
+  if (i < mine) return worker + i * nworkers;
+  i -= mine;
+  int t = g.na;
+  if (rest > 0) {
+    if (worker >= rest) {
+      if (i < g.give) return t + (worker - rest) * g.give + i;
+      i -= g.give;
+    }
+    t += (nworkers - rest) * g.give;
+  }
+  return t + worker + i * nworkers;
 }
 
 template <int BN, int EPI, bool PAIR>
@@ -240,42 +275,47 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       uint32_t phase = 0;
       bool ok = true;
       const uint32_t leader_full0 = PAIR ? map_to_cta(smem_u32(full_bar), 0u) : 0u;
-      for (int t = worker; ok && tile_at<TM, TN>(g, M0, t, &at); t += nworkers) {
+      for (int it = 0; ok && tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
         const FfnProduct& p = g.p[at.prod];
         const int m0 = at.m * TM + (int)rank * kBM;
         const int n0 = at.n * TN + (EPI == kFfnGlu ? 0 : (int)rank * C::kBRows);
-        const int kb_seg = (p.K + kBK - 1) / kBK, nkb = kb_seg * p.nseg;
-        for (int kb = 0; kb < nkb; ++kb) {
-          if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
-          uint8_t* sa = stages + stage * C::kStageBytes;
-          uint8_t* sb = sa + C::kABytes;
-          const int seg = kb / kb_seg, kk = (kb - seg * kb_seg) * kBK;
-          const uint32_t fb = PAIR ? leader_full0 + (uint32_t)stage * 8u : 0u;
-          if (PAIR) {
-            if (rank == 0) mbar_expect_tx(full_bar + stage, 2u * (uint32_t)C::kStageBytes);
-          } else {
-            mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
-          }
-          auto load = [&](uint8_t* dst, const CUtensorMap* tm, int c0, int c1) {
-            if (PAIR) tma_load_2d_pair(dst, tm, c0, c1, fb);
-            else tma_load_2d(dst, tm, c0, c1, full_bar + stage);
-          };
-          if (p.a_mn) {
+        const int K = p.K, nseg = p.nseg;
+        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
+        for (int seg = 0; seg < nseg && ok; ++seg) {
+          const CUtensorMap* ta = &p.a[seg];
+          // the tile's columns of Wg, then those of Wu: one CTA of a pair each, or one after the other
+          const CUtensorMap* tb = &p.b[EPI == kFfnGlu && PAIR ? (int)rank : seg];
+          for (int kk = 0; kk < K; kk += kBK) {
+            if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
+            uint8_t* sa = stages + stage * C::kStageBytes;
+            uint8_t* sb = sa + C::kABytes;
+            const uint32_t fb = PAIR ? leader_full0 + (uint32_t)stage * 8u : 0u;
+            if (PAIR) {
+              if (rank == 0) mbar_expect_tx(full_bar + stage, 2u * (uint32_t)C::kStageBytes);
+            } else {
+              mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
+            }
+            auto load = [&](uint8_t* dst, const CUtensorMap* tm, int c0, int c1) {
+              if (PAIR) tma_load_2d_pair(dst, tm, c0, c1, fb);
+              else tma_load_2d(dst, tm, c0, c1, full_bar + stage);
+            };
+            if (a_mn) {
 #pragma unroll
-            for (int j = 0; j < kBM / 64; ++j) load(sa + j * kChunkBytes, &p.a[seg], m0 + 64 * j, kk);
-          } else {
-            load(sa, &p.a[seg], kk, m0);
-          }
-          if (EPI == kFfnGlu) {                   // the tile's columns of Wg, then those of Wu (one CTA of a pair each)
-            if (PAIR) load(sb, rank == 0 ? &p.b[0] : &p.b[1], kk, n0);
-            else { load(sb, &p.b[0], kk, n0); load(sb + C::kBBytes / 2, &p.b[1], kk, n0); }
-          } else if (p.b_mn) {
+              for (int j = 0; j < kBM / 64; ++j) load(sa + j * kChunkBytes, ta, m0 + 64 * j, kk);
+            } else {
+              load(sa, ta, kk, m0);
+            }
+            if (EPI == kFfnGlu && !PAIR) {
+              load(sb, tb, kk, n0);
+              load(sb + C::kBBytes / 2, tb + 1, kk, n0);
+            } else if (b_mn) {
 #pragma unroll
-            for (int j = 0; j < C::kBRows / 64; ++j) load(sb + j * kChunkBytes, &p.b[seg], n0 + 64 * j, kk);
-          } else {
-            load(sb, &p.b[seg], kk, n0);
+              for (int j = 0; j < C::kBRows / 64; ++j) load(sb + j * kChunkBytes, tb, n0 + 64 * j, kk);
+            } else {
+              load(sb, tb, kk, n0);
+            }
+            if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
           }
-          if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
         }
       }
       if (!ok) {
@@ -289,7 +329,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       int stage = 0, it = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int t = worker; ok && tile_at<TM, TN>(g, M0, t, &at); t += nworkers, ++it) {
+      bool more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, 0), &at);
+      for (; ok && more; ++it) {
         const FfnProduct& p = g.p[at.prod];
         const uint32_t idesc = make_idesc(TM, BN, g.f16 != 0, p.a_mn != 0, p.b_mn != 0);
         const int nkb = (p.K + kBK - 1) / kBK * p.nseg;
@@ -299,11 +340,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
         if (!mbar_wait(tempty_bar + buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_s)) { ok = false; break; }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
+        const uint64_t adesc0 = make_sdesc(smem_u32(stages), a_chunk), bdesc0 = make_sdesc(smem_u32(stages) + C::kABytes, b_chunk);
         for (int kb = 0; kb < nkb; ++kb) {
           if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t sa = smem_u32(stages + stage * C::kStageBytes);
-          const uint64_t adesc = make_sdesc(sa, a_chunk), bdesc = make_sdesc(sa + C::kABytes, b_chunk);
+          const uint64_t adesc = adesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
+          const uint64_t bdesc = bdesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
 #pragma unroll
           for (int k = 0; k < kBK / 16; ++k) {
             if (PAIR) umma_f16_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
@@ -311,6 +353,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
           }
           if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
           if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+          // where the next tile lies takes a few divisions: worked out while this tile's products run
+          if (kb == 0) more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
         }
         if (ok) { if (PAIR) umma_commit_pair(tfull_bar + buf); else umma_commit(tfull_bar + buf); }
       }
@@ -321,15 +365,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
     }
   } else {
     // ---------------- epilogue: a warp reaches the 32 tensor-memory lanes of quarter warp % 4 ----------------
-    const int q = warp & 3, share = (warp - 2) >> 2;
-    constexpr int kChunks = TN / 32;              // chunks of 32 output columns, dealt to the four warps of a quarter
-    constexpr int kLast = (kChunks + 3) / 4 - 1;  // a warp's last round
+    const int q = warp & 3;
+    constexpr int kChunks = TN / 32;              // chunks of 32 output columns
     uint4* stg = reinterpret_cast<uint4*>(epi_stage + (warp - 2) * kWarpStage);
     const uint32_t drained0 = (PAIR && rank != 0) ? map_to_cta(smem_u32(tempty_bar), 0u) : 0u;
     const int f16 = g.f16;
     int it = 0;
     bool ok = true;
-    for (int t = worker; ok && tile_at<TM, TN>(g, M0, t, &at); t += nworkers, ++it) {
+    for (; ok && tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
       const FfnProduct& p = g.p[at.prod];
       const int M = at.prod == 0 ? M0 : p.M, N = p.N;
       const int buf = it & 1;
@@ -348,19 +391,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
           kq[i] = in ? __ldg(kp0 + (8 + i) * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
       };
-      if (EPI == kFfnDGlu && share < kChunks) keep_fetch(n0 + share * 32);
+      if (EPI == kFfnDGlu) keep_fetch(n0);
       if (!mbar_wait_warp(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s)) { ok = false; break; }
       tc_fence_after();
-#pragma unroll
-      for (int rnd = 0; rnd <= kLast; ++rnd) {
-        const int c = (share + 4 * rnd) * 32, col = n0 + c;
-        const bool have = share + 4 * rnd < kChunks;
+#pragma unroll 1
+      for (int chunk = 0; chunk < kChunks; ++chunk) {
+        const int c = chunk * 32, col = n0 + c;
         uint32_t acc[32], up[EPI == kFfnGlu ? 32 : 1];
-        if (have) {
-          tmem_ld32(tbase + (uint32_t)c, acc);
-          if (EPI == kFfnGlu) tmem_ld32(tbase + (uint32_t)(BN / 2 + c), reinterpret_cast<uint32_t(&)[32]>(up));
-        }
-        if (rnd == kLast) {                       // accumulator read: hand the buffer back
+        tmem_ld32(tbase + (uint32_t)c, acc);
+        if (EPI == kFfnGlu) tmem_ld32(tbase + (uint32_t)(BN / 2 + c), reinterpret_cast<uint32_t(&)[32]>(up));
+        if (chunk == kChunks - 1) {               // accumulator read: hand the buffer back
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -368,30 +408,41 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
             else mbar_arrive(tempty_bar + buf);
           }
         }
-        if (!have || nlive <= 0 || col >= N) continue;            // (uniform over the warp)
+        if (nlive <= 0 || col >= N) continue;     // (uniform over the warp)
         const int npieces = min(4, (N - col) >> 3);               // pieces of eight 16-bit columns
         if (EPI == kFfnGlu) {
           uint32_t w[16];
           float4* keep = g.keep ? reinterpret_cast<float4*>(g.keep + keep_index(row0 + lane, col, ncc, 0)) : nullptr;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float pg[4], pu[4], hh[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float uu = __uint_as_float(up[(4 * i + u) % (EPI == kFfnGlu ? 32 : 1)]);
-              float a, da;
-              activation(g.act, __uint_as_float(acc[4 * i + u]), a, da);
-              hh[u] = a * uu;
-              pg[u] = da * uu;
-              pu[u] = a;
-            }
-            w[2 * i] = pack16(hh[0], hh[1], f16);
-            w[2 * i + 1] = pack16(hh[2], hh[3], f16);
+          with_activation(g.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
             if (keep) {
-              keep[i * 32] = make_float4(pg[0], pg[1], pg[2], pg[3]);
-              keep[(8 + i) * 32] = make_float4(pu[0], pu[1], pu[2], pu[3]);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float pg[4], pu[4], hh[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  const float uu = __uint_as_float(up[(4 * i + u) % (EPI == kFfnGlu ? 32 : 1)]);
+                  float da;
+                  activation<ACT>(__uint_as_float(acc[4 * i + u]), pu[u], da);
+                  hh[u] = pu[u] * uu;
+                  pg[u] = da * uu;
+                }
+                w[2 * i] = pack16(hh[0], hh[1], f16);
+                w[2 * i + 1] = pack16(hh[2], hh[3], f16);
+                keep[i * 32] = make_float4(pg[0], pg[1], pg[2], pg[3]);
+                keep[(8 + i) * 32] = make_float4(pu[0], pu[1], pu[2], pu[3]);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float a0, a1, da;
+                activation<ACT>(__uint_as_float(acc[2 * i]), a0, da);
+                activation<ACT>(__uint_as_float(acc[2 * i + 1]), a1, da);
+                w[i] = pack16(a0 * __uint_as_float(up[(2 * i) % (EPI == kFfnGlu ? 32 : 1)]),
+                              a1 * __uint_as_float(up[(2 * i + 1) % (EPI == kFfnGlu ? 32 : 1)]), f16);
+              }
             }
-          }
+          });
           store_rows64(stg, w, static_cast<char*>(p.out) + ((size_t)row0 * p.ldo + col) * 2, (size_t)p.ldo * 2, nlive,
                        npieces, lane);
         } else if (EPI == kFfnOut) {
@@ -417,7 +468,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
             wur[2 * i] = pack16(a0 * kq[i].x, a1 * kq[i].y, f16);
             wur[2 * i + 1] = pack16(a2 * kq[i].z, a3 * kq[i].w, f16);
           }
-          if (rnd < kLast) keep_fetch(n0 + (share + 4 * (rnd + 1)) * 32);
+          if (chunk < kChunks - 1) keep_fetch(col + 32);
           const size_t off = ((size_t)row0 * p.ldo + col) * 2;
           store_rows64(stg, wgr, static_cast<char*>(p.out) + off, (size_t)p.ldo * 2, nlive, npieces, lane);
           store_rows64(stg, wur, static_cast<char*>(g.out2) + off, (size_t)p.ldo * 2, nlive, npieces, lane);
@@ -613,8 +664,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_ffn_split(const __grid_con
       const int col = n0 + 4 * lane;
       if (lane < 16 && col < g.N) {
         float4 a, da;
-        activation(g.act, s.x, a.x, da.x); activation(g.act, s.y, a.y, da.y);
-        activation(g.act, s.z, a.z, da.z); activation(g.act, s.w, a.w, da.w);
+        with_activation(g.act, [&](auto act) {
+          constexpr int ACT = decltype(act)::value;
+          activation<ACT>(s.x, a.x, da.x); activation<ACT>(s.y, a.y, da.y);
+          activation<ACT>(s.z, a.z, da.z); activation<ACT>(s.w, a.w, da.w);
+        });
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.out) + (size_t)tok * g.ldo + col) =
             make_uint2(pack16(a.x * u.x, a.y * u.y, g.f16), pack16(a.z * u.z, a.w * u.w, g.f16));
         if (g.keep) {
@@ -741,20 +795,34 @@ struct ProductSpec {
   int64_t ldo;
 };
 
+inline int64_t tiles_of(const ProductSpec& s, int tm, int tn) {
+  return (int64_t)((s.M + tm - 1) / tm) * ((s.N + tn - 1) / tn);
+}
+inline int ksteps(const ProductSpec& s) { return (s.K + kBK - 1) / kBK * s.nseg; }
+
 // Tile shape: single CTAs on 128 x 128 tiles while these are at most one per SM (each has an SM of its own), pairs on
-// 256 x 256 tiles above that.
+// 256 x 256 tiles above that. Several products of one launch: those with the longer tiles come first; there are at most
+// two lengths (specs[0] may differ from the others).
 template <int EPI>
-cudaError_t launch_tiles(const FfnArgs& a, const ProductSpec* specs, int n, cudaStream_t st, float* keep = nullptr,
+cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, cudaStream_t st, float* keep = nullptr,
                          void* out2 = nullptr) {
   constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
+  if (n > 1 && ksteps(specs[0]) < ksteps(specs[n - 1])) std::swap(specs[0], specs[n - 1]);
   int64_t small = 0, wide = 0;
   for (int i = 0; i < n; ++i) {
-    small += (int64_t)((specs[i].M + 127) / 128) * ((specs[i].N + kNarrow - 1) / kNarrow);
-    wide += (int64_t)((specs[i].M + 255) / 256) * ((specs[i].N + kWide - 1) / kWide);
+    small += tiles_of(specs[i], 128, kNarrow);
+    wide += tiles_of(specs[i], 256, kWide);
   }
   const bool pair = small > 148;
+  // tiles of the longer class, and how many of the shorter one take as long
+  int first = 1;
+  while (first < n && ksteps(specs[first]) == ksteps(specs[0])) ++first;
+  int64_t na = 0;
+  for (int i = 0; i < first; ++i) na += pair ? tiles_of(specs[i], 256, kWide) : tiles_of(specs[i], 128, kNarrow);
   FfnTileArgs g;
   g.np = n;
+  g.na = (int)na;
+  g.give = first < n ? (ksteps(specs[0]) + ksteps(specs[n - 1]) / 2) / ksteps(specs[n - 1]) : 0;
   g.f16 = a.f16;
   g.act = a.act;
   g.nrows_dev = a.nrows_dev;
@@ -767,6 +835,7 @@ cudaError_t launch_tiles(const FfnArgs& a, const ProductSpec* specs, int n, cuda
     p.M = s.M; p.N = s.N; p.K = s.K;
     p.nseg = s.nseg; p.a_mn = s.a_mn; p.b_mn = s.b_mn;
     p.out = s.out; p.ldo = s.ldo;
+    p.band = (int)std::max<int64_t>(8, std::min<int64_t>(32, (32 << 20) / ((pair ? 256 : 128) * 2 * (int64_t)ksteps(s) * kBK)));
     const int box_b = EPI == kFfnGlu && !pair ? 64 : 128;
     for (int k = 0; k < (EPI == kFfnGlu ? 2 : s.nseg); ++k) {
       if (k < s.nseg && !map_operand(&p.a[k], s.a[k], a.f16 != 0, s.M, s.K, s.a_mn, 128)) return cudaErrorInvalidValue;
@@ -918,22 +987,20 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
     }
     if (e != cudaSuccess) return e;
   }
-  if (a.dx) {
-    if (few) {
-      SplitSpec s{};
-      s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.dg, a.f}; s.t[1] = {a.du, a.f};
-      s.nseg = 2; s.w_mn = true; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
-      e = launch_split<kFfnOut>(a, s, nullptr, st);
-    } else {
-      ProductSpec s{};
-      s.a[0] = {a.dg, a.f}; s.a[1] = {a.du, a.f}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
-      s.nseg = 2; s.b_mn = true; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
-      e = launch_tiles<kFfnOut>(a, &s, 1, st);
-    }
-    if (e != cudaSuccess) return e;
-  }
-  ProductSpec w[3];
+  // the gradients of x and of the weights read the same dG and dU: one launch where x's product takes tiles too
+  ProductSpec w[4];
   int n = 0;
+  if (a.dx && few) {
+    SplitSpec s{};
+    s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.dg, a.f}; s.t[1] = {a.du, a.f};
+    s.nseg = 2; s.w_mn = true; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
+    if ((e = launch_split<kFfnOut>(a, s, nullptr, st)) != cudaSuccess) return e;
+  } else if (a.dx) {
+    ProductSpec s{};
+    s.a[0] = {a.dg, a.f}; s.a[1] = {a.du, a.f}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
+    s.nseg = 2; s.b_mn = true; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
+    w[n++] = s;
+  }
   const auto gradient = [&](const Mat& left, const Mat& right, int M, int N, void* out) {
     ProductSpec s{};
     s.a[0] = left; s.b[0] = right;
