@@ -73,6 +73,7 @@ struct FfnTileArgs {
   float* keep;
   void* out2;                                     // kFfnDGlu: dU (out is dG)
   int* err;
+  int clear_err;                                  // (see FfnSplitArgs)
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -163,6 +164,11 @@ __device__ __forceinline__ void add_rows64(uint4* stg, const uint32_t* w, float*
   __syncwarp();
 }
 
+// Kernels of one call overlap their starts: a kernel may be started when all CTAs of the one before it have begun, and
+// waits for that kernel's end (and for its writes) here.
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_prior_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ---------------------------------------------------------------------------------------------
 // batches: persistent tiles
 // ---------------------------------------------------------------------------------------------
@@ -242,6 +248,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const int worker = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
   const int nworkers = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  wait_for_prior_kernel();
+  launch_dependents();
   const int M0 = g.nrows_dev ? min(*g.nrows_dev, g.p[0].M) : g.p[0].M;
 
   if (threadIdx.x == 0) {
@@ -266,6 +274,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   if (PAIR) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_s;
+  if (g.clear_err && blockIdx.x == 0 && threadIdx.x == 0) *g.err = 0;
 
   TileAt at;
   if (warp == 0) {
@@ -511,15 +520,18 @@ struct FfnSplitArgs {
   void* out2;
   int64_t ldo;
   int* err;
+  int clear_err;                                  // first kernel of a call: the status word starts at zero. A wait gives
+                                                  // up only after millions of polls, long after the first CTA began.
 };
 
 constexpr int kSplitThreads = 256;
 
 template <int BN> struct FfnSplit {
   static constexpr int kABytes = kBM * kBK * 2, kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
-  static constexpr int kFixedBytes = 1024 + 512;
-  static constexpr int kFit = (227 * 1024 - kFixedBytes) / kStageBytes;
-  static constexpr int kStages = kFit > 12 ? 12 : kFit;
+  static constexpr int kFixedBytes = 1024 + 256;
+  // half of an SM's shared memory, so that two CTAs share an SM: clusters of eight are then all resident at once, and
+  // the CTAs of the next product request their weights while the last ones of this product finish
+  static constexpr int kStages = (113 * 1024 - kFixedBytes) / kStageBytes;
   static constexpr int kSmemBytes = kStages * kStageBytes + kFixedBytes;
   static constexpr int kTmemCols = BN < 32 ? 32 : BN;
   static_assert(kStages * kStageBytes >= BN * kBM * 4, "the partial sums fit where the stages were");
@@ -533,7 +545,7 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
 }
 
 template <int BN, int EPI>
-__global__ void __launch_bounds__(kSplitThreads, 1) k_ffn_split(const __grid_constant__ FfnSplitArgs g) {
+__global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_constant__ FfnSplitArgs g) {
   using C = FfnSplit<BN>;
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;   // output columns of a CTA
   extern __shared__ uint8_t smem_raw[];
@@ -568,15 +580,15 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_ffn_split(const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_s;
+  launch_dependents();
 
   if (warp == 0 && lane == 0) {
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
+    auto weights = [&](int kb) {
       uint8_t* sa = stages + stage * C::kStageBytes;
-      const int seg = kb / kb_seg, kk = (kb - seg * kb_seg) * kBK;
+      const int seg = kb >= kb_seg ? 1 : 0, kk = (kb - seg * kb_seg) * kBK;
       mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
       if (EPI == kFfnGlu) {                       // rows 0..63 of the instruction: Wg, rows 64..127: Wu
         tma_load_2d(sa, &g.w[0], kk, n0, full_bar + stage);
@@ -587,7 +599,23 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_ffn_split(const __grid_con
       } else {
         tma_load_2d(sa, &g.w[seg], kk, n0, full_bar + stage);
       }
-      tma_load_2d(sa + C::kABytes, &g.t[EPI == kFfnGlu ? 0 : seg], kk, tok0, full_bar + stage);
+    };
+    auto tokens = [&](int kb) {
+      const int seg = kb >= kb_seg ? 1 : 0, kk = (kb - seg * kb_seg) * kBK;
+      tma_load_2d(stages + stage * C::kStageBytes + C::kABytes, &g.t[seg], kk, tok0, full_bar + stage);
+    };
+    // The kernel before this one writes the tokens, not the weights: the first stages' weights are requested before
+    // it has ended (what ran before that kernel had ended when it began).
+    const int ahead = min(kb1 - kb0, C::kStages);
+    for (int i = 0; i < ahead; ++i) { weights(kb0 + i); ++stage; }
+    wait_for_prior_kernel();
+    for (stage = 0; stage < ahead; ++stage) tokens(kb0 + stage);
+    stage = 0;
+    phase = 1;
+    for (int kb = kb0 + ahead; kb < kb1; ++kb) {
+      if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
+      weights(kb);
+      tokens(kb);
       if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
     }
     if (!ok) {
@@ -621,6 +649,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_ffn_split(const __grid_con
   }
   __syncwarp();
 
+  wait_for_prior_kernel();                        // (nothing in device memory is read or written before)
+  if (g.clear_err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
   // the accumulator to shared memory, [token][row of the instruction]
   const bool ok = mbar_wait_warp(tfull_bar, 0u, abort_s);
   if (ok) {
@@ -715,6 +745,19 @@ int current_device() {
   return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : -1;
 }
 
+// cluster size, and whether the launch may overlap the end of the kernel before it (see wait_for_prior_kernel); the
+// first kernel of a call never does: what it reads may come from any kernel
+int launch_attributes(cudaLaunchAttribute (&attr)[2], int cluster, bool overlap) {
+  attr[0] = cudaLaunchAttribute{};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  if (!overlap) return 1;
+  attr[1] = cudaLaunchAttribute{};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  return 2;
+}
+
 // a kernel's shared-memory limit and the number of its clusters that are resident at once, per device, looked up once
 struct KernelInfo {
   std::atomic<int> resident[kMaxDevices];         // 0: not looked up; else 1 + resident CTAs (clusters of a pair)
@@ -755,7 +798,7 @@ cudaError_t tile_resident(int* n) {
 }
 
 template <int BN, int EPI, bool PAIR>
-cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) {
+cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, bool overlap, cudaStream_t st) {
   using C = FfnTile<BN, PAIR>;
   int resident = 0;
   const cudaError_t e = tile_resident<BN, EPI, PAIR>(&resident);
@@ -766,11 +809,9 @@ cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) 
   cfg.blockDim = dim3(kTileThreads);
   cfg.dynamicSmemBytes = C::kSmemBytes;
   cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = PAIR ? 2 : 1; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  cfg.numAttrs = launch_attributes(attr, PAIR ? 2 : 1, overlap);
   return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR>, g);
 }
 
@@ -804,8 +845,8 @@ inline int ksteps(const ProductSpec& s) { return (s.K + kBK - 1) / kBK * s.nseg;
 // 256 x 256 tiles above that. Several products of one launch: those with the longer tiles come first; there are at most
 // two lengths (specs[0] may differ from the others).
 template <int EPI>
-cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, cudaStream_t st, float* keep = nullptr,
-                         void* out2 = nullptr) {
+cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first, cudaStream_t st,
+                         float* keep = nullptr, void* out2 = nullptr) {
   constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
   if (n > 1 && ksteps(specs[0]) < ksteps(specs[n - 1])) std::swap(specs[0], specs[n - 1]);
   int64_t small = 0, wide = 0;
@@ -815,20 +856,22 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, cudaStream
   }
   const bool pair = small > 148;
   // tiles of the longer class, and how many of the shorter one take as long
-  int first = 1;
-  while (first < n && ksteps(specs[first]) == ksteps(specs[0])) ++first;
+  int longer = 1;
+  while (longer < n && ksteps(specs[longer]) == ksteps(specs[0])) ++longer;
   int64_t na = 0;
-  for (int i = 0; i < first; ++i) na += pair ? tiles_of(specs[i], 256, kWide) : tiles_of(specs[i], 128, kNarrow);
+  for (int i = 0; i < longer; ++i) na += pair ? tiles_of(specs[i], 256, kWide) : tiles_of(specs[i], 128, kNarrow);
   FfnTileArgs g;
   g.np = n;
   g.na = (int)na;
-  g.give = first < n ? (ksteps(specs[0]) + ksteps(specs[n - 1]) / 2) / ksteps(specs[n - 1]) : 0;
+  g.give = longer < n ? (ksteps(specs[0]) + ksteps(specs[n - 1]) / 2) / ksteps(specs[n - 1]) : 0;
   g.f16 = a.f16;
   g.act = a.act;
   g.nrows_dev = a.nrows_dev;
   g.keep = keep;
   g.out2 = out2;
   g.err = a.err;
+  g.clear_err = first && !a.res;
+  const bool overlap = !first;
   for (int i = 0; i < n; ++i) {
     const ProductSpec& s = specs[i];
     FfnProduct& p = g.p[i];
@@ -843,7 +886,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, cudaStream
     }
   }
   if (pair) {
-    const cudaError_t e = launch_tile_t<256, EPI, true>(g, wide, st);
+    const cudaError_t e = launch_tile_t<256, EPI, true>(g, wide, overlap, st);
     if (e != cudaErrorLaunchOutOfResources) return e;
     // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
     for (int i = 0; EPI == kFfnGlu && i < n; ++i)
@@ -851,11 +894,11 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, cudaStream
         if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, specs[i].b_mn, 64))
           return cudaErrorInvalidValue;
   }
-  return launch_tile_t<128, EPI, false>(g, small, st);
+  return launch_tile_t<128, EPI, false>(g, small, overlap, st);
 }
 
 template <int BN, int EPI>
-cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, cudaStream_t st) {
+cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, bool overlap, cudaStream_t st) {
   using C = FfnSplit<BN>;
   static KernelInfo info;
   const int dev = current_device();
@@ -870,11 +913,9 @@ cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, cudaStr
   cfg.blockDim = dim3(kSplitThreads);
   cfg.dynamicSmemBytes = C::kSmemBytes;
   cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = (unsigned)splits; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  cfg.numAttrs = launch_attributes(attr, splits, overlap);
   return cudaLaunchKernelEx(&cfg, k_ffn_split<BN, EPI>, g);
 }
 
@@ -889,10 +930,37 @@ struct SplitSpec {
   int64_t ldo;
 };
 
+inline int ksteps(const SplitSpec& s) { return (s.K + kBK - 1) / kBK * s.nseg; }
+inline int split_tokens(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+// CTAs per tile along K: until two CTAs on every SM read weights, with at least four steps of K each
+inline int split_count(int rows, int tiles, int nkb) {
+  const int bn = split_tokens(rows), tok = (rows + bn - 1) / bn;
+  int s = 1;
+  while (s < 8 && (int64_t)tiles * tok * 2 * s <= 2 * 148 && nkb / (2 * s) >= 4) s *= 2;
+  return s;
+}
+
+// Which form a product of `rows` tokens with N output columns takes: the shorter estimated time, in steps of K of one
+// CTA (about 0.35 us where few CTAs run, 0.3 us for those of a full launch of pairs) plus what a launch and its
+// epilogue cost.
 template <int EPI>
-cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, cudaStream_t st) {
+bool prefer_split(int rows, int N, int nkb) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
-  const int bn = a.rows <= 16 ? 16 : a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
+  if (rows <= 64) return true;                    // half a tile of rows and more would be empty
+  if (rows > 2048) return false;
+  const int tok = (rows + 127) / 128, tiles = (N + TN - 1) / TN;
+  const int splits = split_count(rows, tiles, nkb);
+  const int64_t ctas = (int64_t)tiles * tok * splits;
+  const double split = (double)((ctas + 147) / 148) * ((nkb + splits - 1) / splits) * 0.35 + 2.0 + 0.5 * splits;
+  const int64_t small = (int64_t)tok * tiles, wide = (int64_t)((rows + 255) / 256) * ((N + 2 * TN - 1) / (2 * TN));
+  const double tile = small <= 148 ? nkb * 0.35 + 2.0 : (double)((wide + 73) / 74) * nkb * 0.3 + 4.0;
+  return split < tile;
+}
+
+template <int EPI>
+cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st) {
+  constexpr int TN = EPI == kFfnGlu ? 64 : 128;
+  const int bn = split_tokens(a.rows);
   FfnSplitArgs g;
   g.rows = a.rows; g.N = s.N; g.K = s.K;
   g.nseg = s.nseg; g.w_mn = s.w_mn;
@@ -900,26 +968,21 @@ cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, cuda
   g.keep = keep;
   g.out = s.out; g.out2 = s.out2; g.ldo = s.ldo;
   g.err = a.err;
+  g.clear_err = first;
   const int nw = EPI == kFfnGlu ? 2 : s.nseg;
   for (int k = 0; k < nw; ++k)
     if (!map_operand(&g.w[k], s.w[k], a.f16 != 0, s.N, s.K, s.w_mn, EPI == kFfnGlu ? 64 : 128)) return cudaErrorInvalidValue;
   for (int k = 0; k < s.nseg; ++k)
     if (!map_operand(&g.t[k], s.t[k], a.f16 != 0, a.rows, s.K, false, bn)) return cudaErrorInvalidValue;
-  const int tiles = (s.N + TN - 1) / TN, tok = (a.rows + bn - 1) / bn;
-  const int nkb = (s.K + kBK - 1) / kBK * s.nseg;
-  // enough CTAs that nearly every SM reads weights, with at least four steps of K each
-  int splits = 1;
-  while (splits < 8 && (int64_t)tiles * tok * splits < 120 && nkb / (2 * splits) >= 4) splits *= 2;
+  const int tiles = (s.N + TN - 1) / TN;
+  const int splits = split_count(a.rows, tiles, ksteps(s));
   switch (bn) {
-    case 16: return launch_split_t<16, EPI>(g, tiles, splits, st);
-    case 32: return launch_split_t<32, EPI>(g, tiles, splits, st);
-    case 64: return launch_split_t<64, EPI>(g, tiles, splits, st);
-    default: return launch_split_t<128, EPI>(g, tiles, splits, st);
+    case 16: return launch_split_t<16, EPI>(g, tiles, splits, !first, st);
+    case 32: return launch_split_t<32, EPI>(g, tiles, splits, !first, st);
+    case 64: return launch_split_t<64, EPI>(g, tiles, splits, !first, st);
+    default: return launch_split_t<128, EPI>(g, tiles, splits, !first, st);
   }
 }
-
-// rows up to which the products take the form that reads the weights as the instruction's rows
-constexpr int kSplitRows = 128;
 
 }  // namespace
 
@@ -927,74 +990,88 @@ size_t ffn_keep_floats(int64_t rows, int64_t f) {
   return (size_t)((rows + 31) / 32 * 32) * (size_t)((f + 31) / 32 * 32) * 2;
 }
 
-cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
-  cudaError_t e = cudaMemsetAsync(a.err, 0, sizeof(int), st);
-  if (e != cudaSuccess || a.rows <= 0) return e;
-  if (a.rows <= kSplitRows) {
-    SplitSpec s{};
-    s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.x, a.ldx};
-    s.nseg = 1; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
-    if ((e = launch_split<kFfnGlu>(a, s, a.keep, st)) != cudaSuccess) return e;
-    SplitSpec o{};
-    o.w[0] = {a.wd, a.f}; o.t[0] = {a.h, a.f};
-    o.nseg = 1; o.N = a.d; o.K = a.f; o.out = a.y; o.ldo = a.ldy;
-    return launch_split<kFfnOut>(a, o, nullptr, st);
-  }
+namespace {
+
+// h = act(x Wg^T) * (x Wu^T); y = h Wd^T
+ProductSpec forward_in(const FfnArgs& a) {
   ProductSpec s{};
   s.a[0] = {a.x, a.ldx}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
   s.nseg = 1; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
-  if ((e = launch_tiles<kFfnGlu>(a, &s, 1, st, a.keep)) != cudaSuccess) return e;
-  ProductSpec o{};
-  o.a[0] = {a.h, a.f}; o.b[0] = {a.wd, a.f};
-  o.nseg = 1; o.M = a.rows; o.N = a.d; o.K = a.f; o.out = a.y; o.ldo = a.ldy;
-  return launch_tiles<kFfnOut>(a, &o, 1, st);
+  return s;
+}
+ProductSpec forward_out(const FfnArgs& a, void* out, int64_t ldo) {
+  ProductSpec s{};
+  s.a[0] = {a.h, a.f}; s.b[0] = {a.wd, a.f};
+  s.nseg = 1; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = out; s.ldo = ldo;
+  return s;
+}
+
+inline int steps(int k) { return (k + kBK - 1) / kBK; }
+
+}  // namespace
+
+cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
+  if (a.rows <= 0) return cudaMemsetAsync(a.err, 0, sizeof(int), st);
+  cudaError_t e;
+  if (prefer_split<kFfnGlu>(a.rows, a.f, steps(a.d))) {
+    SplitSpec s{};
+    s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.x, a.ldx};
+    s.nseg = 1; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
+    e = launch_split<kFfnGlu>(a, s, a.keep, true, st);
+  } else {
+    ProductSpec s = forward_in(a);
+    e = launch_tiles<kFfnGlu>(a, &s, 1, true, st, a.keep);
+  }
+  if (e != cudaSuccess) return e;
+  if (prefer_split<kFfnOut>(a.rows, a.d, steps(a.f))) {
+    SplitSpec s{};
+    s.w[0] = {a.wd, a.f}; s.t[0] = {a.h, a.f};
+    s.nseg = 1; s.N = a.d; s.K = a.f; s.out = a.y; s.ldo = a.ldy;
+    return launch_split<kFfnOut>(a, s, nullptr, false, st);
+  }
+  ProductSpec s = forward_out(a, a.y, a.ldy);
+  return launch_tiles<kFfnOut>(a, &s, 1, false, st);
 }
 
 cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaSuccess;
-  ProductSpec s{};
-  s.a[0] = {a.x, a.ldx}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
-  s.nseg = 1; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.h; s.ldo = a.f;
-  const cudaError_t e = launch_tiles<kFfnGlu>(a, &s, 1, st);
-  if (e != cudaSuccess) return e;
-  ProductSpec o{};
-  o.a[0] = {a.h, a.f}; o.b[0] = {a.wd, a.f};
-  o.nseg = 1; o.M = a.rows; o.N = a.d; o.K = a.f; o.out = a.res; o.ldo = a.d;
-  return launch_tiles<kFfnAdd>(a, &o, 1, st);
+  ProductSpec in = forward_in(a), out = forward_out(a, a.res, a.d);
+  const cudaError_t e = launch_tiles<kFfnGlu>(a, &in, 1, true, st);
+  return e != cudaSuccess ? e : launch_tiles<kFfnAdd>(a, &out, 1, false, st);
 }
 
 cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
-  const size_t wbytes = (size_t)a.d * a.f * 2;
-  cudaError_t e = cudaMemsetAsync(a.err, 0, sizeof(int), st);
-  if (e != cudaSuccess) return e;
+  cudaError_t e = cudaSuccess;
   if (a.rows <= 0) {                              // an empty sum: the weights' gradients are zeros
+    if ((e = cudaMemsetAsync(a.err, 0, sizeof(int), st)) != cudaSuccess) return e;
     for (void* w : {a.dwg, a.dwu, a.dwd})
-      if (w && (e = cudaMemsetAsync(w, 0, wbytes, st)) != cudaSuccess) return e;
+      if (w && (e = cudaMemsetAsync(w, 0, (size_t)a.d * a.f * 2, st)) != cudaSuccess) return e;
     return cudaSuccess;
   }
-  const bool few = a.rows <= kSplitRows;
+  bool first = true;
   if (a.dx || a.dwg || a.dwu) {                   // dH = dy Wd, dG and dU
-    if (few) {
+    if (prefer_split<kFfnDGlu>(a.rows, a.f, steps(a.d))) {
       SplitSpec s{};
       s.w[0] = {a.wd, a.f}; s.t[0] = {a.dy, a.lddy};
       s.nseg = 1; s.w_mn = true; s.N = a.f; s.K = a.d; s.out = a.dg; s.out2 = a.du; s.ldo = a.f;
-      e = launch_split<kFfnDGlu>(a, s, a.keep, st);
+      e = launch_split<kFfnDGlu>(a, s, a.keep, first, st);
     } else {
       ProductSpec s{};
       s.a[0] = {a.dy, a.lddy}; s.b[0] = {a.wd, a.f};
       s.nseg = 1; s.b_mn = true; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.dg; s.ldo = a.f;
-      e = launch_tiles<kFfnDGlu>(a, &s, 1, st, a.keep, a.du);
+      e = launch_tiles<kFfnDGlu>(a, &s, 1, first, st, a.keep, a.du);
     }
     if (e != cudaSuccess) return e;
+    first = false;
   }
   // the gradients of x and of the weights read the same dG and dU: one launch where x's product takes tiles too
   ProductSpec w[4];
   int n = 0;
-  if (a.dx && few) {
+  if (a.dx && prefer_split<kFfnOut>(a.rows, a.d, 2 * steps(a.f))) {
     SplitSpec s{};
     s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.dg, a.f}; s.t[1] = {a.du, a.f};
     s.nseg = 2; s.w_mn = true; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
-    if ((e = launch_split<kFfnOut>(a, s, nullptr, st)) != cudaSuccess) return e;
+    if ((e = launch_split<kFfnOut>(a, s, nullptr, false, st)) != cudaSuccess) return e;
   } else if (a.dx) {
     ProductSpec s{};
     s.a[0] = {a.dg, a.f}; s.a[1] = {a.du, a.f}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
@@ -1010,7 +1087,7 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
   if (a.dwg) gradient({a.dg, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwg);
   if (a.dwu) gradient({a.du, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwu);
   if (a.dwd) gradient({a.dy, a.lddy}, {a.h, a.f}, a.d, a.f, a.dwd);
-  return n > 0 ? launch_tiles<kFfnOut>(a, w, n, st) : cudaSuccess;
+  return n > 0 ? launch_tiles<kFfnOut>(a, w, n, first, st) : cudaSuccess;
 }
 
 }  // namespace sds
