@@ -10,9 +10,9 @@
 // walks over rows with the weights in registers, so that they are read once per group and not once per row.
 // The next row is requested before the current one is reduced.
 //
-// The mean is rounded to 32 bits, which for rows far from zero is an error that every element shares. The second
-// reduction therefore also sums x - mean (exact differences) and the remainder c0 is taken off every element; the
-// backward pass does the same in its one reduction.
+// Rows may lie far from zero, where a mean rounded to 32 bits is off by an error that every element shares. The sums are
+// therefore taken around a number p near the row's elements (exact differences), and the remainder c0 = <x - p> is
+// taken off every element; the backward pass does the same with p = the stored mean.
 //
 // Gradients of the weights: a CTA keeps the sums of its columns in registers over all rows it visits and stores
 // them once; a second kernel adds the CTAs' sums in a fixed order (no atomics: same bits on every run).
@@ -20,6 +20,8 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "../../include/sds.h"
 #include "sds_layers.h"
@@ -48,6 +50,75 @@ template <> struct Conv<F16> {
 // V consecutive elements as one access of sizeof(T) * V bytes
 template <class T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 
+// two floats in one instruction (the kernels below would otherwise be bound by issue, not by memory)
+__device__ __forceinline__ unsigned long long bits(float2 v) { return *reinterpret_cast<unsigned long long*>(&v); }
+__device__ __forceinline__ float2 floats(unsigned long long v) { return *reinterpret_cast<float2*>(&v); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return floats(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return floats(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+  return floats(r);
+}
+// the same operations on single floats, for rows that are not aligned
+__device__ __forceinline__ float add2(float a, float b) { return a + b; }
+__device__ __forceinline__ float mul2(float a, float b) { return a * b; }
+__device__ __forceinline__ float fma2(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float total(float2 v) { return v.x + v.y; }
+__device__ __forceinline__ float total(float v) { return v; }
+
+// what a vector of V elements is worked on in: pairs, or its single element
+template <int V> struct Unit {
+  using type = float2;
+  static constexpr int count = V / 2;
+  __device__ static float2 all(float v) { return make_float2(v, v); }
+};
+template <> struct Unit<1> {
+  using type = float;
+  static constexpr int count = 1;
+  __device__ static float all(float v) { return v; }
+};
+template <int V> using unit_t = typename Unit<V>::type;
+template <int V> constexpr int units = Unit<V>::count;
+
+template <int V> using if_vector = typename std::enable_if<(V > 1)>::type;
+
+// unit k of a pack
+template <class T> __device__ __forceinline__ float get2(const Pack<T, 1>& p, int) { return Conv<T>::get(p.v[0]); }
+template <int V, class = if_vector<V>>
+__device__ __forceinline__ float2 get2(const Pack<float, V>& p, int k) { return make_float2(p.v[2 * k], p.v[2 * k + 1]); }
+template <int V, class = if_vector<V>>
+__device__ __forceinline__ float2 get2(const Pack<Bf16, V>& p, int k) {
+  const uint32_t w = reinterpret_cast<const uint32_t*>(p.v)[k];
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <int V, class = if_vector<V>>
+__device__ __forceinline__ float2 get2(const Pack<F16, V>& p, int k) {
+  const uint32_t w = reinterpret_cast<const uint32_t*>(p.v)[k];
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <class T> __device__ __forceinline__ void put2(Pack<T, 1>& p, int, float v) { p.v[0] = Conv<T>::put(v); }
+template <int V, class = if_vector<V>>
+__device__ __forceinline__ void put2(Pack<float, V>& p, int k, float2 v) { p.v[2 * k] = v.x; p.v[2 * k + 1] = v.y; }
+template <int V, class = if_vector<V>>
+__device__ __forceinline__ void put2(Pack<Bf16, V>& p, int k, float2 v) {
+  const __nv_bfloat162 h = __float22bfloat162_rn(v);
+  reinterpret_cast<uint32_t*>(p.v)[k] = *reinterpret_cast<const uint32_t*>(&h);
+}
+template <int V, class = if_vector<V>>
+__device__ __forceinline__ void put2(Pack<F16, V>& p, int k, float2 v) {
+  const __half2 h = __float22half2_rn(v);
+  reinterpret_cast<uint32_t*>(p.v)[k] = *reinterpret_cast<const uint32_t*>(&h);
+}
+
 // a column vector of any of the three types, read once per thread group
 __device__ __forceinline__ float load_any(const void* p, int type, size_t i) {
   if (type == SDS_F32) return static_cast<const float*>(p)[i];
@@ -60,59 +131,144 @@ __device__ __forceinline__ void store_any(void* p, int type, size_t i, float v) 
   else static_cast<F16*>(p)[i] = Conv<F16>::put(v);
 }
 
-// sum of N values over the TPR threads of a row's group, the result in every thread. `slot`: shared memory of the
-// group, N * (TPR / 32) floats, not reused before the group's next barrier.
-template <int TPR, int N>
+// Sums of N <= 4 values over the TPR threads of a row's group, in every thread. Inside a warp the values are folded into
+// one another while they are summed (a lane keeps the value its number selects: 3 values take 6 shuffles, not 15).
+// Between the warps: slot, shared memory of the group, 4 * TPR / 32 floats, not written again before the group has
+// passed another barrier. CL > 1: the group is spread over a cluster of CL CTAs, every warp's sums go to all of
+// them. The order of the additions is fixed.
+template <int TPR, int N, int CL = 1>
 __device__ __forceinline__ void group_sum(float (&v)[N], float* slot, int t, int bar) {
+  constexpr unsigned kAll = 0xffffffffu;
   constexpr int W = TPR < 32 ? TPR : 32;
+  constexpr int F = N == 1 ? 1 : N == 2 ? 2 : 4;                // values folded over F neighbouring lanes
+  const int lane = t & 31;
+  float x = v[0];
+  if (F >= 2) {
+    const bool odd = lane & 1;
+    const float v1 = v[N > 1 ? 1 : 0];
+    x = (odd ? v1 : v[0]) + __shfl_xor_sync(kAll, odd ? v[0] : v1, 1);
+    if (F == 4) {
+      const float v2 = v[N > 2 ? 2 : 0], v3 = N > 3 ? v[N > 3 ? 3 : 0] : 0.f;
+      const float y = (odd ? v3 : v2) + __shfl_xor_sync(kAll, odd ? v2 : v3, 1);
+      const bool high = lane & 2;
+      x = (high ? y : x) + __shfl_xor_sync(kAll, high ? x : y, 2);
+    }
+  }
 #pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1)
+  for (int o = F; o < W; o <<= 1) x += __shfl_xor_sync(kAll, x, o);
+  if (TPR <= 32) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
-  if (TPR > 32) {
-    constexpr int NW = TPR > 32 ? TPR / 32 : 1;
-    if ((t & 31) == 0)
+    for (int n = 0; n < N; ++n) v[n] = F == 1 ? x : __shfl_sync(kAll, x, n, W);
+  } else {
+    constexpr int NW = TPR > 32 ? TPR / 32 : 2;
+    if (CL > 1) {
+      if (lane < N) {
+        const uint32_t mine = (uint32_t)__cvta_generic_to_shared(slot + lane * NW + (t >> 5));
 #pragma unroll
-      for (int n = 0; n < N; ++n) slot[n * NW + (t >> 5)] = v[n];
-    asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(TPR) : "memory");
+        for (int c = 0; c < CL; ++c) {
+          uint32_t to;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine), "r"(c));
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(x) : "memory");
+        }
+      }
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+      if (lane < N) slot[lane * NW + (t >> 5)] = x;
+      asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(TPR) : "memory");
+    }
+    if (NW <= 8) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      float s = slot[n * NW + ((t & 31) & (NW - 1))];
+      for (int n = 0; n < N; ++n) {
+        float s = 0.f;
 #pragma unroll
-      for (int o = NW / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      v[n] = s;
+        for (int w = 0; w < NW; w += 2) {
+          const float2 q = *reinterpret_cast<const float2*>(slot + n * NW + w);
+          s += q.x + q.y;
+        }
+        v[n] = s;
+      }
+    } else {                                                    // eight lanes add one value's NW sums
+      const int n8 = lane >> 3;
+      float s = 0.f;
+      if (n8 < N)
+#pragma unroll
+        for (int w = 0; w < NW / 8; ++w) s += slot[n8 * NW + (lane & 7) * (NW / 8) + w];
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(kAll, s, o);
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] = __shfl_sync(kAll, s, n * 8);
     }
   }
 }
 
-// threads of a row's group and elements per thread; groups of up to 128 threads share a CTA of 256
-template <int TPR> constexpr int norm_cta = TPR < 256 ? 256 : TPR;
+// Where the columns of a group's thread t lie. A row: vector i, element u = column (i * TPR + t) * V + u. Shared memory: quads
+// of a thread's columns, T quads side by side (T threads of the group in this CTA), so that 128-bit accesses are free
+// of bank conflicts.
+template <int T, int V>
+__device__ __forceinline__ int slot_of(int i, int u, int t) {
+  return V == 1 ? i * T + t : ((i * (V / 4) + (u >> 2)) * T + t) * 4 + (u & 3);
+}
+template <int T, int V, class = if_vector<V>>
+__device__ __forceinline__ void load_cols(const float* s, int i, int t, float2 (&o)[units<V>]) {
+#pragma unroll
+  for (int q = 0; q < V / 4; ++q) {
+    const float4 v = *reinterpret_cast<const float4*>(s + slot_of<T, V>(i, 4 * q, t));
+    o[2 * q] = make_float2(v.x, v.y);
+    o[2 * q + 1] = make_float2(v.z, v.w);
+  }
+}
+template <int T, int V>
+__device__ __forceinline__ void load_cols(const float* s, int i, int t, float (&o)[1]) { o[0] = s[slot_of<T, V>(i, 0, t)]; }
+// a column vector of the caller's as floats in that order (`fill` where there is none). t0: the group's first thread in
+// this CTA.
+template <int TPR, int T, int E, int V>
+__device__ __forceinline__ void stage_cols(float* s, const void* p, int type, float fill, int d, int threads, int t0) {
+  for (int k = threadIdx.x; k < T * E; k += threads) {
+    const int vec = k / V, i = vec / T, t = vec % T, u = k % V;
+    const int c = (i * TPR + t0 + t) * V + u;
+    s[slot_of<T, V>(i, u, t)] = (p && c < d) ? load_any(p, type, c) : fill;
+  }
+}
+// unit k of vector i, straight from the caller's column vector
+template <int V>
+__device__ __forceinline__ unit_t<V> col_unit(const void* p, int type, float fill, int c, int d) {
+  unit_t<V> r = Unit<V>::all(fill);
+  if (p && c < d) {
+    float* f = reinterpret_cast<float*>(&r);
+    f[0] = load_any(p, type, c);
+    if (V > 1) f[V > 1 ? 1 : 0] = load_any(p, type, c + 1);   // (vectors only where d is a multiple of theirs)
+  }
+  return r;
+}
 
-template <class TX, class TY, int TPR, int E, bool VEC, bool RES>
-__global__ void __launch_bounds__(norm_cta<TPR>) k_norm(const NormArgs a) {
-  constexpr int RPC = norm_cta<TPR> / TPR;                    // rows of a CTA at a time
-  constexpr int V = VEC ? (sizeof(TX) == 4 ? 4 : 8) : 1;
-  constexpr int NV = E / V;
+template <class TX> constexpr int vec_len = sizeof(TX) == 4 ? 4 : 8;   // elements of a 16-byte access
+
+// FEW: at most one row or two for every group of the launch. The weights are then read with the first row, into
+// registers; else they are brought to shared memory once and read from there for every row. 16-bit rows up to 4096: three
+// CTAs per SM (16384 x 2048 bf16: 27.4 us against 30.3 with the two that the compiler's own register count gives; float
+// rows 37.2 against 39.6 the other way round).
+template <class TX, class TY, int TPR, int E, bool VEC, bool RES, bool FEW>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && sizeof(TX) == 2 ? 3 : 1)
+    k_norm(const NormArgs a) {
+  constexpr int CTA = TPR < 256 ? 256 : TPR, RPC = CTA / TPR;   // RPC: rows of a CTA at a time
+  constexpr int V = VEC ? vec_len<TX> : 1;
+  constexpr int NV = E / V, P = units<V>;
   constexpr int NW = TPR > 32 ? TPR / 32 : 1;
-  __shared__ float slots[RPC * 3 * NW];
-  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  float* slot = slots + sub * 3 * NW;
-  const int rows = a.nrows_dev ? min(*a.nrows_dev, a.rows) : a.rows;
-  const int d = a.d;
-  const float inv_d = 1.0f / (float)d;
+  using U = unit_t<V>;
   using PX = Pack<TX, V>;
   using PY = Pack<TY, V>;
-  float w[E], b[E];
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int u = 0; u < V; ++u) {
-      const int c = (i * TPR + t) * V + u;
-      w[i * V + u] = (a.w && c < d) ? load_any(a.w, a.tw, c) : 1.0f;
-      b[i * V + u] = (a.b && c < d) ? load_any(a.b, a.tw, c) : 0.0f;
-    }
+  extern __shared__ float4 shared[];                            // weights [2][TPR * E] (not FEW)
+  float* w_s = reinterpret_cast<float*>(shared);
+  float* b_s = w_s + TPR * E;
+  __shared__ __align__(16) float slots[2 * RPC * 4 * NW];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float* slot = slots + sub * 8 * NW;
+  const int rows = a.nrows_dev ? min(*a.nrows_dev, a.rows) : a.rows;
+  const int d = a.d, step = (int)gridDim.x * RPC;
+  const float inv_d = 1.0f / (float)d;
   PX nxt[NV];
-  auto fetch = [&](int row) {
+  const auto fetch = [&](int row) {
     const TX* xr = static_cast<const TX*>(a.x) + (size_t)row * a.ldx;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -122,52 +278,64 @@ __global__ void __launch_bounds__(norm_cta<TPR>) k_norm(const NormArgs a) {
     }
   };
   int base = blockIdx.x * RPC;
-  if (base < rows) fetch(base + sub);
-  for (; base < rows; base += gridDim.x * RPC) {
-    const int row = base + sub;
-    const bool live = row < rows;
-    float x[E];
+  fetch(base + sub);
+  U wr[FEW ? NV : 1][P], br[FEW ? NV : 1][P];
+  if (FEW) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int u = 0; u < V; ++u) x[i * V + u] = Conv<TX>::get(nxt[i].v[u]);
-    if (RES && live) {                                          // x + temb[k], kept as the residual stream
-      const uint16_t* te = a.temb ? a.temb + (size_t)__ldg(a.rowk + row) * d : nullptr;
-      float* rr = a.res + (size_t)row * d;
+      for (int k = 0; k < P; ++k) {
+        wr[FEW ? i : 0][k] = col_unit<V>(a.w, a.tw, 1.0f, (i * TPR + t) * V + 2 * k, d);
+        br[FEW ? i : 0][k] = col_unit<V>(a.b, a.tw, 0.0f, (i * TPR + t) * V + 2 * k, d);
+      }
+  } else {
+    stage_cols<TPR, TPR, E, V>(w_s, a.w, a.tw, 1.0f, d, CTA, 0);
+    stage_cols<TPR, TPR, E, V>(b_s, a.b, a.tw, 0.0f, d, CTA, 0);
+    __syncthreads();
+  }
+  for (; base < rows; base += step) {
+    const int row = base + sub;
+    const bool live = row < rows;
+    U x[NV][P];
+    U s0 = Unit<V>::all(0.f);
+    const uint16_t* te = RES && live && a.temb ? a.temb + (size_t)__ldg(a.rowk + row) * d : nullptr;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + t) * V;
-        if (c < d) {
-          Pack<float, V> o;
-          if (te) {
-            const Pack<Bf16, V> e = *reinterpret_cast<const Pack<Bf16, V>*>(te + c);
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + t) * V;
+      if (RES && live && c < d) {                               // x + temb[k], kept as the residual stream
+        if (te) {
+          const Pack<Bf16, V> e = *reinterpret_cast<const Pack<Bf16, V>*>(te + c);
 #pragma unroll
-            for (int u = 0; u < V; ++u) x[i * V + u] += Conv<Bf16>::get(e.v[u]);
-          }
+          for (int k = 0; k < P; ++k) put2(nxt[i], k, add2(get2(nxt[i], k), get2(e, k)));
+        }
+        *reinterpret_cast<PX*>(a.res + (size_t)row * d + c) = nxt[i];
+      }
 #pragma unroll
-          for (int u = 0; u < V; ++u) o.v[u] = x[i * V + u];
-          *reinterpret_cast<Pack<float, V>*>(rr + c) = o;
+      for (int k = 0; k < P; ++k) x[i][k] = get2(nxt[i], k);
+    }
+    fetch(row + step);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < P; ++k) s0 = add2(s0, x[i][k]);       // (elements past d hold zeros)
+    float s[1] = {total(s0)};
+    group_sum<TPR, 1>(s, slot, t, 1 + sub);
+    const float mean = __fmul_rn(s[0], inv_d);                  // (a rounded number: the same one with and without statistics)
+    const U minus = Unit<V>::all(-mean);
+    U q0 = Unit<V>::all(0.f), q1 = q0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if ((i * TPR + t) * V < d) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          x[i][k] = add2(x[i][k], minus);
+          q0 = add2(q0, x[i][k]);
+          q1 = fma2(x[i][k], x[i][k], q1);
         }
       }
     }
-    fetch(row + gridDim.x * RPC);
-    float s[1] = {0.f};
-#pragma unroll
-    for (int e = 0; e < E; ++e) s[0] += x[e];                   // (elements past d hold zeros)
-    group_sum<TPR, 1>(s, slot, t, 1 + sub);
-    const float mean = __fmul_rn(s[0], inv_d);                  // (a rounded number: the same one with and without statistics)
-    float q[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const bool in = (i * TPR + t) * V < d;
-#pragma unroll
-      for (int u = 0; u < V; ++u) {
-        const float c = x[i * V + u] - mean;
-        x[i * V + u] = c;
-        if (in) { q[0] += c; q[1] = fmaf(c, c, q[1]); }
-      }
-    }
-    group_sum<TPR, 2>(q, slot + NW, t, 1 + sub);
+    float q[2] = {total(q0), total(q1)};
+    group_sum<TPR, 2>(q, slot + 4 * NW, t, 1 + sub);
     const float c0 = __fmul_rn(q[0], inv_d);
     const float rstd = rsqrtf(fmaxf(fmaf(-c0, c0, q[1] * inv_d), 0.f) + a.eps);
     if (!live) continue;
@@ -176,13 +344,20 @@ __global__ void __launch_bounds__(norm_cta<TPR>) k_norm(const NormArgs a) {
       if (a.rstd) a.rstd[row] = rstd;
     }
     TY* yr = static_cast<TY*>(a.y) + (size_t)row * a.ldy;
+    const U scale = Unit<V>::all(rstd), shift = Unit<V>::all(-c0 * rstd);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
       if (c < d) {
+        U w[P], b[P];
+        if (!FEW) {
+          load_cols<TPR, V>(w_s, i, t, w);
+          load_cols<TPR, V>(b_s, i, t, b);
+        }
         PY o;
 #pragma unroll
-        for (int u = 0; u < V; ++u) o.v[u] = Conv<TY>::put(fmaf((x[i * V + u] - c0) * rstd, w[i * V + u], b[i * V + u]));
+        for (int k = 0; k < P; ++k)
+          put2(o, k, fma2(fma2(x[i][k], scale, shift), FEW ? wr[FEW ? i : 0][k] : w[k], FEW ? br[FEW ? i : 0][k] : b[k]));
         *reinterpret_cast<PY*>(yr + c) = o;
       }
     }
@@ -222,140 +397,190 @@ __global__ void __launch_bounds__(1024) k_norm_long(const NormArgs a) {
   }
 }
 
-// Backward. SMEM: the CTA's weight-gradient sums live in shared memory (rows so long that a thread holds 16
-// elements: x, dy and two sums of 16 would not fit the 64 registers a thread of 1024 has), else in registers.
-template <class TX, class TY, int TPR, int E, bool VEC, bool SMEM>
-__global__ void __launch_bounds__(norm_cta<TPR>) k_norm_bwd(const NormArgs a) {
-  constexpr int CTA = norm_cta<TPR>, RPC = CTA / TPR;
-  constexpr int V = VEC ? (sizeof(TX) == 4 ? 4 : 8) : 1;
-  constexpr int NV = E / V;
+// Copies of a thread's own vectors into shared memory, asynchronous and in groups: a thread reads back only what it
+// asked for itself, so no barrier is needed. `in` false: zeros.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src, bool in) {
+  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+  const int n = in ? BYTES : 0;
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES < 4 ? 4 : BYTES), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+constexpr int kSmem = 226 * 1024;                               // of an SM's 227 KB a CTA may have
+
+// TPR threads per row, CL CTAs of them; CTAs of 512 threads (fewer CTAs, fewer partial sums for the second kernel to
+// add up) that hold 512 / TPR rows at a time, or half a row each
+template <class TX, class TY, int TPR, int E, bool VEC, int CL> struct NormBwd {
+  static constexpr int kT = TPR / CL, kCta = 512, kGroups = kCta / kT;
+  static constexpr int kWeights = kT * E * 4;
+  // rows in flight: a group keeps kRing rows in shared memory, kRing - 1 of them on their way while one is worked on
+  static constexpr int kRow = VEC ? kT * E * (int)(sizeof(TX) + sizeof(TY)) : 0;
+  static constexpr int kFit = VEC ? (kSmem - kWeights) / (kRow * kGroups + (VEC ? 0 : 1)) : 2;
+  static constexpr int kRing = kFit > 4 ? 4 : kFit;
+  static constexpr int kJoin = kGroups > 1 ? kGroups * 2 * TPR * E * 4 : 0;   // the groups' sums, where the ring was
+  static constexpr int kRingBytes = kRing * kRow * kGroups;
+  static constexpr int kSmemBytes = kWeights + (kRingBytes > kJoin ? kRingBytes : kJoin);
+  static_assert(kRing >= 2 && kSmemBytes <= kSmem && kGroups * CL <= 64, "shared memory");
+};
+
+// Backward. The sums of the weights' gradients stay in registers over all rows of a group, the weights in shared
+// memory; the rows of x and dy pass through a ring there and are held as floats between the two passes.
+template <class TX, class TY, int TPR, int E, bool VEC, int CL>
+__global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
+  using C = NormBwd<TX, TY, TPR, E, VEC, CL>;
+  constexpr int CTA = C::kCta, RPC = C::kGroups, R = C::kRing, T = C::kT;
+  constexpr int V = VEC ? vec_len<TX> : 1;
+  constexpr int NV = E / V, P = units<V>;
   constexpr int NW = TPR > 32 ? TPR / 32 : 1;
-  constexpr int AE = SMEM ? 1 : E;
-  extern __shared__ float acc_s[];                              // SMEM: [2][TPR * E]; else [RPC][2][TPR * E] if RPC > 1
-  __shared__ float slots[2 * RPC * 3 * NW];
-  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const int rows = a.rows, d = a.d;
-  const float inv_d = 1.0f / (float)d;
-  const bool want_w = a.dw || a.db;
+  using U = unit_t<V>;
   using PX = Pack<TX, V>;
   using PY = Pack<TY, V>;
-  float w[AE], dw[AE], db[AE];
+  extern __shared__ float4 shared[];                            // weights [T * E], then the ring
+  float* w_s = reinterpret_cast<float*>(shared);
+  uint8_t* rest = reinterpret_cast<uint8_t*>(shared) + C::kWeights;
+  __shared__ __align__(16) float slots[2 * RPC * 4 * NW];
+  const int rank = CL > 1 ? (int)(blockIdx.x % CL) : 0;         // this CTA's part of the row
+  const int tl = threadIdx.x % T, sub = threadIdx.x / T, t = rank * T + tl;
+  const int rows = a.rows, d = a.d, groups = (int)gridDim.x / CL, step = groups * RPC;
+  const float inv_d = 1.0f / (float)d;
+  PX* ring_x = reinterpret_cast<PX*>(rest + (size_t)sub * R * C::kRow) + tl;
+  PY* ring_y = reinterpret_cast<PY*>(rest + (size_t)sub * R * C::kRow + (size_t)R * T * E * sizeof(TX)) + tl;
+  U dw[NV][P], db[NV][P];
 #pragma unroll
-  for (int e = 0; e < AE; ++e) { w[e] = 1.0f; dw[e] = db[e] = 0.f; }
-  if (!SMEM) {
+  for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int u = 0; u < V; ++u) {
-        const int c = (i * TPR + t) * V + u;
-        if (a.w && c < d) w[(i * V + u) % AE] = load_any(a.w, a.tw, c);
-      }
-  } else {
-    for (int i = t; i < 2 * TPR * E; i += CTA) acc_s[i] = 0.f;
-    __syncthreads();
-  }
-  PX xn[NV];
-  PY yn[NV];
-  float mean_n = 0.f, rstd_n = 0.f;
-  auto fetch = [&](int row) {
-    const TX* xr = static_cast<const TX*>(a.x) + (size_t)row * a.ldx;
-    const TY* yr = static_cast<const TY*>(a.dy) + (size_t)row * a.lddy;
-    const bool in = row < rows;
-    mean_n = in ? __ldg(a.mean + row) : 0.f;
-    rstd_n = in ? __ldg(a.rstd + row) : 0.f;
+    for (int k = 0; k < P; ++k) dw[i][k] = db[i][k] = Unit<V>::all(0.f);
+  const auto fetch = [&](int64_t row, int r) {
+    if (!VEC) return;
+    const bool live = row < rows;
+    const TX* xr = static_cast<const TX*>(a.x) + (live ? row : 0) * a.ldx;
+    const TY* yr = static_cast<const TY*>(a.dy) + (live ? row : 0) * a.lddy;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
-      if (in && c < d) {
-        xn[i] = *reinterpret_cast<const PX*>(xr + c);
-        yn[i] = *reinterpret_cast<const PY*>(yr + c);
-      } else {
-        xn[i] = PX{};
-        yn[i] = PY{};
-      }
+      const bool in = live && c < d;
+      copy_async<sizeof(PX)>(ring_x + (r * NV + i) * T, xr + (in ? c : 0), in);
+      copy_async<sizeof(PY)>(ring_y + (r * NV + i) * T, yr + (in ? c : 0), in);
     }
+    copies_commit();
   };
-  int base = blockIdx.x * RPC, flip = 0;
-  if (base < rows) fetch(base + sub);
-  for (; base < rows; base += gridDim.x * RPC, flip ^= 1) {
+  const auto stats_of = [&](int64_t row) {
+    return row < rows ? make_float2(__ldg(a.mean + row), __ldg(a.rstd + row)) : make_float2(0.f, 0.f);
+  };
+  int base = (int)blockIdx.x / CL * RPC, flip = 0, at = 0;
+#pragma unroll
+  for (int r = 0; r < R - 1; ++r) fetch((int64_t)base + sub + (int64_t)r * step, r);
+  float2 stats = stats_of(base + sub);
+  stage_cols<TPR, T, E, V>(w_s, a.w, a.tw, 1.0f, d, CTA, rank * T);
+  __syncthreads();
+  if (CL > 1) {                                                 // the peers run before anything is written to them
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  for (; base < rows; base += step, flip ^= 1) {
     const int row = base + sub;
     const bool live = row < rows;
-    const float mean = mean_n, rstd = rstd_n;
-    PX xp[NV];
-    PY yp[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) { xp[i] = xn[i]; yp[i] = yn[i]; }
-    if (!SMEM) fetch(row + gridDim.x * RPC);
-    float q[3] = {0.f, 0.f, 0.f};                               // sums of x - mean, w dy, w dy (x - mean)
+    const float mean = stats.x, rstd = stats.y;
+    const U minus = Unit<V>::all(-mean);
+    const TX* xr = static_cast<const TX*>(a.x) + (size_t)row * a.ldx;
+    const TY* yr = static_cast<const TY*>(a.dy) + (size_t)row * a.lddy;
+    if (VEC) copies_wait<R - 2>();
+    U xc[NV][P], yf[NV][P];
+    U q0 = Unit<V>::all(0.f), q1 = q0, q2 = q0;                 // sums of x - mean, w dy, w dy (x - mean)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
       if (c < d) {
+        PX px{};
+        PY py{};
+        if (VEC) {
+          px = ring_x[(at * NV + i) * T];
+          py = ring_y[(at * NV + i) * T];
+        } else if (live) {
+          px = *reinterpret_cast<const PX*>(xr + c);
+          py = *reinterpret_cast<const PY*>(yr + c);
+        }
+        U w[P];
+        load_cols<T, V>(w_s, i, tl, w);
 #pragma unroll
-        for (int u = 0; u < V; ++u) {
-          const float xc = Conv<TX>::get(xp[i].v[u]) - mean;
-          const float we = SMEM ? (a.w ? load_any(a.w, a.tw, c + u) : 1.0f) : w[(i * V + u) % AE];
-          const float g = Conv<TY>::get(yp[i].v[u]) * we;
-          q[0] += xc;
-          q[1] += g;
-          q[2] = fmaf(g, xc, q[2]);
+        for (int k = 0; k < P; ++k) {
+          xc[i][k] = add2(get2(px, k), minus);
+          yf[i][k] = get2(py, k);
+          const U g = mul2(yf[i][k], w[k]);
+          q0 = add2(q0, xc[i][k]);
+          q1 = add2(q1, g);
+          q2 = fma2(g, xc[i][k], q2);
         }
       }
     }
-    group_sum<TPR, 3>(q, slots + (flip * RPC + sub) * 3 * NW, t, 1 + sub);
+    stats = stats_of((int64_t)row + step);
+    fetch((int64_t)row + (int64_t)(R - 1) * step, at == 0 ? R - 1 : at - 1);
+    float q[3] = {total(q0), total(q1), total(q2)};
+    group_sum<TPR, 3, CL>(q, slots + (flip * RPC + sub) * 4 * NW, t, 1 + sub);
     const float c0 = __fmul_rn(q[0], inv_d), c1 = __fmul_rn(q[1], inv_d), c2 = rstd * fmaf(-c0, c1, q[2] * inv_d);
     TX* dxr = static_cast<TX*>(a.dx) + (size_t)row * a.lddx;
+    const U scale = Unit<V>::all(rstd), shift = Unit<V>::all(-c0 * rstd), less = Unit<V>::all(-c1), slope = Unit<V>::all(-c2);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
       if (live && c < d) {
+        U w[P];
+        load_cols<T, V>(w_s, i, tl, w);
         PX o;
 #pragma unroll
-        for (int u = 0; u < V; ++u) {
-          const float xhat = (Conv<TX>::get(xp[i].v[u]) - mean - c0) * rstd;
-          const float dy = Conv<TY>::get(yp[i].v[u]);
-          const float we = SMEM ? (a.w ? load_any(a.w, a.tw, c + u) : 1.0f) : w[(i * V + u) % AE];
-          o.v[u] = Conv<TX>::put(rstd * (fmaf(dy, we, -c1) - xhat * c2));
-          if (SMEM) {
-            acc_s[c + u] = fmaf(dy, xhat, acc_s[c + u]);
-            acc_s[TPR * E + c + u] += dy;
-          } else {
-            dw[(i * V + u) % AE] = fmaf(dy, xhat, dw[(i * V + u) % AE]);
-            db[(i * V + u) % AE] += dy;
-          }
+        for (int k = 0; k < P; ++k) {
+          const U xhat = fma2(xc[i][k], scale, shift);
+          put2(o, k, mul2(fma2(xhat, slope, fma2(yf[i][k], w[k], less)), scale));
+          dw[i][k] = fma2(yf[i][k], xhat, dw[i][k]);
+          db[i][k] = add2(db[i][k], yf[i][k]);
         }
         if (a.dx) *reinterpret_cast<PX*>(dxr + c) = o;
       }
     }
-    if (SMEM) fetch(row + gridDim.x * RPC);
+    at = at == R - 1 ? 0 : at + 1;
   }
-  if (!want_w) return;
-  float* part = a.part + (size_t)blockIdx.x * 2 * d;
-  if (SMEM) {
-    __syncthreads();                                            // (columns are stored in another order than they were summed)
-    for (int c = t; c < d; c += CTA) { part[c] = acc_s[c]; part[d + c] = acc_s[TPR * E + c]; }
-  } else if (RPC == 1) {
+  if (VEC) copies_wait<0>();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the joining kernel may be started
+  if (!a.dw && !a.db) return;
+  float* part = a.part + (size_t)(blockIdx.x / CL) * 2 * d;
+  const auto store = [&](float* to, const U (&sums)[P]) {       // a thread's V columns
+    if (V == 1) {
+      to[0] = total(sums[0]);
+    } else {
+      const float* f = reinterpret_cast<const float*>(sums);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int q = 0; q < V / 4; ++q)
+        reinterpret_cast<float4*>(to)[q] = make_float4(f[(4 * q) % V], f[(4 * q + 1) % V], f[(4 * q + 2) % V], f[(4 * q + 3) % V]);
+    }
+  };
+  if (RPC == 1) {
 #pragma unroll
-      for (int u = 0; u < V; ++u) {
-        const int c = (i * TPR + t) * V + u;
-        if (c < d) { part[c] = dw[(i * V + u) % AE]; part[d + c] = db[(i * V + u) % AE]; }
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + t) * V;
+      if (c < d) {
+        store(part + c, dw[i]);
+        store(part + d + c, db[i]);
       }
+    }
   } else {                                                      // the CTA's row groups, added in order
+    float* sum_s = reinterpret_cast<float*>(rest);
+    __syncthreads();                                            // every group is done with its ring
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int u = 0; u < V; ++u) {
-        const int c = (i * TPR + t) * V + u;
-        acc_s[(sub * 2 + 0) * TPR * E + c] = dw[(i * V + u) % AE];
-        acc_s[(sub * 2 + 1) * TPR * E + c] = db[(i * V + u) % AE];
-      }
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * TPR + t) * V;
+      store(sum_s + (sub * 2 + 0) * TPR * E + c, dw[i]);
+      store(sum_s + (sub * 2 + 1) * TPR * E + c, db[i]);
+    }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * TPR * E; c += CTA) {
       const int which = c / (TPR * E), col = c % (TPR * E);
       float s = 0.f;
-      for (int g = 0; g < RPC; ++g) s += acc_s[(g * 2 + which) * TPR * E + col];
+#pragma unroll 8
+      for (int g = 0; g < RPC; ++g) s += sum_s[(g * 2 + which) * TPR * E + col];
       if (col < d) part[(size_t)which * d + col] = s;
     }
   }
@@ -410,88 +635,143 @@ __global__ void __launch_bounds__(256) k_norm_bwd_cols(const NormArgs a, int par
   a.part[((size_t)blockIdx.y * 2 + 1) * a.d + c] = db;
 }
 
-// dw[c], db[c] = sum over the CTAs' partial sums: a CTA takes 32 columns of the 2 d, eight warps an eighth of the
-// partial rows each, and the eight sums are added in order
-__global__ void __launch_bounds__(256) k_norm_bwd_join(const NormArgs a, int parts) {
-  __shared__ float s[8][32];
+// dw[c], db[c] = sum over the CTAs' partial sums: a CTA takes 32 columns of the 2 d, each of its 32 warps a 32nd of the
+// partial rows, and the 32 sums are added in order
+__global__ void __launch_bounds__(1024) k_norm_bwd_join(const NormArgs a, int parts) {
+  __shared__ float s[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t col = (int64_t)blockIdx.x * 32 + lane, n = 2 * (int64_t)a.d;
+  asm volatile("griddepcontrol.wait;" ::: "memory");            // the sums come from the kernel in front (launched to overlap its end)
   float v = 0.f;
   if (col < n) {
     const float* p = a.part + col;
-#pragma unroll 4
-    for (int g = warp; g < parts; g += 8) v += p[(size_t)g * n];
+#pragma unroll 8
+    for (int g = warp; g < parts; g += 32) v += p[(size_t)g * n];
   }
   s[warp][lane] = v;
   __syncthreads();
-  if (warp == 0 && col < n) {
-    float r = 0.f;
+  float r = s[lane][warp];                                      // 32 sums of column `warp`
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r += s[i][lane];
-    if (col < a.d) { if (a.dw) store_any(a.dw, a.tw, col, r); }
-    else if (a.db) store_any(a.db, a.tw, col - a.d, r);
+  for (int o = 16; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+  const int64_t out = (int64_t)blockIdx.x * 32 + warp;
+  if (lane == 0 && out < n) {
+    if (out < a.d) { if (a.dw) store_any(a.dw, a.tw, out, r); }
+    else if (a.db) store_any(a.db, a.tw, out - a.d, r);
   }
 }
 
 constexpr int kSms = 148;
 constexpr int kLongParts = 32;
+constexpr int kMaxDevices = 64;
 
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; }
 
-// CTAs of a launch: as many as are resident at once, or as the rows need
-inline int grid_for(int rows, int rpc, int per_sm) { return std::max(1, std::min((rows + rpc - 1) / rpc, kSms * per_sm)); }
-
-inline int bwd_threads(int d) { return d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
-inline int bwd_rpc(int d) { return d <= 64 ? 32 : d <= 256 ? 8 : d <= 1024 ? 2 : 1; }
-
 template <class TX, class TY>
 bool vec_ok(const NormArgs& a, bool bwd) {
-  constexpr int V = sizeof(TX) == 4 ? 4 : 8;
+  constexpr int V = vec_len<TX>;
   if (a.d % V || a.ldx % V || !aligned(a.x, V * sizeof(TX))) return false;
   if (!bwd) return a.ldy % V == 0 && aligned(a.y, V * sizeof(TY));
   return a.lddy % V == 0 && aligned(a.dy, V * sizeof(TY)) && (!a.dx || (a.lddx % V == 0 && aligned(a.dx, V * sizeof(TX))));
 }
 
-template <class TX, class TY, int TPR, int E, bool RES>
-cudaError_t fwd_t(const NormArgs& a, cudaStream_t st) {
-  constexpr int cta = norm_cta<TPR>, rpc = cta / TPR;
-  const int grid = grid_for(a.rows, rpc, std::max(1, 2048 / cta / (E > 8 ? 2 : 1)));
-  if (RES || vec_ok<TX, TY>(a, false)) k_norm<TX, TY, TPR, E, true, RES><<<grid, cta, 0, st>>>(a);
-  else k_norm<TX, TY, TPR, E, false, false><<<grid, cta, 0, st>>>(a);
+// CTAs of a kernel that an SM holds, looked up once per device (and its shared-memory limit raised)
+template <class K>
+cudaError_t ctas_per_sm(K kernel, std::atomic<int>* cache, int threads, int smem, int* n) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  int r = cache[dev].load(std::memory_order_acquire);
+  if (r == 0) {
+    if (smem > 48 * 1024 &&
+        (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess)
+      return e;
+    if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r, kernel, threads, smem)) != cudaSuccess) return e;
+    if (r < 1) return cudaErrorLaunchOutOfResources;
+    cache[dev].store(r, std::memory_order_release);
+  }
+  *n = r;
+  return cudaSuccess;
+}
+
+template <class TX, class TY, int TPR, int E, bool VEC, bool RES, bool FEW>
+cudaError_t fwd_k(const NormArgs& a, cudaStream_t st) {
+  constexpr int cta = TPR < 256 ? 256 : TPR, rpc = cta / TPR, smem = FEW ? 0 : 2 * TPR * E * 4;
+  static std::atomic<int> cache[kMaxDevices];
+  int per_sm = 0;
+  const cudaError_t e = ctas_per_sm(k_norm<TX, TY, TPR, E, VEC, RES, FEW>, cache, cta, smem, &per_sm);
+  if (e != cudaSuccess) return e;
+  const int grid = std::min((a.rows + rpc - 1) / rpc, kSms * per_sm);
+  k_norm<TX, TY, TPR, E, VEC, RES, FEW><<<grid, cta, smem, st>>>(a);
   return cudaGetLastError();
 }
 
+template <class TX, class TY, int TPR, int E, bool RES, bool FEW>
+cudaError_t fwd_t(const NormArgs& a, cudaStream_t st) {
+  if (RES || vec_ok<TX, TY>(a, false)) return fwd_k<TX, TY, TPR, E, true, RES, FEW>(a, st);
+  return fwd_k<TX, TY, TPR, E, false, false, FEW>(a, st);
+}
+
+// Threads per row. Many rows: 32 elements per thread (few shuffles and barriers per element; the weights pass through
+// shared memory). Up to two rows per SM: 8 elements, the shortest way through one row (64 x 2048: 2.7 us against 5.5).
 template <class TX, class TY, bool RES>
 cudaError_t fwd(const NormArgs& a, cudaStream_t st) {
-  if (a.d <= 64) return fwd_t<TX, TY, 8, 8, RES>(a, st);
-  if (a.d <= 256) return fwd_t<TX, TY, 32, 8, RES>(a, st);
-  if (a.d <= 1024) return fwd_t<TX, TY, 128, 8, RES>(a, st);
-  if (a.d <= 2048) return fwd_t<TX, TY, 256, 8, RES>(a, st);
-  if (a.d <= 4096) return fwd_t<TX, TY, 512, 8, RES>(a, st);
-  if (a.d <= 8192) return fwd_t<TX, TY, 1024, 8, RES>(a, st);
-  if (a.d <= 16384) return fwd_t<TX, TY, 1024, 16, RES>(a, st);
+  if (!RES && a.rows <= 2 * kSms && a.d > 256 && a.d <= 8192) {   // (the denoiser's rows always take one way: same bits for any number of rows)
+    if (a.d <= 1024) return fwd_t<TX, TY, 128, 8, RES, true>(a, st);
+    if (a.d <= 2048) return fwd_t<TX, TY, 256, 8, RES, true>(a, st);
+    if (a.d <= 4096) return fwd_t<TX, TY, 512, 8, RES, true>(a, st);
+    return fwd_t<TX, TY, 1024, 8, RES, true>(a, st);
+  }
+  if (a.d <= 64) return fwd_t<TX, TY, 8, 8, RES, false>(a, st);
+  if (a.d <= 256) return fwd_t<TX, TY, 32, 8, RES, false>(a, st);
+  if (a.d <= 512) return fwd_t<TX, TY, 32, 16, RES, false>(a, st);
+  if (a.d <= 1024) return fwd_t<TX, TY, 32, 32, RES, false>(a, st);
+  if (a.d <= 2048) return fwd_t<TX, TY, 64, 32, RES, false>(a, st);
+  if (a.d <= 4096) return fwd_t<TX, TY, 128, 32, RES, false>(a, st);
+  if (a.d <= 8192) return fwd_t<TX, TY, 256, 32, RES, false>(a, st);
+  if (a.d <= 16384) return fwd_t<TX, TY, 512, 32, RES, false>(a, st);
   if (RES) return cudaErrorInvalidValue;
   k_norm_long<TX, TY><<<std::min(a.rows, 2 * kSms), 1024, 0, st>>>(a);
   return cudaGetLastError();
 }
 
-template <class TX, class TY, int TPR, int E, bool VEC, bool SMEM>
-cudaError_t bwd_k(const NormArgs& a, int grid, cudaStream_t st) {
-  constexpr int cta = norm_cta<TPR>, rpc = cta / TPR;
-  constexpr int smem = SMEM ? 2 * TPR * E * 4 : (rpc > 1 ? rpc * 2 * TPR * E * 4 : 0);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_norm_bwd<TX, TY, TPR, E, VEC, SMEM>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
+// backward: threads of a row's group by its length
+inline int bwd_tpr(int d) { return d <= 64 ? 8 : d <= 512 ? 32 : d <= 1024 ? 64 : d <= 2048 ? 128 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024; }
+
+template <class TX, class TY, int TPR, int E, bool VEC, int CL>
+cudaError_t bwd_k(const NormArgs& a, int* parts, cudaStream_t st) {
+  using C = NormBwd<TX, TY, TPR, E, VEC, CL>;
+  static std::atomic<int> cache[kMaxDevices], clusters[kMaxDevices];
+  int per_sm = 0, dev = 0;
+  cudaError_t e = ctas_per_sm(k_norm_bwd<TX, TY, TPR, E, VEC, CL>, cache, C::kCta, C::kSmemBytes, &per_sm);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(*parts * CL));
+  cfg.blockDim = dim3(C::kCta);
+  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = CL; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = CL > 1 ? 1 : 0;
+  if (CL > 1) {                                    // no more clusters than are resident at once (some SMs have no partner)
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    int r = clusters[dev].load(std::memory_order_acquire);
+    if (r == 0) {
+      if ((e = cudaOccupancyMaxActiveClusters(&r, k_norm_bwd<TX, TY, TPR, E, VEC, CL>, &cfg)) != cudaSuccess) return e;
+      if (r < 1) return cudaErrorLaunchOutOfResources;
+      clusters[dev].store(r, std::memory_order_release);
+    }
+    *parts = std::min(*parts, r);
+    cfg.gridDim = dim3((unsigned)(*parts * CL));
   }
-  k_norm_bwd<TX, TY, TPR, E, VEC, SMEM><<<grid, cta, smem, st>>>(a);
-  return cudaGetLastError();
+  return cudaLaunchKernelEx(&cfg, k_norm_bwd<TX, TY, TPR, E, VEC, CL>, a);
 }
 
-template <class TX, class TY, int TPR, int E, bool SMEM>
-cudaError_t bwd_t(const NormArgs& a, int grid, cudaStream_t st) {
-  return vec_ok<TX, TY>(a, true) ? bwd_k<TX, TY, TPR, E, true, SMEM>(a, grid, st)
-                                 : bwd_k<TX, TY, TPR, E, false, SMEM>(a, grid, st);
+template <class TX, class TY, int TPR, int E, int CL = 1>
+cudaError_t bwd_t(const NormArgs& a, int* parts, cudaStream_t st) {
+  return vec_ok<TX, TY>(a, true) ? bwd_k<TX, TY, TPR, E, true, CL>(a, parts, st) : bwd_k<TX, TY, TPR, E, false, CL>(a, parts, st);
 }
 
 template <class TX, class TY>
@@ -499,13 +779,14 @@ cudaError_t bwd(const NormArgs& a, cudaStream_t st) {
   int parts = norm_parts(a.rows, a.d);
   cudaError_t e = cudaSuccess;
   if (a.rows > 0) {
-    if (a.d <= 64) e = bwd_t<TX, TY, 8, 8, false>(a, parts, st);
-    else if (a.d <= 256) e = bwd_t<TX, TY, 32, 8, false>(a, parts, st);
-    else if (a.d <= 1024) e = bwd_t<TX, TY, 128, 8, false>(a, parts, st);
-    else if (a.d <= 2048) e = bwd_t<TX, TY, 256, 8, false>(a, parts, st);
-    else if (a.d <= 4096) e = bwd_t<TX, TY, 512, 8, false>(a, parts, st);
-    else if (a.d <= 8192) e = bwd_t<TX, TY, 1024, 8, false>(a, parts, st);
-    else if (a.d <= 16384) e = bwd_t<TX, TY, 1024, 16, true>(a, parts, st);
+    if (a.d <= 64) e = bwd_t<TX, TY, 8, 8>(a, &parts, st);
+    else if (a.d <= 256) e = bwd_t<TX, TY, 32, 8>(a, &parts, st);
+    else if (a.d <= 512) e = bwd_t<TX, TY, 32, 16>(a, &parts, st);
+    else if (a.d <= 1024) e = bwd_t<TX, TY, 64, 16>(a, &parts, st);
+    else if (a.d <= 2048) e = bwd_t<TX, TY, 128, 16>(a, &parts, st);
+    else if (a.d <= 4096) e = bwd_t<TX, TY, 256, 16>(a, &parts, st);
+    else if (a.d <= 8192) e = bwd_t<TX, TY, 512, 16>(a, &parts, st);
+    else if (a.d <= 16384) e = bwd_t<TX, TY, 1024, 16, 2>(a, &parts, st);   // a cluster of two CTAs per row
     else {
       k_norm_bwd_long<TX, TY><<<std::min(a.rows, 2 * kSms), 1024, 0, st>>>(a);
       e = cudaGetLastError();
@@ -519,8 +800,16 @@ cudaError_t bwd(const NormArgs& a, cudaStream_t st) {
     parts = 0;                                     // no rows: the gradients are zeros
   }
   if (!a.dw && !a.db) return cudaSuccess;
-  k_norm_bwd_join<<<(int)((2 * (int64_t)a.d + 31) / 32), 256, 0, st>>>(a, parts);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((2 * (int64_t)a.d + 31) / 32));
+  cfg.blockDim = dim3(1024);
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_norm_bwd_join, a, parts);
 }
 
 }  // namespace
@@ -529,7 +818,8 @@ bool norm_is_long(int d) { return d > 16384; }
 
 int norm_parts(int rows, int d) {
   if (norm_is_long(d)) return std::max(1, std::min(rows, kLongParts));
-  return grid_for(rows, bwd_rpc(d), std::max(1, 768 / bwd_threads(d)));
+  const int tpr = bwd_tpr(d), rpc = std::max(1, 512 / tpr), resident = tpr > 512 ? kSms / 2 : kSms;
+  return std::max(1, std::min((rows + rpc - 1) / rpc, resident));
 }
 
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
