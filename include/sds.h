@@ -56,6 +56,7 @@ extern "C" {
 #define SDS_DEN_MLP       2     /* bf16 MLP with per-step embedding rows */
 #define SDS_DEN_CALLBACK  3     /* user function on device buffers */
 #define SDS_DEN_PHI4      4     /* energy gradient of the phi^4 lattice model (Langevin chains, Appendix K) */
+#define SDS_DEN_GATED     5     /* residual blocks of layer norm and gated feed-forward (the layer operators below) */
 
 #define SDS_F32           0
 #define SDS_BF16          1
@@ -136,6 +137,13 @@ typedef int (*sds_denoise_fn)(void* user, const float* x_dev, const int32_t* k_d
  *   h_l = SiLU(W_l h_{l-1} + bias_l + temb_l[k]) for l < nlayer, output = W_nlayer h + bias (float).
  *   W_dev[l]: [dims[l+1], dims[l]] bf16 row-major; bias_dev[l]: [dims[l+1]] float;
  *   temb_dev[l]: [K, dims[l+1]] bf16 (NULL for the last layer). Every dims[] a multiple of 128.
+ * GATED: nlayer residual blocks on a float stream r_0 = x, output r_nlayer (float):
+ *   r' = r_l + temb_l[k],   n = layer norm of r' (eps 1e-5, rounded to bf16),
+ *   r_{l+1} = r' + ( act(n Wg_l^T) * (n Wu_l^T) ) Wd_l^T   (the bracket rounded to bf16, products accumulated in float).
+ *   dims = { d, f, act }: f the hidden width, act one of SDS_ACT_*; d <= 16384, d and f multiples of 8.
+ *   W_dev[3l], [3l+1], [3l+2]: Wg_l [f, d], Wu_l [f, d], Wd_l [d, f], bf16 row-major, 16-byte aligned;
+ *   bias_dev[2l], [2l+1]: [d] float weight and bias of the norm (NULL = ones, zeros); temb_dev[l]: [K, d] bf16 embedding
+ *   rows, 16-byte aligned (NULL = none).
  * PHI4: D(x) = grad E(x), E(x) = coupling/2 sum_{|i-j|=1} (x_i - x_j)^2 + sum_i (x_i^2 - 1)^2 on a
  *   grid_side x grid_side lattice (d = grid_side^2), every neighbouring pair once, free boundaries
  *   unless periodic != 0. Used with the Langevin schedule a = 1, c = -gamma, sigma = sqrt(2 gamma). */

@@ -11,6 +11,7 @@ What each function follows:
                                        (Eq. 3 target transition; Langevin Eq. 13)
   gmm_posterior_mean, gmm_grad_energy  exact denoiser / score of a Gaussian mixture (Tweedie)
   mlp_forward                          bf16-operand MLP denoiser
+  gated_forward                        residual blocks of layer norm and gated feed-forward, bf16 operands
   phi4_energy, phi4_grad_energy        the lattice energy of the Langevin experiment (Appendix K)
   rejection_discrete                   Algorithm 2 (generic maximal coupling), finite space
   rejection_reflection                 Algorithm 3 (reflection maximal coupling)
@@ -280,6 +281,33 @@ def mlp_forward(x, k, weights, bias, temb):
         else:
             h = y
     return h
+
+
+def gated_activation(g, name):
+    """g times the logistic function, the normal distribution function or its tanh approximation."""
+    if name == "silu":
+        return silu(g)
+    if name == "gelu":
+        return g * np.array([0.5 * math.erfc(-v / math.sqrt(2.0)) for v in np.ravel(g)]).reshape(np.shape(g))
+    if name == "gelu_tanh":
+        return 0.5 * g * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (g + 0.044715 * g ** 3)))
+    raise ValueError(name)
+
+
+def gated_forward(x, k, w_gate, w_up, w_down, norm_w, norm_b, temb, activation, eps=1e-5):
+    """Residual blocks on r_0 = x: r' = r + temb_l[k], n = layer norm of r', r = r' + (act(Wg n) * (Wu n)) Wd^T. The normed
+    row and the gated hidden row are rounded to bfloat16 (operands of the products); everything else in double."""
+    r = np.asarray(x, dtype=np.float64)
+    for l in range(len(w_gate)):
+        if temb[l] is not None:
+            r = r + np.asarray(temb[l][k], dtype=np.float64)
+        c = r - np.mean(r)
+        n = c / np.sqrt(np.mean(c * c) + eps)
+        n = n * (1.0 if norm_w[l] is None else np.asarray(norm_w[l], np.float64))
+        n = bf16_round(n + (0.0 if norm_b[l] is None else np.asarray(norm_b[l], np.float64)))
+        h = gated_activation(np.asarray(w_gate[l], np.float64) @ n, activation) * (np.asarray(w_up[l], np.float64) @ n)
+        r = r + np.asarray(w_down[l], np.float64) @ bf16_round(h)
+    return r
 
 
 # ----------------------------------------------------------------------------------------

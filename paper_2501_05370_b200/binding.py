@@ -18,9 +18,10 @@ from . import build as _build
 SDS_OK = 0
 SDS_EINVAL, SDS_ESTATE, SDS_ENOMEM, SDS_EUNSUPPORTED = -1, -2, -3, -4
 SDS_ECUDA, SDS_ETIMEOUT, SDS_ENONFINITE, SDS_ECALLBACK = -5, -6, -7, -8
-SDS_DEN_GMM, SDS_DEN_MLP, SDS_DEN_CALLBACK, SDS_DEN_PHI4 = 1, 2, 3, 4
+SDS_DEN_GMM, SDS_DEN_MLP, SDS_DEN_CALLBACK, SDS_DEN_PHI4, SDS_DEN_GATED = 1, 2, 3, 4, 5
 SDS_F32, SDS_BF16, SDS_F16 = 0, 1, 2
 SDS_ACT_SILU, SDS_ACT_GELU, SDS_ACT_GELU_TANH = 0, 1, 2
+ACTIVATIONS = {"silu": SDS_ACT_SILU, "gelu": SDS_ACT_GELU, "gelu_tanh": SDS_ACT_GELU_TANH}
 SDS_FROZEN_PREV, SDS_FROZEN_EXACT, SDS_INDEPENDENT, SDS_PICARD = 0, 1, 2, 3
 (GET_X, GET_TAIL, GET_DQ, GET_DC, GET_Y, GET_N, GET_ACT, GET_ROWOFF, GET_S1, GET_S2, GET_ELL, GET_LOGU,
  GET_ACCMASK, GET_JSTAR, GET_NFE_CALLS, GET_NFE_ROWS, GET_CTL, GET_ROWK, GET_DP) = range(1, 20)
@@ -142,7 +143,7 @@ class Sampler:
 
     def __init__(self, a, c, sigma, B: int, d: int, L: int, *, gmm_means=None, gmm_logw=None, tcond=None,
                  gmm_bf16: bool = False, mlp=None, callback=None, phi4=None, seed: int = 0, chain_id_offset: int = 0,
-                 drafter_mode: int = 0, drafter=None, picard=None, device="cuda:0", stream=None):
+                 drafter_mode: int = 0, drafter=None, picard=None, device="cuda:0", stream=None, gated=None):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("libsds needs a CUDA device; there is no CPU path")
@@ -162,13 +163,14 @@ class Sampler:
             tcond = np.ascontiguousarray(tcond, np.float64)
             sch.tcond, sch.tcond_dim = tcond.ctypes.data, tcond.shape[1]
         self._keep += [a, c, sigma, tcond]
-        den = self._make_denoiser("tgt", gmm_means, gmm_logw, gmm_bf16, mlp, phi4, callback)
+        den = self._make_denoiser("tgt", gmm_means, gmm_logw, gmm_bf16, mlp, phi4, callback, gated)
         if den is None:
             raise ValueError("a denoiser is required")
         dden, dtc = None, None
-        if drafter is not None:                  # independent draft model: dict(gmm_means=, gmm_logw=, tcond=, gmm_bf16=, mlp=, phi4=)
+        if drafter is not None:                  # independent draft model: dict(gmm_means=, gmm_logw=, tcond=, gmm_bf16=, mlp=, phi4=, gated=)
             dden = self._make_denoiser("drf", drafter.get("gmm_means"), drafter.get("gmm_logw"),
-                                       drafter.get("gmm_bf16", False), drafter.get("mlp"), drafter.get("phi4"), None)
+                                       drafter.get("gmm_bf16", False), drafter.get("mlp"), drafter.get("phi4"), None,
+                                       drafter.get("gated"))
             if dden is None:
                 raise ValueError("the drafter needs a denoiser")
             if drafter.get("tcond") is not None:
@@ -210,7 +212,7 @@ class Sampler:
         self._chk(self.lib.sds_bind(self.h, base, nbytes.value, self.stream.cuda_stream, seed, drafter_mode,
                                     chain_id_offset), "sds_bind")
 
-    def _make_denoiser(self, tag, gmm_means, gmm_logw, gmm_bf16, mlp, phi4, callback):
+    def _make_denoiser(self, tag, gmm_means, gmm_logw, gmm_bf16, mlp, phi4, callback, gated=None):
         """Fills an SdsDenoiser and keeps the device arrays it names alive under self.<tag>_*."""
         torch = self.torch
         den = SdsDenoiser()
@@ -246,6 +248,19 @@ class Sampler:
             den.W_dev = C.cast(Wp, C.c_void_p)
             den.bias_dev = C.cast(bp, C.c_void_p)
             den.temb_dev = C.cast(tp, C.c_void_p)
+            den.dims = dims.ctypes.data
+        elif gated is not None:                  # residual blocks (fields as in workloads.GatedParams)
+            bits = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.uint16).view(np.int16)).to(self.device)
+            vec = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(self.device)
+            W = [bits(w) for l in range(len(gated.w_gate)) for w in (gated.w_gate[l], gated.w_up[l], gated.w_down[l])]
+            norm = [vec(v) if v is not None else None
+                    for l in range(len(gated.w_gate)) for v in (gated.norm_w[l], gated.norm_b[l])]
+            temb = [bits(x) if x is not None else None for x in gated.temb]
+            dims = np.array([gated.d, gated.f, ACTIVATIONS[gated.activation]], np.int32)
+            ptrs = [(C.c_void_p * len(v))(*[(x.data_ptr() if x is not None else None) for x in v]) for v in (W, norm, temb)]
+            setattr(self, tag + "_gated", (W, norm, temb, dims, ptrs))
+            den.kind, den.nlayer = SDS_DEN_GATED, len(gated.w_gate)
+            den.W_dev, den.bias_dev, den.temb_dev = (C.cast(p, C.c_void_p) for p in ptrs)
             den.dims = dims.ctypes.data
         elif phi4 is not None:                   # (grid side, coupling beta, periodic)
             den.kind, den.grid_side, den.coupling, den.periodic = SDS_DEN_PHI4, int(phi4[0]), float(phi4[1]), int(bool(phi4[2]))

@@ -11,6 +11,7 @@
 
 #include "sds_device.cuh"
 #include "sds_internal.h"
+#include "sds_layers.h"
 #include "sds_tc.h"
 
 using namespace sds;
@@ -49,7 +50,7 @@ struct Layout {
 // workspace regions private to one denoiser (the target, or the independent draft model)
 struct DenLayout {
   size_t tcond, musq;
-  size_t H0, H1;          // MLP hidden activations (bf16)
+  size_t H0, H1;          // MLP hidden activations (bf16); gated blocks: normed rows and hidden rows (bf16)
   size_t logits, R, Mt;   // large mixture: logits (f32), responsibilities (bf16), transposed means (bf16)
   size_t Xs, Ms;          // float mixture on tensor cores: 3 bf16 planes of the rows / of the means
   size_t flags;           // one int per 128 rows: responsibilities with a non-zero second or third plane
@@ -59,7 +60,7 @@ struct DenLayout {
 
 struct Engine {
   sds_denoiser den{};
-  std::vector<int32_t> mlp_dims;                 // copies of the caller's MLP description
+  std::vector<int32_t> mlp_dims;                 // copies of the caller's MLP or gated-block description
   std::vector<const void*> mlp_W, mlp_temb;
   std::vector<const float*> mlp_bias;
   std::vector<double> tcond;
@@ -152,6 +153,10 @@ void den_layout(Carve& cv, const sds_denoiser* den, size_t K, int tcond_dim, siz
     for (int i = 1; i < den->nlayer; ++i) width = std::max(width, (size_t)den->dims[i]);
     l->H0 = cv.take(rows * width * 2);
     l->H1 = cv.take(rows * width * 2);
+  }
+  if (den->kind == SDS_DEN_GATED) {
+    l->H0 = cv.take(rows * (size_t)d * 2);
+    l->H1 = cv.take(rows * (size_t)den->dims[1] * 2);
   }
   if (den->kind == SDS_DEN_GMM && den->means_dtype == SDS_BF16) {
     l->logits = cv.take(rows * (size_t)den->ncomp * 4);
@@ -259,6 +264,21 @@ int validate_den(const sds_denoiser* den, const double* tcond, int tcond_dim, in
         if (i < den->nlayer - 1 && !den->temb_dev[i]) return SDS_EINVAL;
       }
       break;
+    case SDS_DEN_GATED: {
+      if (den->nlayer < 1 || den->nlayer > 64 || !den->dims || !den->W_dev || !den->bias_dev || !den->temb_dev)
+        return SDS_EINVAL;
+      const int32_t f = den->dims[1], act = den->dims[2];
+      if (den->dims[0] != d || f <= 0) return SDS_EINVAL;
+      if (d > 16384 || d % 8 != 0 || f % 8 != 0) return SDS_EUNSUPPORTED;
+      if (act != SDS_ACT_SILU && act != SDS_ACT_GELU && act != SDS_ACT_GELU_TANH) return SDS_EUNSUPPORTED;
+      for (int i = 0; i < 3 * den->nlayer; ++i) {
+        if (!den->W_dev[i]) return SDS_EINVAL;
+        if (reinterpret_cast<uintptr_t>(den->W_dev[i]) % 16) return SDS_EUNSUPPORTED;
+      }
+      for (int i = 0; i < den->nlayer; ++i)
+        if (reinterpret_cast<uintptr_t>(den->temb_dev[i]) % 16) return SDS_EUNSUPPORTED;
+      break;
+    }
     default:
       return SDS_EUNSUPPORTED;
   }
@@ -528,6 +548,31 @@ int run_denoiser(sds_ctx* c, Engine& e, const float* X, const uint16_t* Xb, cons
       }
       return SDS_OK;
     }
+    case SDS_DEN_GATED: {
+      // the residual stream is the output buffer; every row's result is the same bits whatever rows it shares the launch
+      // with (the drafter evaluated at Y_n relies on it)
+      const int f = e.mlp_dims[1];
+      uint16_t* normed = at<uint16_t>(c, e.lay.H0);
+      for (int l = 0; l < e.den.nlayer; ++l) {
+        NormArgs n{};
+        n.x = l == 0 ? X : out; n.ldx = c->d; n.tx = SDS_F32;
+        n.y = normed; n.ldy = c->d; n.ty = SDS_BF16;
+        n.w = e.mlp_bias[2 * l]; n.b = e.mlp_bias[2 * l + 1]; n.tw = SDS_F32;
+        n.rows = (int)rows_ub; n.d = c->d; n.eps = 1e-5f;
+        n.nrows_dev = nrows_dev; n.rowk = rowk;
+        n.temb = static_cast<const uint16_t*>(e.mlp_temb[l]); n.res = out;
+        SDS_LAUNCH(c, ks, launch_norm(n, c->stream));
+        FfnArgs a{};
+        a.rows = (int)rows_ub; a.d = c->d; a.f = f; a.act = e.mlp_dims[2];
+        a.x = normed; a.ldx = c->d; a.h = at<void>(c, e.lay.H1);
+        a.wg = e.mlp_W[3 * l]; a.wu = e.mlp_W[3 * l + 1]; a.wd = e.mlp_W[3 * l + 2];
+        a.nrows_dev = nrows_dev; a.res = out;
+        a.err = at<int>(c, c->lay.ctl) + kCtlTcError;
+        SDS_LAUNCH(c, kd, launch_ffn_hidden(a, c->stream));
+        SDS_LAUNCH(c, kd, launch_ffn_residual(a, c->stream));
+      }
+      return SDS_OK;
+    }
     case SDS_DEN_PHI4:
       SDS_LAUNCH(c, kd, launch_phi4_grad(X, nrows_dev, (int)rows_ub, e.den.grid_side, e.den.coupling,
                                                         e.den.periodic, out, c->stream));
@@ -573,6 +618,13 @@ void engine_init(Engine& e, const sds_denoiser* den, const double* tcond, int tc
     e.mlp_dims.assign(den->dims, den->dims + den->nlayer + 1);
     e.mlp_W.assign(den->W_dev, den->W_dev + den->nlayer);
     e.mlp_bias.assign(den->bias_dev, den->bias_dev + den->nlayer);
+    e.mlp_temb.assign(den->temb_dev, den->temb_dev + den->nlayer);
+    e.den.dims = e.mlp_dims.data();
+  }
+  if (den->kind == SDS_DEN_GATED) {
+    e.mlp_dims.assign(den->dims, den->dims + 3);
+    e.mlp_W.assign(den->W_dev, den->W_dev + 3 * den->nlayer);
+    e.mlp_bias.assign(den->bias_dev, den->bias_dev + 2 * den->nlayer);
     e.mlp_temb.assign(den->temb_dev, den->temb_dev + den->nlayer);
     e.den.dims = e.mlp_dims.data();
   }

@@ -1033,11 +1033,16 @@ cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
   return launch_tiles<kFfnOut>(a, &s, 1, false, st);
 }
 
+cudaError_t launch_ffn_hidden(const FfnArgs& a, cudaStream_t st) {
+  if (a.rows <= 0) return cudaSuccess;
+  ProductSpec s = forward_in(a);
+  return launch_tiles<kFfnGlu>(a, &s, 1, true, st);
+}
+
 cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaSuccess;
-  ProductSpec in = forward_in(a), out = forward_out(a, a.res, a.d);
-  const cudaError_t e = launch_tiles<kFfnGlu>(a, &in, 1, true, st);
-  return e != cudaSuccess ? e : launch_tiles<kFfnAdd>(a, &out, 1, false, st);
+  ProductSpec s = forward_out(a, a.res, a.d);
+  return launch_tiles<kFfnAdd>(a, &s, 1, false, st);      // (its caller launched launch_ffn_hidden before it)
 }
 
 cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {

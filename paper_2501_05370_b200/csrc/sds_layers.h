@@ -68,7 +68,8 @@ size_t ffn_keep_floats(int64_t rows, int64_t f);
 cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st);
 cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st);
 // the denoiser's form of the two products (row count on the device, any number of rows through the same tiles):
-// h = act(x Wg^T) * (x Wu^T), res += h Wd^T. Every output element is the same bits however many rows there are.
+// h = act(x Wg^T) * (x Wu^T), then res += h Wd^T. Every output element is the same bits however many rows there are.
+cudaError_t launch_ffn_hidden(const FfnArgs& a, cudaStream_t st);
 cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st);
 
 }  // namespace sds

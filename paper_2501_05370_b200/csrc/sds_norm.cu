@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && s
 #pragma unroll
           for (int k = 0; k < P; ++k) put2(nxt[i], k, add2(get2(nxt[i], k), get2(e, k)));
         }
-        *reinterpret_cast<PX*>(a.res + (size_t)row * d + c) = nxt[i];
+        if (te || a.x != a.res) *reinterpret_cast<PX*>(a.res + (size_t)row * d + c) = nxt[i];
       }
 #pragma unroll
       for (int k = 0; k < P; ++k) x[i][k] = get2(nxt[i], k);

@@ -13,7 +13,7 @@ import functools
 
 from . import binding as sb
 
-ACTIVATIONS = {"silu": sb.SDS_ACT_SILU, "gelu": sb.SDS_ACT_GELU, "gelu_tanh": sb.SDS_ACT_GELU_TANH}
+ACTIVATIONS = sb.ACTIVATIONS
 
 _torch = None        # set by _load
 _lib = None

@@ -20,8 +20,8 @@ def schedule_for(w):
     return a, c, sigma, tcond
 
 
-def drafter_for(w, *, gmm=None, mlp=None):
-    """Description of an independent draft model for workload w: a (smaller) mixture or MLP."""
+def drafter_for(w, *, gmm=None, mlp=None, gated=None):
+    """Description of an independent draft model for workload w: a (smaller) mixture, MLP or gated network."""
     if gmm is not None:
         if w.sampler == "ddpm":
             tc = sc.gmm_tcond_posterior_mean(sc.ddpm_schedule(w.beta())[3], gmm.comp_std)
@@ -30,6 +30,8 @@ def drafter_for(w, *, gmm=None, mlp=None):
         return dict(gmm_means=gmm.means, gmm_logw=gmm.logw, tcond=tc, gmm_bf16=bool(getattr(gmm, "means_bf16", False)))
     if mlp is not None:
         return dict(mlp=mlp)
+    if gated is not None:
+        return dict(gated=gated)
     raise ValueError("a draft model is required")
 
 
@@ -44,7 +46,7 @@ def picard_for(w, calls: int):
 
 
 def sampler_for(w, *, seed=None, chain_id_offset=0, B=None, device="cuda:0", gmm=None, mlp=None, drafter_mode=None,
-                drafter=None, picard=None):
+                drafter=None, picard=None, gated=None):
     a, c, sigma, tcond = schedule_for(w)
     if drafter_mode is None:
         drafter_mode = getattr(w, "drafter_mode", 0)
@@ -58,6 +60,10 @@ def sampler_for(w, *, seed=None, chain_id_offset=0, B=None, device="cuda:0", gmm
     if w.denoiser == "mlp":
         mp = mlp if mlp is not None else w.mlp_params()
         return sb.Sampler(a, c, sigma, B, w.d, w.L, mlp=mp, seed=seed, chain_id_offset=chain_id_offset, drafter_mode=drafter_mode, drafter=drafter, picard=picard, device=device)
+    if w.denoiser == "gated":
+        gp = gated if gated is not None else w.gated_params()
+        return sb.Sampler(a, c, sigma, B, w.d, w.L, gated=gp, seed=seed, chain_id_offset=chain_id_offset,
+                          drafter_mode=drafter_mode, drafter=drafter, picard=picard, device=device)
     if w.denoiser == "phi4":
         p4 = w.phi4
         return sb.Sampler(a, c, sigma, B, w.d, w.L, phi4=(p4["side"], p4["beta"], p4.get("periodic", False)), seed=seed,

@@ -132,3 +132,47 @@ def test_host_checks_of_the_tensor_functions():
         sds.layer_norm(x)                                           # not a CUDA tensor
     with pytest.raises(ValueError):
         sds.gated_ffn(x, x, x, x)
+
+
+def _gated_den(d=64, f=128, act=0, nblock=2, drop=None, shift=0):
+    n = 3 * nblock
+    W = (C.c_void_p * n)(*[0x100000 + 0x1000 * i + shift for i in range(n)])
+    if drop is not None:
+        W[drop] = None
+    norm = (C.c_void_p * (2 * nblock))(*([None] * (2 * nblock)))
+    temb = (C.c_void_p * nblock)(*([None] * nblock))
+    dims = (C.c_int32 * 3)(d, f, act)
+    den = sb.SdsDenoiser()
+    den.kind, den.nlayer = sb.SDS_DEN_GATED, nblock
+    den.W_dev, den.bias_dev, den.temb_dev, den.dims = (C.cast(v, C.c_void_p) for v in (W, norm, temb, dims))
+    return den, (W, norm, temb, dims)
+
+
+def test_gated_denoiser_validation():
+    import numpy as np
+    a = np.full(5, 0.5, np.float32)
+    sch = sb.SdsSchedule(5, a.ctypes.data, a.ctypes.data, a.ctypes.data, None, 0)
+    n = C.c_size_t(0)
+    ask = lambda den, d=64: sds.load().sds_workspace_bytes(C.byref(sch), C.byref(den[0]), 8, d, 4, C.byref(n))
+    assert ask(_gated_den()) == sb.SDS_OK
+    assert n.value >= 8 * 4 * (64 * 4 * 2 + 64 * 2 + 128 * 2)      # rows and outputs, normed and hidden rows
+    assert ask(_gated_den(d=128)) == sb.SDS_EINVAL                  # another width than the context's
+    assert ask(_gated_den(f=0)) == sb.SDS_EINVAL and ask(_gated_den(nblock=2, drop=4)) == sb.SDS_EINVAL
+    assert ask(_gated_den(f=100)) == sb.SDS_EUNSUPPORTED and ask(_gated_den(act=7)) == sb.SDS_EUNSUPPORTED
+    assert ask(_gated_den(d=60), 60) == sb.SDS_EUNSUPPORTED and ask(_gated_den(shift=8)) == sb.SDS_EUNSUPPORTED
+    assert ask(_gated_den(d=16392), 16392) == sb.SDS_EUNSUPPORTED
+
+
+def test_oracle_gated_block_by_hand():
+    """One block on a row of two, worked out on paper: the norm of (1, 3) is (-1, 1) up to eps, gate and up pick its
+    elements, and the product with Wd is added to the row."""
+    import math
+    from oracle import sds_oracle as o
+    eye = [[1.0, 0.0], [0.0, 1.0]]
+    got = o.gated_forward([0.5, 2.5], 1, [eye], [eye], [[[2.0, 0.0], [0.0, 1.0]]], [None], [None], [[[0.0, 0.0], [0.5, 0.5]]], "silu", eps=0.0)
+    h = (1.0 / (1.0 + math.e)) , 1.0 / (1.0 + math.exp(-1.0))        # silu(-1) * -1, silu(1) * 1
+    h = o.bf16_round(o.np.array(h))
+    assert abs(got[0] - (1.0 + 2.0 * h[0])) < 1e-12 and abs(got[1] - (3.0 + h[1])) < 1e-12
+    for name in ("silu", "gelu", "gelu_tanh"):
+        assert o.gated_activation(o.np.zeros(3), name).tolist() == [0.0, 0.0, 0.0]
+        assert abs(o.gated_activation(o.np.array([30.0]), name)[0] - 30.0) < 1e-9

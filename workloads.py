@@ -128,6 +128,43 @@ def mlp_params(seed: int, dims: list, K: int, temb_dim: int = 128) -> MlpParams:
     return MlpParams(dims=list(dims), weights=weights, bias=bias, temb=temb, K=K)
 
 
+@dataclass
+class GatedParams:
+    """Random-init residual network of gated feed-forward blocks (per block l):
+
+    w_gate[l], w_up[l]: [f, d], w_down[l]: [d, f] as bf16 bit patterns (uint16), N(0, 1/fan_in), w_down scaled by `gain`
+    norm_w[l], norm_b[l]: [d] float32 around one and zero (None: ones, zeros)
+    temb[l]: [K, d] bf16 bits, added to the stream before the block's norm (None: no embedding)
+    """
+    d: int
+    f: int
+    activation: str
+    w_gate: list
+    w_up: list
+    w_down: list
+    norm_w: list
+    norm_b: list
+    temb: list
+    K: int
+
+
+def gated_params(seed: int, d: int, f: int, nblock: int, K: int, activation: str = "silu", gain: float = 0.5,
+                 temb_dim: int = 128) -> GatedParams:
+    rng = np.random.default_rng(seed)
+    tau = time_features(K, temb_dim)
+    g = GatedParams(d, f, activation, [], [], [], [], [], [], K)
+    for l in range(nblock):
+        mat = lambda n, m, s: f32_to_bf16_bits((rng.standard_normal((n, m)) * s).astype(np.float32))
+        g.w_gate.append(mat(f, d, d ** -0.5))
+        g.w_up.append(mat(f, d, d ** -0.5))
+        g.w_down.append(mat(d, f, gain * f ** -0.5))
+        g.norm_w.append((1.0 + 0.1 * rng.standard_normal(d)).astype(np.float32))
+        g.norm_b.append((0.1 * rng.standard_normal(d)).astype(np.float32))
+        P = rng.standard_normal((d, temb_dim)) * math.sqrt(0.1 / temb_dim)
+        g.temb.append(f32_to_bf16_bits((tau @ P.T).astype(np.float32)))
+    return g
+
+
 # ----------------------------------------------------------------------------------------
 # the five workloads
 # ----------------------------------------------------------------------------------------
@@ -143,9 +180,10 @@ class Workload:
     sampler: str                # "ddpm" | "ula"
     schedule: str = ""          # "linear" | "cosine" (ddpm)
     ula_gamma: float = 0.0
-    denoiser: str = "gmm"       # "gmm" | "mlp"
+    denoiser: str = "gmm"       # "gmm" | "mlp" | "gated" | "phi4"
     gmm: dict = field(default_factory=dict)
     mlp_dims: list = field(default_factory=list)
+    gated: dict = field(default_factory=dict)    # f, nblock, activation (residual network of gated blocks)
     phi4: dict = field(default_factory=dict)     # side, beta, periodic (lattice energy workload)
     drafter_mode: int = 0                        # 0: carried target output, 1: target evaluated at Y_n
     param_seed: int = 0
@@ -164,6 +202,10 @@ class Workload:
 
     def mlp_params(self, dims: list | None = None, K: int | None = None) -> MlpParams:
         return mlp_params(self.param_seed, dims or self.mlp_dims, K or self.K)
+
+    def gated_params(self, K: int | None = None) -> GatedParams:
+        g = self.gated
+        return gated_params(self.param_seed, self.d, g["f"], g["nblock"], K or self.K, g.get("activation", "silu"))
 
     def scaled(self, **kw) -> "Workload":
         """A smaller instance of the same recipe (for parity tests the oracle can finish)."""
