@@ -1,4 +1,5 @@
-"""Builds libsds.so (the CUDA kernels and their C ABI) in-tree with nvcc for sm_100a."""
+"""Builds libsds.so (the CUDA kernels and their C ABI) in-tree with nvcc for sm_100a, and _sds_torch.so (the layer
+operators on torch tensors, host code only) with the C++ compiler."""
 from __future__ import annotations
 
 import os
@@ -8,6 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsds.so")
+EXT = os.path.join(HERE, "_sds_torch.so")
+EXT_SRC = os.path.join(CSRC, "sds_torch.cpp")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -20,16 +23,16 @@ def sources() -> list:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(EXT):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(EXT))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "sds.h")]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu under csrc/ (one nvcc process per file, side by side) and link libsds.so;
-    returns the library path. Objects go to _build/ next to this file and are rebuilt only when a
+    returns the library path; then the torch extension. Objects go to _build/ next to this file and are rebuilt only when a
     source or header is newer."""
     if not force and not needs_build():
         return LIB
@@ -59,7 +62,26 @@ def build(force: bool = False, verbose: bool = False) -> str:
     res = subprocess.run([nvcc] + NVCC_FLAGS + ["-o", LIB] + [o for o, _ in results], capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("nvcc link failed:\n" + res.stdout + res.stderr)
+    build_ext()
     return LIB
+
+
+def build_ext() -> str:
+    """Compile and link _sds_torch.so against torch and the libsds.so next to it."""
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    include = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] + ["-isystem" + i for i in include]
+           + [EXT_SRC, "-o", EXT, "-L" + torch_lib, "-L" + HERE, "-l:libsds.so", "-ltorch_python", "-ltorch_cpu",
+              "-ltorch_cuda", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + torch_lib])
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("building _sds_torch.so failed:\n" + res.stdout + res.stderr)
+    return EXT
 
 
 if __name__ == "__main__":

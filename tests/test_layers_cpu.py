@@ -132,6 +132,10 @@ def test_host_checks_of_the_tensor_functions():
         sds.layer_norm(x)                                           # not a CUDA tensor
     with pytest.raises(ValueError):
         sds.gated_ffn(x, x, x, x)
+    for call in (lambda: sds.layer_norm(None), lambda: sds.layer_norm([1.0]), lambda: sds.gated_ffn(x, x, x, x, "relu"),
+                 lambda: sds.layer_norm_backward(x, x, None, x, x), lambda: sds.gated_ffn_backward(x, x, x, x, x, x)):
+        with pytest.raises(ValueError):
+            call()
 
 
 def _gated_den(d=64, f=128, act=0, nblock=2, drop=None, shift=0):
