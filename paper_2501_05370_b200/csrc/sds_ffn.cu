@@ -57,7 +57,7 @@ constexpr int kWarpStage = 2048;                  // staging bytes of an epilogu
 struct FfnProduct {
   CUtensorMap a[2], b[2];                         // kFfnGlu: b[0] = Wg, b[1] = Wu, one segment
   int M, N, K;                                    // K of one segment
-  int nseg, a_mn, b_mn;
+  int nseg, a_mn;
   int band;                                       // tile rows of a band (see tile_at)
   void* out;
   int64_t ldo;
@@ -74,6 +74,9 @@ struct FfnTileArgs {
   void* out2;                                     // kFfnDGlu: dU (out is dG)
   int* err;
   int clear_err;                                  // (see FfnSplitArgs)
+  int beside;                                     // reads nothing of the kernel in front, which was itself started after the
+                                                  // end of the one before it (FfnSplitArgs::late): runs beside it, and
+                                                  // waits for it only in the end
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -103,6 +106,7 @@ __device__ __forceinline__ void activation(float g, float& a, float& da) {
 }
 
 template <int N> struct Act { static constexpr int value = N; };
+template <bool B> struct Bool { static constexpr bool value = B; };
 // f(Act<act>): the choice is made once per tile or row and not per element
 template <class F>
 __device__ __forceinline__ void with_activation(int act, F f) {
@@ -230,7 +234,10 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
   return t + worker + i * nworkers;
 }
 
-template <int BN, int EPI, bool PAIR>
+// MN: B is MN-major and A either (the gradients); else both are K-major. The loops of the two single threads that feed the
+// tensor cores are written out per order: with the order looked up in every step they took 735 cycles per step of K where
+// the products take 512 (16384 x 2048 x 8192, forward projections: 676 -> 605 us at full clocks).
+template <int BN, int EPI, bool PAIR, bool MN>
 __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
   using C = FfnTile<BN, PAIR>;
   constexpr int TM = C::kTM, TN = EPI == kFfnGlu ? BN / 2 : BN;    // output columns of a tile
@@ -248,7 +255,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const int worker = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
   const int nworkers = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-  wait_for_prior_kernel();
+  if (!g.beside) wait_for_prior_kernel();
   launch_dependents();
   const int M0 = g.nrows_dev ? min(*g.nrows_dev, g.p[0].M) : g.p[0].M;
 
@@ -289,43 +296,46 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
         const int m0 = at.m * TM + (int)rank * kBM;
         const int n0 = at.n * TN + (EPI == kFfnGlu ? 0 : (int)rank * C::kBRows);
         const int K = p.K, nseg = p.nseg;
-        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
-        for (int seg = 0; seg < nseg && ok; ++seg) {
-          const CUtensorMap* ta = &p.a[seg];
-          // the tile's columns of Wg, then those of Wu: one CTA of a pair each, or one after the other
-          const CUtensorMap* tb = &p.b[EPI == kFfnGlu && PAIR ? (int)rank : seg];
-          for (int kk = 0; kk < K; kk += kBK) {
-            if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
-            uint8_t* sa = stages + stage * C::kStageBytes;
-            uint8_t* sb = sa + C::kABytes;
-            const uint32_t fb = PAIR ? leader_full0 + (uint32_t)stage * 8u : 0u;
-            if (PAIR) {
-              if (rank == 0) mbar_expect_tx(full_bar + stage, 2u * (uint32_t)C::kStageBytes);
-            } else {
-              mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
-            }
-            auto load = [&](uint8_t* dst, const CUtensorMap* tm, int c0, int c1) {
-              if (PAIR) tma_load_2d_pair(dst, tm, c0, c1, fb);
-              else tma_load_2d(dst, tm, c0, c1, full_bar + stage);
-            };
-            if (a_mn) {
+        const auto feed = [&](auto order) {
+          constexpr bool a_mn = decltype(order)::value;
+          for (int seg = 0; seg < nseg && ok; ++seg) {
+            const CUtensorMap* ta = &p.a[seg];
+            // the tile's columns of Wg, then those of Wu: one CTA of a pair each, or one after the other
+            const CUtensorMap* tb = &p.b[EPI == kFfnGlu && PAIR ? (int)rank : seg];
+            for (int kk = 0; kk < K; kk += kBK) {
+              if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
+              uint8_t* sa = stages + stage * C::kStageBytes;
+              uint8_t* sb = sa + C::kABytes;
+              const uint32_t fb = PAIR ? leader_full0 + (uint32_t)stage * 8u : 0u;
+              if (PAIR) {
+                if (rank == 0) mbar_expect_tx(full_bar + stage, 2u * (uint32_t)C::kStageBytes);
+              } else {
+                mbar_expect_tx(full_bar + stage, (uint32_t)C::kStageBytes);
+              }
+              const auto load = [&](uint8_t* dst, const CUtensorMap* tm, int c0, int c1) {
+                if (PAIR) tma_load_2d_pair(dst, tm, c0, c1, fb);
+                else tma_load_2d(dst, tm, c0, c1, full_bar + stage);
+              };
+              if (a_mn) {
 #pragma unroll
-              for (int j = 0; j < kBM / 64; ++j) load(sa + j * kChunkBytes, ta, m0 + 64 * j, kk);
-            } else {
-              load(sa, ta, kk, m0);
-            }
-            if (EPI == kFfnGlu && !PAIR) {
-              load(sb, tb, kk, n0);
-              load(sb + C::kBBytes / 2, tb + 1, kk, n0);
-            } else if (b_mn) {
+                for (int j = 0; j < kBM / 64; ++j) load(sa + j * kChunkBytes, ta, m0 + 64 * j, kk);
+              } else {
+                load(sa, ta, kk, m0);
+              }
+              if (EPI == kFfnGlu && !PAIR) {
+                load(sb, tb, kk, n0);
+                load(sb + C::kBBytes / 2, tb + 1, kk, n0);
+              } else if (MN) {
 #pragma unroll
-              for (int j = 0; j < C::kBRows / 64; ++j) load(sb + j * kChunkBytes, tb, n0 + 64 * j, kk);
-            } else {
-              load(sb, tb, kk, n0);
+                for (int j = 0; j < C::kBRows / 64; ++j) load(sb + j * kChunkBytes, tb, n0 + 64 * j, kk);
+              } else {
+                load(sb, tb, kk, n0);
+              }
+              if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
             }
-            if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
           }
-        }
+        };
+        if (MN && p.a_mn) feed(Bool<MN>()); else feed(Bool<false>());
       }
       if (!ok) {
         raise_abort(abort_s, PAIR);
@@ -341,30 +351,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       bool more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, 0), &at);
       for (; ok && more; ++it) {
         const FfnProduct& p = g.p[at.prod];
-        const uint32_t idesc = make_idesc(TM, BN, g.f16 != 0, p.a_mn != 0, p.b_mn != 0);
         const int nkb = (p.K + kBK - 1) / kBK * p.nseg;
-        const uint32_t a_chunk = p.a_mn ? (uint32_t)kChunkBytes : 0u, b_chunk = p.b_mn ? (uint32_t)kChunkBytes : 0u;
-        const uint64_t a_step = p.a_mn ? 128u : 2u, b_step = p.b_mn ? 128u : 2u;    // 16 elements of K, in 16 bytes
         const int buf = it & 1;
         if (!mbar_wait(tempty_bar + buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_s)) { ok = false; break; }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
-        const uint64_t adesc0 = make_sdesc(smem_u32(stages), a_chunk), bdesc0 = make_sdesc(smem_u32(stages) + C::kABytes, b_chunk);
-        for (int kb = 0; kb < nkb; ++kb) {
-          if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
-          tc_fence_after();
-          const uint64_t adesc = adesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
-          const uint64_t bdesc = bdesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
+        const auto multiply = [&](auto order) {
+          constexpr bool a_mn = decltype(order)::value;
+          const uint32_t idesc = make_idesc(TM, BN, g.f16 != 0, a_mn, MN);
+          const uint64_t adesc0 = make_sdesc(smem_u32(stages), a_mn ? (uint32_t)kChunkBytes : 0u);
+          const uint64_t bdesc0 = make_sdesc(smem_u32(stages) + C::kABytes, MN ? (uint32_t)kChunkBytes : 0u);
+          constexpr uint64_t a_step = a_mn ? 128u : 2u, b_step = MN ? 128u : 2u;    // 16 elements of K, in 16 bytes
+          for (int kb = 0; kb < nkb; ++kb) {
+            if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t adesc = adesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
+            const uint64_t bdesc = bdesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
 #pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) {
-            if (PAIR) umma_f16_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
-            else umma_f16(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
+            for (int k = 0; k < kBK / 16; ++k) {
+              if (PAIR) umma_f16_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
+              else umma_f16(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
+            }
+            if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
+            if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+            // where the next tile lies takes a few divisions: worked out while this tile's products run
+            if (kb == 0) more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
           }
-          if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
-          if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
-          // where the next tile lies takes a few divisions: worked out while this tile's products run
-          if (kb == 0) more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
-        }
+        };
+        if (MN && p.a_mn) multiply(Bool<MN>()); else multiply(Bool<false>());
         if (ok) { if (PAIR) umma_commit_pair(tfull_bar + buf); else umma_commit(tfull_bar + buf); }
       }
       if (!ok) {
@@ -495,6 +509,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   if (*abort_s && threadIdx.x == 0) {
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies still in flight land before the memory is released
   }
+  if (g.beside) wait_for_prior_kernel();
   __syncthreads();
   if (PAIR) cluster_sync_all();
   if (warp == 1) {
@@ -522,6 +537,7 @@ struct FfnSplitArgs {
   int* err;
   int clear_err;                                  // first kernel of a call: the status word starts at zero. A wait gives
                                                   // up only after millions of polls, long after the first CTA began.
+  int late;                                       // the next kernel may be started only when the one before this has ended
 };
 
 constexpr int kSplitThreads = 256;
@@ -580,7 +596,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_s;
-  launch_dependents();
+  if (!g.late) launch_dependents();
 
   if (warp == 0 && lane == 0) {
     int stage = 0;
@@ -650,6 +666,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   __syncwarp();
 
   wait_for_prior_kernel();                        // (nothing in device memory is read or written before)
+  if (g.late) launch_dependents();
   if (g.clear_err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
   // the accumulator to shared memory, [token][row of the instruction]
   const bool ok = mbar_wait_warp(tfull_bar, 0u, abort_s);
@@ -763,7 +780,7 @@ struct KernelInfo {
   std::atomic<int> resident[kMaxDevices];         // 0: not looked up; else 1 + resident CTAs (clusters of a pair)
 };
 
-template <int BN, int EPI, bool PAIR>
+template <int BN, int EPI, bool PAIR, bool MN>
 cudaError_t tile_resident(int* n) {
   static KernelInfo info;                         // zero-initialised
   using C = FfnTile<BN, PAIR>;
@@ -771,7 +788,7 @@ cudaError_t tile_resident(int* n) {
   if (dev < 0) return cudaErrorInvalidDevice;
   int r = info.resident[dev].load(std::memory_order_acquire);
   if (r == 0) {
-    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     int sms = 0, got = 0;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
@@ -786,7 +803,7 @@ cudaError_t tile_resident(int* n) {
       attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
-      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR>, &cfg)) != cudaSuccess) return e;
+      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN>, &cfg)) != cudaSuccess) return e;
       got = std::min(got, sms / 2);
     }
     if (got < 1) return cudaErrorLaunchOutOfResources;
@@ -797,11 +814,11 @@ cudaError_t tile_resident(int* n) {
   return cudaSuccess;
 }
 
-template <int BN, int EPI, bool PAIR>
+template <int BN, int EPI, bool PAIR, bool MN>
 cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, bool overlap, cudaStream_t st) {
   using C = FfnTile<BN, PAIR>;
   int resident = 0;
-  const cudaError_t e = tile_resident<BN, EPI, PAIR>(&resident);
+  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN>(&resident);
   if (e != cudaSuccess) return e;
   const int workers = (int)std::min<int64_t>(tiles, resident);
   cudaLaunchConfig_t cfg{};
@@ -812,7 +829,7 @@ cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, bool overlap, cud
   cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
   cfg.numAttrs = launch_attributes(attr, PAIR ? 2 : 1, overlap);
-  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR>, g);
+  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN>, g);
 }
 
 // where an operand lies: [rows, cols] with rows ld elements apart; K-major if K runs along the columns
@@ -830,7 +847,7 @@ bool map_operand(CUtensorMap* tm, const Mat& m, bool f16, int64_t mn, int64_t k,
 struct ProductSpec {
   Mat a[2], b[2];
   int nseg;
-  bool a_mn, b_mn;
+  bool a_mn;
   int M, N, K;
   void* out;
   int64_t ldo;
@@ -844,9 +861,9 @@ inline int ksteps(const ProductSpec& s) { return (s.K + kBK - 1) / kBK * s.nseg;
 // Tile shape: single CTAs on 128 x 128 tiles while these are at most one per SM (each has an SM of its own), pairs on
 // 256 x 256 tiles above that. Several products of one launch: those with the longer tiles come first; there are at most
 // two lengths (specs[0] may differ from the others).
-template <int EPI>
+template <int EPI, bool MN>
 cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first, cudaStream_t st,
-                         float* keep = nullptr, void* out2 = nullptr) {
+                         float* keep = nullptr, void* out2 = nullptr, bool beside = false) {
   constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
   if (n > 1 && ksteps(specs[0]) < ksteps(specs[n - 1])) std::swap(specs[0], specs[n - 1]);
   int64_t small = 0, wide = 0;
@@ -854,7 +871,10 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     small += tiles_of(specs[i], 128, kNarrow);
     wide += tiles_of(specs[i], 256, kWide);
   }
-  const bool pair = small > 148;
+#ifndef PAIRMIN
+#define PAIRMIN 148
+#endif
+  const bool pair = small > PAIRMIN;
   // tiles of the longer class, and how many of the shorter one take as long
   int longer = 1;
   while (longer < n && ksteps(specs[longer]) == ksteps(specs[0])) ++longer;
@@ -871,30 +891,31 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
   g.out2 = out2;
   g.err = a.err;
   g.clear_err = first && !a.res;
+  g.beside = beside;
   const bool overlap = !first;
   for (int i = 0; i < n; ++i) {
     const ProductSpec& s = specs[i];
     FfnProduct& p = g.p[i];
     p.M = s.M; p.N = s.N; p.K = s.K;
-    p.nseg = s.nseg; p.a_mn = s.a_mn; p.b_mn = s.b_mn;
+    p.nseg = s.nseg; p.a_mn = s.a_mn;
     p.out = s.out; p.ldo = s.ldo;
     p.band = (int)std::max<int64_t>(8, std::min<int64_t>(32, (32 << 20) / ((pair ? 256 : 128) * 2 * (int64_t)ksteps(s) * kBK)));
     const int box_b = EPI == kFfnGlu && !pair ? 64 : 128;
     for (int k = 0; k < (EPI == kFfnGlu ? 2 : s.nseg); ++k) {
       if (k < s.nseg && !map_operand(&p.a[k], s.a[k], a.f16 != 0, s.M, s.K, s.a_mn, 128)) return cudaErrorInvalidValue;
-      if (!map_operand(&p.b[k], s.b[k], a.f16 != 0, s.N, s.K, s.b_mn, box_b)) return cudaErrorInvalidValue;
+      if (!map_operand(&p.b[k], s.b[k], a.f16 != 0, s.N, s.K, MN, box_b)) return cudaErrorInvalidValue;
     }
   }
   if (pair) {
-    const cudaError_t e = launch_tile_t<256, EPI, true>(g, wide, overlap, st);
+    const cudaError_t e = launch_tile_t<256, EPI, true, MN>(g, wide, overlap, st);
     if (e != cudaErrorLaunchOutOfResources) return e;
     // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
     for (int i = 0; EPI == kFfnGlu && i < n; ++i)
       for (int k = 0; k < 2; ++k)
-        if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, specs[i].b_mn, 64))
+        if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, MN, 64))
           return cudaErrorInvalidValue;
   }
-  return launch_tile_t<128, EPI, false>(g, small, overlap, st);
+  return launch_tile_t<128, EPI, false, MN>(g, small, overlap, st);
 }
 
 template <int BN, int EPI>
@@ -947,6 +968,12 @@ template <int EPI>
 bool prefer_split(int rows, int N, int nkb) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   if (rows <= 64) return true;                    // half a tile of rows and more would be empty
+#ifdef NOSPLIT
+  if (rows > NOSPLIT) return false;
+#endif
+#ifdef ALLSPLIT
+  return rows <= 2048;
+#endif
   if (rows > 2048) return false;
   const int tok = (rows + 127) / 128, tiles = (N + TN - 1) / TN;
   const int splits = split_count(rows, tiles, nkb);
@@ -958,7 +985,7 @@ bool prefer_split(int rows, int N, int nkb) {
 }
 
 template <int EPI>
-cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st) {
+cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st, bool late = false) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   const int bn = split_tokens(a.rows);
   FfnSplitArgs g;
@@ -969,6 +996,7 @@ cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool
   g.out = s.out; g.out2 = s.out2; g.ldo = s.ldo;
   g.err = a.err;
   g.clear_err = first;
+  g.late = late;
   const int nw = EPI == kFfnGlu ? 2 : s.nseg;
   for (int k = 0; k < nw; ++k)
     if (!map_operand(&g.w[k], s.w[k], a.f16 != 0, s.N, s.K, s.w_mn, EPI == kFfnGlu ? 64 : 128)) return cudaErrorInvalidValue;
@@ -1020,7 +1048,7 @@ cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
     e = launch_split<kFfnGlu>(a, s, a.keep, true, st);
   } else {
     ProductSpec s = forward_in(a);
-    e = launch_tiles<kFfnGlu>(a, &s, 1, true, st, a.keep);
+    e = launch_tiles<kFfnGlu, false>(a, &s, 1, true, st, a.keep);
   }
   if (e != cudaSuccess) return e;
   if (prefer_split<kFfnOut>(a.rows, a.d, steps(a.f))) {
@@ -1030,19 +1058,19 @@ cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
     return launch_split<kFfnOut>(a, s, nullptr, false, st);
   }
   ProductSpec s = forward_out(a, a.y, a.ldy);
-  return launch_tiles<kFfnOut>(a, &s, 1, false, st);
+  return launch_tiles<kFfnOut, false>(a, &s, 1, false, st);
 }
 
 cudaError_t launch_ffn_hidden(const FfnArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaSuccess;
   ProductSpec s = forward_in(a);
-  return launch_tiles<kFfnGlu>(a, &s, 1, true, st);
+  return launch_tiles<kFfnGlu, false>(a, &s, 1, true, st);
 }
 
 cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaSuccess;
   ProductSpec s = forward_out(a, a.res, a.d);
-  return launch_tiles<kFfnAdd>(a, &s, 1, false, st);      // (its caller launched launch_ffn_hidden before it)
+  return launch_tiles<kFfnAdd, false>(a, &s, 1, false, st);      // (its caller launched launch_ffn_hidden before it)
 }
 
 cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
@@ -1063,8 +1091,8 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
     } else {
       ProductSpec s{};
       s.a[0] = {a.dy, a.lddy}; s.b[0] = {a.wd, a.f};
-      s.nseg = 1; s.b_mn = true; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.dg; s.ldo = a.f;
-      e = launch_tiles<kFfnDGlu>(a, &s, 1, first, st, a.keep, a.du);
+      s.nseg = 1; s.M = a.rows; s.N = a.f; s.K = a.d; s.out = a.dg; s.ldo = a.f;
+      e = launch_tiles<kFfnDGlu, true>(a, &s, 1, first, st, a.keep, a.du);
     }
     if (e != cudaSuccess) return e;
     first = false;
@@ -1072,27 +1100,29 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
   // the gradients of x and of the weights read the same dG and dU: one launch where x's product takes tiles too
   ProductSpec w[4];
   int n = 0;
+  bool beside = false;
   if (a.dx && prefer_split<kFfnOut>(a.rows, a.d, 2 * steps(a.f))) {
     SplitSpec s{};
     s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.dg, a.f}; s.t[1] = {a.du, a.f};
     s.nseg = 2; s.w_mn = true; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
-    if ((e = launch_split<kFfnOut>(a, s, nullptr, false, st)) != cudaSuccess) return e;
+    beside = true;                                // (the weights' gradients, launched next, do not read dx)
+    if ((e = launch_split<kFfnOut>(a, s, nullptr, false, st, beside)) != cudaSuccess) return e;
   } else if (a.dx) {
     ProductSpec s{};
     s.a[0] = {a.dg, a.f}; s.a[1] = {a.du, a.f}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};
-    s.nseg = 2; s.b_mn = true; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
+    s.nseg = 2; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
     w[n++] = s;
   }
   const auto gradient = [&](const Mat& left, const Mat& right, int M, int N, void* out) {
     ProductSpec s{};
     s.a[0] = left; s.b[0] = right;
-    s.nseg = 1; s.a_mn = s.b_mn = true; s.M = M; s.N = N; s.K = a.rows; s.out = out; s.ldo = N;
+    s.nseg = 1; s.a_mn = true; s.M = M; s.N = N; s.K = a.rows; s.out = out; s.ldo = N;
     w[n++] = s;
   };
   if (a.dwg) gradient({a.dg, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwg);
   if (a.dwu) gradient({a.du, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwu);
   if (a.dwd) gradient({a.dy, a.lddy}, {a.h, a.f}, a.d, a.f, a.dwd);
-  return n > 0 ? launch_tiles<kFfnOut>(a, w, n, first, st) : cudaSuccess;
+  return n > 0 ? launch_tiles<kFfnOut, true>(a, w, n, first, st, nullptr, nullptr, beside) : cudaSuccess;
 }
 
 }  // namespace sds
