@@ -168,8 +168,8 @@ __device__ __forceinline__ void add_rows64(uint4* stg, const uint32_t* w, float*
   __syncwarp();
 }
 
-// Kernels of one call overlap their starts: a kernel may be started when all CTAs of the one before it have begun, and
-// waits for that kernel's end (and for its writes) here.
+// Kernels overlap their starts: one may be started when all CTAs of the one in front have said so (or ended), and waits
+// for that kernel's end, and for its writes, here.
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_prior_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -255,10 +255,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const int worker = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
   const int nworkers = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-  if (!g.beside) wait_for_prior_kernel();
-  launch_dependents();
-  const int M0 = g.nrows_dev ? min(*g.nrows_dev, g.p[0].M) : g.p[0].M;
-
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar + s, 1); mbar_init(empty_bar + s, 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(tfull_bar + s, 1); mbar_init(tempty_bar + s, PAIR ? 2 * kEpiWarps : kEpiWarps); }
@@ -281,7 +277,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   if (PAIR) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_s;
+  launch_dependents();
+  if (!g.beside) wait_for_prior_kernel();         // (nothing in device memory is read or written before)
   if (g.clear_err && blockIdx.x == 0 && threadIdx.x == 0) *g.err = 0;
+  const int M0 = g.nrows_dev ? min(*g.nrows_dev, g.p[0].M) : g.p[0].M;
 
   TileAt at;
   if (warp == 0) {
@@ -620,9 +619,10 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       const int seg = kb >= kb_seg ? 1 : 0, kk = (kb - seg * kb_seg) * kBK;
       tma_load_2d(stages + stage * C::kStageBytes + C::kABytes, &g.t[seg], kk, tok0, full_bar + stage);
     };
-    // The kernel before this one writes the tokens, not the weights: the first stages' weights are requested before
-    // it has ended (what ran before that kernel had ended when it began).
+    // Behind a kernel of the same call: that one writes the tokens, not the weights, and what ran before it had ended
+    // when it went past its own wait. So the first stages' weights are requested before it has ended.
     const int ahead = min(kb1 - kb0, C::kStages);
+    if (g.clear_err) wait_for_prior_kernel();
     for (int i = 0; i < ahead; ++i) { weights(kb0 + i); ++stage; }
     wait_for_prior_kernel();
     for (stage = 0; stage < ahead; ++stage) tokens(kb0 + stage);
@@ -762,17 +762,14 @@ int current_device() {
   return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : -1;
 }
 
-// cluster size, and whether the launch may overlap the end of the kernel before it (see wait_for_prior_kernel); the
-// first kernel of a call never does: what it reads may come from any kernel
-int launch_attributes(cudaLaunchAttribute (&attr)[2], int cluster, bool overlap) {
+// cluster size, and the permission to start before the kernel in front has ended (see wait_for_prior_kernel)
+void launch_attributes(cudaLaunchAttribute (&attr)[2], int cluster) {
   attr[0] = cudaLaunchAttribute{};
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  if (!overlap) return 1;
   attr[1] = cudaLaunchAttribute{};
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
-  return 2;
 }
 
 // a kernel's shared-memory limit and the number of its clusters that are resident at once, per device, looked up once
@@ -815,7 +812,7 @@ cudaError_t tile_resident(int* n) {
 }
 
 template <int BN, int EPI, bool PAIR, bool MN>
-cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, bool overlap, cudaStream_t st) {
+cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) {
   using C = FfnTile<BN, PAIR>;
   int resident = 0;
   const cudaError_t e = tile_resident<BN, EPI, PAIR, MN>(&resident);
@@ -828,7 +825,8 @@ cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, bool overlap, cud
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
-  cfg.numAttrs = launch_attributes(attr, PAIR ? 2 : 1, overlap);
+  cfg.numAttrs = 2;
+  launch_attributes(attr, PAIR ? 2 : 1);
   return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN>, g);
 }
 
@@ -871,10 +869,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     small += tiles_of(specs[i], 128, kNarrow);
     wide += tiles_of(specs[i], 256, kWide);
   }
-#ifndef PAIRMIN
-#define PAIRMIN 148
-#endif
-  const bool pair = small > PAIRMIN;
+  const bool pair = small > 148;
   // tiles of the longer class, and how many of the shorter one take as long
   int longer = 1;
   while (longer < n && ksteps(specs[longer]) == ksteps(specs[0])) ++longer;
@@ -892,7 +887,6 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
   g.err = a.err;
   g.clear_err = first && !a.res;
   g.beside = beside;
-  const bool overlap = !first;
   for (int i = 0; i < n; ++i) {
     const ProductSpec& s = specs[i];
     FfnProduct& p = g.p[i];
@@ -907,7 +901,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     }
   }
   if (pair) {
-    const cudaError_t e = launch_tile_t<256, EPI, true, MN>(g, wide, overlap, st);
+    const cudaError_t e = launch_tile_t<256, EPI, true, MN>(g, wide, st);
     if (e != cudaErrorLaunchOutOfResources) return e;
     // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
     for (int i = 0; EPI == kFfnGlu && i < n; ++i)
@@ -915,11 +909,11 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
         if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, MN, 64))
           return cudaErrorInvalidValue;
   }
-  return launch_tile_t<128, EPI, false, MN>(g, small, overlap, st);
+  return launch_tile_t<128, EPI, false, MN>(g, small, st);
 }
 
 template <int BN, int EPI>
-cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, bool overlap, cudaStream_t st) {
+cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, cudaStream_t st) {
   using C = FfnSplit<BN>;
   static KernelInfo info;
   const int dev = current_device();
@@ -936,7 +930,8 @@ cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, bool ov
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
-  cfg.numAttrs = launch_attributes(attr, splits, overlap);
+  cfg.numAttrs = 2;
+  launch_attributes(attr, splits);
   return cudaLaunchKernelEx(&cfg, k_ffn_split<BN, EPI>, g);
 }
 
@@ -968,12 +963,6 @@ template <int EPI>
 bool prefer_split(int rows, int N, int nkb) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   if (rows <= 64) return true;                    // half a tile of rows and more would be empty
-#ifdef NOSPLIT
-  if (rows > NOSPLIT) return false;
-#endif
-#ifdef ALLSPLIT
-  return rows <= 2048;
-#endif
   if (rows > 2048) return false;
   const int tok = (rows + 127) / 128, tiles = (N + TN - 1) / TN;
   const int splits = split_count(rows, tiles, nkb);
@@ -1005,10 +994,10 @@ cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool
   const int tiles = (s.N + TN - 1) / TN;
   const int splits = split_count(a.rows, tiles, ksteps(s));
   switch (bn) {
-    case 16: return launch_split_t<16, EPI>(g, tiles, splits, !first, st);
-    case 32: return launch_split_t<32, EPI>(g, tiles, splits, !first, st);
-    case 64: return launch_split_t<64, EPI>(g, tiles, splits, !first, st);
-    default: return launch_split_t<128, EPI>(g, tiles, splits, !first, st);
+    case 16: return launch_split_t<16, EPI>(g, tiles, splits, st);
+    case 32: return launch_split_t<32, EPI>(g, tiles, splits, st);
+    case 64: return launch_split_t<64, EPI>(g, tiles, splits, st);
+    default: return launch_split_t<128, EPI>(g, tiles, splits, st);
   }
 }
 
