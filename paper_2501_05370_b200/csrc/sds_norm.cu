@@ -242,6 +242,14 @@ __device__ __forceinline__ unit_t<V> col_unit(const void* p, int type, float fil
   return r;
 }
 
+// Kernels overlap their starts: the next one may be started once all CTAs of this one have begun (their launch takes about
+// as long as a small call runs), and this one waits here for the end of the kernel in front, and for its writes.
+// Nothing in device memory is read or written before.
+__device__ __forceinline__ void start_after_prior_kernel() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 template <class TX> constexpr int vec_len = sizeof(TX) == 4 ? 4 : 8;   // elements of a 16-byte access
 
 // FEW: at most one row or two for every group of the launch. The weights are then read with the first row, into
@@ -264,6 +272,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && s
   __shared__ __align__(16) float slots[2 * RPC * 4 * NW];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float* slot = slots + sub * 8 * NW;
+  start_after_prior_kernel();
   const int rows = a.nrows_dev ? min(*a.nrows_dev, a.rows) : a.rows;
   const int d = a.d, step = (int)gridDim.x * RPC;
   const float inv_d = 1.0f / (float)d;
@@ -367,6 +376,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && s
 // rows longer than the register kernels hold: one CTA per row, the row read three times (the later passes from L2)
 template <class TX, class TY>
 __global__ void __launch_bounds__(1024) k_norm_long(const NormArgs a) {
+  start_after_prior_kernel();
   __shared__ float slot[96];
   const int t = threadIdx.x;
   const double inv_d = 1.0 / (double)a.d;
@@ -443,6 +453,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
   float* w_s = reinterpret_cast<float*>(shared);
   uint8_t* rest = reinterpret_cast<uint8_t*>(shared) + C::kWeights;
   __shared__ __align__(16) float slots[2 * RPC * 4 * NW];
+  start_after_prior_kernel();
   const int rank = CL > 1 ? (int)(blockIdx.x % CL) : 0;         // this CTA's part of the row
   const int tl = threadIdx.x % T, sub = threadIdx.x / T, t = rank * T + tl;
   const int rows = a.rows, d = a.d, groups = (int)gridDim.x / CL, step = groups * RPC;
@@ -544,7 +555,6 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
     at = at == R - 1 ? 0 : at + 1;
   }
   if (VEC) copies_wait<0>();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the joining kernel may be started
   if (!a.dw && !a.db) return;
   float* part = a.part + (size_t)(blockIdx.x / CL) * 2 * d;
   const auto store = [&](float* to, const U (&sums)[P]) {       // a thread's V columns
@@ -589,6 +599,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
 // long rows: dx and the row offsets c0, then the columns' sums over chunks of rows
 template <class TX, class TY>
 __global__ void __launch_bounds__(1024) k_norm_bwd_long(const NormArgs a) {
+  start_after_prior_kernel();
   __shared__ float slots[2][96];
   const int t = threadIdx.x;
   const double inv_d = 1.0 / (double)a.d;
@@ -620,6 +631,7 @@ __global__ void __launch_bounds__(1024) k_norm_bwd_long(const NormArgs a) {
 }
 template <class TX, class TY>
 __global__ void __launch_bounds__(256) k_norm_bwd_cols(const NormArgs a, int parts) {
+  start_after_prior_kernel();
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= a.d) return;
   const int per = (a.rows + parts - 1) / parts;
@@ -641,7 +653,7 @@ __global__ void __launch_bounds__(1024) k_norm_bwd_join(const NormArgs a, int pa
   __shared__ float s[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t col = (int64_t)blockIdx.x * 32 + lane, n = 2 * (int64_t)a.d;
-  asm volatile("griddepcontrol.wait;" ::: "memory");            // the sums come from the kernel in front (launched to overlap its end)
+  start_after_prior_kernel();
   float v = 0.f;
   if (col < n) {
     const float* p = a.part + col;
@@ -674,6 +686,24 @@ bool vec_ok(const NormArgs& a, bool bwd) {
   return a.lddy % V == 0 && aligned(a.dy, V * sizeof(TY)) && (!a.dx || (a.lddx % V == 0 && aligned(a.dx, V * sizeof(TX))));
 }
 
+// a launch that may start before the kernel in front has ended (see start_after_prior_kernel), in clusters of `cluster`
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // CTAs of a kernel that an SM holds, looked up once per device (and its shared-memory limit raised)
 template <class K>
 cudaError_t ctas_per_sm(K kernel, std::atomic<int>* cache, int threads, int smem, int* n) {
@@ -702,8 +732,7 @@ cudaError_t fwd_k(const NormArgs& a, cudaStream_t st) {
   const cudaError_t e = ctas_per_sm(k_norm<TX, TY, TPR, E, VEC, RES, FEW>, cache, cta, smem, &per_sm);
   if (e != cudaSuccess) return e;
   const int grid = std::min((a.rows + rpc - 1) / rpc, kSms * per_sm);
-  k_norm<TX, TY, TPR, E, VEC, RES, FEW><<<grid, cta, smem, st>>>(a);
-  return cudaGetLastError();
+  return launch(k_norm<TX, TY, TPR, E, VEC, RES, FEW>, dim3(grid), cta, smem, 1, st, a);
 }
 
 template <class TX, class TY, int TPR, int E, bool RES, bool FEW>
@@ -731,8 +760,7 @@ cudaError_t fwd(const NormArgs& a, cudaStream_t st) {
   if (a.d <= 8192) return fwd_t<TX, TY, 256, 32, RES, false>(a, st);
   if (a.d <= 16384) return fwd_t<TX, TY, 512, 32, RES, false>(a, st);
   if (RES) return cudaErrorInvalidValue;
-  k_norm_long<TX, TY><<<std::min(a.rows, 2 * kSms), 1024, 0, st>>>(a);
-  return cudaGetLastError();
+  return launch(k_norm_long<TX, TY>, dim3(std::min(a.rows, 2 * kSms)), 1024, 0, 1, st, a);
 }
 
 // backward: threads of a row's group by its length
@@ -745,28 +773,26 @@ cudaError_t bwd_k(const NormArgs& a, int* parts, cudaStream_t st) {
   int per_sm = 0, dev = 0;
   cudaError_t e = ctas_per_sm(k_norm_bwd<TX, TY, TPR, E, VEC, CL>, cache, C::kCta, C::kSmemBytes, &per_sm);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(*parts * CL));
-  cfg.blockDim = dim3(C::kCta);
-  cfg.dynamicSmemBytes = C::kSmemBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = CL; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = CL > 1 ? 1 : 0;
   if (CL > 1) {                                    // no more clusters than are resident at once (some SMs have no partner)
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     int r = clusters[dev].load(std::memory_order_acquire);
     if (r == 0) {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3((unsigned)(kSms / CL * CL));
+      cfg.blockDim = dim3(C::kCta);
+      cfg.dynamicSmemBytes = C::kSmemBytes;
+      cudaLaunchAttribute attr{};
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = CL; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
       if ((e = cudaOccupancyMaxActiveClusters(&r, k_norm_bwd<TX, TY, TPR, E, VEC, CL>, &cfg)) != cudaSuccess) return e;
       if (r < 1) return cudaErrorLaunchOutOfResources;
       clusters[dev].store(r, std::memory_order_release);
     }
     *parts = std::min(*parts, r);
-    cfg.gridDim = dim3((unsigned)(*parts * CL));
   }
-  return cudaLaunchKernelEx(&cfg, k_norm_bwd<TX, TY, TPR, E, VEC, CL>, a);
+  return launch(k_norm_bwd<TX, TY, TPR, E, VEC, CL>, dim3((unsigned)(*parts * CL)), C::kCta, C::kSmemBytes, CL, st, a);
 }
 
 template <class TX, class TY, int TPR, int E, int CL = 1>
@@ -788,28 +814,16 @@ cudaError_t bwd(const NormArgs& a, cudaStream_t st) {
     else if (a.d <= 8192) e = bwd_t<TX, TY, 512, 16>(a, &parts, st);
     else if (a.d <= 16384) e = bwd_t<TX, TY, 1024, 16, 2>(a, &parts, st);   // a cluster of two CTAs per row
     else {
-      k_norm_bwd_long<TX, TY><<<std::min(a.rows, 2 * kSms), 1024, 0, st>>>(a);
-      e = cudaGetLastError();
-      if (e == cudaSuccess && (a.dw || a.db)) {
-        k_norm_bwd_cols<TX, TY><<<dim3((a.d + 255) / 256, parts), 256, 0, st>>>(a, parts);
-        e = cudaGetLastError();
-      }
+      e = launch(k_norm_bwd_long<TX, TY>, dim3(std::min(a.rows, 2 * kSms)), 1024, 0, 1, st, a);
+      if (e == cudaSuccess && (a.dw || a.db))
+        e = launch(k_norm_bwd_cols<TX, TY>, dim3((a.d + 255) / 256, parts), 256, 0, 1, st, a, parts);
     }
     if (e != cudaSuccess) return e;
   } else {
     parts = 0;                                     // no rows: the gradients are zeros
   }
   if (!a.dw && !a.db) return cudaSuccess;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)((2 * (int64_t)a.d + 31) / 32));
-  cfg.blockDim = dim3(1024);
-  cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_norm_bwd_join, a, parts);
+  return launch(k_norm_bwd_join, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), 1024, 0, 1, st, a, parts);
 }
 
 }  // namespace
