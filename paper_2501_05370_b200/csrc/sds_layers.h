@@ -24,6 +24,7 @@ struct NormArgs {
   int tx, ty, tw;        // SDS_F32, SDS_BF16, SDS_F16
   int rows, d;
   float eps;
+  bool wide;             // w and b are 16-byte aligned (set by the launchers)
   // denoiser form (float in, 16-bit out): the row norms follow `x + temb[rowk[row]]`, which is also written to
   // res [rows, d] float; the true row count lives on the device
   const int* nrows_dev;

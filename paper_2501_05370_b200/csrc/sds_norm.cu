@@ -220,26 +220,47 @@ __device__ __forceinline__ void load_cols(const float* s, int i, int t, float2 (
 }
 template <int T, int V>
 __device__ __forceinline__ void load_cols(const float* s, int i, int t, float (&o)[1]) { o[0] = s[slot_of<T, V>(i, 0, t)]; }
-// a column vector of the caller's as floats in that order (`fill` where there is none). t0: the group's first thread in
-// this CTA.
-template <int TPR, int T, int E, int V>
-__device__ __forceinline__ void stage_cols(float* s, const void* p, int type, float fill, int d, int threads, int t0) {
-  for (int k = threadIdx.x; k < T * E; k += threads) {
-    const int vec = k / V, i = vec / T, t = vec % T, u = k % V;
-    const int c = (i * TPR + t0 + t) * V + u;
-    s[slot_of<T, V>(i, u, t)] = (p && c < d) ? load_any(p, type, c) : fill;
+// V columns from c on of a caller's column vector (c and d multiples of V where V > 1), as floats; `fill` where there is no
+// vector. wide: the vector is 16-byte aligned.
+template <int V>
+__device__ __forceinline__ void load_vector(const void* p, int type, bool wide, float fill, int c, int d, float (&o)[V]) {
+  if (!p || c >= d) {
+#pragma unroll
+    for (int u = 0; u < V; ++u) o[u] = fill;
+  } else if (V > 1 && wide && type == SDS_F32) {
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + c) + q);
+      o[(4 * q) % V] = v.x; o[(4 * q + 1) % V] = v.y; o[(4 * q + 2) % V] = v.z; o[(4 * q + 3) % V] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < V; ++u) o[u] = load_any(p, type, c + u);
   }
 }
-// unit k of vector i, straight from the caller's column vector
 template <int V>
-__device__ __forceinline__ unit_t<V> col_unit(const void* p, int type, float fill, int c, int d) {
-  unit_t<V> r = Unit<V>::all(fill);
-  if (p && c < d) {
-    float* f = reinterpret_cast<float*>(&r);
-    f[0] = load_any(p, type, c);
-    if (V > 1) f[V > 1 ? 1 : 0] = load_any(p, type, c + 1);   // (vectors only where d is a multiple of theirs)
+__device__ __forceinline__ void as_units(const float (&f)[V], unit_t<V> (&o)[units<V>]) {
+  float* to = reinterpret_cast<float*>(o);
+#pragma unroll
+  for (int u = 0; u < V; ++u) to[u] = f[u];
+}
+// such a vector in shared memory, in the order of slot_of. t0: the group's first thread in this CTA.
+template <int TPR, int T, int E, int V>
+__device__ __forceinline__ void stage_cols(float* s, const void* p, int type, bool wide, float fill, int d, int threads, int t0) {
+#pragma unroll 2
+  for (int vec = threadIdx.x; vec < T * E / V; vec += threads) {
+    const int i = vec / T, t = vec % T;
+    float f[V];
+    load_vector<V>(p, type, wide, fill, (i * TPR + t0 + t) * V, d, f);
+    if (V == 1) {
+      s[slot_of<T, V>(i, 0, t)] = f[0];
+    } else {
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q)
+        *reinterpret_cast<float4*>(s + slot_of<T, V>(i, 4 * q, t)) =
+            make_float4(f[(4 * q) % V], f[(4 * q + 1) % V], f[(4 * q + 2) % V], f[(4 * q + 3) % V]);
+    }
   }
-  return r;
 }
 
 // Kernels overlap their starts: the next one may be started once all CTAs of this one have begun (their launch takes about
@@ -252,9 +273,9 @@ __device__ __forceinline__ void start_after_prior_kernel() {
 
 template <class TX> constexpr int vec_len = sizeof(TX) == 4 ? 4 : 8;   // elements of a 16-byte access
 
-// FEW: at most one row or two for every group of the launch. The weights are then read with the first row, into
-// registers; else they are brought to shared memory once and read from there for every row. 16-bit rows up to 4096: three
-// CTAs per SM (16384 x 2048 bf16: 27.4 us against 30.3 with the two that the compiler's own register count gives; float
+// FEW: at most two rows for every group of the launch, 8 elements per thread. The weights are then read with the first row,
+// into registers; else they are brought to shared memory once and read from there for every row.
+// 16-bit rows up to 4096: three CTAs per SM (16384 x 2048 bf16: 27.4 us against 30.3 with the two that the compiler's own register count gives; float
 // rows 37.2 against 39.6 the other way round).
 template <class TX, class TY, int TPR, int E, bool VEC, bool RES, bool FEW>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && sizeof(TX) == 2 ? 3 : 1)
@@ -291,15 +312,16 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && s
   U wr[FEW ? NV : 1][P], br[FEW ? NV : 1][P];
   if (FEW) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int k = 0; k < P; ++k) {
-        wr[FEW ? i : 0][k] = col_unit<V>(a.w, a.tw, 1.0f, (i * TPR + t) * V + 2 * k, d);
-        br[FEW ? i : 0][k] = col_unit<V>(a.b, a.tw, 0.0f, (i * TPR + t) * V + 2 * k, d);
-      }
+    for (int i = 0; i < NV; ++i) {
+      float f[V];
+      load_vector<V>(a.w, a.tw, a.wide, 1.0f, (i * TPR + t) * V, d, f);
+      as_units<V>(f, wr[FEW ? i : 0]);
+      load_vector<V>(a.b, a.tw, a.wide, 0.0f, (i * TPR + t) * V, d, f);
+      as_units<V>(f, br[FEW ? i : 0]);
+    }
   } else {
-    stage_cols<TPR, TPR, E, V>(w_s, a.w, a.tw, 1.0f, d, CTA, 0);
-    stage_cols<TPR, TPR, E, V>(b_s, a.b, a.tw, 0.0f, d, CTA, 0);
+    stage_cols<TPR, TPR, E, V>(w_s, a.w, a.tw, a.wide, 1.0f, d, CTA, 0);
+    stage_cols<TPR, TPR, E, V>(b_s, a.b, a.tw, a.wide, 0.0f, d, CTA, 0);
     __syncthreads();
   }
   for (; base < rows; base += step) {
@@ -486,7 +508,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
 #pragma unroll
   for (int r = 0; r < R - 1; ++r) fetch((int64_t)base + sub + (int64_t)r * step, r);
   float2 stats = stats_of(base + sub);
-  stage_cols<TPR, T, E, V>(w_s, a.w, a.tw, 1.0f, d, CTA, rank * T);
+  stage_cols<TPR, T, E, V>(w_s, a.w, a.tw, a.wide, 1.0f, d, CTA, rank * T);
   __syncthreads();
   if (CL > 1) {                                                 // the peers run before anything is written to them
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -647,29 +669,27 @@ __global__ void __launch_bounds__(256) k_norm_bwd_cols(const NormArgs a, int par
   a.part[((size_t)blockIdx.y * 2 + 1) * a.d + c] = db;
 }
 
-// dw[c], db[c] = sum over the CTAs' partial sums: a CTA takes 32 columns of the 2 d, each of its 32 warps a 32nd of the
-// partial rows, and the 32 sums are added in order
+// dw[c], db[c] = sum over the CTAs' partial sums: a CTA takes 32 columns of the 2 d, each of its warps every n-th of the
+// partial rows, and the warps' sums are added in order
 __global__ void __launch_bounds__(1024) k_norm_bwd_join(const NormArgs a, int parts) {
-  __shared__ float s[32][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ float s[32][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int64_t col = (int64_t)blockIdx.x * 32 + lane, n = 2 * (int64_t)a.d;
   start_after_prior_kernel();
   float v = 0.f;
   if (col < n) {
     const float* p = a.part + col;
 #pragma unroll 8
-    for (int g = warp; g < parts; g += 32) v += p[(size_t)g * n];
+    for (int g = warp; g < parts; g += warps) v += p[(size_t)g * n];
   }
   s[warp][lane] = v;
   __syncthreads();
-  float r = s[lane][warp];                                      // 32 sums of column `warp`
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
-  const int64_t out = (int64_t)blockIdx.x * 32 + warp;
-  if (lane == 0 && out < n) {
-    if (out < a.d) { if (a.dw) store_any(a.dw, a.tw, out, r); }
-    else if (a.db) store_any(a.db, a.tw, out - a.d, r);
-  }
+  if (warp != 0 || col >= n) return;
+  float r = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < warps; ++i) r += s[i][lane];
+  if (col < a.d) { if (a.dw) store_any(a.dw, a.tw, col, r); }
+  else if (a.db) store_any(a.db, a.tw, col - a.d, r);
 }
 
 constexpr int kSms = 148;
@@ -738,14 +758,15 @@ cudaError_t fwd_k(const NormArgs& a, cudaStream_t st) {
 template <class TX, class TY, int TPR, int E, bool RES, bool FEW>
 cudaError_t fwd_t(const NormArgs& a, cudaStream_t st) {
   if (RES || vec_ok<TX, TY>(a, false)) return fwd_k<TX, TY, TPR, E, true, RES, FEW>(a, st);
-  return fwd_k<TX, TY, TPR, E, false, false, FEW>(a, st);
+  return fwd_k<TX, TY, TPR, E, false, false, WM>(a, st);
 }
 
 // Threads per row. Many rows: 32 elements per thread (few shuffles and barriers per element; the weights pass through
 // shared memory). Up to two rows per SM: 8 elements, the shortest way through one row (64 x 2048: 2.7 us against 5.5).
+// The denoiser's rows (RES) always take one way: same bits for any number of rows.
 template <class TX, class TY, bool RES>
 cudaError_t fwd(const NormArgs& a, cudaStream_t st) {
-  if (!RES && a.rows <= 2 * kSms && a.d > 256 && a.d <= 8192) {   // (the denoiser's rows always take one way: same bits for any number of rows)
+  if (!RES && a.rows <= 2 * kSms && a.d > 256 && a.d <= 8192) {
     if (a.d <= 1024) return fwd_t<TX, TY, 128, 8, RES, true>(a, st);
     if (a.d <= 2048) return fwd_t<TX, TY, 256, 8, RES, true>(a, st);
     if (a.d <= 4096) return fwd_t<TX, TY, 512, 8, RES, true>(a, st);
@@ -823,7 +844,9 @@ cudaError_t bwd(const NormArgs& a, cudaStream_t st) {
     parts = 0;                                     // no rows: the gradients are zeros
   }
   if (!a.dw && !a.db) return cudaSuccess;
-  return launch(k_norm_bwd_join, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), 1024, 0, 1, st, a, parts);
+  // 32 warps per CTA where the CTAs are few, else 8
+  const unsigned ctas = (unsigned)((2 * (int64_t)a.d + 31) / 32);
+  return launch(k_norm_bwd_join, dim3(ctas), ctas <= 2 * kSms ? 1024 : 256, 0, 1, st, a, parts);
 }
 
 }  // namespace
@@ -836,7 +859,9 @@ int norm_parts(int rows, int d) {
   return std::max(1, std::min((rows + rpc - 1) / rpc, resident));
 }
 
-cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
+cudaError_t launch_norm(const NormArgs& args, cudaStream_t st) {
+  NormArgs a = args;
+  a.wide = aligned(a.w, 16) && aligned(a.b, 16);
   if (a.rows <= 0) return cudaSuccess;
   if (a.res) return a.tx == SDS_F32 && a.ty == SDS_BF16 ? fwd<float, Bf16, true>(a, st) : cudaErrorInvalidValue;
   if (a.tx == SDS_F32 && a.ty == SDS_F32) return fwd<float, float, false>(a, st);
@@ -847,7 +872,9 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t st) {
+cudaError_t launch_norm_backward(const NormArgs& args, cudaStream_t st) {
+  NormArgs a = args;
+  a.wide = aligned(a.w, 16) && aligned(a.b, 16);
   if (a.tx == SDS_F32 && a.ty == SDS_F32) return bwd<float, float>(a, st);
   if (a.tx == SDS_F32 && a.ty == SDS_BF16) return bwd<float, Bf16>(a, st);
   if (a.tx == SDS_F32 && a.ty == SDS_F16) return bwd<float, F16>(a, st);
