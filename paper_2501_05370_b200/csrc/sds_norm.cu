@@ -758,7 +758,7 @@ cudaError_t fwd_k(const NormArgs& a, cudaStream_t st) {
 template <class TX, class TY, int TPR, int E, bool RES, bool FEW>
 cudaError_t fwd_t(const NormArgs& a, cudaStream_t st) {
   if (RES || vec_ok<TX, TY>(a, false)) return fwd_k<TX, TY, TPR, E, true, RES, FEW>(a, st);
-  return fwd_k<TX, TY, TPR, E, false, false, WM>(a, st);
+  return fwd_k<TX, TY, TPR, E, false, false, FEW>(a, st);
 }
 
 // Threads per row. Many rows: 32 elements per thread (few shuffles and barriers per element; the weights pass through
