@@ -143,7 +143,7 @@ typedef int (*sds_denoise_fn)(void* user, const float* x_dev, const int32_t* k_d
  *   dims = { d, f, act }: f the hidden width, act one of SDS_ACT_*; d <= 16384, d and f multiples of 8.
  *   W_dev[3l], [3l+1], [3l+2]: Wg_l [f, d], Wu_l [f, d], Wd_l [d, f], bf16 row-major, 16-byte aligned;
  *   bias_dev[2l], [2l+1]: [d] float weight and bias of the norm (NULL = ones, zeros); temb_dev[l]: [K, d] bf16 embedding
- *   rows, 16-byte aligned (NULL = none).
+ *   rows, 16-byte aligned (NULL = none). sds_denoise then takes 16-byte aligned rows (else SDS_EUNSUPPORTED).
  * PHI4: D(x) = grad E(x), E(x) = coupling/2 sum_{|i-j|=1} (x_i - x_j)^2 + sum_i (x_i^2 - 1)^2 on a
  *   grid_side x grid_side lattice (d = grid_side^2), every neighbouring pair once, free boundaries
  *   unless periodic != 0. Used with the Langevin schedule a = 1, c = -gamma, sigma = sqrt(2 gamma). */
@@ -429,7 +429,7 @@ int sds_layer_norm_backward(const void* dy_dev, int64_t lddy, int32_t y_dtype, c
  * x_dev, y_dev [rows, d], rows ldx / ldy elements apart; wg_dev, wu_dev [f, d], wd_dev [d, f] dense; all of one
  * dtype, SDS_BF16 or SDS_F16. d, f, ldx and ldy multiples of 8 and every pointer 16-byte aligned (else
  * SDS_EUNSUPPORTED). Products are accumulated in float; the hidden rows h = act(x Wg^T) * (x Wu^T) are rounded to
- * dtype, as operands of the second product. keep_dev: what the backward pass needs of the forward one, opaque, 256-byte
+ * dtype, as operands of the second product (a hidden value beyond dtype's range becomes an infinity). keep_dev: what the backward pass needs of the forward one, opaque, 256-byte
  * aligned, keep_bytes of sds_gated_ffn_bytes (NULL = no backward pass will follow). workspace_dev: 256-byte
  * aligned, forward_bytes (smaller with keep_dev: the hidden rows then live there).
  * The result of a row may differ in the last bit with the number of rows of the call. */

@@ -551,6 +551,7 @@ int run_denoiser(sds_ctx* c, Engine& e, const float* X, const uint16_t* Xb, cons
     case SDS_DEN_GATED: {
       // the residual stream is the output buffer; every row's result is the same bits whatever rows it shares the launch
       // with (the drafter evaluated at Y_n relies on it)
+      if ((reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(out)) % 16) return SDS_EUNSUPPORTED;
       const int f = e.mlp_dims[1];
       uint16_t* normed = at<uint16_t>(c, e.lay.H0);
       for (int l = 0; l < e.den.nlayer; ++l) {

@@ -1,7 +1,8 @@
 """Layer operators of gated denoisers on torch CUDA tensors: layer norm and the gated feed-forward block, each
 with its backward pass (include/sds.h documents the formulas). Every call enqueues on the current stream of its
 tensors' device and does not wait. Outputs and workspaces are allocated by torch unless they are passed in. A bad
-argument raises ValueError, an error of the library SdsError.
+argument raises ValueError, an error of the library SdsError. Nothing is recorded for autograd: the backward calls are
+the gradients.
 """
 from __future__ import annotations
 

@@ -146,3 +146,19 @@ def test_layer_calls_give_the_denoisers_rows():
     # (the public call rounds the block's output to bfloat16 before it is added, half a step of it)
     assert float((r - want).norm() / want.norm()) <= 2.0 ** -8
     s.close()
+
+
+def test_picard_drafter_and_misaligned_rows():
+    import torch
+    w = _workload(128, 256, 1, 20, 30, 4)
+    s = sds.sampler_for(w, gated=w.gated_params(), picard=sds.picard_for(w, 2))
+    out = s.sample_all()[0].cpu().numpy()
+    assert np.all(np.isfinite(out)) and np.array_equal(s.get(sb.GET_N), np.full(30, 20))
+    s.close()
+    s = sds.sampler_for(w, gated=w.gated_params())
+    buf = torch.zeros(4 * 128 + 1, device="cuda")
+    k = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(sds.SdsError) as e:
+        s.denoise(buf[1:].view(4, 128), k)
+    assert e.value.code == sb.SDS_EUNSUPPORTED
+    s.close()

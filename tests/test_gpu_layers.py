@@ -500,3 +500,107 @@ def test_status_word_of_the_workspace():
     assert e.value.code == sb.SDS_ETIMEOUT
     sds.gated_ffn(x, wg, wu, wd, workspace=ws)
     sds.gated_ffn_status(ws)
+
+
+def test_capture_of_a_first_call():
+    """A process whose first call of an operator is a captured one (nothing is looked up on the device before)."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2501_05370_b200 as sds
+torch.manual_seed(0)
+x, w = torch.randn(300, 256, device="cuda").bfloat16(), torch.randn(3, 512, 256, device="cuda").bfloat16()
+wd = w[2].t().contiguous()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    n, m, r = sds.layer_norm(x, stats=True)
+    y, k = sds.gated_ffn(n, w[0], w[1], wd, keep=True)
+    d = sds.gated_ffn_backward(y, n, w[0], w[1], wd, k)
+    e = sds.layer_norm_backward(d[0], x, None, m, r)
+g.replay()
+torch.cuda.synchronize()
+n, m, r = sds.layer_norm(x, stats=True)
+y2, k = sds.gated_ffn(n, w[0], w[1], wd, keep=True)
+d2 = sds.gated_ffn_backward(y2, n, w[0], w[1], wd, k)
+e2 = sds.layer_norm_backward(d2[0], x, None, m, r)
+assert all(torch.equal(a, b) for a, b in zip((y,) + d + e, (y2,) + d2 + e2))
+print("same")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=root, timeout=240)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+def test_backward_on_two_streams_at_once():
+    a, b = ffn_inputs(700, 256, 1024, BF16, 50), ffn_inputs(90, 512, 768, BF16, 51)
+
+    def step(x, wg, wu, wd, dy):
+        n, m, r = sds.layer_norm(x, stats=True)
+        y, kept = sds.gated_ffn(n, wg, wu, wd, keep=True)
+        g = sds.gated_ffn_backward(dy, n, wg, wu, wd, kept)
+        return (y,) + g + sds.layer_norm_backward(g[0], x, None, m, r)
+    alone = [step(*v) for v in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(4):
+        for k, v in enumerate((a, b)):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(step(*v))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out in got[k]:
+            assert all(torch.equal(p, q) for p, q in zip(out, alone[k]))
+
+
+def test_a_call_behind_a_kernel_that_writes_its_inputs():
+    """Kernels start beside the end of the kernel in front: what that one writes, weights included, is what they read."""
+    x, wg, wu, wd, dy = ffn_inputs(40, 512, 1024, BF16, 60)
+    fresh = [ffn_inputs(40, 512, 1024, BF16, 61 + k) for k in range(6)]
+    w, b = torch.ones(512, device="cuda"), torch.zeros(512, device="cuda")
+    got = []
+    for v in fresh:
+        for to, src in zip((x, wg, wu, wd, dy), v):
+            to.copy_(src)
+        w.mul_(1.25)
+        n, m, r = sds.layer_norm(x, w, b, stats=True)
+        wg.mul_(2.0)
+        y, kept = sds.gated_ffn(n, wg, wu, wd, keep=True)
+        got.append((y, sds.gated_ffn_backward(dy, n, wg, wu, wd, kept)))
+    torch.cuda.synchronize()
+    scale = 1.0
+    for v, (y, g) in zip(fresh, got):
+        scale *= 1.25
+        n = sds.layer_norm(v[0], torch.full_like(w, scale), b)
+        torch.cuda.synchronize()
+        y2, kept = sds.gated_ffn(n, v[1] * 2, v[2], v[3], keep=True)
+        assert torch.equal(y, y2)
+        assert all(torch.equal(p, q) for p, q in zip(g, sds.gated_ffn_backward(v[4], n, v[1] * 2, v[2], v[3], kept)))
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes (and 2^31 elements) per array: the last rows are what they are in a small call."""
+    rows, d = 140000, 16384
+    r = gen(70)
+    x = torch.zeros(rows, d, device="cuda", dtype=BF16)
+    x[-3:] = r(3, d).to(BF16)
+    y, m, rs = sds.layer_norm(x, stats=True)
+    want, _, _, xhat = plain_norm(x[-3:], None, None, 1e-5)
+    close(y[-3:], want, norm_bound(xhat, None, None, d))
+    dy = torch.zeros_like(x)
+    dy[-3:] = r(3, d).to(BF16)
+    dx = sds.layer_norm_backward(dy, x, None, m, rs, want=(True, False, False))[0]
+    small = sds.layer_norm_backward(dy[-3:], x[-3:], None, m[-3:], rs[-3:], want=(True, False, False))[0]
+    assert torch.equal(dx[-3:], small) and (dx[:-3] == 0).all()
+    del x, y, dy, dx, m, rs
+    rows, d, f = 300000, 64, 8192
+    x, wg, wu, wd, dy = ffn_inputs(rows, d, f, BF16, 71)
+    y, kept = sds.gated_ffn(x, wg, wu, wd, keep=True)
+    dx = sds.gated_ffn_backward(dy, x, wg, wu, wd, kept, want=(1, 0, 0, 0))[0]
+    tail = slice(rows - 500, rows)
+    ref = Ffn64(x[tail], wg, wu, wd, "silu", BF16)
+    close(y[tail], ref.y, ref.ey)
+    ref.backward(dy[tail])
+    close(dx[tail], ref.dx, ref.edx)
