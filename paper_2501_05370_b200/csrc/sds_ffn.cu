@@ -74,9 +74,8 @@ struct FfnTileArgs {
   void* out2;                                     // kFfnDGlu: dU (out is dG)
   int* err;
   int clear_err;                                  // (see FfnSplitArgs)
-  int beside;                                     // reads nothing of the kernel in front, which was itself started after the
-                                                  // end of the one before it (FfnSplitArgs::late): runs beside it, and
-                                                  // waits for it only in the end
+  int beside;                                     // reads nothing of the kernel in front: runs beside it, and waits for
+                                                  // it only in the end
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -169,7 +168,10 @@ __device__ __forceinline__ void add_rows64(uint4* stg, const uint32_t* w, float*
 }
 
 // Kernels overlap their starts: one may be started when all CTAs of the one in front have said so (or ended), and waits
-// for that kernel's end, and for its writes, here.
+// for that kernel's end, and for its writes, here. Every kernel of this file says so only once its own wait is over. What
+// ran before the kernel in front has then ended before this one starts: weights, which the kernel in front
+// does not write, may be read ahead of the wait (k_ffn_split), and kernels that read nothing of the one in front may
+// run beside it (FfnTileArgs::beside).
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_prior_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -277,8 +279,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   if (PAIR) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_s;
-  launch_dependents();
   if (!g.beside) wait_for_prior_kernel();         // (nothing in device memory is read or written before)
+  launch_dependents();
   if (g.clear_err && blockIdx.x == 0 && threadIdx.x == 0) *g.err = 0;
   const int M0 = g.nrows_dev ? min(*g.nrows_dev, g.p[0].M) : g.p[0].M;
 
@@ -536,7 +538,6 @@ struct FfnSplitArgs {
   int* err;
   int clear_err;                                  // first kernel of a call: the status word starts at zero. A wait gives
                                                   // up only after millions of polls, long after the first CTA began.
-  int late;                                       // the next kernel may be started only when the one before this has ended
 };
 
 constexpr int kSplitThreads = 256;
@@ -595,7 +596,6 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_s;
-  if (!g.late) launch_dependents();
 
   if (warp == 0 && lane == 0) {
     int stage = 0;
@@ -619,8 +619,8 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       const int seg = kb >= kb_seg ? 1 : 0, kk = (kb - seg * kb_seg) * kBK;
       tma_load_2d(stages + stage * C::kStageBytes + C::kABytes, &g.t[seg], kk, tok0, full_bar + stage);
     };
-    // Behind a kernel of the same call: that one writes the tokens, not the weights, and what ran before it had ended
-    // when it went past its own wait. So the first stages' weights are requested before it has ended.
+    // Behind a kernel of the same call: that one writes the tokens, not the weights. So the first stages' weights are
+    // requested before it has ended.
     const int ahead = min(kb1 - kb0, C::kStages);
     if (g.clear_err) wait_for_prior_kernel();
     for (int i = 0; i < ahead; ++i) { weights(kb0 + i); ++stage; }
@@ -645,6 +645,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
+    wait_for_prior_kernel();                      // (however long that one runs: the polls below count from here)
     for (int kb = kb0; kb < kb1; ++kb) {
       if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
       tc_fence_after();
@@ -665,8 +666,8 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   }
   __syncwarp();
 
-  wait_for_prior_kernel();                        // (nothing in device memory is read or written before)
-  if (g.late) launch_dependents();
+  wait_for_prior_kernel();                        // (nothing else in device memory is read or written before)
+  launch_dependents();
   if (g.clear_err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
   // the accumulator to shared memory, [token][row of the instruction]
   const bool ok = mbar_wait_warp(tfull_bar, 0u, abort_s);
@@ -974,7 +975,7 @@ bool prefer_split(int rows, int N, int nkb) {
 }
 
 template <int EPI>
-cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st, bool late = false) {
+cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   const int bn = split_tokens(a.rows);
   FfnSplitArgs g;
@@ -985,7 +986,6 @@ cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool
   g.out = s.out; g.out2 = s.out2; g.ldo = s.ldo;
   g.err = a.err;
   g.clear_err = first;
-  g.late = late;
   const int nw = EPI == kFfnGlu ? 2 : s.nseg;
   for (int k = 0; k < nw; ++k)
     if (!map_operand(&g.w[k], s.w[k], a.f16 != 0, s.N, s.K, s.w_mn, EPI == kFfnGlu ? 64 : 128)) return cudaErrorInvalidValue;
@@ -1095,7 +1095,7 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
     s.w[0] = {a.wg, a.d}; s.w[1] = {a.wu, a.d}; s.t[0] = {a.dg, a.f}; s.t[1] = {a.du, a.f};
     s.nseg = 2; s.w_mn = true; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
     beside = true;                                // (the weights' gradients, launched next, do not read dx)
-    if ((e = launch_split<kFfnOut>(a, s, nullptr, false, st, beside)) != cudaSuccess) return e;
+    if ((e = launch_split<kFfnOut>(a, s, nullptr, false, st)) != cudaSuccess) return e;
   } else if (a.dx) {
     ProductSpec s{};
     s.a[0] = {a.dg, a.f}; s.a[1] = {a.du, a.f}; s.b[0] = {a.wg, a.d}; s.b[1] = {a.wu, a.d};

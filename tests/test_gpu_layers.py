@@ -604,3 +604,46 @@ def test_offsets_past_32_bits():
     close(y[tail], ref.y, ref.ey)
     ref.backward(dy[tail])
     close(dx[tail], ref.dx, ref.edx)
+
+
+def test_weights_written_by_an_operator_in_front():
+    """The second product's kernel asks for its weights before the first one has ended, and must not read them before the
+    operator in front of the whole call has written them: here that operator makes every weight in turn."""
+    d, f = 1024, 2048
+    x, wg, wu, wd, dy = ffn_inputs(8, d, f, BF16, 80)
+    raw = [ffn_inputs(8, d, f, BF16, 81 + k)[1:4] for k in range(12)]
+    weights = [torch.empty_like(v) for v in (wg, wu, wd)]
+    got = []
+    for v in raw:
+        for which in (2, 0, 1, 2):                 # the forward call comes right behind the one that writes w_down
+            sds.layer_norm(v[which], out=weights[which])
+        y, kept = sds.gated_ffn(x, *weights, keep=True)
+        for which in (2, 0, 1):                    # the gradient call behind the one that writes w_up (the same values)
+            sds.layer_norm(v[which], out=weights[which])
+        got.append((y,) + sds.gated_ffn_backward(dy, x, *weights, kept))
+        for w in weights:
+            sds.layer_norm(raw[0][0].reshape(w.shape), out=w)      # (other values again)
+    torch.cuda.synchronize()
+    for v, out in zip(raw, got):
+        normed = [sds.layer_norm(w) for w in v]
+        torch.cuda.synchronize()
+        y, kept = sds.gated_ffn(x, *normed, keep=True)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, (y,) + sds.gated_ffn_backward(dy, x, *normed, kept)))
+
+
+def test_a_small_call_behind_a_long_one():
+    """A few-row call starts on the SMs that a long call leaves free, and waits there without counting its polls."""
+    big = torch.randn(1 << 22, 64, device="cuda").to(BF16)
+    w = [torch.randn(64, 64, device="cuda").to(BF16) for _ in range(3)]
+    _, kept = sds.gated_ffn(big, *w, keep=True)
+    ws = torch.empty(sds.gated_ffn_bytes(1 << 22, 64, 64).backward_bytes, device="cuda", dtype=torch.uint8)
+    x, wg, wu, wd, _ = ffn_inputs(4, 512, 1024, BF16, 90)
+    want = sds.gated_ffn(x, wg, wu, wd)
+    ws2 = torch.empty(sds.gated_ffn_bytes(4, 512, 1024).forward_bytes, device="cuda", dtype=torch.uint8)
+    torch.cuda.synchronize()
+    sds.gated_ffn_backward(big, big, *w, kept, workspace=ws)
+    y = sds.gated_ffn(x, wg, wu, wd, workspace=ws2)
+    sds.gated_ffn_status(ws2)
+    sds.gated_ffn_status(ws)
+    assert torch.equal(y, want)
