@@ -400,7 +400,8 @@ int sds_gmm_denoise_static(const float* x_dev, const int32_t* k_dev, int64_t row
  * Layer operators: the parts of a gated denoiser, forward and backward, for programs that train one or run
  * one outside a context. Like sds_gmm_denoise_static they need no context: device pointers and a stream in, work
  * enqueued on cuda_stream (cudaStream_t, NULL = default stream) of the current device, no wait, no allocation.
- * Outputs must not overlap inputs or workspaces. rows = 0 is allowed. Two calls that can run at the same time
+ * Outputs must not overlap inputs or workspaces. rows = 0 is allowed; rows, d and f
+ * are at most 2^30 (else SDS_EINVAL). Two calls that can run at the same time
  * (other streams, or two captured graphs) need workspaces of their own. The calls can be captured into a graph.
  *
  * Layer norm over rows of d elements:
@@ -429,9 +430,10 @@ int sds_layer_norm_backward(const void* dy_dev, int64_t lddy, int32_t y_dtype, c
  * x_dev, y_dev [rows, d], rows ldx / ldy elements apart; wg_dev, wu_dev [f, d], wd_dev [d, f] dense; all of one
  * dtype, SDS_BF16 or SDS_F16. d, f, ldx and ldy multiples of 8 and every pointer 16-byte aligned (else
  * SDS_EUNSUPPORTED). Products are accumulated in float; the hidden rows h = act(x Wg^T) * (x Wu^T) are rounded to
- * dtype, as operands of the second product (a hidden value beyond dtype's range becomes an infinity). keep_dev: what the backward pass needs of the forward one, opaque, 256-byte
- * aligned, keep_bytes of sds_gated_ffn_bytes (NULL = no backward pass will follow). workspace_dev: 256-byte
- * aligned, forward_bytes (smaller with keep_dev: the hidden rows then live there).
+ * dtype, as operands of the second product (a hidden value beyond dtype's range becomes an infinity). keep_dev: what
+ * the backward pass needs of the forward one, opaque, 256-byte aligned, keep_bytes of sds_gated_ffn_bytes (NULL = no
+ * backward pass will follow). workspace_dev: 256-byte aligned, forward_bytes (smaller with keep_dev: the hidden rows
+ * then live there).
  * The result of a row may differ in the last bit with the number of rows of the call. */
 #define SDS_ACT_SILU      0     /* g / (1 + exp(-g)) */
 #define SDS_ACT_GELU      1     /* g Phi(g), Phi the normal distribution function */

@@ -1064,7 +1064,7 @@ cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st) {
 
 cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
-  if (a.rows <= 0) {                              // an empty sum: the weights' gradients are zeros
+  if (a.rows <= 0 || !(a.dx || a.dwg || a.dwu || a.dwd)) {   // an empty sum: the weights' gradients are zeros
     if ((e = cudaMemsetAsync(a.err, 0, sizeof(int), st)) != cudaSuccess) return e;
     for (void* w : {a.dwg, a.dwu, a.dwd})
       if (w && (e = cudaMemsetAsync(w, 0, (size_t)a.d * a.f * 2, st)) != cudaSuccess) return e;

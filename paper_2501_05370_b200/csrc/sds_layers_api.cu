@@ -10,7 +10,7 @@ using namespace sds;
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxSize = (int64_t)1 << 30;   // of rows, d and f each: the kernels count them in 32 bits
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 inline bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline bool is_type(int32_t t) { return t == SDS_F32 || t == SDS_BF16 || t == SDS_F16; }
@@ -23,7 +23,7 @@ int result(cudaError_t e) {
 }
 
 int check_norm(int64_t rows, int32_t d, int32_t x_dtype, int32_t y_dtype, int32_t w_dtype) {
-  if (rows < 0 || rows > kMaxRows || d <= 0) return SDS_EINVAL;
+  if (rows < 0 || rows > kMaxSize || d <= 0 || d > kMaxSize) return SDS_EINVAL;
   if (!is_type(x_dtype) || !is_type(y_dtype) || !is_type(w_dtype)) return SDS_EUNSUPPORTED;
   if (y_dtype != x_dtype && x_dtype != SDS_F32) return SDS_EUNSUPPORTED;
   return SDS_OK;
@@ -46,7 +46,7 @@ size_t norm_bytes(int64_t rows, int32_t d) {
 }
 
 int check_ffn(int64_t rows, int32_t d, int32_t f) {
-  if (rows < 0 || rows > kMaxRows || d <= 0 || f <= 0) return SDS_EINVAL;
+  if (rows < 0 || rows > kMaxSize || d <= 0 || d > kMaxSize || f <= 0 || f > kMaxSize) return SDS_EINVAL;
   return d % 8 || f % 8 ? SDS_EUNSUPPORTED : SDS_OK;
 }
 
@@ -95,7 +95,7 @@ int sds_layer_norm(const void* x_dev, int64_t ldx, int32_t x_dtype, const void* 
 }
 
 int sds_layer_norm_workspace_bytes(int64_t rows, int32_t d, size_t* bytes) {
-  if (!bytes || rows < 0 || rows > kMaxRows || d <= 0) return SDS_EINVAL;
+  if (!bytes || rows < 0 || rows > kMaxSize || d <= 0 || d > kMaxSize) return SDS_EINVAL;
   *bytes = norm_bytes(rows, d);
   return SDS_OK;
 }

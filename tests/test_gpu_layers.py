@@ -647,3 +647,11 @@ def test_a_small_call_behind_a_long_one():
     sds.gated_ffn_status(ws2)
     sds.gated_ffn_status(ws)
     assert torch.equal(y, want)
+
+
+def test_backward_of_nothing_sets_the_status_word():
+    x, wg, wu, wd, dy = ffn_inputs(5, 64, 64, BF16, 95)
+    _, kept = sds.gated_ffn(x, wg, wu, wd, keep=True)
+    ws = torch.full((sds.gated_ffn_bytes(5, 64, 64).backward_bytes,), 255, device="cuda", dtype=torch.uint8)
+    assert sds.gated_ffn_backward(dy, x, wg, wu, wd, kept, want=(0, 0, 0, 0), workspace=ws) == (None,) * 4
+    sds.gated_ffn_status(ws)

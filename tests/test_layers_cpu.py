@@ -180,3 +180,14 @@ def test_oracle_gated_block_by_hand():
     for name in ("silu", "gelu", "gelu_tanh"):
         assert o.gated_activation(o.np.zeros(3), name).tolist() == [0.0, 0.0, 0.0]
         assert abs(o.gated_activation(o.np.array([30.0]), name)[0] - 30.0) < 1e-9
+
+
+def test_sizes_beyond_32_bit_counters_are_refused():
+    big = (1 << 30) + 8
+    n, s = C.c_size_t(0), sb.SdsGatedFfnSizes()
+    assert _norm(d=big, ldx=big, ldy=big) == sb.SDS_EINVAL
+    assert _norm_bwd(d=big, ldx=big, lddy=big, lddx=big, bytes=1 << 60) == sb.SDS_EINVAL
+    assert sds.load().sds_layer_norm_workspace_bytes(1, big, C.byref(n)) == sb.SDS_EINVAL
+    assert _ffn(d=big, ldx=big, ldy=big, bytes=1 << 60) == sb.SDS_EINVAL and _ffn(f=big, bytes=1 << 60) == sb.SDS_EINVAL
+    assert _ffn_bwd(f=big, bytes=1 << 60) == sb.SDS_EINVAL
+    assert sds.load().sds_gated_ffn_bytes(1, 64, big, C.byref(s)) == sb.SDS_EINVAL
