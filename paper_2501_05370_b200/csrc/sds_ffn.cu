@@ -59,6 +59,8 @@ struct FfnProduct {
   int M, N, K;                                    // K of one segment
   int nseg, a_mn;
   int band;                                       // tile rows of a band (see tile_at)
+  int parts;                                      // > 1: K is cut into so many, a tile is one part of one output tile, and
+  float* part;                                    // its sums go here (part_index) for k_ffn_join
   void* out;
   int64_t ldo;
 };
@@ -175,6 +177,15 @@ __device__ __forceinline__ void add_rows64(uint4* stg, const uint32_t* w, float*
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_prior_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// A wait for the products of `steps` steps of K: the limit of one wait, and of another for every 2^15 steps (about 10 ms).
+__device__ __forceinline__ bool wait_for_sums(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int steps) {
+  for (int i = 0; i <= steps >> 15; ++i) {
+    if (mbar_wait_warp(bar, parity, abort_flag)) return true;
+    if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
+  }
+  return false;
+}
+
 // ---------------------------------------------------------------------------------------------
 // batches: persistent tiles
 // ---------------------------------------------------------------------------------------------
@@ -193,18 +204,31 @@ template <int BN, bool PAIR> struct FfnTile {
 };
 
 struct TileAt {
-  int prod, m, n;                                 // product, tile row, tile column
+  int prod, m, n, part;                           // product, tile row, tile column, part of K
 };
+
+// first step of K of part `i`
+__device__ __forceinline__ int first_step(int steps, int parts, int i) { return (int)((int64_t)steps * i / parts); }
+
+// the sums of a cut product, in 32 x 32 blocks: [row block][column block][part][column quad][row] quads, the order in which an
+// epilogue's threads hold them
+__device__ __forceinline__ size_t part_index(int row, int col, int ncc, int parts, int part) {
+  return ((((size_t)(row >> 5) * ncc + (col >> 5)) * parts + part) * 8 + ((col & 31) >> 2)) * 128 + (size_t)(row & 31) * 4;
+}
 
 // Tiles of all products in one sequence. Within a product, bands of `band` tile rows are walked column by column: the
 // band's rows of A stay in L2 while B passes by.
-template <int TM, int TN>
+template <int TM, int TN, bool CUT>
 __device__ __forceinline__ bool tile_at(const FfnTileArgs& g, int m0_rows, int t, TileAt* at) {
   for (int p = 0; p < g.np; ++p) {
     const int M = p == 0 ? m0_rows : g.p[p].M;
     const int mt = (M + TM - 1) / TM, nt = (g.p[p].N + TN - 1) / TN;
-    const int n = mt * nt;
+    const int n = mt * nt * (CUT ? g.p[p].parts : 1);
     if (t < n) {
+      if (CUT) {
+        at->part = t / (mt * nt);
+        t -= at->part * mt * nt;
+      }
       const int height = g.p[p].band, band = t / (height * nt), in = t - band * height * nt;
       const int rows = min(height, mt - band * height);
       at->prod = p;
@@ -239,7 +263,8 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
 // MN: B is MN-major and A either (the gradients); else both are K-major. The loops of the two single threads that feed the
 // tensor cores are written out per order: with the order looked up in every step they took 735 cycles per step of K where
 // the products take 512 (16384 x 2048 x 8192, forward projections: 676 -> 605 us at full clocks).
-template <int BN, int EPI, bool PAIR, bool MN>
+// CUT: products whose K is cut (FfnProduct::parts); its own kernel, as the others lose up to 5 % to the arithmetic.
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT>
 __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
   using C = FfnTile<BN, PAIR>;
   constexpr int TM = C::kTM, TN = EPI == kFfnGlu ? BN / 2 : BN;    // output columns of a tile
@@ -292,18 +317,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       uint32_t phase = 0;
       bool ok = true;
       const uint32_t leader_full0 = PAIR ? map_to_cta(smem_u32(full_bar), 0u) : 0u;
-      for (int it = 0; ok && tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
+      for (int it = 0; ok && tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
         const FfnProduct& p = g.p[at.prod];
         const int m0 = at.m * TM + (int)rank * kBM;
         const int n0 = at.n * TN + (EPI == kFfnGlu ? 0 : (int)rank * C::kBRows);
         const int K = p.K, nseg = p.nseg;
+        int seg_steps = 0, kb0 = 0, kb1 = 0;      // CUT: of a segment; first and behind the last of this part
+        if (CUT) {
+          seg_steps = (K + kBK - 1) / kBK;
+          kb0 = first_step(seg_steps * nseg, p.parts, at.part);
+          kb1 = first_step(seg_steps * nseg, p.parts, at.part + 1);
+        }
         const auto feed = [&](auto order) {
           constexpr bool a_mn = decltype(order)::value;
           for (int seg = 0; seg < nseg && ok; ++seg) {
             const CUtensorMap* ta = &p.a[seg];
             // the tile's columns of Wg, then those of Wu: one CTA of a pair each, or one after the other
             const CUtensorMap* tb = &p.b[EPI == kFfnGlu && PAIR ? (int)rank : seg];
-            for (int kk = 0; kk < K; kk += kBK) {
+            const int begin = CUT ? max(kb0 - seg * seg_steps, 0) * kBK : 0;
+            const int end = CUT ? min(kb1 - seg * seg_steps, seg_steps) * kBK : K;
+            for (int kk = begin; kk < end; kk += kBK) {
               if (!mbar_wait(empty_bar + stage, phase ^ 1u, abort_s)) { ok = false; break; }
               uint8_t* sa = stages + stage * C::kStageBytes;
               uint8_t* sb = sa + C::kABytes;
@@ -349,10 +382,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       int stage = 0, it = 0;
       uint32_t phase = 0;
       bool ok = true;
-      bool more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, 0), &at);
+      bool more = tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, 0), &at);
       for (; ok && more; ++it) {
         const FfnProduct& p = g.p[at.prod];
-        const int nkb = (p.K + kBK - 1) / kBK * p.nseg;
+        const int all = (p.K + kBK - 1) / kBK * p.nseg;
+        const int nkb = CUT ? first_step(all, p.parts, at.part + 1) - first_step(all, p.parts, at.part) : all;
         const int buf = it & 1;
         if (!mbar_wait(tempty_bar + buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_s)) { ok = false; break; }
         tc_fence_after();
@@ -376,7 +410,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
             if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
             if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
             // where the next tile lies takes a few divisions: worked out while this tile's products run
-            if (kb == 0) more = tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
+            if (kb == 0) more = tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
           }
         };
         if (MN && p.a_mn) multiply(Bool<MN>()); else multiply(Bool<false>());
@@ -396,7 +430,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
     const int f16 = g.f16;
     int it = 0;
     bool ok = true;
-    for (; ok && tile_at<TM, TN>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
+    for (; ok && tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
       const FfnProduct& p = g.p[at.prod];
       const int M = at.prod == 0 ? M0 : p.M, N = p.N;
       const int buf = it & 1;
@@ -416,7 +450,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
         }
       };
       if (EPI == kFfnDGlu) keep_fetch(n0);
-      if (!mbar_wait_warp(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s)) { ok = false; break; }
+      if (!wait_for_sums(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s, (p.K + kBK - 1) / kBK * p.nseg)) { ok = false; break; }
       tc_fence_after();
 #pragma unroll 1
       for (int chunk = 0; chunk < kChunks; ++chunk) {
@@ -469,6 +503,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
           });
           store_rows64(stg, w, static_cast<char*>(p.out) + ((size_t)row0 * p.ldo + col) * 2, (size_t)p.ldo * 2, nlive,
                        npieces, lane);
+        } else if (CUT && p.parts > 1) {
+          float4* to = reinterpret_cast<float4*>(p.part + part_index(row0 + lane, col, ncc, p.parts, at.part));
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            to[i * 32] = make_float4(__uint_as_float(acc[4 * i]), __uint_as_float(acc[4 * i + 1]),
+                                     __uint_as_float(acc[4 * i + 2]), __uint_as_float(acc[4 * i + 3]));
         } else if (EPI == kFfnOut) {
           uint32_t w[16];
 #pragma unroll
@@ -519,6 +559,39 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
     else
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+  }
+}
+
+struct FfnJoinArgs {
+  struct { const float* part; uint16_t* out; int M, N; } p[3];
+  int np, parts, f16;
+};
+
+// The parts of cut products, added in the order of K. A warp takes a quad of columns of a 32 x 32 block, a lane one row of
+// it. Bound by the latency of reading the parts, which lie in L2 (products are cut only where they are small).
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) k_ffn_join(const FfnJoinArgs g) {
+  const int lane = threadIdx.x & 31;
+  int64_t b = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) >> 5;
+  wait_for_prior_kernel();
+  launch_dependents();
+  for (int p = 0; p < g.np; ++p) {
+    const int M = g.p[p].M, N = g.p[p].N, ncc = (N + 31) >> 5;
+    const int64_t n = (int64_t)((M + 31) >> 5) * ncc * 8;
+    if (b < n) {
+      const int block = (int)(b >> 3), row = block / ncc * 32 + lane, col = block % ncc * 32 + (int)(b & 7) * 4;
+      if (row >= M || col >= N) return;
+      const float4* from = reinterpret_cast<const float4*>(g.p[p].part + part_index(row, col, ncc, g.parts, 0));
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int i = 0; i < g.parts; ++i) {
+        const float4 v = from[(size_t)i * 256];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      *reinterpret_cast<uint2*>(g.p[p].out + (size_t)row * N + col) = make_uint2(pack16(s.x, s.y, g.f16), pack16(s.z, s.w, g.f16));
+      return;
+    }
+    b -= n;
   }
 }
 
@@ -670,7 +743,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   launch_dependents();
   if (g.clear_err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
   // the accumulator to shared memory, [token][row of the instruction]
-  const bool ok = mbar_wait_warp(tfull_bar, 0u, abort_s);
+  const bool ok = wait_for_sums(tfull_bar, 0u, abort_s, kb1 - kb0);
   if (ok) {
     tc_fence_after();
     const int q = warp & 3, half = warp >> 2;
@@ -778,7 +851,7 @@ struct KernelInfo {
   std::atomic<int> resident[kMaxDevices];         // 0: not looked up; else 1 + resident CTAs (clusters of a pair)
 };
 
-template <int BN, int EPI, bool PAIR, bool MN>
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT>
 cudaError_t tile_resident(int* n) {
   static KernelInfo info;                         // zero-initialised
   using C = FfnTile<BN, PAIR>;
@@ -786,7 +859,7 @@ cudaError_t tile_resident(int* n) {
   if (dev < 0) return cudaErrorInvalidDevice;
   int r = info.resident[dev].load(std::memory_order_acquire);
   if (r == 0) {
-    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     int sms = 0, got = 0;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
@@ -801,7 +874,7 @@ cudaError_t tile_resident(int* n) {
       attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
-      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN>, &cfg)) != cudaSuccess) return e;
+      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN, CUT>, &cfg)) != cudaSuccess) return e;
       got = std::min(got, sms / 2);
     }
     if (got < 1) return cudaErrorLaunchOutOfResources;
@@ -812,11 +885,11 @@ cudaError_t tile_resident(int* n) {
   return cudaSuccess;
 }
 
-template <int BN, int EPI, bool PAIR, bool MN>
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT>
 cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) {
   using C = FfnTile<BN, PAIR>;
   int resident = 0;
-  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN>(&resident);
+  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN, CUT>(&resident);
   if (e != cudaSuccess) return e;
   const int workers = (int)std::min<int64_t>(tiles, resident);
   cudaLaunchConfig_t cfg{};
@@ -828,7 +901,7 @@ cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) 
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   launch_attributes(attr, PAIR ? 2 : 1);
-  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN>, g);
+  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN, CUT>, g);
 }
 
 // where an operand lies: [rows, cols] with rows ld elements apart; K-major if K runs along the columns
@@ -850,17 +923,19 @@ struct ProductSpec {
   int M, N, K;
   void* out;
   int64_t ldo;
+  int parts = 1;                                  // of K, each with its own tiles
+  float* part = nullptr;
 };
 
-inline int64_t tiles_of(const ProductSpec& s, int tm, int tn) {
-  return (int64_t)((s.M + tm - 1) / tm) * ((s.N + tn - 1) / tn);
-}
-inline int ksteps(const ProductSpec& s) { return (s.K + kBK - 1) / kBK * s.nseg; }
+inline int64_t tiles_of(int64_t m, int64_t n, int tm, int tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); }
+inline int64_t tiles_of(const ProductSpec& s, int tm, int tn) { return tiles_of(s.M, s.N, tm, tn) * s.parts; }
+inline int steps(int k) { return (k + kBK - 1) / kBK; }
+inline int ksteps(const ProductSpec& s) { return (steps(s.K) * s.nseg + s.parts - 1) / s.parts; }   // of a tile
 
 // Tile shape: single CTAs on 128 x 128 tiles while these are at most one per SM (each has an SM of its own), pairs on
 // 256 x 256 tiles above that. Several products of one launch: those with the longer tiles come first; there are at most
 // two lengths (specs[0] may differ from the others).
-template <int EPI, bool MN>
+template <int EPI, bool MN, bool CUT = false>
 cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first, cudaStream_t st,
                          float* keep = nullptr, void* out2 = nullptr, bool beside = false) {
   constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
@@ -894,6 +969,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     p.M = s.M; p.N = s.N; p.K = s.K;
     p.nseg = s.nseg; p.a_mn = s.a_mn;
     p.out = s.out; p.ldo = s.ldo;
+    p.parts = s.parts; p.part = s.part;
     p.band = (int)std::max<int64_t>(8, std::min<int64_t>(32, (32 << 20) / ((pair ? 256 : 128) * 2 * (int64_t)ksteps(s) * kBK)));
     const int box_b = EPI == kFfnGlu && !pair ? 64 : 128;
     for (int k = 0; k < (EPI == kFfnGlu ? 2 : s.nseg); ++k) {
@@ -902,7 +978,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     }
   }
   if (pair) {
-    const cudaError_t e = launch_tile_t<256, EPI, true, MN>(g, wide, st);
+    const cudaError_t e = launch_tile_t<256, EPI, true, MN, CUT>(g, wide, st);
     if (e != cudaErrorLaunchOutOfResources) return e;
     // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
     for (int i = 0; EPI == kFfnGlu && i < n; ++i)
@@ -910,7 +986,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
         if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, MN, 64))
           return cudaErrorInvalidValue;
   }
-  return launch_tile_t<128, EPI, false, MN>(g, small, st);
+  return launch_tile_t<128, EPI, false, MN, CUT>(g, small, st);
 }
 
 template <int BN, int EPI>
@@ -1023,9 +1099,36 @@ ProductSpec forward_out(const FfnArgs& a, void* out, int64_t ldo) {
   return s;
 }
 
-inline int steps(int k) { return (k + kBK - 1) / kBK; }
+// Parts into which the contractions over the rows are cut, so that the few tiles of small weights' gradients fill the
+// machine: the shortest estimated time (see prefer_split) of the launch that holds them, the tiles of dx included.
+int gradient_parts(int rows, int d, int f) {
+  const bool dx_tiles = !prefer_split<kFfnOut>(rows, d, 2 * steps(f));
+  const int k = steps(rows), kx = dx_tiles ? 2 * steps(f) : 0;
+  const int64_t small = 3 * tiles_of(f, d, 128, 128), wide = 3 * tiles_of(f, d, 256, 256);
+  const int64_t xs = dx_tiles ? tiles_of(rows, d, 128, 128) : 0, xw = dx_tiles ? tiles_of(rows, d, 256, 256) : 0;
+  const auto time = [&](int parts) {
+    const int len = (k + parts - 1) / parts;
+    const double join = parts > 1 ? 4.0 + (double)parts * d * f * 24.0 / 4e6 : 0.0;
+    if (xs + small * parts <= 148) return 0.35 * std::max(kx, len) + 2.0 + join;
+    const double full = ((double)xw * kx + (double)wide * parts * len) / 74.0;
+    return 0.3 * std::max(full + 0.5 * std::min(kx ? kx : len, len), (double)std::max(kx, len)) + 4.0 + join;
+  };
+  int best = 1;
+  double least = time(1);
+  for (int parts = 2; parts <= 64 && k / parts >= 4; ++parts)
+    if (time(parts) < least) { least = time(parts); best = parts; }
+  return best;
+}
+
+size_t part_floats(int m, int n, int parts) {
+  return parts > 1 ? (size_t)((m + 31) / 32 * 32) * (size_t)((n + 31) / 32 * 32) * (size_t)parts : 0;
+}
 
 }  // namespace
+
+size_t ffn_part_floats(int64_t rows, int32_t d, int32_t f) {
+  return rows > 0 ? 3 * part_floats(f, d, gradient_parts((int)rows, d, f)) : 0;
+}
 
 cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaMemsetAsync(a.err, 0, sizeof(int), st);
@@ -1102,16 +1205,36 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st) {
     s.nseg = 2; s.M = a.rows; s.N = a.d; s.K = a.f; s.out = a.dx; s.ldo = a.lddx;
     w[n++] = s;
   }
+  const int parts = gradient_parts(a.rows, a.d, a.f);
+  FfnJoinArgs join{};
+  int64_t blocks = 0;
+  join.parts = parts; join.f16 = a.f16;
   const auto gradient = [&](const Mat& left, const Mat& right, int M, int N, void* out) {
     ProductSpec s{};
     s.a[0] = left; s.b[0] = right;
     s.nseg = 1; s.a_mn = true; s.M = M; s.N = N; s.K = a.rows; s.out = out; s.ldo = N;
+    s.parts = parts; s.part = a.part + (size_t)join.np * part_floats(M, N, parts);
+    join.p[join.np].part = s.part; join.p[join.np].out = static_cast<uint16_t*>(out);
+    join.p[join.np].M = M; join.p[join.np].N = N;
+    blocks += (int64_t)((M + 31) / 32) * ((N + 31) / 32);
+    ++join.np;
     w[n++] = s;
   };
   if (a.dwg) gradient({a.dg, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwg);
   if (a.dwu) gradient({a.du, a.f}, {a.x, a.ldx}, a.f, a.d, a.dwu);
   if (a.dwd) gradient({a.dy, a.lddy}, {a.h, a.f}, a.d, a.f, a.dwd);
-  return n > 0 ? launch_tiles<kFfnOut, true>(a, w, n, first, st, nullptr, nullptr, beside) : cudaSuccess;
+  if (n == 0) return cudaSuccess;
+  if (join.np == 0 || parts == 1) return launch_tiles<kFfnOut, true>(a, w, n, first, st, nullptr, nullptr, beside);
+  if ((e = launch_tiles<kFfnOut, true, true>(a, w, n, first, st, nullptr, nullptr, beside)) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)blocks);           // eight warps each: the eight quads of columns of a block
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  launch_attributes(attr, 1);
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, k_ffn_join, join);
 }
 
 }  // namespace sds

@@ -59,6 +59,7 @@ struct FfnArgs {
   void* dx; int64_t lddx;                      // any of the four gradients may be NULL
   void* dwg; void* dwu; void* dwd;
   void* dg; void* du;    // [rows, f] workspace
+  float* part;           // workspace of the weights' gradients (ffn_part_floats)
   int* err;              // device word, set non-zero if a bounded wait gave up
   // denoiser form: the true row count lives on the device, and the product with Wd is added to res [rows, d]
   const int* nrows_dev;
@@ -66,6 +67,7 @@ struct FfnArgs {
 };
 
 size_t ffn_keep_floats(int64_t rows, int64_t f);
+size_t ffn_part_floats(int64_t rows, int32_t d, int32_t f);
 cudaError_t launch_ffn(const FfnArgs& a, cudaStream_t st);
 cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st);
 // the denoiser's form of the two products (row count on the device, any number of rows through the same tiles):

@@ -60,12 +60,12 @@ int check_ffn_rows(const void* p, int64_t ld, int64_t rows, int32_t d) {
 size_t hidden_bytes(int64_t rows, int32_t f) { return align_up((size_t)rows * f * 2); }
 size_t factor_bytes(int64_t rows, int32_t f) { return align_up(ffn_keep_floats(rows, f) * 4); }
 
-sds_gated_ffn_sizes ffn_sizes(int64_t rows, int32_t f) {
+sds_gated_ffn_sizes ffn_sizes(int64_t rows, int32_t d, int32_t f) {
   sds_gated_ffn_sizes s;
   s.keep_bytes = factor_bytes(rows, f) + hidden_bytes(rows, f) + kAlign;
   s.forward_keep_bytes = kAlign;                       // the status word
   s.forward_bytes = kAlign + hidden_bytes(rows, f);
-  s.backward_bytes = kAlign + 2 * hidden_bytes(rows, f);
+  s.backward_bytes = kAlign + 2 * hidden_bytes(rows, f) + align_up(ffn_part_floats(rows, d, f) * 4);
   return s;
 }
 
@@ -132,7 +132,7 @@ int sds_gated_ffn_bytes(int64_t rows, int32_t d, int32_t f, sds_gated_ffn_sizes*
   if (!sizes) return SDS_EINVAL;
   const int rc = check_ffn(rows, d, f);
   if (rc != SDS_OK) return rc;
-  *sizes = ffn_sizes(rows, f);
+  *sizes = ffn_sizes(rows, d, f);
   return SDS_OK;
 }
 
@@ -147,7 +147,7 @@ int sds_gated_ffn(const void* x_dev, int64_t ldx, int32_t dtype, int64_t rows, i
   if (!aligned(wg_dev, 16) || !aligned(wu_dev, 16) || !aligned(wd_dev, 16)) return SDS_EUNSUPPORTED;
   if ((rc = check_ffn_rows(x_dev, ldx, rows, d)) != SDS_OK) return rc;
   if ((rc = check_ffn_rows(y_dev, ldy, rows, d)) != SDS_OK) return rc;
-  const sds_gated_ffn_sizes s = ffn_sizes(rows, f);
+  const sds_gated_ffn_sizes s = ffn_sizes(rows, d, f);
   if ((rc = check_workspace(workspace_dev, workspace_bytes, keep_dev ? s.forward_keep_bytes : s.forward_bytes)) != SDS_OK)
     return rc;
   if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
@@ -178,7 +178,7 @@ int sds_gated_ffn_backward(const void* dy_dev, int64_t lddy, const void* x_dev, 
   if (dx_dev && (rc = check_ffn_rows(dx_dev, lddx, rows, d)) != SDS_OK) return rc;
   if (rows > 0 && !keep_dev) return SDS_EINVAL;
   if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
-  if ((rc = check_workspace(workspace_dev, workspace_bytes, ffn_sizes(rows, f).backward_bytes)) != SDS_OK) return rc;
+  if ((rc = check_workspace(workspace_dev, workspace_bytes, ffn_sizes(rows, d, f).backward_bytes)) != SDS_OK) return rc;
   FfnArgs a{};
   a.rows = (int)rows; a.d = d; a.f = f;
   a.f16 = dtype == SDS_F16;
@@ -189,6 +189,7 @@ int sds_gated_ffn_backward(const void* dy_dev, int64_t lddy, const void* x_dev, 
   a.err = reinterpret_cast<int*>(ws);
   a.dg = ws + kAlign;
   a.du = ws + kAlign + hidden_bytes(rows, f);
+  a.part = reinterpret_cast<float*>(ws + kAlign + 2 * hidden_bytes(rows, f));
   a.keep = static_cast<float*>(const_cast<void*>(keep_dev));
   a.h = static_cast<char*>(const_cast<void*>(keep_dev)) + factor_bytes(rows, f);
   return result(launch_ffn_backward(a, static_cast<cudaStream_t>(cuda_stream)));

@@ -655,3 +655,22 @@ def test_backward_of_nothing_sets_the_status_word():
     ws = torch.full((sds.gated_ffn_bytes(5, 64, 64).backward_bytes,), 255, device="cuda", dtype=torch.uint8)
     assert sds.gated_ffn_backward(dy, x, wg, wu, wd, kept, want=(0, 0, 0, 0), workspace=ws) == (None,) * 4
     sds.gated_ffn_status(ws)
+
+
+# many rows of small layers: the weights' gradients cut their sums over the rows into parts
+@pytest.mark.parametrize("rows,d,f,t", [(16421, 64, 128, BF16), (9000, 72, 200, F16), (5000, 1024, 256, BF16), (16384, 256, 512, F16),
+                                        (3001, 8, 8, BF16), ((1 << 20) + 5, 64, 64, BF16)])
+def test_ffn_gradients_over_many_rows(rows, d, f, t):
+    x, wg, wu, wd, dy = ffn_inputs(rows, d, f, t, rows + d)
+    y, kept = sds.gated_ffn(x, wg, wu, wd, keep=True)
+    ws = torch.empty(sds.gated_ffn_bytes(rows, d, f).backward_bytes + 4096, device="cuda", dtype=torch.uint8).fill_(77)
+    got = sds.gated_ffn_backward(dy, x, wg, wu, wd, kept, workspace=ws)
+    assert (ws[-4096:] == 77).all()
+    sds.gated_ffn_status(ws)
+    ref = Ffn64(x, wg, wu, wd, "silu", t)
+    ref.backward(dy)
+    for name, v in zip(("dx", "dwg", "dwu", "dwd"), got):
+        close(v, getattr(ref, name), getattr(ref, "e" + name), name)
+    for want in ((0, 1, 0, 0), (0, 0, 1, 1), (1, 0, 0, 1)):
+        for p, q, w in zip(sds.gated_ffn_backward(dy, x, wg, wu, wd, kept, want=want), got, want):
+            assert torch.equal(p, q) if w else p is None
