@@ -86,6 +86,11 @@ struct FfnTileArgs {
 
 // a = act(g), da = act'(g). The fast exponential and division are accurate to a few units of the 24-bit
 // significand, far inside the 16-bit operands' rounding.
+// GELU: with z = |g| / sqrt(2), Phi(-|g|) = erfcx(z) exp(-z^2) / 2, and the exponential is that of the density. The scaled
+// function is smooth in t = 1 / (1 + 0.33 z): t times a polynomial of degree 7, fitted (least squares, reweighted towards the
+// smallest largest relative error) to 8.2e-8 for z up to 9.6. In floats Phi(-|g|) is off by at most 6e-7 of
+// itself up to |g| = 3 and 1.3e-6 up to 6. (With erfcf and a second exponential the epilogue took longer than the
+// products up to d = 2048: 16384 x 512 x 2048 forward 182 us.)
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float& a, float& da) {
   if (ACT == SDS_ACT_SILU) {
@@ -93,9 +98,17 @@ __device__ __forceinline__ void activation(float g, float& a, float& da) {
     a = g * p;
     da = p * fmaf(g, 1.0f - p, 1.0f);
   } else if (ACT == SDS_ACT_GELU) {
-    const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+    const float e = __expf(-0.5f * g * g), t = __fdividef(1.0f, fmaf(fabsf(g), 0.23334524f, 1.0f));
+    float q = fmaf(t, -0.067964397f, 0.23134409f);
+    q = fmaf(q, t, -0.17771943f);
+    q = fmaf(q, t, 0.20627075f);
+    q = fmaf(q, t, 0.022505348f);
+    q = fmaf(q, t, 0.10096190f);
+    q = fmaf(q, t, 0.091418624f);
+    q = fmaf(q, t, 0.093183056f) * t * e;                     // Phi(-|g|)
+    const float p = g < 0.f ? q : 1.0f - q;
     a = g * p;
-    da = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
+    da = fmaf(g * 0.39894228040143268f, e, p);
   } else {
     const float k2 = 1.5957691216057308f, c = 0.044715f;      // 2 sqrt(2 / pi)
     const float g2 = g * g;
