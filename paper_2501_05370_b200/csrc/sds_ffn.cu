@@ -1048,19 +1048,20 @@ inline int split_count(int rows, int tiles, int nkb) {
 
 // Which form a product of `rows` tokens with N output columns takes: the shorter estimated time, in steps of K of one
 // CTA (about 0.35 us where few CTAs run, 0.3 us for those of a full launch of pairs) plus what a launch and its
-// epilogue cost.
+// epilogue cost. Beyond 2048 rows the few-row form has to be clearly ahead, as it is for few columns and a long K
+// (3000 x 64 x 8192 forward 80 -> 53 us, 2100 x 512 x 12288 112 -> 85); close calls there went the other way
+// (4096 x 128 x 512 forward 13.8 -> 17.4).
 template <int EPI>
 bool prefer_split(int rows, int N, int nkb) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   if (rows <= 64) return true;                    // half a tile of rows and more would be empty
-  if (rows > 2048) return false;
   const int tok = (rows + 127) / 128, tiles = (N + TN - 1) / TN;
   const int splits = split_count(rows, tiles, nkb);
   const int64_t ctas = (int64_t)tiles * tok * splits;
   const double split = (double)((ctas + 147) / 148) * ((nkb + splits - 1) / splits) * 0.35 + 2.0 + 0.5 * splits;
   const int64_t small = (int64_t)tok * tiles, wide = (int64_t)((rows + 255) / 256) * ((N + 2 * TN - 1) / (2 * TN));
   const double tile = small <= 148 ? nkb * 0.35 + 2.0 : (double)((wide + 73) / 74) * nkb * 0.3 + 4.0;
-  return split < tile;
+  return split < (rows <= 2048 ? 1.0 : 0.7) * tile;
 }
 
 template <int EPI>
