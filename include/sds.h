@@ -400,9 +400,10 @@ int sds_gmm_denoise_static(const float* x_dev, const int32_t* k_dev, int64_t row
  * Layer operators: the parts of a gated denoiser, forward and backward, for programs that train one or run
  * one outside a context. Like sds_gmm_denoise_static they need no context: device pointers and a stream in, work
  * enqueued on cuda_stream (cudaStream_t, NULL = default stream) of the current device, no wait, no allocation.
- * Outputs must not overlap inputs or workspaces. rows = 0 is allowed; rows, d and f
- * are at most 2^30 (else SDS_EINVAL). Two calls that can run at the same time
- * (other streams, or two captured graphs) need workspaces of their own. The calls can be captured into a graph.
+ * Outputs must not overlap inputs or workspaces, except that a forward call's y may be its x (same
+ * rows, same type), where no backward pass will need x. rows = 0 is allowed; rows, d and f are at most 2^30 (else
+ * SDS_EINVAL). Two calls that can run at the same time (other streams, or two captured graphs) need workspaces of their
+ * own. The calls can be captured into a graph.
  *
  * Layer norm over rows of d elements:
  *   y = (x - mean) / sqrt(var + eps) * w + b,   var = sum (x - mean)^2 / d

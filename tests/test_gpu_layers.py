@@ -674,3 +674,66 @@ def test_ffn_gradients_over_many_rows(rows, d, f, t):
     for want in ((0, 1, 0, 0), (0, 0, 1, 1), (1, 0, 0, 1)):
         for p, q, w in zip(sds.gated_ffn_backward(dy, x, wg, wu, wd, kept, want=want), got, want):
             assert torch.equal(p, q) if w else p is None
+
+
+def test_capture_behind_two_joined_streams():
+    """A captured call with two kernels in front of it, on the capturing stream and on one that it has joined."""
+    x, wg, wu, wd, dy = ffn_inputs(48, 256, 512, BF16, 97)
+    src = [v.clone() for v in (x, wd)]
+    side = torch.cuda.Stream()
+
+    def step():
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            wd.copy_(src[1])
+            extra = sds.layer_norm(src[0])
+        x.copy_(src[0])
+        here.wait_stream(side)
+        y, kept = sds.gated_ffn(x, wg, wu, wd, keep=True)
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            g = sds.gated_ffn_backward(dy, x, wg, wu, wd, kept)
+        here.wait_stream(side)
+        return (sds.layer_norm(y), extra) + g
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(3):
+        src[0].mul_(-1.5)
+        src[1].mul_(0.5)
+        x.zero_()
+        wd.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in out]
+        assert all(torch.equal(p, q) for p, q in zip(got, step()))
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("rows", [7, 700])
+def test_output_in_the_place_of_the_input(rows):
+    """A row is read before it is written, and x is not read again after the first product."""
+    x, wg, wu, wd, _ = ffn_inputs(rows, 256, 512, BF16, 98)
+    n, y = sds.layer_norm(x), sds.gated_ffn(x, wg, wu, wd)
+    a, b = x.clone(), x.clone()
+    assert torch.equal(sds.layer_norm(a, out=a), n) and torch.equal(sds.gated_ffn(b, wg, wu, wd, out=b), y)
+
+
+def test_most_rows():
+    """2^30 rows, the limit, of eight elements (sixteen gigabytes each way)."""
+    rows = 1 << 30
+    _, wg, wu, wd, _ = ffn_inputs(1, 8, 8, BF16, 99)
+    x = torch.zeros(rows, 8, device="cuda", dtype=BF16)
+    x[-5:] = gen(99)(5, 8).to(BF16)
+    x[12345] = x[-1]
+    y = sds.layer_norm(x)
+    assert torch.equal(y[-5:], sds.layer_norm(x[-5:])) and torch.equal(y[12345], y[-1]) and int((y[1::4099] != 0).sum()) == 0
+    ws = torch.empty(sds.gated_ffn_bytes(rows, 8, 8).forward_bytes, device="cuda", dtype=torch.uint8)
+    sds.gated_ffn(x, wg, wu, wd, out=y, workspace=ws)
+    sds.gated_ffn_status(ws)
+    ref = Ffn64(x[-5:], wg, wu, wd, "silu", BF16)
+    close(y[-5:], ref.y, ref.ey)
+    assert torch.equal(y[12345], y[-1]) and int((y[1::4099] != 0).sum()) == 0
