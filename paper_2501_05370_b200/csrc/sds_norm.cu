@@ -131,17 +131,16 @@ __device__ __forceinline__ void store_any(void* p, int type, size_t i, float v) 
   else static_cast<F16*>(p)[i] = Conv<F16>::put(v);
 }
 
-// Sums of N <= 4 values over the TPR threads of a row's group, in every thread. Inside a warp the values are folded into
-// one another while they are summed (a lane keeps the value its number selects: 3 values take 6 shuffles, not 15).
+// Sums of N <= 4 values over the TPR threads of a row's group, in every thread: group_sum. Inside a warp the values are folded
+// into one another while they are summed (a lane keeps the value its number selects: 3 values take 6 shuffles, not 15).
 // Between the warps: slot, shared memory of the group, 4 * TPR / 32 floats, not written again before the group has
 // passed another barrier. CL > 1: the group is spread over a cluster of CL CTAs, every warp's sums go to all of
-// them. The order of the additions is fixed.
-template <int TPR, int N, int CL = 1>
-__device__ __forceinline__ void group_sum(float (&v)[N], float* slot, int t, int bar) {
-  constexpr unsigned kAll = 0xffffffffu;
+// them. The order of the additions is fixed. In two steps, with the cluster's barrier between: group_post, group_take.
+constexpr unsigned kAll = 0xffffffffu;
+template <int TPR, int N>
+__device__ __forceinline__ float group_fold(const float (&v)[N], int lane) {
   constexpr int W = TPR < 32 ? TPR : 32;
   constexpr int F = N == 1 ? 1 : N == 2 ? 2 : 4;                // values folded over F neighbouring lanes
-  const int lane = t & 31;
   float x = v[0];
   if (F >= 2) {
     const bool odd = lane & 1;
@@ -156,49 +155,72 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* slot, int t, int
   }
 #pragma unroll
   for (int o = F; o < W; o <<= 1) x += __shfl_xor_sync(kAll, x, o);
-  if (TPR <= 32) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = F == 1 ? x : __shfl_sync(kAll, x, n, W);
-  } else {
-    constexpr int NW = TPR > 32 ? TPR / 32 : 2;
-    if (CL > 1) {
-      if (lane < N) {
-        const uint32_t mine = (uint32_t)__cvta_generic_to_shared(slot + lane * NW + (t >> 5));
-#pragma unroll
-        for (int c = 0; c < CL; ++c) {
-          uint32_t to;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine), "r"(c));
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(x) : "memory");
-        }
-      }
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  return x;
+}
+template <int TPR, int N, int CL>
+__device__ __forceinline__ void group_post(const float (&v)[N], float* slot, int t) {
+  constexpr int NW = TPR / 32;
+  const int lane = t & 31;
+  const float x = group_fold<TPR>(v, lane);
+  if (lane < N) {
+    float* mine = slot + lane * NW + (t >> 5);
+    if (CL == 1) {
+      *mine = x;
     } else {
-      if (lane < N) slot[lane * NW + (t >> 5)] = x;
+#pragma unroll
+      for (int c = 0; c < CL; ++c) {
+        uint32_t to;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(c));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(x) : "memory");
+      }
+    }
+  }
+}
+template <int TPR, int N>
+__device__ __forceinline__ void group_take(float (&v)[N], const float* slot, int t) {
+  constexpr int NW = TPR / 32;
+  const int lane = t & 31;
+  if (NW <= 8) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; w += 2) {
+        const float2 q = *reinterpret_cast<const float2*>(slot + n * NW + w);
+        s += q.x + q.y;
+      }
+      v[n] = s;
+    }
+  } else {                                                      // eight lanes add one value's NW sums
+    const int n8 = lane >> 3;
+    float s = 0.f;
+    if (n8 < N)
+#pragma unroll
+      for (int w = 0; w < NW / 8; ++w) s += slot[n8 * NW + (lane & 7) * (NW / 8) + w];
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(kAll, s, o);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(kAll, s, n * 8);
+  }
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+template <int TPR, int N, int CL = 1>
+__device__ __forceinline__ void group_sum(float (&v)[N], float* slot, int t, int bar) {
+  if constexpr (TPR <= 32) {
+    constexpr int W = TPR < 32 ? TPR : 32;
+    const float x = group_fold<TPR>(v, t & 31);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = N == 1 ? x : __shfl_sync(kAll, x, n, W);
+  } else {
+    group_post<TPR, N, CL>(v, slot, t);
+    if (CL > 1) {
+      cluster_arrive();
+      cluster_wait();
+    } else {
       asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(TPR) : "memory");
     }
-    if (NW <= 8) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) {
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; w += 2) {
-          const float2 q = *reinterpret_cast<const float2*>(slot + n * NW + w);
-          s += q.x + q.y;
-        }
-        v[n] = s;
-      }
-    } else {                                                    // eight lanes add one value's NW sums
-      const int n8 = lane >> 3;
-      float s = 0.f;
-      if (n8 < N)
-#pragma unroll
-        for (int w = 0; w < NW / 8; ++w) s += slot[n8 * NW + (lane & 7) * (NW / 8) + w];
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(kAll, s, o);
-#pragma unroll
-      for (int n = 0; n < N; ++n) v[n] = __shfl_sync(kAll, s, n * 8);
-    }
+    group_take<TPR>(v, slot, t);
   }
 }
 
@@ -508,15 +530,17 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
     return row < rows ? make_float2(__ldg(a.mean + row), __ldg(a.rstd + row)) : make_float2(0.f, 0.f);
   };
   int base = (int)blockIdx.x / CL * RPC, flip = 0, at = 0;
+  constexpr bool SKEW = CL > 1 && VEC;                          // (see the loop at the end)
 #pragma unroll
-  for (int r = 0; r < R - 1; ++r) fetch((int64_t)base + sub + (int64_t)r * step, r);
+  for (int r = 0; r < (SKEW ? R : R - 1); ++r) fetch((int64_t)base + sub + (int64_t)r * step, r);
   float2 stats = stats_of(base + sub);
   stage_cols<TPR, T, E, V>(w_s, a.w, a.tw, a.wide, 1.0f, d, CTA, rank * T);
   __syncthreads();
   if (CL > 1) {                                                 // the peers run before anything is written to them
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
   }
+  if constexpr (!SKEW)
   for (; base < rows; base += step, flip ^= 1) {
     const int row = base + sub;
     const bool live = row < rows;
@@ -578,6 +602,82 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
       }
     }
     at = at == R - 1 ? 0 : at + 1;
+  }
+  // A cluster's barrier takes about a third of a row's time: the sums of the next row are posted before the results of this
+  // one are computed, from the ring again (no registers for two rows), and awaited after them.
+  if constexpr (SKEW) {
+    const auto post = [&](int slot, float mean, float* to) {
+      U q0 = Unit<V>::all(0.f), q1 = q0, q2 = q0;
+      const U minus = Unit<V>::all(-mean);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if ((i * TPR + t) * V < d) {
+          const PX px = ring_x[(slot * NV + i) * T];
+          const PY py = ring_y[(slot * NV + i) * T];
+          U w[P];
+          load_cols<T, V>(w_s, i, tl, w);
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            const U xc = add2(get2(px, k), minus), g = mul2(get2(py, k), w[k]);
+            q0 = add2(q0, xc);
+            q1 = add2(q1, g);
+            q2 = fma2(g, xc, q2);
+          }
+        }
+      }
+      const float q[3] = {total(q0), total(q1), total(q2)};
+      group_post<TPR, 3, CL>(q, to, t);
+      cluster_arrive();
+    };
+    float q[3] = {0.f, 0.f, 0.f};
+    float2 ahead = stats_of((int64_t)base + step);
+    if (base < rows) {
+      copies_wait<R - 1>();
+      post(0, stats.x, slots);
+      cluster_wait();
+      group_take<TPR>(q, slots, t);
+    }
+    for (int row = base; row < rows; row += step) {
+      const float mean = stats.x, rstd = stats.y;
+      const bool more = (int64_t)row + step < rows;
+      const int next = at == R - 1 ? 0 : at + 1;
+      flip ^= 1;
+      float* to = slots + flip * 4 * NW;
+      stats = ahead;
+      ahead = stats_of((int64_t)row + 2 * (int64_t)step);
+      if (more) {
+        copies_wait<R - 2>();
+        post(next, stats.x, to);
+      }
+      const float c0 = __fmul_rn(q[0], inv_d), c1 = __fmul_rn(q[1], inv_d), c2 = rstd * fmaf(-c0, c1, q[2] * inv_d);
+      TX* dxr = static_cast<TX*>(a.dx) + (size_t)row * a.lddx;
+      const U minus = Unit<V>::all(-mean), scale = Unit<V>::all(rstd), shift = Unit<V>::all(-c0 * rstd), less = Unit<V>::all(-c1), slope = Unit<V>::all(-c2);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * V;
+        if (c < d) {
+          const PX px = ring_x[(at * NV + i) * T];
+          const PY py = ring_y[(at * NV + i) * T];
+          U w[P];
+          load_cols<T, V>(w_s, i, tl, w);
+          PX o;
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            const U yf = get2(py, k), xhat = fma2(add2(get2(px, k), minus), scale, shift);
+            put2(o, k, mul2(fma2(xhat, slope, fma2(yf, w[k], less)), scale));
+            dw[i][k] = fma2(yf, xhat, dw[i][k]);
+            db[i][k] = add2(db[i][k], yf);
+          }
+          if (a.dx) *reinterpret_cast<PX*>(dxr + c) = o;
+        }
+      }
+      fetch((int64_t)row + (int64_t)R * step, at);
+      at = next;
+      if (more) {
+        cluster_wait();
+        group_take<TPR>(q, to, t);
+      }
+    }
   }
   if (VEC) copies_wait<0>();
   if (!a.dw && !a.db) return;
