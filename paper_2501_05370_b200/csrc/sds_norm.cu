@@ -606,6 +606,9 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
   // A cluster's barrier takes about a third of a row's time: the sums of the next row are posted before the results of this
   // one are computed, from the ring again (no registers for two rows), and awaited after them.
   if constexpr (SKEW) {
+    U w[NV][P];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_cols<T, V>(w_s, i, tl, w[i]);
     const auto post = [&](int slot, float mean, float* to) {
       U q0 = Unit<V>::all(0.f), q1 = q0, q2 = q0;
       const U minus = Unit<V>::all(-mean);
@@ -614,11 +617,9 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
         if ((i * TPR + t) * V < d) {
           const PX px = ring_x[(slot * NV + i) * T];
           const PY py = ring_y[(slot * NV + i) * T];
-          U w[P];
-          load_cols<T, V>(w_s, i, tl, w);
 #pragma unroll
           for (int k = 0; k < P; ++k) {
-            const U xc = add2(get2(px, k), minus), g = mul2(get2(py, k), w[k]);
+            const U xc = add2(get2(px, k), minus), g = mul2(get2(py, k), w[i][k]);
             q0 = add2(q0, xc);
             q1 = add2(q1, g);
             q2 = fma2(g, xc, q2);
@@ -658,13 +659,11 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
         if (c < d) {
           const PX px = ring_x[(at * NV + i) * T];
           const PY py = ring_y[(at * NV + i) * T];
-          U w[P];
-          load_cols<T, V>(w_s, i, tl, w);
           PX o;
 #pragma unroll
           for (int k = 0; k < P; ++k) {
             const U yf = get2(py, k), xhat = fma2(add2(get2(px, k), minus), scale, shift);
-            put2(o, k, mul2(fma2(xhat, slope, fma2(yf, w[k], less)), scale));
+            put2(o, k, mul2(fma2(xhat, slope, fma2(yf, w[i][k], less)), scale));
             dw[i][k] = fma2(yf, xhat, dw[i][k]);
             db[i][k] = add2(db[i][k], yf);
           }
