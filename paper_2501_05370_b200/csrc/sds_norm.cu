@@ -452,14 +452,18 @@ __global__ void __launch_bounds__(1024) k_norm_long(const NormArgs a) {
   }
 }
 
-// Copies of a thread's own vectors into shared memory, asynchronous and in groups: a thread reads back only what it
-// asked for itself, so no barrier is needed. `in` false: zeros.
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* dst, const void* src, bool in) {
-  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-  const int n = in ? BYTES : 0;
-  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES < 4 ? 4 : BYTES), "r"(n) : "memory");
+// Copies of 16 bytes into shared memory, asynchronous and in groups; of the source only the first n bytes are read, zeros fill
+// the rest.
+__device__ __forceinline__ void copy_async(void* dst, const void* src, int n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(n) : "memory");
+}
+template <class PACK, class T>
+__device__ __forceinline__ void copy_pack(PACK* dst, const T* src, bool in) {
+  if (sizeof(PACK) == 16)
+    copy_async(dst, src, in ? 16 : 0);
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+                 "n"(sizeof(PACK) < 4 ? 4 : sizeof(PACK)), "r"(in ? (int)sizeof(PACK) : 0) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -472,9 +476,11 @@ constexpr int kSmem = 226 * 1024;                               // of an SM's 22
 template <class TX, class TY, int TPR, int E, bool VEC, int CL> struct NormBwd {
   static constexpr int kT = TPR / CL, kCta = 512, kGroups = kCta / kT;
   static constexpr int kWeights = kT * E * 4;
-  // rows in flight: a group keeps kRing rows in shared memory, kRing - 1 of them on their way while one is worked on
-  static constexpr int kRow = VEC ? kT * E * (int)(sizeof(TX) + sizeof(TY)) : 0;
-  static constexpr int kFit = VEC ? (kSmem - kWeights) / (kRow * kGroups + (VEC ? 0 : 1)) : 2;
+  // rows in flight: a group keeps kRing rows in shared memory, kRing - 1 of them on their way while one is worked on.
+  // Unaligned rows: the aligned vectors that cover a row, up to two more than its own length takes.
+  static constexpr int kPad = VEC ? 0 : 32;
+  static constexpr int kRowX = kT * E * (int)sizeof(TX) + kPad, kRow = kRowX + kT * E * (int)sizeof(TY) + kPad;
+  static constexpr int kFit = (kSmem - kWeights) / (kRow * kGroups);
   static constexpr int kRing = kFit > 4 ? 4 : kFit;
   static constexpr int kJoin = kGroups > 1 ? kGroups * 2 * TPR * E * 4 : 0;   // the groups' sums, where the ring was
   static constexpr int kRingBytes = kRing * kRow * kGroups;
@@ -505,24 +511,49 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
   const int tl = threadIdx.x % T, sub = threadIdx.x / T, t = rank * T + tl;
   const int rows = a.rows, d = a.d, groups = (int)gridDim.x / CL, step = groups * RPC;
   const float inv_d = 1.0f / (float)d;
-  PX* ring_x = reinterpret_cast<PX*>(rest + (size_t)sub * R * C::kRow) + tl;
-  PY* ring_y = reinterpret_cast<PY*>(rest + (size_t)sub * R * C::kRow + (size_t)R * T * E * sizeof(TX)) + tl;
+  uint8_t* ring = rest + (size_t)sub * R * C::kRow;
+  PX* ring_x = reinterpret_cast<PX*>(ring) + tl;                // aligned rows: a thread's own vectors, all of x in front of all of dy
+  PY* ring_y = reinterpret_cast<PY*>(ring + (size_t)R * T * E * sizeof(TX)) + tl;
+  const int part0 = VEC ? 0 : rank * ((d + CL - 1) / CL);       // unaligned rows: first column of this CTA, its columns side by side,
+  const int last = VEC ? d : min(d, part0 + (d + CL - 1) / CL); // and the end of its columns
+  const auto column = [&](int i) { return VEC ? (i * TPR + t) * V : part0 + i * T + tl; };
   U dw[NV][P], db[NV][P];
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int k = 0; k < P; ++k) dw[i][k] = db[i][k] = Unit<V>::all(0.f);
+  // A thread of an aligned row copies what it will read. Unaligned: the group copies the 16-byte vectors that cover the row's part,
+  // whatever lies in front of it included (it is not read back), but not in front of the array: there element by element.
+  const auto cover = [&](uint8_t* to, const auto* array, int64_t ld, int64_t row) {
+    using E1 = typename std::remove_const<typename std::remove_pointer<decltype(array)>::type>::type;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(array + row * ld + part0), begin = first & ~(uintptr_t)15;
+    const uintptr_t end = first + (uintptr_t)(last - part0) * sizeof(E1);
+    for (uintptr_t p = begin + 16 * (uintptr_t)tl; p < end; p += 16 * (uintptr_t)T) {
+      const int n = (int)min((uintptr_t)16, end - p);
+      if (p >= reinterpret_cast<uintptr_t>(array)) {
+        copy_async(to + (p - begin), reinterpret_cast<const void*>(p), n);
+      } else {
+        for (uintptr_t q = first; q < p + n; q += sizeof(E1))
+          *reinterpret_cast<E1*>(to + (q - begin)) = *reinterpret_cast<const E1*>(q);
+      }
+    }
+  };
   const auto fetch = [&](int64_t row, int r) {
-    if (!VEC) return;
     const bool live = row < rows;
-    const TX* xr = static_cast<const TX*>(a.x) + (live ? row : 0) * a.ldx;
-    const TY* yr = static_cast<const TY*>(a.dy) + (live ? row : 0) * a.lddy;
+    if constexpr (VEC) {
+      const TX* xr = static_cast<const TX*>(a.x) + (live ? row : 0) * a.ldx;
+      const TY* yr = static_cast<const TY*>(a.dy) + (live ? row : 0) * a.lddy;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + t) * V;
-      const bool in = live && c < d;
-      copy_async<sizeof(PX)>(ring_x + (r * NV + i) * T, xr + (in ? c : 0), in);
-      copy_async<sizeof(PY)>(ring_y + (r * NV + i) * T, yr + (in ? c : 0), in);
+      for (int i = 0; i < NV; ++i) {
+        const int c = column(i);
+        const bool in = live && c < last;
+        // (a pack of 16-bit elements beside floats is half as long)
+        copy_pack(ring_x + (r * NV + i) * T, xr + (in ? c : 0), in);
+        copy_pack(ring_y + (r * NV + i) * T, yr + (in ? c : 0), in);
+      }
+    } else if (live && part0 < last) {
+      cover(ring + r * C::kRow, static_cast<const TX*>(a.x), a.ldx, row);
+      cover(ring + r * C::kRow + C::kRowX, static_cast<const TY*>(a.dy), a.lddy, row);
     }
     copies_commit();
   };
@@ -534,7 +565,8 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
 #pragma unroll
   for (int r = 0; r < (SKEW ? R : R - 1); ++r) fetch((int64_t)base + sub + (int64_t)r * step, r);
   float2 stats = stats_of(base + sub);
-  stage_cols<TPR, T, E, V>(w_s, a.w, a.tw, a.wide, 1.0f, d, CTA, rank * T);
+  if constexpr (VEC) stage_cols<TPR, T, E, V>(w_s, a.w, a.tw, a.wide, 1.0f, d, CTA, rank * T);
+  else stage_cols<T, T, E, V>(w_s, a.w, a.tw, a.wide, 1.0f, d, CTA, part0);
   __syncthreads();
   if (CL > 1) {                                                 // the peers run before anything is written to them
     cluster_arrive();
@@ -546,23 +578,31 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
     const bool live = row < rows;
     const float mean = stats.x, rstd = stats.y;
     const U minus = Unit<V>::all(-mean);
-    const TX* xr = static_cast<const TX*>(a.x) + (size_t)row * a.ldx;
-    const TY* yr = static_cast<const TY*>(a.dy) + (size_t)row * a.lddy;
-    if (VEC) copies_wait<R - 2>();
+    copies_wait<R - 2>();
+    const TX* row_x = nullptr;                                  // unaligned: this thread's first elements of the row in the ring
+    const TY* row_y = nullptr;
+    if constexpr (!VEC) {                                       // (the group's copies, and no one reads the slot that is filled next)
+      if (T <= 32) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "r"(T) : "memory");
+      const uintptr_t fx = reinterpret_cast<uintptr_t>(static_cast<const TX*>(a.x) + (int64_t)row * a.ldx + part0);
+      const uintptr_t fy = reinterpret_cast<uintptr_t>(static_cast<const TY*>(a.dy) + (int64_t)row * a.lddy + part0);
+      row_x = reinterpret_cast<const TX*>(ring + at * C::kRow + (fx & 15)) + tl;
+      row_y = reinterpret_cast<const TY*>(ring + at * C::kRow + C::kRowX + (fy & 15)) + tl;
+    }
     U xc[NV][P], yf[NV][P];
     U q0 = Unit<V>::all(0.f), q1 = q0, q2 = q0;                 // sums of x - mean, w dy, w dy (x - mean)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (c < d) {
+      const int c = column(i);
+      if (c < last) {
         PX px{};
         PY py{};
-        if (VEC) {
+        if constexpr (VEC) {
           px = ring_x[(at * NV + i) * T];
           py = ring_y[(at * NV + i) * T];
         } else if (live) {
-          px = *reinterpret_cast<const PX*>(xr + c);
-          py = *reinterpret_cast<const PY*>(yr + c);
+          px.v[0] = row_x[i * T];
+          py.v[0] = row_y[i * T];
         }
         U w[P];
         load_cols<T, V>(w_s, i, tl, w);
@@ -586,8 +626,8 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
     const U scale = Unit<V>::all(rstd), shift = Unit<V>::all(-c0 * rstd), less = Unit<V>::all(-c1), slope = Unit<V>::all(-c2);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (live && c < d) {
+      const int c = column(i);
+      if (live && c < last) {
         U w[P];
         load_cols<T, V>(w_s, i, tl, w);
         PX o;
@@ -614,7 +654,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
       const U minus = Unit<V>::all(-mean);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        if ((i * TPR + t) * V < d) {
+        if (column(i) < last) {
           const PX px = ring_x[(slot * NV + i) * T];
           const PY py = ring_y[(slot * NV + i) * T];
 #pragma unroll
@@ -655,8 +695,8 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
       const U minus = Unit<V>::all(-mean), scale = Unit<V>::all(rstd), shift = Unit<V>::all(-c0 * rstd), less = Unit<V>::all(-c1), slope = Unit<V>::all(-c2);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + t) * V;
-        if (c < d) {
+        const int c = column(i);
+        if (c < last) {
           const PX px = ring_x[(at * NV + i) * T];
           const PY py = ring_y[(at * NV + i) * T];
           PX o;
@@ -678,7 +718,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
       }
     }
   }
-  if (VEC) copies_wait<0>();
+  copies_wait<0>();
   if (!a.dw && !a.db) return;
   float* part = a.part + (size_t)(blockIdx.x / CL) * 2 * d;
   const auto store = [&](float* to, const U (&sums)[P]) {       // a thread's V columns
@@ -694,8 +734,8 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
   if (RPC == 1) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (c < d) {
+      const int c = column(i);
+      if (c < last) {
         store(part + c, dw[i]);
         store(part + d + c, db[i]);
       }
@@ -705,7 +745,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
     __syncthreads();                                            // every group is done with its ring
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + t) * V;
+      const int c = column(i);
       store(sum_s + (sub * 2 + 0) * TPR * E + c, dw[i]);
       store(sum_s + (sub * 2 + 1) * TPR * E + c, db[i]);
     }

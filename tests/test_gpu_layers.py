@@ -737,3 +737,21 @@ def test_most_rows():
     ref = Ffn64(x[-5:], wg, wu, wd, "silu", BF16)
     close(y[-5:], ref.y, ref.ey)
     assert torch.equal(y[12345], y[-1]) and int((y[1::4099] != 0).sum()) == 0
+
+
+@pytest.mark.parametrize("rows,d,tx,ty", [(4000, 33, BF16, BF16), (1500, 1, F32, BF16), (2000, 7, F16, F16), (3000, 1001, BF16, BF16),
+                                          (2500, 1002, F32, F16), (1300, 3001, F32, F32), (700, 6001, F16, F16), (400, 9001, F32, BF16),
+                                          (300, 16383, BF16, BF16)])
+def test_norm_backward_of_many_unaligned_rows(rows, d, tx, ty):
+    """Rows that share 16-byte vectors with their neighbours, several per group of threads; the array starts at an odd place and
+    what lies around it does not matter."""
+    r = gen(rows + d)
+    flat = torch.full((rows * d + 40,), float("nan"), device="cuda", dtype=tx)
+    x = flat[3:3 + rows * d].view(rows, d)
+    x.copy_(r(rows, d) + r(rows, 1))
+    flat_y = torch.full((rows * d + 40,), float("inf"), device="cuda", dtype=ty)
+    dy = flat_y[5:5 + rows * d].view(rows, d)
+    dy.copy_(0.1 * r(rows, d))
+    w, b = 1 + 0.2 * r(d), 0.2 * r(d)
+    _, m, rs = sds.layer_norm(x, w, b, out_dtype=ty, stats=True)
+    check_norm_grads(sds.layer_norm_backward(dy, x, w, m, rs), dy, x, w, 1e-5)
