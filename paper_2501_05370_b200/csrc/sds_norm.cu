@@ -297,11 +297,11 @@ template <class TX> constexpr int vec_len = sizeof(TX) == 4 ? 4 : 8;   // elemen
 
 // FEW: at most two rows for every group of the launch, 8 elements per thread. The weights are then read with the first row,
 // into registers; else they are brought to shared memory once and read from there for every row.
-// 16-bit rows up to 4096: three CTAs per SM (10 % shorter at 16384 x 2048 bf16 than with the two that the compiler's own register
+// Aligned 16-bit rows up to 4096: three CTAs per SM (10 % shorter at 16384 x 2048 bf16 than with the two that the compiler's own register
 // count gives; float rows lose 6 % that way).
 // 16384 x 2048 float to bf16: 34.2 us, 5.9 TB/s, 90 % of a copy's rate; 2047 x 16384 float 51.4 us, 5.2 TB/s; 64 x 2048 4.1 us.
 template <class TX, class TY, int TPR, int E, bool VEC, bool RES, bool FEW>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR <= 128 && !FEW && sizeof(TX) == 2 ? 3 : 1)
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, VEC && TPR <= 128 && !FEW && sizeof(TX) == 2 ? 3 : 1)
     k_norm(const NormArgs a) {
   constexpr int CTA = TPR < 256 ? 256 : TPR, RPC = CTA / TPR;   // RPC: rows of a CTA at a time
   constexpr int V = VEC ? vec_len<TX> : 1;
@@ -900,7 +900,9 @@ cudaError_t fwd_k(const NormArgs& a, cudaStream_t st) {
 template <class TX, class TY, int TPR, int E, bool RES, bool FEW>
 cudaError_t fwd_t(const NormArgs& a, cudaStream_t st) {
   if (RES || vec_ok<TX, TY>(a, false)) return fwd_k<TX, TY, TPR, E, true, RES, FEW>(a, st);
-  return fwd_k<TX, TY, TPR, E, false, false, FEW>(a, st);
+  // unaligned rows, read element by element: twice the threads with 16 elements each (30000 x 1001 bf16 42 -> 35 us, 10000 x 3001
+  // 48 -> 51)
+  return fwd_k<TX, TY, E == 32 ? 2 * TPR : TPR, E == 32 ? 16 : E, false, false, FEW>(a, st);
 }
 
 // Threads per row. Many rows: 32 elements per thread (few shuffles and barriers per element; the weights pass through
