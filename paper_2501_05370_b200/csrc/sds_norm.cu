@@ -491,7 +491,7 @@ template <class TX, class TY, int TPR, int E, bool VEC, int CL> struct NormBwd {
 // Backward. The sums of the weights' gradients stay in registers over all rows of a group, the weights in shared
 // memory; the rows of x and dy pass through a ring there and are held as floats between the two passes. Bound by HBM for many
 // rows (16384 x 2048 bf16, forward and backward 67 us of the 51 that two passes' bytes take), by the latency of the row's barriers for
-// few (512 x 16384 float and bf16, both 48 us).
+// few (512 x 16384 float and bf16, both 46 us).
 template <class TX, class TY, int TPR, int E, bool VEC, int CL>
 __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
   using C = NormBwd<TX, TY, TPR, E, VEC, CL>;
