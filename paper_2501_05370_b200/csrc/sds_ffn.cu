@@ -1059,6 +1059,7 @@ template <int EPI>
 bool prefer_split(int rows, int N, int nkb) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   if (rows <= 64) return true;                    // half a tile of rows and more would be empty
+  if (rows > 65535 * 128) return false;           // (blocks of tokens are the grid's second dimension)
   const int tok = (rows + 127) / 128, tiles = (N + TN - 1) / TN;
   const int splits = split_count(rows, tiles, nkb);
   const int64_t ctas = (int64_t)tiles * tok * splits;
