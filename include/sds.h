@@ -142,8 +142,8 @@ typedef int (*sds_denoise_fn)(void* user, const float* x_dev, const int32_t* k_d
  *   r_{l+1} = r' + ( act(n Wg_l^T) * (n Wu_l^T) ) Wd_l^T   (the bracket rounded to bf16, products accumulated in float).
  *   dims = { d, f, act }: f the hidden width, act one of SDS_ACT_*; d <= 16384, d and f multiples of 8.
  *   W_dev[3l], [3l+1], [3l+2]: Wg_l [f, d], Wu_l [f, d], Wd_l [d, f], bf16 row-major, 16-byte aligned;
- *   bias_dev[2l], [2l+1]: [d] float weight and bias of the norm (NULL = ones, zeros); temb_dev[l]: [K, d] bf16 embedding
- *   rows, 16-byte aligned (NULL = none). sds_denoise then takes 16-byte aligned rows (else SDS_EUNSUPPORTED).
+ *   bias_dev[2l], [2l+1]: [d] float weight and bias of the norm, 4-byte aligned (NULL = ones, zeros);
+ *   temb_dev[l]: [K, d] bf16 embedding rows, 16-byte aligned (NULL = none). sds_denoise then takes 16-byte aligned rows (else SDS_EUNSUPPORTED).
  * PHI4: D(x) = grad E(x), E(x) = coupling/2 sum_{|i-j|=1} (x_i - x_j)^2 + sum_i (x_i^2 - 1)^2 on a
  *   grid_side x grid_side lattice (d = grid_side^2), every neighbouring pair once, free boundaries
  *   unless periodic != 0. Used with the Langevin schedule a = 1, c = -gamma, sigma = sqrt(2 gamma). */

@@ -275,6 +275,8 @@ int validate_den(const sds_denoiser* den, const double* tcond, int tcond_dim, in
         if (!den->W_dev[i]) return SDS_EINVAL;
         if (reinterpret_cast<uintptr_t>(den->W_dev[i]) % 16) return SDS_EUNSUPPORTED;
       }
+      for (int i = 0; i < 2 * den->nlayer; ++i)      // (NULL: ones, zeros)
+        if (reinterpret_cast<uintptr_t>(den->bias_dev[i]) % sizeof(float)) return SDS_EINVAL;
       for (int i = 0; i < den->nlayer; ++i)
         if (reinterpret_cast<uintptr_t>(den->temb_dev[i]) % 16) return SDS_EUNSUPPORTED;
       break;
