@@ -464,6 +464,15 @@ int sds_gated_ffn_backward(const void* dy_dev, int64_t lddy, const void* x_dev, 
  * call that used workspace_dev gave up (its outputs are then invalid), else SDS_OK. */
 int sds_gated_ffn_status(const void* workspace_dev, void* cuda_stream);
 
+/* The same without a workspace, for callers that have let theirs go: waits for cuda_stream and returns SDS_ETIMEOUT if a wait
+ * of any feed-forward kernel on the current device, a gated denoiser's included, gave up since this was asked last, else
+ * SDS_OK. */
+int sds_gated_ffn_gave_up(void* cuda_stream);
+
+/* Self-test of both reports: launches one thread that polls a barrier nobody arrives on `polls` times (1 to 65536, about 10 us
+ * each), gives up as the feed-forward kernels do, and ends. workspace_dev: 256-byte aligned, 4 bytes at least. */
+int sds_selftest_gated_ffn_wait(int32_t polls, void* workspace_dev, void* cuda_stream);
+
 const char* sds_strerror(int code);
 int sds_last_cuda_error(const sds_ctx* ctx);
 void sds_destroy(sds_ctx* ctx);

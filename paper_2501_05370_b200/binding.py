@@ -92,6 +92,8 @@ EXPORTS = {
                                          C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "sds_gated_ffn_status": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "sds_gated_ffn_gave_up": (C.c_int, [C.c_void_p]),
+    "sds_selftest_gated_ffn_wait": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p]),
     "sds_strerror": (C.c_char_p, [C.c_int]),
     "sds_last_cuda_error": (C.c_int, [C.c_void_p]),
     "sds_destroy": (None, [C.c_void_p]),

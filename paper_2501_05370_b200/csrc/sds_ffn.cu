@@ -199,6 +199,25 @@ __device__ __forceinline__ bool wait_for_sums(uint64_t* bar, uint32_t parity, vo
   return false;
 }
 
+// A role that gave up says so in the call's status word, and in one per device that stays until it is asked for: the status word
+// lies in the workspace, which a caller may have let go by then (sds_gated_ffn_gave_up).
+__device__ int gave_up_word;
+__device__ __forceinline__ void give_up(int* err, int role) {
+  atomicExch(err, role);
+  atomicExch(&gave_up_word, role);
+}
+
+// Self-test of that report: one thread waits on a barrier that nobody arrives on, with a limit of its own.
+__global__ void k_ffn_wait_selftest(uint32_t polls, int* err) {
+  __shared__ uint64_t bar;
+  mbar_init(&bar, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  *err = 0;
+  bool done = false;
+  for (uint32_t it = 0; it < polls && !done; ++it) done = mbar_try_wait(&bar, 0u);
+  if (!done) give_up(err, 3);
+}
+
 // ---------------------------------------------------------------------------------------------
 // batches: persistent tiles
 // ---------------------------------------------------------------------------------------------
@@ -388,7 +407,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       }
       if (!ok) {
         raise_abort(abort_s, PAIR);
-        atomicExch(g.err, 1);
+        give_up(g.err, 1);
       }
     }
   } else if (warp == 1) {
@@ -433,7 +452,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
       }
       if (!ok) {
         raise_abort(abort_s, PAIR);
-        atomicExch(g.err, 2);
+        give_up(g.err, 2);
       }
     }
   } else {
@@ -556,7 +575,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
     }
     if (!ok && lane == 0) {
       raise_abort(abort_s, PAIR);
-      atomicExch(g.err, 3);
+      give_up(g.err, 3);
     }
   }
 
@@ -726,7 +745,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
     }
     if (!ok) {
       *abort_s = 1;
-      atomicExch(g.err, 1);
+      give_up(g.err, 1);
     }
   } else if (warp == 1 && lane == 0) {
     const uint32_t idesc = make_idesc(kBM, BN, g.f16 != 0, g.w_mn != 0, false);
@@ -751,7 +770,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       umma_commit(tfull_bar);
     } else {
       *abort_s = 1;
-      atomicExch(g.err, 2);
+      give_up(g.err, 2);
     }
   }
   __syncwarp();
@@ -773,7 +792,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
     for (int c = 0; c < BN / 2; ++c) part[(half * (BN / 2) + c) * kBM + q * 32 + lane] = __uint_as_float(acc[c]);
   } else if (lane == 0) {
     *abort_s = 1;
-    atomicExch(g.err, 3);
+    give_up(g.err, 3);
   }
   tc_fence_before();
   if (nsplit > 1) cluster_sync_all(); else __syncthreads();
@@ -1097,6 +1116,21 @@ cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool
 }
 
 }  // namespace
+
+cudaError_t ffn_gave_up(int* role, cudaStream_t st) {
+  *role = 0;
+  const int none = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(role, gave_up_word, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess || *role == 0) return e;
+  e = cudaMemcpyToSymbolAsync(gave_up_word, &none, sizeof(int), 0, cudaMemcpyHostToDevice, st);
+  return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
+}
+
+cudaError_t launch_ffn_wait_selftest(uint32_t polls, int* err, cudaStream_t st) {
+  k_ffn_wait_selftest<<<1, 1, 0, st>>>(polls, err);
+  return cudaGetLastError();
+}
 
 size_t ffn_keep_floats(int64_t rows, int64_t f) {
   return (size_t)((rows + 31) / 32 * 32) * (size_t)((f + 31) / 32 * 32) * 2;

@@ -74,5 +74,8 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st);
 // h = act(x Wg^T) * (x Wu^T), then res += h Wd^T. Every output element is the same bits however many rows there are.
 cudaError_t launch_ffn_hidden(const FfnArgs& a, cudaStream_t st);
 cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st);
+// waits for st; *role: non-zero if a wait on the current device gave up since this was asked last
+cudaError_t ffn_gave_up(int* role, cudaStream_t st);
+cudaError_t launch_ffn_wait_selftest(uint32_t polls, int* err, cudaStream_t st);
 
 }  // namespace sds

@@ -205,5 +205,17 @@ int sds_gated_ffn_status(const void* workspace_dev, void* cuda_stream) {
   return word != 0 ? SDS_ETIMEOUT : SDS_OK;
 }
 
+int sds_gated_ffn_gave_up(void* cuda_stream) {
+  int role = 0;
+  const cudaError_t e = ffn_gave_up(&role, static_cast<cudaStream_t>(cuda_stream));
+  if (e != cudaSuccess) return result(e);
+  return role != 0 ? SDS_ETIMEOUT : SDS_OK;
+}
+
+int sds_selftest_gated_ffn_wait(int32_t polls, void* workspace_dev, void* cuda_stream) {
+  if (!workspace_dev || !aligned(workspace_dev, kAlign) || polls <= 0 || polls > (1 << 16)) return SDS_EINVAL;
+  return result(launch_ffn_wait_selftest((uint32_t)polls, static_cast<int*>(workspace_dev), static_cast<cudaStream_t>(cuda_stream)));
+}
+
 #pragma GCC visibility pop
 }  // extern "C"

@@ -74,11 +74,15 @@ def gated_ffn_backward(dy, x, w_gate, w_up, w_down, kept, *, want=(True, True, T
     return (_native or _ext()).gated_ffn_backward(dy, x, w_gate, w_up, w_down, kept, want, workspace)
 
 
-def gated_ffn_status(workspace) -> None:
+def gated_ffn_status(workspace=None) -> None:
     """Waits for the current stream and raises if a bounded wait of the last gated_ffn call (or its backward) that
-    was given this workspace gave up."""
+    was given this workspace gave up. Without one: if a wait of any such call on the current device did since this was asked
+    last, whatever its workspace (those that the calls allocate themselves have no other report)."""
     import torch
-    with torch.cuda.device(workspace.device):
-        rc = sb.load().sds_gated_ffn_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    if workspace is None:
+        where, rc = "sds_gated_ffn_gave_up", sb.load().sds_gated_ffn_gave_up(torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(workspace.device):
+            where, rc = "sds_gated_ffn_status", sb.load().sds_gated_ffn_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream)
     if rc != sb.SDS_OK:
-        raise sb.SdsError(rc, "sds_gated_ffn_status")
+        raise sb.SdsError(rc, where)

@@ -25,3 +25,9 @@ def test_gated_denoiser_norm_vectors_are_floats(at, shift, code):
     sch = sb.SdsSchedule(5, a.ctypes.data, a.ctypes.data, a.ctypes.data, None, 0)
     n = C.c_size_t(0)
     assert sds.load().sds_workspace_bytes(C.byref(sch), C.byref(den), 8, d, 4, C.byref(n)) == code
+
+
+def test_report_of_a_wait_that_gave_up_checks_its_arguments():
+    f = sds.load().sds_selftest_gated_ffn_wait
+    for polls, ws in ((0, 0x10000), (-1, 0x10000), ((1 << 16) + 1, 0x10000), (10, None), (10, 0x10010)):
+        assert f(polls, ws, None) == sb.SDS_EINVAL
