@@ -7,6 +7,7 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdexcept>
@@ -161,8 +162,8 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F f) {
   } catch (const PythonError&) {
   } catch (const BadArgument& e) {
     PyErr_SetString(PyExc_ValueError, e.what());
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {                                  // torch's own, an allocation that failed among them
+    torch::translate_exception_to_python(std::current_exception());
   }
   return nullptr;
 }

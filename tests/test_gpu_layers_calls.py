@@ -31,3 +31,15 @@ def test_a_wait_that_gave_up_is_reported_without_a_workspace():
     sds.gated_ffn_status()
     assert torch.equal(sds.gated_ffn(x, wg, wu, wd), want)
     sds.gated_ffn_status()
+
+
+def test_out_of_memory_is_torchs_error():
+    """What a call allocates and cannot get (11 TB of kept state, 2 TB of workspace) raises as torch's own allocations do; the next
+    call runs."""
+    x, wg, wu, wd, _ = ffn_inputs(1 << 20, 8, 1 << 20, BF16, 41)
+    for keep in (True, False):
+        with pytest.raises(torch.OutOfMemoryError) as e:
+            sds.gated_ffn(x, wg, wu, wd, keep=keep)
+        assert "C++" not in str(e.value) and "frame #" not in str(e.value)
+    y = sds.gated_ffn(x[:3], wg[:64].contiguous(), wu[:64].contiguous(), wd[:, :64].contiguous())
+    assert torch.isfinite(y).all()
