@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -130,6 +131,20 @@ bool wanted(PyObject* want, Py_ssize_t k, Py_ssize_t n) {
   return r != 0;
 }
 
+// Nothing is recorded for autograd: a warning, at the line that called layers.py, where torch would have recorded something.
+void warn_unrecorded(const char* name, std::initializer_list<PyObject*> inputs) {
+  const bool recording = c10::GradMode::is_enabled();
+  for (PyObject* o : inputs) {
+    if (o == Py_None) continue;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!(recording && t.requires_grad()) && !t._fw_grad(0).defined()) continue;
+    const std::string what = std::string(name) + " records nothing for autograd, and an input requires a gradient: call " + name +
+                             "_backward for it, and " + name + " under torch.no_grad() or on detached tensors";
+    if (PyErr_WarnEx(PyExc_UserWarning, what.c_str(), 2) != 0) throw PythonError{};
+    return;
+  }
+}
+
 PyObject* wrap(const at::Tensor& t) {
   if (!t.defined()) Py_RETURN_NONE;
   return THPVariable_Wrap(t);
@@ -188,6 +203,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
       yt = reinterpret_cast<THPDtype*>(a[4])->scalar_type;
     }
     const int tx = type_code(x.scalar_type()), ty = type_code(yt), tw = type_code(w ? wt : bt);
+    warn_unrecorded("layer_norm", {a[0], a[1], a[2]});
     const c10::cuda::CUDAGuard guard(x.device());
     int64_t ldy = 0;
     const at::Tensor y = output(a[6], x, yt, &ldy);
@@ -269,6 +285,7 @@ PyObject* gated_ffn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const long act = PyLong_AsLong(a[4]);
     if (act == -1 && PyErr_Occurred()) throw PythonError{};
     const bool keep = truth(a[5]);
+    warn_unrecorded("gated_ffn", {a[0], a[1], a[2], a[3]});
     const c10::cuda::CUDAGuard guard(x.device());
     int64_t ldy = 0;
     const at::Tensor y = output(a[6], x, x.scalar_type(), &ldy);

@@ -2,7 +2,8 @@
 with its backward pass (include/sds.h documents the formulas). Every call enqueues on the current stream of its
 tensors' device and does not wait. Outputs and workspaces are allocated by torch unless they are passed in. A bad
 argument raises ValueError, an error of the library SdsError. Nothing is recorded for autograd: the backward calls are
-the gradients.
+the gradients. A forward call whose inputs require gradients (or carry forward-mode tangents) outside torch.no_grad()
+warns of that.
 """
 from __future__ import annotations
 

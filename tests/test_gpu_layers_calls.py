@@ -43,3 +43,41 @@ def test_out_of_memory_is_torchs_error():
         assert "C++" not in str(e.value) and "frame #" not in str(e.value)
     y = sds.gated_ffn(x[:3], wg[:64].contiguous(), wu[:64].contiguous(), wd[:, :64].contiguous())
     assert torch.isfinite(y).all()
+
+
+def test_a_call_that_drops_a_gradient_says_so():
+    """Nothing is recorded for autograd. Where torch would record something, a forward call warns; its values stay the same."""
+    import warnings
+    x, wg, wu, wd, dy = ffn_inputs(9, 64, 64, BF16, 42)
+    w = torch.ones(64, device="cuda")
+    norm = lambda x, w: sds.layer_norm(x, w)  # noqa: E731
+    block = lambda x, w: sds.gated_ffn(x, wg, w, wd)  # noqa: E731
+    leaf = lambda v: v.clone().requires_grad_(True)  # noqa: E731
+    for call, v in ((norm, w), (block, wu)):
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            want = call(x, v)
+            with torch.no_grad():
+                assert torch.equal(call(leaf(x), leaf(v)), want)
+            with torch.inference_mode():
+                assert torch.equal(call(x, v), want)
+        for args in ((leaf(x), v), (x, leaf(v)), (leaf(x) * 1, leaf(v))):
+            with pytest.warns(UserWarning, match="autograd") as caught:
+                y = call(*args)
+            assert torch.equal(y, want) and not y.requires_grad
+            assert caught[0].filename == __file__
+        with torch.autograd.forward_ad.dual_level():
+            with pytest.warns(UserWarning, match="autograd"):
+                call(torch.autograd.forward_ad.make_dual(x, x), v)
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            with pytest.raises(UserWarning):                        # a warning made an error is raised as that
+                call(leaf(x), v)
+    # the gradients' calls are what a training step makes instead, with its parameters as they are
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        with torch.no_grad():
+            y, mean, rstd = sds.layer_norm(leaf(x), leaf(w), stats=True)
+            _, kept = sds.gated_ffn(leaf(x), leaf(wg), wu, wd, keep=True)
+        sds.layer_norm_backward(dy, leaf(x), leaf(w), mean, rstd)
+        sds.gated_ffn_backward(dy, leaf(x), leaf(wg), wu, wd, kept)
