@@ -113,7 +113,7 @@ def load() -> C.CDLL:
     if _lib is not None:
         return _lib
     if _build.needs_build():
-        _build.build()
+        _build.build_lib()
     if not os.path.exists(_build.LIB):
         raise RuntimeError("libsds.so is missing and could not be built")
     lib = C.CDLL(_build.LIB)

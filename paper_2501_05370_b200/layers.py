@@ -17,12 +17,21 @@ _native = None       # the extension that checks arguments, allocates and calls 
 
 
 def _ext():
+    """The extension, built first if its source is newer (or it was built for another torch); a call on tensors needs it."""
     global _native
     if _native is None:
+        import importlib.machinery
+        import importlib.util
         import torch  # noqa: F401  (the extension's libraries)
+        from . import build
         sb.load()
-        from . import _sds_torch
-        _native = _sds_torch
+        if build.needs_ext_build():
+            build.build_ext()
+        name, path = __package__ + "._sds_torch", build.ext_path()
+        loader = importlib.machinery.ExtensionFileLoader(name, path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(name, path, loader=loader))
+        loader.exec_module(module)
+        _native = module
     return _native
 
 
