@@ -42,13 +42,20 @@ CSRC = os.path.join(ROOT, "paper_2501_05370_b200", "csrc")
 TRAFFIC_TABLE = os.path.join(ROOT, "profiles", "dram_traffic.md")
 
 
+def source_hash(name: str):
+    """The first 12 hex digits of the SHA-256 of a file of the kernels' sources; None if there is none."""
+    path = os.path.join(CSRC, name)
+    return hashlib.sha256(open(path, "rb").read()).hexdigest()[:12] if os.path.isfile(path) else None
+
+
 def measured_traffic():
     """DRAM bytes (read + written) and warp instructions per launch from the profiler captures listed
     in the traffic table: rows `| workload | kernel kind | chains | DRAM bytes per launch | warp
-    instructions per launch | source file:hash | note |`. A capture is taken at a reduced number of
+    instructions per launch | sources | note |`. A capture is taken at a reduced number of
     chains; every chain moves the same bytes, so a launch at B chains moves B / chains times as much.
-    A row whose source file no longer has the recorded hash describes a kernel that has changed since:
-    it is ignored (the figure is then null). Returns {(workload, kind): (chains, bytes, inst)}."""
+    Its sources are `file:hash` each, the kernel's .cu and the .cuh files that it includes. A row one of whose sources no longer
+    has the recorded hash describes a kernel that has changed since: it is ignored (the figure is then null).
+    Returns {(workload, kind): (chains, bytes, inst)}."""
     out = {}
     if not os.path.exists(TRAFFIC_TABLE):
         return out
@@ -56,9 +63,8 @@ def measured_traffic():
         f = [x.strip() for x in ln.strip().strip("|").split("|")]
         if len(f) < 6 or not f[2].isdigit():
             continue
-        src, _, want = f[5].partition(":")
-        path = os.path.join(CSRC, src)
-        if not os.path.exists(path) or hashlib.sha256(open(path, "rb").read()).hexdigest()[:12] != want:
+        sources = [x.partition(":") for x in f[5].split()]
+        if not sources or any(source_hash(src) != want for src, _, want in sources):
             continue
         num = lambda x: float(x) if x not in ("", "-") else None
         out[(f[0], f[1])] = (int(f[2]), num(f[3]), num(f[4]))
