@@ -900,9 +900,11 @@ cudaError_t fwd_k(const NormArgs& a, cudaStream_t st) {
 template <class TX, class TY, int TPR, int E, bool RES, bool FEW>
 cudaError_t fwd_t(const NormArgs& a, cudaStream_t st) {
   if (RES || vec_ok<TX, TY>(a, false)) return fwd_k<TX, TY, TPR, E, true, RES, FEW>(a, st);
-  // unaligned rows, read element by element: twice the threads with 16 elements each (30000 x 1001 bf16 42 -> 35 us, 10000 x 3001
-  // 48 -> 51)
-  return fwd_k<TX, TY, E == 32 ? 2 * TPR : TPR, E == 32 ? 16 : E, false, false, FEW>(a, st);
+  // Unaligned rows, read element by element: twice the threads with 16 elements each, except where a group has 64 or 128 threads
+  // (1025 to 4096 columns), which lose by it. 30 million elements, us with 32 and with 16 each, bf16 and float: 1001 columns 44 -> 37
+  // and 47 -> 45, 1501 45 -> 48 and 45 -> 50, 3001 48 -> 52 and 48 -> 59, 5001 77 -> 65 and 80 -> 68, 12001 57 -> 53 and 61 -> 60.
+  constexpr bool kMore = E == 32 && TPR != 64 && TPR != 128;
+  return fwd_k<TX, TY, kMore ? 2 * TPR : TPR, kMore ? 16 : E, false, false, FEW>(a, st);
 }
 
 // Threads per row. Many rows: 32 elements per thread (few shuffles and barriers per element; the weights pass through

@@ -1,7 +1,9 @@
 """Layer norm on as many rows as make every group of threads take several, on the GPU against 64 bits.
 
 Bounds as derived in test_gpu_layers.py: a float sum is off by at most (terms added one after the other + levels of the
-tree) 2^-24 of the sum of sizes. A thread adds at most 16 terms of a row one after the other (`serial`). A column's sum over the
+tree) 2^-24 of the sum of sizes. A thread adds at most 16 terms of a row one after the other (`serial`), 32 in unaligned rows of
+1025 to 4096 columns: 37 additions deep there. They reach the statistics and y by the mean, times <|x - mean|>, which is 0.8 standard
+deviations of these normal rows, and halved by rstd: 30 and 19 steps, within the serial + 18 = 34 allowed for either. A column's sum over the
 rows adds the rows of a group (at most 14 here), the groups of a CTA (64 / 16 / 8 / 4 / 2 / 1 with the width) and the CTAs' sums (19 and 8,
 or 5 and 32): always less than the rows / 148 + min(rows, 888) / 8 + 16 that check_norm_grads allows beside the rows' own error.
 """
