@@ -1,5 +1,4 @@
 """How the layer operators are called, on the GPU: reports of waits that gave up, errors, warnings, host threads."""
-import threading
 
 import pytest
 import torch
@@ -81,3 +80,85 @@ def test_a_call_that_drops_a_gradient_says_so():
             _, kept = sds.gated_ffn(leaf(x), leaf(wg), wu, wd, keep=True)
         sds.layer_norm_backward(dy, leaf(x), leaf(w), mean, rstd)
         sds.gated_ffn_backward(dy, leaf(x), leaf(wg), wu, wd, kept)
+
+
+def test_first_calls_from_several_host_threads():
+    """Four host threads make a process's first calls at once, through the C entries (which do not hold the interpreter's lock) and
+    through the functions on tensors, each on a stream and with workspaces of its own: what they give alone, bit for bit."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import ctypes as C, threading, torch
+import paper_2501_05370_b200 as sds
+from paper_2501_05370_b200 import binding as sb
+lib = sds.load()
+g = torch.Generator(device="cuda"); g.manual_seed(3)
+rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+SIZES = [(40, 256, 512), (700, 512, 256), (9, 1000, 264), (2000, 136, 520)]
+data = [(rnd(r, d), rnd(f, d) * d ** -0.5, rnd(f, d) * d ** -0.5, rnd(d, f) * f ** -0.5, rnd(r, d)) for r, d, f in SIZES]
+torch.cuda.synchronize()
+
+
+def raw(k, stream):
+    x, wg, wu, wd, dy = data[k]
+    (r, d), f, p = x.shape, wg.shape[0], (lambda t: t.data_ptr())
+    s, n = sds.gated_ffn_bytes(r, d, f), C.c_size_t(0)
+    assert lib.sds_layer_norm_workspace_bytes(r, d, C.byref(n)) == 0
+    byte = lambda b: torch.empty(b, dtype=torch.uint8, device="cuda")
+    y, h, dx, dn = (torch.empty_like(x) for _ in range(4))
+    gw, gu, gd, dw, db = (torch.empty_like(t) for t in (wg, wu, wd, x[0].float(), x[0].float()))
+    m, q = (torch.empty(r, device="cuda") for _ in range(2))
+    keep, ws, wb, wn, t = byte(s.keep_bytes), byte(s.forward_keep_bytes), byte(s.backward_bytes), byte(n.value), sb.SDS_BF16
+    rc = [lib.sds_layer_norm(p(x), d, t, None, None, 0, r, d, 1e-5, p(y), d, t, p(m), p(q), stream),
+          lib.sds_gated_ffn(p(y), d, t, r, d, f, p(wg), p(wu), p(wd), 0, p(h), d, p(keep), p(ws), ws.numel(), stream),
+          lib.sds_gated_ffn_backward(p(dy), d, p(y), d, t, r, d, f, p(wg), p(wu), p(wd), p(keep), p(dn), d, p(gw), p(gu), p(gd), p(wb),
+                                     wb.numel(), stream),
+          lib.sds_layer_norm_backward(p(dn), d, t, p(x), d, t, None, 0, p(m), p(q), r, d, p(dx), d, p(dw), p(db), p(wn), wn.numel(), stream)]
+    assert rc == [0] * 4, rc
+    return [y, h, dn, gw, gu, gd, dx, dw, db], (keep, ws, wb, wn, m, q)
+
+
+def tensors(k):
+    x, wg, wu, wd, dy = data[k]
+    y, m, q = sds.layer_norm(x, stats=True)
+    h, keep = sds.gated_ffn(y, wg, wu, wd, keep=True)
+    dn, gw, gu, gd = sds.gated_ffn_backward(dy, y, wg, wu, wd, keep)
+    return [y, h, dn, gw, gu, gd, *sds.layer_norm_backward(dn, x, None, m, q)]
+
+
+got, failed, gate = [[] for _ in SIZES], [], threading.Barrier(len(SIZES))
+
+
+def work(k):
+    try:
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            gate.wait(60)
+            kept = []
+            for _ in range(5):
+                out, more = raw(k, stream.cuda_stream)
+                kept.append(more)
+                got[k] += [out, tensors(k)]
+            stream.synchronize()
+    except BaseException as e:
+        failed.append(repr(e))
+
+
+threads = [threading.Thread(target=work, args=(k,)) for k in range(len(SIZES))]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert not failed, failed
+torch.cuda.synchronize()
+for k in range(len(SIZES)):
+    want = tensors(k)
+    torch.cuda.synchronize()
+    assert len(got[k]) == 10
+    for out in got[k]:
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+sds.gated_ffn_status()
+print("same")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=root, timeout=240)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout[-500:] + r.stderr[-2000:]
