@@ -183,10 +183,12 @@ __device__ __forceinline__ void add_rows64(uint4* stg, const uint32_t* w, float*
 }
 
 // Kernels overlap their starts: one may be started when all CTAs of the one in front have said so (or ended), and waits
-// for that kernel's end, and for its writes, here. Every kernel of this file says so only once its own wait is over. What
-// ran before the kernel in front has then ended before this one starts: weights, which the kernel in front
-// does not write, may be read ahead of the wait (k_ffn_split), and kernels that read nothing of the one in front may
-// run beside it (FfnTileArgs::beside).
+// for that kernel's end, and for its writes, here. Two kinds read device memory before that wait: k_ffn_split in a call's later
+// products, the weights, which nothing in the call writes; and a tile launch `beside` (FfnTileArgs), all it needs, as it reads
+// nothing of the kernel in front. Both are right only because the kernel directly in front is one of the same call that said so
+// after its own wait: what ran before that one had then ended. So neither a norm kernel (it says so before its wait) nor
+// a launch `beside` (it waits in the end) may stand there: behind these come only first kernels of calls and k_ffn_join, which
+// wait before they read anything.
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_prior_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -294,7 +296,7 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
 
 // MN: B is MN-major and A either (the gradients); else both are K-major. The loops of the two single threads that feed the
 // tensor cores are written out per order: with the order looked up in every step they took 735 cycles per step of K where
-// the products take 512 (16384 x 2048 x 8192, forward projections: 676 -> 605 us at full clocks).
+// the products take 512 (16384 x 2048 x 8192, forward projections: 676 -> 611 us at full clocks).
 // Bound by the tensor cores: 16384 x 2048 x 8192 forward 1280 us, 1290 TFLOP/s (92 % of the library's rate in a long run, where power
 // sets the clock); 8192 rows forward and backward 2130 us, 1160 TFLOP/s beside the kept factors.
 // CUT: products whose K is cut (FfnProduct::parts); its own kernel, as the others lose up to 5 % to the arithmetic.
@@ -728,8 +730,8 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       const int seg = kb >= kb_seg ? 1 : 0, kk = (kb - seg * kb_seg) * kBK;
       tma_load_2d(stages + stage * C::kStageBytes + C::kABytes, &g.t[seg], kk, tok0, full_bar + stage);
     };
-    // Behind a kernel of the same call: that one writes the tokens, not the weights. So the first stages' weights are
-    // requested before it has ended.
+    // Behind a kernel of the same call, which waited before it let this one start and writes the tokens, not the weights: the
+    // first stages' weights are requested before it has ended. A call's first kernel may have anything in front and waits.
     const int ahead = min(kb1 - kb0, C::kStages);
     if (g.clear_err) wait_for_prior_kernel();
     for (int i = 0; i < ahead; ++i) { weights(kb0 + i); ++stage; }

@@ -287,7 +287,8 @@ __device__ __forceinline__ void stage_cols(float* s, const void* p, int type, bo
 
 // Kernels overlap their starts: the next one may be started once all CTAs of this one have begun (their launch takes about
 // as long as a small call runs), and this one waits here for the end of the kernel in front, and for its writes.
-// Nothing in device memory is read or written before.
+// Nothing in device memory is read or written before. The next one is let go before this wait: it may begin while what ran
+// in front of this kernel still runs, so it has to wait in full as well before it reads anything.
 __device__ __forceinline__ void start_after_prior_kernel() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
