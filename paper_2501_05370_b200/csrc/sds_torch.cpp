@@ -76,6 +76,7 @@ Rows rows_of(const at::Tensor& x, const char* what) {
     span *= sizes[k];
   }
   if (ld >= 0) r.ld = ld;
+  if (r.ld < r.d) throw BadArgument(name + ": rows must not overlap (call contiguous() on broadcast rows)");
   return r;
 }
 

@@ -42,7 +42,7 @@ def _ext():
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, *, out_dtype=None, stats: bool = False, out=None):
     """sds_layer_norm over the last dimension of x (float32, bfloat16 or float16; leading dimensions that make evenly
-    spaced rows). weight, bias: vectors of one type, or None. out_dtype: x's type (default), or for float x any of the
+    spaced rows, which do not overlap). weight, bias: vectors of one type, or None. out_dtype: x's type (default), or for float x any of the
     three. Returns y, with stats=True (y, mean, rstd): the float row statistics that layer_norm_backward takes."""
     return (_native or _ext()).layer_norm(x, weight, bias, eps, out_dtype, stats, out)
 

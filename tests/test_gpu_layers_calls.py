@@ -162,3 +162,22 @@ print("same")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=root, timeout=240)
     assert r.returncode == 0 and "same" in r.stdout, r.stdout[-500:] + r.stderr[-2000:]
+
+
+def test_rows_that_overlap_are_a_bad_argument():
+    """Broadcast rows (a stride of zero, as the gradient of a sum has) and overlapping windows, as input, gradient or output: a
+    ValueError that names the argument, on the host."""
+    x, wg, wu, wd, dy = ffn_inputs(6, 64, 64, BF16, 43)
+    _, mean, rstd = sds.layer_norm(x, stats=True)
+    _, kept = sds.gated_ffn(x, wg, wu, wd, keep=True)
+    row, windows = x[:1].expand(6, 64), torch.as_strided(x, (6, 64), (8, 1))
+    for bad in (row, windows):
+        for call in (lambda: sds.layer_norm(bad), lambda: sds.gated_ffn(bad, wg, wu, wd), lambda: sds.layer_norm(x, out=bad),
+                     lambda: sds.gated_ffn(x, wg, wu, wd, out=bad), lambda: sds.layer_norm_backward(bad, x, None, mean, rstd),
+                     lambda: sds.layer_norm_backward(dy, bad, None, mean, rstd), lambda: sds.gated_ffn_backward(bad, x, wg, wu, wd, kept),
+                     lambda: sds.gated_ffn_backward(dy, bad, wg, wu, wd, kept)):
+            with pytest.raises(ValueError, match="overlap"):
+                call()
+    one = x[:1].expand(1, 64)                                        # (a single row overlaps nothing)
+    assert torch.equal(sds.layer_norm(one), sds.layer_norm(x)[:1])
+    assert torch.equal(sds.layer_norm(row.contiguous())[5], sds.layer_norm(x)[0])
