@@ -473,6 +473,55 @@ int sds_gated_ffn_gave_up(void* cuda_stream);
  * each), gives up as the feed-forward kernels do, and ends. workspace_dev: 256-byte aligned, 4 bytes at least. */
 int sds_selftest_gated_ffn_wait(int32_t polls, void* workspace_dev, void* cuda_stream);
 
+/* Linear layer with its epilogue (a layer of the MLP denoiser, or a block's product that ends on the residual stream):
+ *   z = x W^T + bias + table[step],   y = act(z) + residual
+ * x_dev [rows, k] (rows ldx apart), w_dev [n, k] dense and table_dev [steps, n] dense of one dtype, SDS_BF16 or SDS_F16; bias_dev [n] of
+ * bias_dtype, any of the three; y_dev, residual_dev [rows, n] (rows ldy, ldr apart) of y_dtype: dtype or SDS_F32. bias_dev, table_dev
+ * and residual_dev may be NULL (none). step_dev [rows] int32: row of the table for every row of x (needed with a table only); a
+ * row whose step is not in [0, steps) becomes NaN. act one of SDS_ACT_*. Products and all that is added to them are held in
+ * float and rounded once, to y_dtype. k and ldx multiples of 8, x_dev and w_dev 16-byte aligned, steps <= 65535 (else
+ * SDS_EUNSUPPORTED); n, ldy and ldr are free, and the other arrays aligned to their elements (rows of whole 16-byte pieces are faster).
+ * residual_dev may be y_dev (same rows). keep_dev: what the backward pass needs of the forward one (act'(z), rounded to
+ * f16), 256-byte aligned, keep_bytes (0 without an activation, where NULL will do); NULL = no backward pass will follow.
+ * workspace_dev: 256-byte aligned, forward_bytes or backward_bytes. The result of a row may differ in the last bit with
+ * the number of rows of the call. */
+#define SDS_ACT_NONE      3     /* g; sds_linear only */
+typedef struct {
+  int32_t k, n, steps;          /* steps: rows of the table (0 without one) */
+  int32_t dtype;
+  int32_t act;
+  const void* w_dev;
+  const void* bias_dev;
+  int32_t bias_dtype;
+  const void* table_dev;
+} sds_linear_layer;
+typedef struct {
+  size_t keep_bytes;            /* keep_dev */
+  size_t forward_bytes;         /* workspace of sds_linear */
+  size_t backward_bytes;        /* workspace of sds_linear_backward */
+} sds_linear_sizes;
+int sds_linear_bytes(const sds_linear_layer* layer, int64_t rows, sds_linear_sizes* sizes);   /* (reads no pointer of the layer but
+                                                                                                 whether there is a table) */
+int sds_linear(const sds_linear_layer* layer, const void* x_dev, int64_t ldx, const int32_t* step_dev, int64_t rows,
+               const void* residual_dev, int64_t ldr, void* y_dev, int64_t ldy, int32_t y_dtype, void* keep_dev,
+               void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* Its gradients, from dy_dev [rows, n] of y_dtype (rows lddy apart) and the forward call's x, layer, steps and keep_dev:
+ *   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  dbias = sum_rows dz,  dtable[s] = sum of dz over the rows with step s
+ * (that of the residual is dy itself). dx_dev [rows, k] (rows lddx apart, lddx a multiple of 8), dw_dev [n, k], both 16-byte
+ * aligned, and dtable_dev [steps, n] of dtype, dbias_dev [n] of bias_dtype; any may be NULL. dz is rounded to dtype as an operand of
+ * the two products; the sums take it unrounded, are held in float and added in a fixed order: same bits on every run. Rows
+ * whose step is outside the table add nothing to dtable. With rows = 0 the parameters' gradients are zeros. */
+int sds_linear_backward(const sds_linear_layer* layer, const void* dy_dev, int64_t lddy, int32_t y_dtype,
+                        const void* x_dev, int64_t ldx, const int32_t* step_dev, int64_t rows, const void* keep_dev,
+                        void* dx_dev, int64_t lddx, void* dw_dev, void* dbias_dev, void* dtable_dev,
+                        void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* The products' waits are bounded, as the feed-forward kernels' are; these report them for the linear layer: of the last call that
+ * used workspace_dev, and of any call on the current device since this was asked last. */
+int sds_linear_status(const void* workspace_dev, void* cuda_stream);
+int sds_linear_gave_up(void* cuda_stream);
+
 const char* sds_strerror(int code);
 int sds_last_cuda_error(const sds_ctx* ctx);
 void sds_destroy(sds_ctx* ctx);

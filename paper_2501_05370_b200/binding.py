@@ -21,6 +21,7 @@ SDS_ECUDA, SDS_ETIMEOUT, SDS_ENONFINITE, SDS_ECALLBACK = -5, -6, -7, -8
 SDS_DEN_GMM, SDS_DEN_MLP, SDS_DEN_CALLBACK, SDS_DEN_PHI4, SDS_DEN_GATED = 1, 2, 3, 4, 5
 SDS_F32, SDS_BF16, SDS_F16 = 0, 1, 2
 SDS_ACT_SILU, SDS_ACT_GELU, SDS_ACT_GELU_TANH = 0, 1, 2
+SDS_ACT_NONE = 3
 ACTIVATIONS = {"silu": SDS_ACT_SILU, "gelu": SDS_ACT_GELU, "gelu_tanh": SDS_ACT_GELU_TANH}
 SDS_FROZEN_PREV, SDS_FROZEN_EXACT, SDS_INDEPENDENT, SDS_PICARD = 0, 1, 2, 3
 (GET_X, GET_TAIL, GET_DQ, GET_DC, GET_Y, GET_N, GET_ACT, GET_ROWOFF, GET_S1, GET_S2, GET_ELL, GET_LOGU,
@@ -39,6 +40,15 @@ class SdsDenoiser(C.Structure):
                 ("means_dtype", C.c_int32), ("nlayer", C.c_int32), ("W_dev", C.c_void_p), ("bias_dev", C.c_void_p),
                 ("temb_dev", C.c_void_p), ("dims", C.c_void_p), ("fn", DENOISE_FN), ("user", C.c_void_p),
                 ("grid_side", C.c_int32), ("coupling", C.c_float), ("periodic", C.c_int32)]
+
+
+class SdsLinearLayer(C.Structure):
+    _fields_ = [("k", C.c_int32), ("n", C.c_int32), ("steps", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32),
+                ("w_dev", C.c_void_p), ("bias_dev", C.c_void_p), ("bias_dtype", C.c_int32), ("table_dev", C.c_void_p)]
+
+
+class SdsLinearSizes(C.Structure):
+    _fields_ = [("keep_bytes", C.c_size_t), ("forward_bytes", C.c_size_t), ("backward_bytes", C.c_size_t)]
 
 
 class SdsGatedFfnSizes(C.Structure):
@@ -93,6 +103,14 @@ EXPORTS = {
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "sds_gated_ffn_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "sds_gated_ffn_gave_up": (C.c_int, [C.c_void_p]),
+    "sds_linear_bytes": (C.c_int, [C.POINTER(SdsLinearLayer), C.c_int64, C.POINTER(SdsLinearSizes)]),
+    "sds_linear": (C.c_int, [C.POINTER(SdsLinearLayer), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                             C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "sds_linear_backward": (C.c_int, [C.POINTER(SdsLinearLayer), C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                                      C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_size_t, C.c_void_p]),
+    "sds_linear_status": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "sds_linear_gave_up": (C.c_int, [C.c_void_p]),
     "sds_selftest_gated_ffn_wait": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p]),
     "sds_strerror": (C.c_char_p, [C.c_int]),
     "sds_last_cuda_error": (C.c_int, [C.c_void_p]),

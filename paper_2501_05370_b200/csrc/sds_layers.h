@@ -74,6 +74,35 @@ cudaError_t launch_ffn_backward(const FfnArgs& a, cudaStream_t st);
 // h = act(x Wg^T) * (x Wu^T), then res += h Wd^T. Every output element is the same bits however many rows there are.
 cudaError_t launch_ffn_hidden(const FfnArgs& a, cudaStream_t st);
 cudaError_t launch_ffn_residual(const FfnArgs& a, cudaStream_t st);
+
+// ---- linear layer with its epilogue (sds_linear.cu) ----
+// y = act(x W^T + b + table[step]) + residual with x [rows, k], W [n, k]; x, W, table of one 16-bit type, k a multiple of 8.
+
+struct LinearArgs {
+  int rows, k, n;
+  int f16;               // x, W and the table are f16 (else bf16)
+  int act;               // SDS_ACT_*
+  const void* x; int64_t ldx;
+  const void* w;
+  const void* bias; int tbias;                 // [n] of any type, NULL = none
+  const void* table; const int* step; int steps;
+  const void* residual; int64_t ldr;           // of type ty, NULL = none
+  void* y; int64_t ldy; int ty;                // SDS_F32 or the operands' type
+  uint16_t* factor;      // act'(z) [rows, n rounded up to 8] f16, or NULL
+  // backward
+  const void* dy; int64_t lddy;                // of type ty
+  void* dx; int64_t lddx;                      // any of the four gradients may be NULL
+  void* dw; void* db; void* dtable;
+  int* err;              // status word, at the workspace's begin
+};
+
+struct LinearWorkspace { size_t dz, db, dw, begin, list, table, bytes; };   // offsets of a backward call's parts, and their end
+LinearWorkspace linear_workspace(int64_t rows, int32_t k, int32_t n, int32_t nsteps, bool has_table);
+size_t linear_factor_bytes(int64_t rows, int32_t n);
+cudaError_t launch_linear(const LinearArgs& a, cudaStream_t st);
+cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st);
+cudaError_t linear_gave_up(int* role, cudaStream_t st);
+
 // waits for st; *role: non-zero if a wait on the current device gave up since this was asked last
 cudaError_t ffn_gave_up(int* role, cudaStream_t st);
 cudaError_t launch_ffn_wait_selftest(uint32_t polls, int* err, cudaStream_t st);

@@ -69,6 +69,61 @@ sds_gated_ffn_sizes ffn_sizes(int64_t rows, int32_t d, int32_t f) {
   return s;
 }
 
+int check_linear(const sds_linear_layer* l, int64_t rows) {
+  if (!l || rows < 0 || rows > kMaxSize || l->k <= 0 || l->k > kMaxSize || l->n <= 0 || l->n > kMaxSize) return SDS_EINVAL;
+  if (l->table_dev ? l->steps <= 0 : l->steps < 0) return SDS_EINVAL;
+  if (l->dtype != SDS_BF16 && l->dtype != SDS_F16) return SDS_EUNSUPPORTED;
+  if (l->act != SDS_ACT_NONE && l->act != SDS_ACT_SILU && l->act != SDS_ACT_GELU && l->act != SDS_ACT_GELU_TANH)
+    return SDS_EUNSUPPORTED;
+  return l->k % 8 || (l->table_dev && l->steps > 65535) ? SDS_EUNSUPPORTED : SDS_OK;
+}
+
+// the layer's arrays, and what both directions read
+int check_linear_call(const sds_linear_layer* l, const void* x, int64_t ldx, const int32_t* step, int64_t rows, int32_t y_dtype) {
+  int rc = check_linear(l, rows);
+  if (rc != SDS_OK) return rc;
+  if (y_dtype != SDS_F32 && y_dtype != l->dtype) return SDS_EUNSUPPORTED;
+  if (!l->w_dev) return SDS_EINVAL;
+  if (!aligned(l->w_dev, 16)) return SDS_EUNSUPPORTED;
+  if (l->bias_dev && (!is_type(l->bias_dtype) || !aligned(l->bias_dev, type_bytes(l->bias_dtype))))
+    return is_type(l->bias_dtype) ? SDS_EINVAL : SDS_EUNSUPPORTED;
+  if (!aligned(l->table_dev, 2)) return SDS_EINVAL;
+  if (l->table_dev && rows > 0 && (!step || !aligned(step, 4))) return SDS_EINVAL;
+  return check_ffn_rows(x, ldx, rows, l->k);
+}
+
+sds_linear_sizes linear_sizes(const sds_linear_layer* l, int64_t rows) {
+  sds_linear_sizes s;
+  s.keep_bytes = l->act == SDS_ACT_NONE ? 0 : align_up(linear_factor_bytes(rows, l->n));
+  s.forward_bytes = kAlign;                            // the status word
+  s.backward_bytes = linear_workspace(rows, l->k, l->n, l->steps, l->table_dev != nullptr).bytes;
+  return s;
+}
+
+LinearArgs linear_args(const sds_linear_layer* l, const void* x, int64_t ldx, const int32_t* step, int64_t rows, int32_t y_dtype,
+                       const void* keep, void* workspace) {
+  LinearArgs a{};
+  a.rows = (int)rows; a.k = l->k; a.n = l->n;
+  a.f16 = l->dtype == SDS_F16; a.act = l->act;
+  a.x = x; a.ldx = ldx; a.w = l->w_dev;
+  a.bias = l->bias_dev; a.tbias = l->bias_dtype;
+  a.table = l->table_dev; a.step = step; a.steps = l->steps;
+  a.ty = y_dtype;
+  a.factor = static_cast<uint16_t*>(const_cast<void*>(keep));
+  a.err = static_cast<int*>(workspace);
+  return a;
+}
+
+int status_word(const void* workspace, void* cuda_stream) {
+  if (!workspace) return SDS_EINVAL;
+  int word = 0;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return result(e);
+  return word != 0 ? SDS_ETIMEOUT : SDS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -195,15 +250,7 @@ int sds_gated_ffn_backward(const void* dy_dev, int64_t lddy, const void* x_dev, 
   return result(launch_ffn_backward(a, static_cast<cudaStream_t>(cuda_stream)));
 }
 
-int sds_gated_ffn_status(const void* workspace_dev, void* cuda_stream) {
-  if (!workspace_dev) return SDS_EINVAL;
-  int word = 0;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  cudaError_t e = cudaMemcpyAsync(&word, workspace_dev, sizeof(word), cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e != cudaSuccess) return result(e);
-  return word != 0 ? SDS_ETIMEOUT : SDS_OK;
-}
+int sds_gated_ffn_status(const void* workspace_dev, void* cuda_stream) { return status_word(workspace_dev, cuda_stream); }
 
 int sds_gated_ffn_gave_up(void* cuda_stream) {
   int role = 0;
@@ -215,6 +262,60 @@ int sds_gated_ffn_gave_up(void* cuda_stream) {
 int sds_selftest_gated_ffn_wait(int32_t polls, void* workspace_dev, void* cuda_stream) {
   if (!workspace_dev || !aligned(workspace_dev, kAlign) || polls <= 0 || polls > (1 << 16)) return SDS_EINVAL;
   return result(launch_ffn_wait_selftest((uint32_t)polls, static_cast<int*>(workspace_dev), static_cast<cudaStream_t>(cuda_stream)));
+}
+
+int sds_linear_bytes(const sds_linear_layer* layer, int64_t rows, sds_linear_sizes* sizes) {
+  if (!sizes) return SDS_EINVAL;
+  const int rc = check_linear(layer, rows);
+  if (rc != SDS_OK) return rc;
+  *sizes = linear_sizes(layer, rows);
+  return SDS_OK;
+}
+
+int sds_linear(const sds_linear_layer* layer, const void* x_dev, int64_t ldx, const int32_t* step_dev, int64_t rows,
+               const void* residual_dev, int64_t ldr, void* y_dev, int64_t ldy, int32_t y_dtype, void* keep_dev,
+               void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_linear_call(layer, x_dev, ldx, step_dev, rows, y_dtype);
+  if (rc != SDS_OK) return rc;
+  if ((rc = check_rows(y_dev, ldy, y_dtype, rows, layer->n)) != SDS_OK) return rc;
+  if (residual_dev && (rc = check_rows(residual_dev, ldr, y_dtype, rows, layer->n)) != SDS_OK) return rc;
+  if ((rc = check_workspace(workspace_dev, workspace_bytes, kAlign)) != SDS_OK) return rc;
+  if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
+  LinearArgs a = linear_args(layer, x_dev, ldx, step_dev, rows, y_dtype, keep_dev, workspace_dev);
+  a.residual = residual_dev; a.ldr = ldr;
+  a.y = y_dev; a.ldy = ldy;
+  return result(launch_linear(a, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+int sds_linear_backward(const sds_linear_layer* layer, const void* dy_dev, int64_t lddy, int32_t y_dtype,
+                        const void* x_dev, int64_t ldx, const int32_t* step_dev, int64_t rows, const void* keep_dev,
+                        void* dx_dev, int64_t lddx, void* dw_dev, void* dbias_dev, void* dtable_dev,
+                        void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_linear_call(layer, x_dev, ldx, step_dev, rows, y_dtype);
+  if (rc != SDS_OK) return rc;
+  if ((rc = check_rows(dy_dev, lddy, y_dtype, rows, layer->n)) != SDS_OK) return rc;
+  if (dx_dev && (rc = check_ffn_rows(dx_dev, lddx, rows, layer->k)) != SDS_OK) return rc;
+  if ((dbias_dev && !layer->bias_dev) || (dtable_dev && !layer->table_dev)) return SDS_EINVAL;
+  if (!aligned(dw_dev, 16)) return SDS_EUNSUPPORTED;
+  if ((dbias_dev && !aligned(dbias_dev, type_bytes(layer->bias_dtype))) || !aligned(dtable_dev, 2)) return SDS_EINVAL;
+  const sds_linear_sizes s = linear_sizes(layer, rows);
+  if (s.keep_bytes > 0 && !keep_dev) return SDS_EINVAL;
+  if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
+  if ((rc = check_workspace(workspace_dev, workspace_bytes, s.backward_bytes)) != SDS_OK) return rc;
+  LinearArgs a = linear_args(layer, x_dev, ldx, step_dev, rows, y_dtype, keep_dev, workspace_dev);
+  a.dy = dy_dev; a.lddy = lddy;
+  a.dx = dx_dev; a.lddx = lddx;
+  a.dw = dw_dev; a.db = dbias_dev; a.dtable = dtable_dev;
+  return result(launch_linear_backward(a, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+int sds_linear_status(const void* workspace_dev, void* cuda_stream) { return status_word(workspace_dev, cuda_stream); }
+
+int sds_linear_gave_up(void* cuda_stream) {
+  int role = 0;
+  const cudaError_t e = linear_gave_up(&role, static_cast<cudaStream_t>(cuda_stream));
+  if (e != cudaSuccess) return result(e);
+  return role != 0 ? SDS_ETIMEOUT : SDS_OK;
 }
 
 #pragma GCC visibility pop

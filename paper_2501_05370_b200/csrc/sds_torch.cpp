@@ -106,6 +106,23 @@ at::Tensor output(PyObject* o, const at::Tensor& x, at::ScalarType type, int64_t
   return y;
 }
 
+at::ScalarType dtype_or(PyObject* o, at::ScalarType other) {
+  if (o == Py_None) return other;
+  require(THPDtype_Check(o), "out_dtype must be a torch dtype");
+  return reinterpret_cast<THPDtype*>(o)->scalar_type;
+}
+
+// x's leading dimensions with n columns
+bool has_shape(const at::Tensor& y, const at::Tensor& x, int64_t n) {
+  return y.dim() == x.dim() && y.size(-1) == n && y.sizes().slice(0, y.dim() - 1) == x.sizes().slice(0, x.dim() - 1);
+}
+
+int64_t integer(PyObject* o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw PythonError{};
+  return v;
+}
+
 at::Tensor workspace(PyObject* o, size_t need, const at::Tensor& x) {
   if (o == Py_None) return empty({(int64_t)need}, at::kByte, x);
   const at::Tensor& w = tensor(o, "workspace");
@@ -328,9 +345,134 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------------------------
+// linear layer
+// ---------------------------------------------------------------------------------------------
+
+struct Linear {
+  Rows r;
+  sds_linear_layer layer;
+  const int32_t* step;
+  at::ScalarType bias_type;
+};
+// the layer of x, weight, bias, table and step (the last three may be None)
+Linear linear_of(const at::Tensor& x, const at::Tensor& w, PyObject* bias, PyObject* table, PyObject* step, int act) {
+  Linear s{};
+  s.r = rows_of(x, "x");
+  const at::ScalarType t = x.scalar_type();
+  require(w.dim() == 2 && w.size(0) > 0 && w.size(0) <= INT32_MAX && w.size(1) == s.r.d && w.scalar_type() == t && w.device() == x.device() &&
+              w.is_contiguous(),
+          "weight must be a contiguous [n, k] tensor of x's type on x's device, for x [..., k]");
+  const int64_t n = w.size(0);
+  s.layer.k = (int32_t)s.r.d; s.layer.n = (int32_t)n;
+  s.layer.dtype = type_code(t); s.layer.act = act;
+  s.layer.w_dev = w.data_ptr();
+  s.bias_type = at::kFloat;
+  if (bias != Py_None) {
+    const at::Tensor& b = tensor(bias, "bias");
+    require(b.dim() == 1 && b.numel() == n && b.is_contiguous() && b.device() == x.device(),
+            "bias must be a contiguous vector of the weight's first size on x's device");
+    s.bias_type = b.scalar_type();
+    s.layer.bias_dev = b.data_ptr();
+  }
+  s.layer.bias_dtype = type_code(s.bias_type);
+  require((table == Py_None) == (step == Py_None), "table and step come together");
+  if (table != Py_None) {
+    const at::Tensor &v = tensor(table, "table"), &at = tensor(step, "step");
+    require(v.dim() == 2 && v.size(0) > 0 && v.size(0) <= INT32_MAX && v.size(1) == n && v.scalar_type() == t && v.device() == x.device() &&
+                v.is_contiguous(),
+            "table must be a contiguous [steps, n] tensor of x's type on x's device");
+    require(at.scalar_type() == at::kInt && at.numel() == s.r.rows && at.is_contiguous() && at.device() == x.device(),
+            "step must be a contiguous int32 tensor with one value per row of x, on x's device");
+    s.layer.table_dev = v.data_ptr();
+    s.layer.steps = (int32_t)v.size(0);
+    s.step = at.data_ptr<int32_t>();
+  }
+  return s;
+}
+
+sds_linear_sizes linear_sizes(const Linear& s) {
+  sds_linear_sizes sizes;
+  check(sds_linear_bytes(&s.layer, s.r.rows, &sizes), "sds_linear_bytes");
+  return sizes;
+}
+
+// what the forward call returns for the backward one: a single byte that says so where there is nothing to keep
+int64_t kept_size(const sds_linear_sizes& sizes) { return sizes.keep_bytes ? (int64_t)sizes.keep_bytes : 1; }
+
+// (x, weight, bias, act, table, step, residual, out_dtype, keep, out, workspace)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "weight");
+    const Linear s = linear_of(x, w, a[2], a[4], a[5], (int)integer(a[3]));
+    const at::ScalarType yt = dtype_or(a[7], x.scalar_type());
+    const int ty = type_code(yt);
+    const void* residual = nullptr;
+    int64_t ldr = 0;
+    if (a[6] != Py_None) {
+      const at::Tensor& v = tensor(a[6], "residual");
+      require(has_shape(v, x, s.layer.n) && v.scalar_type() == yt && v.device() == x.device(),
+              "residual must have the output's shape and type and x's device");
+      ldr = rows_of(v, "residual").ld;
+      residual = v.data_ptr();
+    }
+    const bool keep = truth(a[8]);
+    warn_unrecorded("linear", {a[0], a[1], a[2], a[4], a[6]});
+    const sds_linear_sizes sizes = linear_sizes(s);
+    const c10::cuda::CUDAGuard guard(x.device());
+    at::Tensor y, kept;
+    int64_t ldy = s.layer.n;
+    if (a[9] == Py_None) {
+      c10::SmallVector<int64_t, 8> shape(x.sizes().begin(), x.sizes().end());
+      shape.back() = s.layer.n;
+      y = empty(shape, yt, x);
+    } else {
+      y = tensor(a[9], "out");
+      require(has_shape(y, x, s.layer.n) && y.scalar_type() == yt && y.device() == x.device(),
+              "out must have the output's shape and type and x's device");
+      ldy = rows_of(y, "out").ld;
+    }
+    if (keep) kept = empty({kept_size(sizes)}, at::kByte, x);
+    const at::Tensor ws = workspace(a[10], sizes.forward_bytes, x);
+    check(sds_linear(&s.layer, x.data_ptr(), s.r.ld, s.step, s.r.rows, residual, ldr, y.data_ptr(), ldy, ty,
+                     sizes.keep_bytes ? ptr(kept) : nullptr, ws.data_ptr(), (size_t)ws.numel(),
+                     c10::cuda::getCurrentCUDAStream(x.get_device()).stream()),
+          "sds_linear");
+    return keep ? tuple({y, kept}) : wrap(y);
+  });
+}
+
+// (dy, x, weight, kept, bias, table, step, want, workspace)
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor &dy = tensor(a[0], "dy"), &x = tensor(a[1], "x"), &w = tensor(a[2], "weight"), &kept = tensor(a[3], "kept");
+    // (which activation it was is in what the forward call kept: one byte, without one)
+    const Linear s = linear_of(x, w, a[4], a[5], a[6], kept.numel() != 1 ? SDS_ACT_SILU : SDS_ACT_NONE);
+    require(has_shape(dy, x, s.layer.n) && dy.device() == x.device(), "dy must have the output's shape and x's device");
+    const int64_t lddy = rows_of(dy, "dy").ld;
+    const int ty = type_code(dy.scalar_type());
+    const sds_linear_sizes sizes = linear_sizes(s);
+    require(kept.scalar_type() == at::kByte && kept.is_contiguous() && kept.device() == x.device() &&
+                kept.numel() == kept_size(sizes),
+            "kept must be what linear(keep=True) returned for these sizes");
+    const c10::cuda::CUDAGuard guard(x.device());
+    at::Tensor g[4];
+    if (wanted(a[7], 0, 4)) g[0] = empty(x.sizes(), x.scalar_type(), x);
+    if (wanted(a[7], 1, 4)) g[1] = empty(w.sizes(), x.scalar_type(), x);
+    if (wanted(a[7], 2, 4) && s.layer.bias_dev) g[2] = empty({s.layer.n}, s.bias_type, x);
+    if (wanted(a[7], 3, 4) && s.layer.table_dev) g[3] = empty({s.layer.steps, s.layer.n}, x.scalar_type(), x);
+    const at::Tensor ws = workspace(a[8], sizes.backward_bytes, x);
+    check(sds_linear_backward(&s.layer, dy.data_ptr(), lddy, ty, x.data_ptr(), s.r.ld, s.step, s.r.rows, sizes.keep_bytes ? kept.data_ptr() : nullptr,
+                              ptr(g[0]), s.r.d, ptr(g[1]), ptr(g[2]), ptr(g[3]), ws.data_ptr(), (size_t)ws.numel(),
+                              c10::cuda::getCurrentCUDAStream(x.get_device()).stream()),
+          "sds_linear_backward");
+    return tuple({g[0], g[1], g[2], g[3]});
+  });
+}
+
 #define SDS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDS_METHOD(layer_norm), SDS_METHOD(layer_norm_backward), SDS_METHOD(gated_ffn),
-                         SDS_METHOD(gated_ffn_backward), {nullptr, nullptr, 0, nullptr}};
+                         SDS_METHOD(gated_ffn_backward), SDS_METHOD(linear), SDS_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sds_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

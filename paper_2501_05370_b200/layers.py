@@ -1,5 +1,5 @@
-"""Layer operators of gated denoisers on torch CUDA tensors: layer norm and the gated feed-forward block, each
-with its backward pass (include/sds.h documents the formulas). Every call enqueues on the current stream of its
+"""Layer operators of denoisers on torch CUDA tensors: layer norm, the gated feed-forward block and the linear layer with its
+epilogue, each with its backward pass (include/sds.h documents the formulas). Every call enqueues on the current stream of its
 tensors' device and does not wait. Outputs and workspaces are allocated by torch unless they are passed in. A bad
 argument raises ValueError, an error of the library SdsError. Nothing is recorded for autograd: the backward calls are
 the gradients. A forward call whose inputs require gradients (or carry forward-mode tangents) outside torch.no_grad()
@@ -84,15 +84,55 @@ def gated_ffn_backward(dy, x, w_gate, w_up, w_down, kept, *, want=(True, True, T
     return (_native or _ext()).gated_ffn_backward(dy, x, w_gate, w_up, w_down, kept, want, workspace)
 
 
+def _wait_status(name: str, workspace) -> None:
+    """Waits for the current stream and raises if a bounded wait gave up: name_status of a workspace, or name_gave_up."""
+    import torch
+    if workspace is None:
+        where, args, device = name + "_gave_up", (), None
+    else:
+        where, args, device = name + "_status", (workspace.data_ptr(),), workspace.device
+    with torch.cuda.device(device):
+        rc = getattr(sb.load(), where)(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != sb.SDS_OK:
+        raise sb.SdsError(rc, where)
+
+
 def gated_ffn_status(workspace=None) -> None:
     """Waits for the current stream and raises if a bounded wait of the last gated_ffn call (or its backward) that
     was given this workspace gave up. Without one: if a wait of any such call on the current device did since this was asked
     last, whatever its workspace (those that the calls allocate themselves have no other report)."""
-    import torch
-    if workspace is None:
-        where, rc = "sds_gated_ffn_gave_up", sb.load().sds_gated_ffn_gave_up(torch.cuda.current_stream().cuda_stream)
-    else:
-        with torch.cuda.device(workspace.device):
-            where, rc = "sds_gated_ffn_status", sb.load().sds_gated_ffn_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream)
-    if rc != sb.SDS_OK:
-        raise sb.SdsError(rc, where)
+    _wait_status("sds_gated_ffn", workspace)
+
+
+# ---------------------------------------------------------------------------------------------
+# linear layer
+# ---------------------------------------------------------------------------------------------
+
+
+def _activation(name) -> int:
+    act = sb.SDS_ACT_NONE if name is None else ACTIVATIONS.get(name)
+    if act is None:
+        raise ValueError(f"activation must be None or one of {sorted(ACTIVATIONS)}")
+    return act
+
+
+def linear(x, weight, bias=None, activation=None, *, table=None, step=None, residual=None, out_dtype=None, keep: bool = False,
+           out=None, workspace=None):
+    """sds_linear: y = act(x W^T + bias + table[step]) + residual for x [..., k] and weight [n, k] (bfloat16 or float16, k a
+    multiple of 8); bias [n] of any of the three types; table [steps, n] of x's type with step, int32, one row of the table per
+    row of x (a row whose step is outside the table becomes NaN); residual [..., n] of the output's type. activation None,
+    "silu", "gelu" or "gelu_tanh". out_dtype: x's type (default) or float32. With keep=True returns (y, kept) with what
+    linear_backward needs."""
+    return (_native or _ext()).linear(x, weight, bias, _activation(activation), table, step, residual, out_dtype, keep, out, workspace)
+
+
+def linear_backward(dy, x, weight, kept, *, bias=None, table=None, step=None, want=(True, True, True, True), workspace=None):
+    """sds_linear_backward: (dx, dweight, dbias, dtable) from dy (of the forward output's type) and the forward call's x,
+    weight, kept, bias, table and step (of bias and table only size and type count). want: which of the four to compute; None
+    is returned for the others, and for the bias and the table where there was none. The residual's gradient is dy."""
+    return (_native or _ext()).linear_backward(dy, x, weight, kept, bias, table, step, want, workspace)
+
+
+def linear_status(workspace=None) -> None:
+    """gated_ffn_status for linear and linear_backward."""
+    _wait_status("sds_linear", workspace)
