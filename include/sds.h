@@ -27,7 +27,7 @@
  *   - A context is used by one host thread at a time. Contexts are independent.
  *   - Random numbers: Philox-4x32-10, counter (q, k, b_lo, stream + 256*b_hi), key = seed, where
  *     q = element index / 4, k = transition index, b = global chain id (chain_id_offset + local
- *     index). Stream 0 = draft noise, 1 = accept uniform, 2 = initial state. Results of a chain
+ *     index). Stream 0 = draft noise, 1 = accept uniform, 2 = initial state, 3 = dropout. Results of a chain
  *     therefore do not depend on which other chains share the context.
  */
 #ifndef SDS_H_
@@ -521,6 +521,89 @@ int sds_linear_backward(const sds_linear_layer* layer, const void* dy_dev, int64
  * used workspace_dev, and of any call on the current device since this was asked last. */
 int sds_linear_status(const void* workspace_dev, void* cuda_stream);
 int sds_linear_gave_up(void* cuda_stream);
+
+/* Dropout from the library's generator, with a mask that is never stored: D is 0 or 1 / (1 - p), a function of (seed, step, row,
+ * column). Philox stream 3, in the layout of the other streams (key = seed): the block with counter (column / 8, step, row) decides
+ * eight columns, 16 bits each, low half of a word first; a column is dropped if its bits are below P = p 65536 rounded to the
+ * nearest integer, and kept with the factor 65536 / (65536 - P). p in [0, 1] (1 drops everything). step >= 0: the training
+ * step, or a layer's own number in it; step_dev (device, int32, NULL = none): added to it when the kernel runs, so that a
+ * captured graph draws anew in every replay. row0 >= 0: global number of row 0 (rows below 2^56), so that shards of a batch draw what
+ * the whole batch draws. */
+typedef struct {
+  double p;
+  uint64_t seed;
+  int32_t step;
+  const int32_t* step_dev;
+  int64_t row0;
+} sds_dropout_spec;
+
+/* y = D x + residual over x_dev [rows, d] of x_dtype, y_dev and residual_dev (NULL = none) [rows, d] of y_dtype, rows ldx, ldy, ldr
+ * elements apart: y_dtype is x_dtype, or one of the two is SDS_F32 (else SDS_EUNSUPPORTED). A dropped element adds 0 whatever it was. y_dev may be x_dev
+ * (same rows, same type) or residual_dev. The gradient of x is the same call on dy without residual, with the same spec. */
+int sds_dropout(const sds_dropout_spec* spec, const void* x_dev, int64_t ldx, int32_t x_dtype, int64_t rows, int32_t d,
+                const void* residual_dev, int64_t ldr, void* y_dev, int64_t ldy, int32_t y_dtype, void* cuda_stream);
+
+/* Residual norm: from one block of a residual network to the next in one pass. With the block's output h and the stream r:
+ *   q = post(h) * post_w  (post != 0; post: the norm below without weight)  or  q = h
+ *   out = r + alpha gate D q                                     (D: dropout as above)
+ *   n = (xhat(out) w + b) (1 + scale) + shift                    (n: what the next block reads)
+ *   xhat(v) = (v - <v>) / sqrt(<(v - <v>)^2> + eps)  (SDS_NORM_LAYER)  or  v / sqrt(<v^2> + eps)  (SDS_NORM_RMS),  <.> mean over a row
+ * r_dev, out_dev [rows, d] of r_dtype, h_dev, n_dev of h_dtype: r_dtype, or for float r any of the three. Without h_dev (NULL) there is no
+ * block behind: n is that of r, and out_dev, gate and post are not used. w_dev, b_dev, post_w_dev [d] of w_dtype (NULL = ones,
+ * zeros, ones); gate_dev, scale_dev, shift_dev [groups, d] of cond_dtype, rows ld_gate, ld_scale, ld_shift elements apart (NULL = ones,
+ * zeros, zeros): rows / groups consecutive rows share one row of them (rows a multiple of groups; groups = 1: one vector for all,
+ * groups = rows: one each). d <= 16384 (else SDS_EUNSUPPORTED). eps >= 0 and alpha finite. All is held in float and rounded once; n is that of the
+ * unrounded out. keep_dev: [6, rows] floats (keep_bytes) that the backward pass needs, 256-byte aligned (NULL = none will follow).
+ * out_dev may be r_dev and n_dev h_dev (same rows) where no backward pass will need them. */
+#define SDS_NORM_LAYER    0
+#define SDS_NORM_RMS      1
+typedef struct {
+  int64_t rows, groups;
+  int32_t d;
+  int32_t r_dtype, h_dtype;
+  int32_t kind, post;
+  float alpha, eps;
+  const void* w_dev;
+  const void* b_dev;
+  const void* post_w_dev;
+  int32_t w_dtype;
+  const void* gate_dev;
+  const void* scale_dev;
+  const void* shift_dev;
+  int64_t ld_gate, ld_scale, ld_shift;
+  int32_t cond_dtype;
+  sds_dropout_spec drop;
+} sds_residual_norm_op;
+int sds_residual_norm(const sds_residual_norm_op* op, const void* r_dev, int64_t ldr, const void* h_dev, int64_t ldh,
+                      void* out_dev, int64_t ldo, void* n_dev, int64_t ldn, float* keep_dev, void* cuda_stream);
+
+/* Its gradients, from dn_dev (of h_dtype), dout_dev (of r_dtype: the gradient that reaches out past the next block; NULL = zeros)
+ * and the forward call's op, r, h and keep_dev. dr_dev of r_dtype, dh_dev of h_dtype, dw_dev, db_dev, dpost_w_dev [d] of w_dtype, dgate_dev,
+ * dscale_dev, dshift_dev [groups, d] of cond_dtype with rows ld_dgate, ld_dscale, ld_dshift elements apart; any may be NULL. A
+ * gradient of something that is NULL in op is computed as for its default. Sums over rows are held in float and added in a fixed
+ * order: same bits on every run. workspace_dev: 256-byte aligned, backward_bytes of sds_residual_norm_bytes for this op (it serves any
+ * choice of gradients). With rows = 0 the gradients of the vectors are zeros. */
+typedef struct {
+  size_t keep_bytes, backward_bytes;
+} sds_residual_norm_sizes;
+typedef struct {
+  void* dr_dev;
+  int64_t ld_dr;
+  void* dh_dev;
+  int64_t ld_dh;
+  void* dw_dev;
+  void* db_dev;
+  void* dpost_w_dev;
+  void* dgate_dev;
+  void* dscale_dev;
+  void* dshift_dev;
+  int64_t ld_dgate, ld_dscale, ld_dshift;
+} sds_residual_norm_grads;
+int sds_residual_norm_bytes(const sds_residual_norm_op* op, sds_residual_norm_sizes* sizes);
+int sds_residual_norm_backward(const sds_residual_norm_op* op, const void* dn_dev, int64_t lddn, const void* dout_dev,
+                               int64_t lddout, const void* r_dev, int64_t ldr, const void* h_dev, int64_t ldh,
+                               const float* keep_dev, const sds_residual_norm_grads* grads, void* workspace_dev,
+                               size_t workspace_bytes, void* cuda_stream);
 
 const char* sds_strerror(int code);
 int sds_last_cuda_error(const sds_ctx* ctx);

@@ -22,6 +22,7 @@ SDS_DEN_GMM, SDS_DEN_MLP, SDS_DEN_CALLBACK, SDS_DEN_PHI4, SDS_DEN_GATED = 1, 2, 
 SDS_F32, SDS_BF16, SDS_F16 = 0, 1, 2
 SDS_ACT_SILU, SDS_ACT_GELU, SDS_ACT_GELU_TANH = 0, 1, 2
 SDS_ACT_NONE = 3
+SDS_NORM_LAYER, SDS_NORM_RMS = 0, 1
 ACTIVATIONS = {"silu": SDS_ACT_SILU, "gelu": SDS_ACT_GELU, "gelu_tanh": SDS_ACT_GELU_TANH}
 SDS_FROZEN_PREV, SDS_FROZEN_EXACT, SDS_INDEPENDENT, SDS_PICARD = 0, 1, 2, 3
 (GET_X, GET_TAIL, GET_DQ, GET_DC, GET_Y, GET_N, GET_ACT, GET_ROWOFF, GET_S1, GET_S2, GET_ELL, GET_LOGU,
@@ -40,6 +41,28 @@ class SdsDenoiser(C.Structure):
                 ("means_dtype", C.c_int32), ("nlayer", C.c_int32), ("W_dev", C.c_void_p), ("bias_dev", C.c_void_p),
                 ("temb_dev", C.c_void_p), ("dims", C.c_void_p), ("fn", DENOISE_FN), ("user", C.c_void_p),
                 ("grid_side", C.c_int32), ("coupling", C.c_float), ("periodic", C.c_int32)]
+
+
+class SdsDropoutSpec(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_int32), ("step_dev", C.c_void_p), ("row0", C.c_int64)]
+
+
+class SdsResidualNormOp(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("groups", C.c_int64), ("d", C.c_int32), ("r_dtype", C.c_int32), ("h_dtype", C.c_int32),
+                ("kind", C.c_int32), ("post", C.c_int32), ("alpha", C.c_float), ("eps", C.c_float), ("w_dev", C.c_void_p),
+                ("b_dev", C.c_void_p), ("post_w_dev", C.c_void_p), ("w_dtype", C.c_int32), ("gate_dev", C.c_void_p),
+                ("scale_dev", C.c_void_p), ("shift_dev", C.c_void_p), ("ld_gate", C.c_int64), ("ld_scale", C.c_int64),
+                ("ld_shift", C.c_int64), ("cond_dtype", C.c_int32), ("drop", SdsDropoutSpec)]
+
+
+class SdsResidualNormSizes(C.Structure):
+    _fields_ = [("keep_bytes", C.c_size_t), ("backward_bytes", C.c_size_t)]
+
+
+class SdsResidualNormGrads(C.Structure):
+    _fields_ = [("dr_dev", C.c_void_p), ("ld_dr", C.c_int64), ("dh_dev", C.c_void_p), ("ld_dh", C.c_int64), ("dw_dev", C.c_void_p),
+                ("db_dev", C.c_void_p), ("dpost_w_dev", C.c_void_p), ("dgate_dev", C.c_void_p), ("dscale_dev", C.c_void_p),
+                ("dshift_dev", C.c_void_p), ("ld_dgate", C.c_int64), ("ld_dscale", C.c_int64), ("ld_dshift", C.c_int64)]
 
 
 class SdsLinearLayer(C.Structure):
@@ -111,6 +134,14 @@ EXPORTS = {
                                       C.c_void_p, C.c_size_t, C.c_void_p]),
     "sds_linear_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "sds_linear_gave_up": (C.c_int, [C.c_void_p]),
+    "sds_dropout": (C.c_int, [C.POINTER(SdsDropoutSpec), C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
+                              C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]),
+    "sds_residual_norm": (C.c_int, [C.POINTER(SdsResidualNormOp), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "sds_residual_norm_bytes": (C.c_int, [C.POINTER(SdsResidualNormOp), C.POINTER(SdsResidualNormSizes)]),
+    "sds_residual_norm_backward": (C.c_int, [C.POINTER(SdsResidualNormOp), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                             C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(SdsResidualNormGrads),
+                                             C.c_void_p, C.c_size_t, C.c_void_p]),
     "sds_selftest_gated_ffn_wait": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p]),
     "sds_strerror": (C.c_char_p, [C.c_int]),
     "sds_last_cuda_error": (C.c_int, [C.c_void_p]),

@@ -103,6 +103,63 @@ cudaError_t launch_linear(const LinearArgs& a, cudaStream_t st);
 cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st);
 cudaError_t linear_gave_up(int* role, cudaStream_t st);
 
+// ---- residual norm (sds_residual.cuh, sds_residual*.cu) and dropout (sds_dropout.cu) ----
+
+// D of dropout: zero or `scale`, from the library's generator (stream kStreamDropout)
+struct DropoutArgs {
+  uint32_t threshold;    // of 16 random bits, out of 65536; 0 = everything is kept, and nothing is drawn
+  float scale;
+  uint64_t seed;
+  uint32_t step;         // counter word; the value at step_dev is added to it
+  const int* step_dev;
+  uint64_t row0;         // global number of row 0
+};
+
+struct ResidualNormArgs {
+  int rows, d, per, groups;                      // per = rows / groups: rows that share a row of gate, scale and shift
+  int tr, th;                                    // types of the stream (r, out, dr, dr_in) and of the branch (h, n, dn, dh)
+  bool rms, post;
+  float alpha, eps;
+  DropoutArgs drop;
+  const void* r; int64_t ldr;
+  const void* h; int64_t ldh;                    // NULL = none: out = r, and out is not written
+  void* out; int64_t ldo;
+  void* n; int64_t ldn;
+  const void* w; const void* b; const void* wp; int tw;                            // [d] each, NULL = ones, zeros, ones
+  const void* gate; const void* scale; const void* shift; int tc;                  // [groups, d] each, NULL = ones, zeros, zeros
+  int64_t ldgate, ldscale, ldshift;
+  bool wide_w, wide_c;                           // the vectors (the rows of gate, scale and shift) lie in whole 16-byte pieces
+  float* stats;                                  // [6][rows]: mean, its remainder, 1 / size, and the same of post; forward: may be NULL
+  // backward
+  const void* dn; int64_t lddn;
+  const void* dr; int64_t lddr;                  // NULL = zeros
+  void* dr_in; int64_t lddr_in;
+  void* dh; int64_t lddh;
+  void* dw; void* db; void* dwp;
+  void* dgate; void* dscale; void* dshift;
+  int64_t lddgate, lddscale, lddshift;
+  // how the rows are dealt out, and where their sums go (residual_norm_plan)
+  int mode, workers, piece, pieces, total;       // rows of a piece, pieces of a group, pieces in all
+  float* part;                                   // [workers][3][d]
+  float* piece_part;                             // [groups * pieces][3][d]
+};
+
+constexpr int kResidualMaxD = 16384;
+// how a backward call deals out its rows: sets mode, workers, piece, pieces and total of a; floats of the two workspaces
+void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* piece_floats);
+cudaError_t launch_residual_norm(const ResidualNormArgs& a, cudaStream_t st);
+cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_t st);
+// y = D x + residual over [rows, d]
+struct DropoutCall {
+  DropoutArgs drop;
+  const void* x; int64_t ldx; int tx;
+  const void* residual; int64_t ldr;             // of type ty, NULL = none
+  void* y; int64_t ldy; int ty;
+  int64_t rows;
+  int d;
+};
+cudaError_t launch_dropout(const DropoutCall& a, cudaStream_t st);
+
 // waits for st; *role: non-zero if a wait on the current device gave up since this was asked last
 cudaError_t ffn_gave_up(int* role, cudaStream_t st);
 cudaError_t launch_ffn_wait_selftest(uint32_t polls, int* err, cudaStream_t st);

@@ -1,6 +1,7 @@
 // C entry points of the layer operators (see include/sds.h): argument checks and workspace carving.
 #include "../../include/sds.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "sds_layers.h"
@@ -112,6 +113,70 @@ LinearArgs linear_args(const sds_linear_layer* l, const void* x, int64_t ldx, co
   a.factor = static_cast<uint16_t*>(const_cast<void*>(keep));
   a.err = static_cast<int*>(workspace);
   return a;
+}
+
+int check_dropout(const sds_dropout_spec& s, int64_t rows) {
+  constexpr int64_t kMostRows = (int64_t)1 << 56;
+  if (!(s.p >= 0.0 && s.p <= 1.0) || s.step < 0 || s.row0 < 0 || s.row0 > kMostRows - rows || !aligned(s.step_dev, 4)) return SDS_EINVAL;
+  return SDS_OK;
+}
+
+DropoutArgs dropout_args(const sds_dropout_spec& s) {
+  DropoutArgs a{};
+  a.threshold = (uint32_t)std::nearbyint(s.p * 65536.0);
+  a.scale = a.threshold < 65536u ? (float)(65536.0 / (65536.0 - a.threshold)) : 0.f;
+  a.seed = s.seed; a.step = (uint32_t)s.step; a.step_dev = s.step_dev; a.row0 = (uint64_t)s.row0;
+  return a;
+}
+
+// a vector per group
+int check_cond(const void* p, int64_t ld, int32_t type, int64_t groups, int32_t d) { return p ? check_rows(p, ld, type, groups, d) : SDS_OK; }
+
+int check_residual_norm(const sds_residual_norm_op* op) {
+  if (!op || op->rows < 0 || op->rows > kMaxSize || op->d <= 0 || op->groups < 1 || (op->rows > 0 && op->rows % op->groups) ||
+      (op->rows == 0 && op->groups > kMaxSize))
+    return SDS_EINVAL;
+  if (op->kind != SDS_NORM_LAYER && op->kind != SDS_NORM_RMS) return SDS_EINVAL;
+  if (!std::isfinite(op->eps) || op->eps < 0.f || !std::isfinite(op->alpha)) return SDS_EINVAL;
+  if (op->d > kResidualMaxD) return SDS_EUNSUPPORTED;
+  if (!is_type(op->r_dtype) || !is_type(op->h_dtype) || !is_type(op->w_dtype) || !is_type(op->cond_dtype)) return SDS_EUNSUPPORTED;
+  if (op->h_dtype != op->r_dtype && op->r_dtype != SDS_F32) return SDS_EUNSUPPORTED;
+  for (const void* p : {op->w_dev, op->b_dev, op->post_w_dev})
+    if (!aligned(p, type_bytes(op->w_dtype))) return SDS_EINVAL;
+  int rc;
+  if ((rc = check_cond(op->gate_dev, op->ld_gate, op->cond_dtype, op->groups, op->d)) != SDS_OK) return rc;
+  if ((rc = check_cond(op->scale_dev, op->ld_scale, op->cond_dtype, op->groups, op->d)) != SDS_OK) return rc;
+  if ((rc = check_cond(op->shift_dev, op->ld_shift, op->cond_dtype, op->groups, op->d)) != SDS_OK) return rc;
+  return check_dropout(op->drop, op->rows);
+}
+
+ResidualNormArgs residual_norm_args(const sds_residual_norm_op* op, const void* r, int64_t ldr, const void* h, int64_t ldh, const float* keep) {
+  ResidualNormArgs a{};
+  a.rows = (int)op->rows; a.d = op->d; a.groups = (int)op->groups; a.per = op->rows > 0 ? (int)(op->rows / op->groups) : 1;
+  a.tr = op->r_dtype; a.th = op->h_dtype;
+  a.rms = op->kind == SDS_NORM_RMS; a.post = h && op->post != 0;
+  a.alpha = op->alpha; a.eps = op->eps;
+  a.drop = dropout_args(op->drop);
+  a.r = r; a.ldr = ldr; a.h = h; a.ldh = ldh;
+  a.w = op->w_dev; a.b = op->b_dev; a.wp = a.post ? op->post_w_dev : nullptr; a.tw = op->w_dtype;
+  a.gate = h ? op->gate_dev : nullptr; a.scale = op->scale_dev; a.shift = op->shift_dev; a.tc = op->cond_dtype;
+  a.ldgate = op->ld_gate; a.ldscale = op->ld_scale; a.ldshift = op->ld_shift;
+  a.stats = const_cast<float*>(keep);
+  return a;
+}
+
+// the workspace of a backward call that wants the gradients of all that op has
+size_t residual_norm_bytes(const sds_residual_norm_op* op) {
+  if (op->rows == 0) return kAlign;
+  size_t most = 0;
+  for (const bool cond : {false, true}) {
+    ResidualNormArgs a = residual_norm_args(op, nullptr, 0, op, 0, nullptr);    // (as if there were an h)
+    a.dgate = cond ? &most : nullptr;
+    size_t part = 0, piece = 0;
+    residual_norm_plan(&a, &part, &piece);
+    most = std::max(most, align_up(part * 4) + align_up(piece * 4));
+  }
+  return most;
 }
 
 int status_word(const void* workspace, void* cuda_stream) {
@@ -316,6 +381,89 @@ int sds_linear_gave_up(void* cuda_stream) {
   const cudaError_t e = linear_gave_up(&role, static_cast<cudaStream_t>(cuda_stream));
   if (e != cudaSuccess) return result(e);
   return role != 0 ? SDS_ETIMEOUT : SDS_OK;
+}
+
+int sds_dropout(const sds_dropout_spec* spec, const void* x_dev, int64_t ldx, int32_t x_dtype, int64_t rows, int32_t d,
+                const void* residual_dev, int64_t ldr, void* y_dev, int64_t ldy, int32_t y_dtype, void* cuda_stream) {
+  if (!spec || rows < 0 || rows > kMaxSize || d <= 0 || d > kMaxSize) return SDS_EINVAL;
+  int rc = check_dropout(*spec, rows);
+  if (rc != SDS_OK) return rc;
+  if (!is_type(x_dtype) || !is_type(y_dtype) || (x_dtype != y_dtype && x_dtype != SDS_F32 && y_dtype != SDS_F32)) return SDS_EUNSUPPORTED;
+  if ((rc = check_rows(x_dev, ldx, x_dtype, rows, d)) != SDS_OK) return rc;
+  if ((rc = check_rows(y_dev, ldy, y_dtype, rows, d)) != SDS_OK) return rc;
+  if (residual_dev && (rc = check_rows(residual_dev, ldr, y_dtype, rows, d)) != SDS_OK) return rc;
+  DropoutCall a{};
+  a.drop = dropout_args(*spec);
+  a.x = x_dev; a.ldx = ldx; a.tx = x_dtype;
+  a.residual = residual_dev; a.ldr = ldr;
+  a.y = y_dev; a.ldy = ldy; a.ty = y_dtype;
+  a.rows = rows; a.d = d;
+  return result(launch_dropout(a, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+int sds_residual_norm(const sds_residual_norm_op* op, const void* r_dev, int64_t ldr, const void* h_dev, int64_t ldh,
+                      void* out_dev, int64_t ldo, void* n_dev, int64_t ldn, float* keep_dev, void* cuda_stream) {
+  int rc = check_residual_norm(op);
+  if (rc != SDS_OK) return rc;
+  if ((rc = check_rows(r_dev, ldr, op->r_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if (h_dev && (rc = check_rows(h_dev, ldh, op->h_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if (h_dev && (rc = check_rows(out_dev, ldo, op->r_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if ((rc = check_rows(n_dev, ldn, op->h_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
+  ResidualNormArgs a = residual_norm_args(op, r_dev, ldr, h_dev, ldh, keep_dev);
+  a.out = out_dev; a.ldo = ldo;
+  a.n = n_dev; a.ldn = ldn;
+  return result(launch_residual_norm(a, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+int sds_residual_norm_bytes(const sds_residual_norm_op* op, sds_residual_norm_sizes* sizes) {
+  if (!sizes) return SDS_EINVAL;
+  const int rc = check_residual_norm(op);
+  if (rc != SDS_OK) return rc;
+  sizes->keep_bytes = (size_t)op->rows * 6 * 4;
+  sizes->backward_bytes = residual_norm_bytes(op);
+  return SDS_OK;
+}
+
+int sds_residual_norm_backward(const sds_residual_norm_op* op, const void* dn_dev, int64_t lddn, const void* dout_dev,
+                               int64_t lddout, const void* r_dev, int64_t ldr, const void* h_dev, int64_t ldh,
+                               const float* keep_dev, const sds_residual_norm_grads* grads, void* workspace_dev,
+                               size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_residual_norm(op);
+  if (rc != SDS_OK) return rc;
+  if (!grads) return SDS_EINVAL;
+  const sds_residual_norm_grads& g = *grads;
+  const struct { const void* p; int64_t ld; int32_t type; bool needed; } arrays[6] = {
+      {dn_dev, lddn, op->h_dtype, true},         {dout_dev, lddout, op->r_dtype, false}, {r_dev, ldr, op->r_dtype, true},
+      {h_dev, ldh, op->h_dtype, false},          {g.dr_dev, g.ld_dr, op->r_dtype, false}, {g.dh_dev, g.ld_dh, op->h_dtype, false}};
+  for (const auto& x : arrays)
+    if ((x.needed || x.p) && (rc = check_rows(x.p, x.ld, x.type, op->rows, op->d)) != SDS_OK) return rc;
+  if (op->rows > 0 && !h_dev && (g.dh_dev || g.dgate_dev || g.dpost_w_dev)) return SDS_EINVAL;
+  if (g.dpost_w_dev && !op->post) return SDS_EINVAL;
+  for (const void* p : {(const void*)g.dw_dev, (const void*)g.db_dev, (const void*)g.dpost_w_dev})
+    if (!aligned(p, type_bytes(op->w_dtype))) return SDS_EINVAL;
+  if ((rc = check_cond(g.dgate_dev, g.ld_dgate, op->cond_dtype, op->groups, op->d)) != SDS_OK) return rc;
+  if ((rc = check_cond(g.dscale_dev, g.ld_dscale, op->cond_dtype, op->groups, op->d)) != SDS_OK) return rc;
+  if ((rc = check_cond(g.dshift_dev, g.ld_dshift, op->cond_dtype, op->groups, op->d)) != SDS_OK) return rc;
+  if (op->rows > 0 && !keep_dev) return SDS_EINVAL;
+  if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
+  if ((rc = check_workspace(workspace_dev, workspace_bytes, residual_norm_bytes(op))) != SDS_OK) return rc;
+  if (!g.dr_dev && !g.dh_dev && !g.dw_dev && !g.db_dev && !g.dpost_w_dev && !g.dgate_dev && !g.dscale_dev && !g.dshift_dev) return SDS_OK;
+  ResidualNormArgs a = residual_norm_args(op, r_dev, ldr, h_dev, ldh, keep_dev);
+  a.dn = dn_dev; a.lddn = lddn;
+  a.dr = dout_dev; a.lddr = lddout;
+  a.dr_in = g.dr_dev; a.lddr_in = g.ld_dr;
+  a.dh = g.dh_dev; a.lddh = g.ld_dh;
+  a.dw = g.dw_dev; a.db = g.db_dev; a.dwp = g.dpost_w_dev;
+  a.dgate = g.dgate_dev; a.dscale = g.dscale_dev; a.dshift = g.dshift_dev;
+  a.lddgate = g.ld_dgate; a.lddscale = g.ld_dscale; a.lddshift = g.ld_dshift;
+  if (op->rows > 0) {
+    size_t part = 0, piece = 0;
+    residual_norm_plan(&a, &part, &piece);
+    a.part = static_cast<float*>(workspace_dev);
+    a.piece_part = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align_up(part * 4));
+  }
+  return result(launch_residual_norm_backward(a, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 #pragma GCC visibility pop

@@ -1,0 +1,169 @@
+// Residual norm: how a backward call deals out its rows, the kernels that add the workers' sums, and the choice of the row kernels.
+#include "sds_residual.cuh"
+
+namespace sds {
+
+namespace {
+
+// groups of threads that run at once in a backward launch: 512 threads per SM (128 registers each)
+int most_workers(int d) {
+  const int tpr = d <= 256 ? 32 : d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : d <= 8192 ? 1024 : 2048;
+  return kRowSms * 512 / tpr;
+}
+
+constexpr int kJoinWarps = 32;
+
+// 32 columns of a CTA; a warp adds every 32nd worker's sums. One group (kSumAll): the plain sums give every gradient; else
+// they are weighted already, and the groups' own gradients were written before.
+__global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(const ResidualNormArgs a) {
+  __shared__ float sums[3][kJoinWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, d = a.d;
+  start_after_prior_kernel();
+  float s[3] = {0.f, 0.f, 0.f};
+  if (c < d) {
+#pragma unroll 4
+    for (int i = warp; i < a.workers; i += kJoinWarps) {
+      const float* from = a.part + (size_t)i * 3 * d + c;
+      s[0] += from[0];
+      s[1] += from[d];
+      s[2] += from[2 * (size_t)d];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) sums[k][warp][lane] = s[k];
+  __syncthreads();
+  if (warp < 3) {
+    float v = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < kJoinWarps; ++i) v += sums[warp][i][lane];
+    __syncwarp();
+    sums[warp][0][lane] = v;
+  }
+  __syncthreads();
+  if (warp != 0 || c >= d) return;
+  const float A = sums[0][0][lane], B = sums[1][0][lane], C = sums[2][0][lane];
+  if (a.mode != kSumAll) {
+    if (a.dw) store_any(a.dw, a.tw, c, A);
+    if (a.db) store_any(a.db, a.tw, c, B);
+    if (a.dwp) store_any(a.dwp, a.tw, c, C);
+    return;
+  }
+  const float w = a.w ? load_any(a.w, a.tw, c) : 1.f, b = a.b ? load_any(a.b, a.tw, c) : 0.f, wp = a.wp ? load_any(a.wp, a.tw, c) : 1.f;
+  const float f = 1.0f + (a.scale ? load_any(a.scale, a.tc, c) : 0.f), gate = a.gate ? load_any(a.gate, a.tc, c) : 1.f;
+  if (a.dw) store_any(a.dw, a.tw, c, f * A);
+  if (a.db) store_any(a.db, a.tw, c, f * B);
+  if (a.dwp) store_any(a.dwp, a.tw, c, a.alpha * gate * C);
+  if (a.dshift) store_any(a.dshift, a.tc, c, B);
+  if (a.dscale) store_any(a.dscale, a.tc, c, fmaf(w, A, b * B));
+  if (a.dgate) store_any(a.dgate, a.tc, c, a.alpha * wp * C);
+}
+
+// The pieces of each group: a CTA takes 32 columns of one group, a warp every eighth piece.
+__global__ void __launch_bounds__(256) k_residual_join_groups(const ResidualNormArgs a, int strips) {
+  __shared__ float sums[3][8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = a.d;
+  const int group = (int)(blockIdx.x / strips), c = (int)(blockIdx.x % strips) * 32 + lane;
+  start_after_prior_kernel();
+  float s[3] = {0.f, 0.f, 0.f};
+  if (c < d) {
+#pragma unroll 4
+    for (int i = warp; i < a.pieces; i += 8) {
+      const float* from = a.piece_part + ((size_t)group * a.pieces + i) * 3 * d + c;
+      s[0] += from[0];
+      s[1] += from[d];
+      s[2] += from[2 * (size_t)d];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) sums[k][warp][lane] = s[k];
+  __syncthreads();
+  if (warp != 0 || c >= d) return;
+  float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[k] += sums[k][i][lane];
+  const float w = a.w ? load_any(a.w, a.tw, c) : 1.f, b = a.b ? load_any(a.b, a.tw, c) : 0.f, wp = a.wp ? load_any(a.wp, a.tw, c) : 1.f;
+  if (a.dshift) store_any(a.dshift, a.tc, (size_t)group * a.lddshift + c, t[1]);
+  if (a.dscale) store_any(a.dscale, a.tc, (size_t)group * a.lddscale + c, fmaf(w, t[0], b * t[1]));
+  if (a.dgate) store_any(a.dgate, a.tc, (size_t)group * a.lddgate + c, a.alpha * wp * t[2]);
+}
+
+cudaError_t launch_rows(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+  if (a.tr == SDS_BF16) return residual_bf16(a, vec, backward, st);
+  if (a.tr == SDS_F16) return residual_f16(a, vec, backward, st);
+  if (a.th == SDS_BF16) return residual_f32_bf16(a, vec, backward, st);
+  if (a.th == SDS_F16) return residual_f32_f16(a, vec, backward, st);
+  return residual_f32(a, vec, backward, st);
+}
+
+bool whole(const void* p, int64_t ld, int type) { return !p || pieces16(p, ld, type); }
+
+}  // namespace
+
+void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* piece_floats) {
+  const int cap = most_workers(a->d);
+  const bool wanted = a->dgate || a->dscale || a->dshift, conditioned = wanted || a->gate || a->scale || a->shift;
+  *piece_floats = 0;
+  a->pieces = 1;
+  if (a->groups > 1 && a->per > 1 && wanted) {
+    // Pieces per group: those with the fewest rows for the busiest worker. A piece costs about two rows more (its sums go to
+    // memory), one where it is a whole group and they are the result.
+    a->mode = kSumGroups;
+    int64_t least = INT64_MAX;
+    const int most = (int)std::min<int64_t>(a->per, 8 * (((int64_t)cap + a->groups - 1) / a->groups));
+    for (int p = 1; p <= most; ++p) {
+      const int rows = (a->per + p - 1) / p, n = (a->per + rows - 1) / rows;
+      const int64_t rounds = ((int64_t)a->groups * n + cap - 1) / cap, cost = rounds * (rows + (n > 1 ? 2 : 1));
+      if (cost < least) { least = cost; a->piece = rows; a->pieces = n; }
+    }
+    a->total = a->groups * a->pieces;
+    a->workers = std::min(cap, a->total);
+    if (a->pieces > 1) *piece_floats = (size_t)a->total * 3 * (size_t)a->d;
+  } else {
+    a->mode = conditioned && a->groups > 1 ? kSumWeighted : kSumAll;
+    a->piece = std::max(1, (a->rows + cap - 1) / cap);
+    a->workers = a->total = (a->rows + a->piece - 1) / a->piece;
+  }
+  *part_floats = (size_t)a->workers * 3 * (size_t)a->d;
+}
+
+cudaError_t launch_residual_norm(const ResidualNormArgs& a, cudaStream_t st) {
+  if (a.rows <= 0) return cudaSuccess;
+  const bool vec = a.d % 8 == 0 && whole(a.r, a.ldr, a.tr) && whole(a.h, a.ldh, a.th) && whole(a.n, a.ldn, a.th) &&
+                   (!a.h || whole(a.out, a.ldo, a.tr));
+  ResidualNormArgs g = a;
+  g.wide_w = whole(a.w, 0, a.tw) && whole(a.b, 0, a.tw) && whole(a.wp, 0, a.tw);
+  g.wide_c = whole(a.gate, a.ldgate, a.tc) && whole(a.scale, a.ldscale, a.tc) && whole(a.shift, a.ldshift, a.tc);
+  return launch_rows(g, vec, false, st);
+}
+
+cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  if (a.rows <= 0) {                              // empty sums
+    const size_t sw = a.tw == SDS_F32 ? 4 : 2, sc = a.tc == SDS_F32 ? 4 : 2;
+    for (void* p : {a.dw, a.db, a.dwp})
+      if (p && (e = cudaMemsetAsync(p, 0, (size_t)a.d * sw, st)) != cudaSuccess) return e;
+    const struct { void* p; int64_t ld; } cond[3] = {{a.dgate, a.lddgate}, {a.dscale, a.lddscale}, {a.dshift, a.lddshift}};
+    for (const auto& c : cond)
+      if (c.p && a.groups > 0 &&
+          (e = cudaMemset2DAsync(c.p, (size_t)c.ld * sc, 0, (size_t)a.d * sc, (size_t)a.groups, st)) != cudaSuccess)
+        return e;
+    return cudaSuccess;
+  }
+  const bool vec = a.d % 8 == 0 && whole(a.r, a.ldr, a.tr) && whole(a.h, a.ldh, a.th) && whole(a.dn, a.lddn, a.th) &&
+                   whole(a.dr, a.lddr, a.tr) && whole(a.dr_in, a.lddr_in, a.tr) && whole(a.dh, a.lddh, a.th);
+  ResidualNormArgs g = a;
+  g.wide_w = whole(a.w, 0, a.tw) && whole(a.b, 0, a.tw) && whole(a.wp, 0, a.tw);
+  g.wide_c = whole(a.gate, a.ldgate, a.tc) && whole(a.scale, a.ldscale, a.tc) && whole(a.shift, a.ldshift, a.tc) &&
+             whole(a.dgate, a.lddgate, a.tc) && whole(a.dscale, a.lddscale, a.tc) && whole(a.dshift, a.lddshift, a.tc);
+  if ((e = launch_rows(g, vec, true, st)) != cudaSuccess) return e;
+  const int strips = (a.d + 31) / 32;
+  if (a.mode == kSumGroups && a.pieces > 1 &&
+      (e = row_launch(k_residual_join_groups, dim3((unsigned)((int64_t)a.groups * strips)), 256, 0, 1, st, g, strips)) != cudaSuccess)
+    return e;
+  const bool any = a.dw || a.db || a.dwp || (a.mode == kSumAll && (a.dgate || a.dscale || a.dshift));
+  return any ? row_launch(k_residual_join, dim3((unsigned)strips), kJoinWarps * 32, 0, 1, st, g) : cudaSuccess;
+}
+
+}  // namespace sds

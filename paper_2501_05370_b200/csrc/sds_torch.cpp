@@ -470,9 +470,212 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------------------------
+// dropout
+// ---------------------------------------------------------------------------------------------
+
+double real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw PythonError{};
+  return v;
+}
+
+// a[0..3] = p, seed, step (a number, or an int32 tensor of one element on x's device), row0
+sds_dropout_spec dropout_of(PyObject* const* a, const at::Tensor& x) {
+  sds_dropout_spec s{};
+  s.p = real(a[0]);
+  s.seed = PyLong_AsUnsignedLongLong(a[1]);
+  if (s.seed == (uint64_t)-1 && PyErr_Occurred()) {
+    if (PyErr_ExceptionMatches(PyExc_TypeError)) throw PythonError{};
+    PyErr_Clear();
+    throw BadArgument("seed must be in [0, 2^64)");
+  }
+  if (THPVariable_Check(a[2])) {
+    const at::Tensor& t = THPVariable_Unpack(a[2]);
+    require(t.scalar_type() == at::kInt && t.numel() == 1 && t.device() == x.device(),
+            "step must be a number or an int32 tensor of one element on x's device");
+    s.step_dev = t.data_ptr<int32_t>();
+  } else {
+    const int64_t step = integer(a[2]);
+    require(step >= 0 && step <= INT32_MAX, "step must be in [0, 2^31)");
+    s.step = (int32_t)step;
+  }
+  s.row0 = integer(a[3]);
+  require(s.p >= 0.0 && s.p <= 1.0, "p must be in [0, 1]");
+  require(s.row0 >= 0, "row0 must not be negative");
+  return s;
+}
+
+// (x, p, seed, step, row0, residual, out_dtype, out)
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const at::Tensor& x = tensor(a[0], "x");
+    const Rows r = rows_of(x, "x");
+    const sds_dropout_spec spec = dropout_of(a + 1, x);
+    const int tx = type_code(x.scalar_type());
+    at::ScalarType yt = dtype_or(a[6], x.scalar_type());
+    const void* residual = nullptr;
+    int64_t ldr = 0;
+    if (a[5] != Py_None) {
+      const at::Tensor& v = tensor(a[5], "residual");
+      require(v.sizes() == x.sizes() && v.device() == x.device(), "residual must have x's shape and device");
+      yt = v.scalar_type();
+      ldr = rows_of(v, "residual").ld;
+      residual = v.data_ptr();
+    }
+    const int ty = type_code(yt);
+    warn_unrecorded("dropout", {a[0], a[5]});
+    const c10::cuda::CUDAGuard guard(x.device());
+    int64_t ldy = 0;
+    const at::Tensor y = output(a[7], x, yt, &ldy);
+    check(sds_dropout(&spec, x.data_ptr(), r.ld, tx, r.rows, (int32_t)r.d, residual, ldr, y.data_ptr(), ldy, ty,
+                      c10::cuda::getCurrentCUDAStream(x.get_device()).stream()),
+          "sds_dropout");
+    return wrap(y);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// residual norm
+// ---------------------------------------------------------------------------------------------
+
+struct ResidualNorm {
+  sds_residual_norm_op op;
+  Rows r;
+  at::ScalarType w_type, c_type;
+  const at::Tensor* cond[3];                       // gate, scale, shift
+  const at::Tensor* h;
+  int64_t ldh;
+};
+// a[0..13] = weight, bias, scale, shift, gate, post, post_weight, rms, alpha, eps, p, seed, step, row0
+ResidualNorm residual_norm_of(const at::Tensor& r, PyObject* h, at::ScalarType n_type, PyObject* const* a) {
+  ResidualNorm s{};
+  s.r = rows_of(r, "r");
+  const int64_t d = s.r.d;
+  sds_residual_norm_op& op = s.op;
+  op.rows = s.r.rows; op.d = (int32_t)d; op.groups = 1;
+  op.r_dtype = type_code(r.scalar_type()); op.h_dtype = type_code(n_type);
+  if (h != Py_None) {
+    s.h = &tensor(h, "h");
+    require(s.h->sizes() == r.sizes() && s.h->device() == r.device() && s.h->scalar_type() == n_type,
+            "h must have r's shape and device and the type of n");
+    s.ldh = rows_of(*s.h, "h").ld;
+  }
+  op.post = truth(a[5]);
+  const struct { PyObject* o; const char* name; const void** to; } vectors[3] = {
+      {a[0], "weight", &op.w_dev}, {a[1], "bias", &op.b_dev}, {a[6], "post_weight", &op.post_w_dev}};
+  s.w_type = at::kFloat;
+  bool first = true;
+  for (const auto& v : vectors) {
+    at::ScalarType t = s.w_type;
+    *v.to = vector_of(v.o, d, r, v.name, &t);
+    if (!*v.to) continue;
+    require(first || t == s.w_type, "weight, bias and post_weight must have the same type");
+    s.w_type = t;
+    first = false;
+  }
+  require(op.post || !op.post_w_dev, "post_weight needs post=True");
+  op.w_dtype = type_code(s.w_type);
+  const struct { PyObject* o; const char* name; const void** to; int64_t* ld; } conds[3] = {
+      {a[4], "gate", &op.gate_dev, &op.ld_gate}, {a[2], "scale", &op.scale_dev, &op.ld_scale}, {a[3], "shift", &op.shift_dev, &op.ld_shift}};
+  s.c_type = at::kFloat;
+  first = true;
+  for (int k = 0; k < 3; ++k) {
+    if (conds[k].o == Py_None) continue;
+    const at::Tensor& t = tensor(conds[k].o, conds[k].name);
+    const Rows g = rows_of(t, conds[k].name);
+    require(t.device() == r.device() && g.d == d && g.rows > 0 && (first || (g.rows == op.groups && t.scalar_type() == s.c_type)),
+            "gate, scale and shift must be [groups, d] tensors of one type on r's device, with r's last size");
+    op.groups = g.rows;
+    *conds[k].to = t.data_ptr();
+    *conds[k].ld = g.ld;
+    s.c_type = t.scalar_type();
+    s.cond[k] = &t;
+    first = false;
+  }
+  require(op.rows % op.groups == 0, "the rows of r must be a multiple of the rows of gate, scale and shift");
+  require(s.h || (!s.cond[0] && !op.post), "gate and post need h");
+  op.cond_dtype = type_code(s.c_type);
+  op.kind = truth(a[7]) ? SDS_NORM_RMS : SDS_NORM_LAYER;
+  op.alpha = (float)real(a[8]);
+  op.eps = (float)real(a[9]);
+  op.drop = dropout_of(a + 10, r);
+  require(s.h || op.drop.p == 0.0, "dropout needs h");
+  return s;
+}
+
+// (r, h, [14 of residual_norm_of], out_dtype, keep, out, stream_out)
+PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 20, [&]() -> PyObject* {
+    const at::Tensor& r = tensor(a[0], "r");
+    const at::ScalarType other = a[1] == Py_None ? r.scalar_type() : tensor(a[1], "h").scalar_type();
+    const at::ScalarType nt = dtype_or(a[16], other);
+    const ResidualNorm s = residual_norm_of(r, a[1], nt, a + 2);
+    const bool keep = truth(a[17]);
+    warn_unrecorded("residual_norm", {a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[8]});
+    sds_residual_norm_sizes sizes;
+    check(sds_residual_norm_bytes(&s.op, &sizes), "sds_residual_norm_bytes");
+    const c10::cuda::CUDAGuard guard(r.device());
+    int64_t ldn = 0, ldo = 0;
+    const at::Tensor y = output(a[18], r, nt, &ldn);
+    at::Tensor out, kept;
+    if (s.h) out = output(a[19], r, r.scalar_type(), &ldo);
+    else require(a[19] == Py_None, "stream_out needs h");
+    if (keep) kept = empty({6, s.r.rows}, at::kFloat, r);
+    check(sds_residual_norm(&s.op, r.data_ptr(), s.r.ld, s.h ? s.h->data_ptr() : nullptr, s.ldh, ptr(out), ldo, y.data_ptr(), ldn,
+                            static_cast<float*>(ptr(kept)), c10::cuda::getCurrentCUDAStream(r.get_device()).stream()),
+          "sds_residual_norm");
+    const at::Tensor& stream = s.h ? out : r;
+    return keep ? tuple({stream, y, kept}) : tuple({stream, y});
+  });
+}
+
+// (dn, dr, r, h, kept, [14 of residual_norm_of], want, workspace)
+PyObject* residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 21, [&]() -> PyObject* {
+    const at::Tensor &dn = tensor(a[0], "dn"), &r = tensor(a[2], "r"), &kept = tensor(a[4], "kept");
+    const ResidualNorm s = residual_norm_of(r, a[3], dn.scalar_type(), a + 5);
+    require(dn.sizes() == r.sizes() && dn.device() == r.device(), "dn must have r's shape and device");
+    const int64_t lddn = rows_of(dn, "dn").ld;
+    const void* dout = nullptr;
+    int64_t lddout = 0;
+    if (a[1] != Py_None) {
+      const at::Tensor& v = tensor(a[1], "dr");
+      require(v.sizes() == r.sizes() && v.device() == r.device() && v.scalar_type() == r.scalar_type(), "dr must have r's shape, type and device");
+      lddout = rows_of(v, "dr").ld;
+      dout = v.data_ptr();
+    }
+    require(kept.scalar_type() == at::kFloat && kept.is_contiguous() && kept.device() == r.device() && kept.numel() == 6 * s.r.rows,
+            "kept must be what residual_norm(keep=True) returned for these sizes");
+    sds_residual_norm_sizes sizes;
+    check(sds_residual_norm_bytes(&s.op, &sizes), "sds_residual_norm_bytes");
+    const c10::cuda::CUDAGuard guard(r.device());
+    // dr, dh, dweight, dbias, dscale, dshift, dgate, dpost_weight
+    at::Tensor g[8];
+    PyObject* want = a[19];
+    if (wanted(want, 0, 8)) g[0] = empty(r.sizes(), r.scalar_type(), r);
+    if (wanted(want, 1, 8) && s.h) g[1] = empty(r.sizes(), dn.scalar_type(), r);
+    if (wanted(want, 2, 8) && s.op.w_dev) g[2] = empty({s.r.d}, s.w_type, r);
+    if (wanted(want, 3, 8) && s.op.b_dev) g[3] = empty({s.r.d}, s.w_type, r);
+    const int at[3] = {6, 4, 5};                   // of gate, scale, shift
+    for (int k = 0; k < 3; ++k)
+      if (wanted(want, at[k], 8) && s.cond[k]) g[at[k]] = empty(s.cond[k]->sizes(), s.c_type, r);
+    if (wanted(want, 7, 8) && s.op.post_w_dev) g[7] = empty({s.r.d}, s.w_type, r);
+    const int64_t d = s.r.d;
+    const sds_residual_norm_grads grads{ptr(g[0]), d, ptr(g[1]), d, ptr(g[2]), ptr(g[3]), ptr(g[7]), ptr(g[6]), ptr(g[4]), ptr(g[5]), d, d, d};
+    const at::Tensor ws = workspace(a[20], sizes.backward_bytes, r);
+    check(sds_residual_norm_backward(&s.op, dn.data_ptr(), lddn, dout, lddout, r.data_ptr(), s.r.ld, s.h ? s.h->data_ptr() : nullptr, s.ldh,
+                                     kept.data_ptr<float>(), &grads, ws.data_ptr(), (size_t)ws.numel(),
+                                     c10::cuda::getCurrentCUDAStream(r.get_device()).stream()),
+          "sds_residual_norm_backward");
+    return tuple({g[0], g[1], g[2], g[3], g[4], g[5], g[6], g[7]});
+  });
+}
+
 #define SDS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SDS_METHOD(layer_norm), SDS_METHOD(layer_norm_backward), SDS_METHOD(gated_ffn),
-                         SDS_METHOD(gated_ffn_backward), SDS_METHOD(linear), SDS_METHOD(linear_backward), {nullptr, nullptr, 0, nullptr}};
+                         SDS_METHOD(gated_ffn_backward), SDS_METHOD(linear), SDS_METHOD(linear_backward),
+                         SDS_METHOD(dropout), SDS_METHOD(residual_norm), SDS_METHOD(residual_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sds_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

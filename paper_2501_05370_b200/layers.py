@@ -1,5 +1,5 @@
-"""Layer operators of denoisers on torch CUDA tensors: layer norm, the gated feed-forward block and the linear layer with its
-epilogue, each with its backward pass (include/sds.h documents the formulas). Every call enqueues on the current stream of its
+"""Layer operators of denoisers on torch CUDA tensors: layer norm, the gated feed-forward block, the linear layer with its
+epilogue, dropout, and the norms around a residual block with its gate, each with its backward pass (include/sds.h documents the formulas). Every call enqueues on the current stream of its
 tensors' device and does not wait. Outputs and workspaces are allocated by torch unless they are passed in. A bad
 argument raises ValueError, an error of the library SdsError. Nothing is recorded for autograd: the backward calls are
 the gradients. A forward call whose inputs require gradients (or carry forward-mode tangents) outside torch.no_grad()
@@ -136,3 +136,57 @@ def linear_backward(dy, x, weight, kept, *, bias=None, table=None, step=None, wa
 def linear_status(workspace=None) -> None:
     """gated_ffn_status for linear and linear_backward."""
     _wait_status("sds_linear", workspace)
+
+
+# ---------------------------------------------------------------------------------------------
+# dropout
+# ---------------------------------------------------------------------------------------------
+
+
+def dropout(x, p: float, seed: int, step=0, *, residual=None, row0: int = 0, out=None):
+    """sds_dropout: D x + residual with D = 0 or 1 / (1 - p) (p rounded to a multiple of 2^-16), drawn from (seed, step, row,
+    column) and never stored. step: the training step, a number or an int32 CUDA tensor of one element (read when the kernel
+    runs: a captured graph draws anew); row0: global number of x's first row. The output has the residual's type, x's without one."""
+    return (_native or _ext()).dropout(x, p, seed, step, row0, residual, None, out)
+
+
+def dropout_backward(dy, p: float, seed: int, step=0, *, row0: int = 0, out_dtype=None, out=None):
+    """The gradient of dropout's x: D dy with the forward call's p, seed, step and row0. out_dtype: x's type, where it is not
+    dy's. The residual's gradient is dy."""
+    return (_native or _ext()).dropout(dy, p, seed, step, row0, None, out_dtype, out)
+
+
+# ---------------------------------------------------------------------------------------------
+# residual norm
+# ---------------------------------------------------------------------------------------------
+
+NORMS = ("layer", "rms")
+
+
+def _rms(kind: str) -> bool:
+    if kind not in NORMS:
+        raise ValueError(f"kind must be one of {NORMS}")
+    return kind == "rms"
+
+
+def residual_norm(r, h=None, *, weight=None, bias=None, scale=None, shift=None, gate=None, post: bool = False, post_weight=None,
+                  kind: str = "layer", alpha: float = 1.0, eps: float = 1e-5, p: float = 0.0, seed: int = 0, step=0, row0: int = 0,
+                  out_dtype=None, keep: bool = False, out=None, stream_out=None):
+    """sds_residual_norm: from one residual block to the next. For the stream r [..., d] and the block's output h:
+    q = post_weight * norm(h) with post=True, else h;  stream = r + alpha gate dropout(q);  n = (norm(stream) weight + bias) (1 + scale) + shift.
+    kind "layer" or "rms" (both norms); gate, scale and shift [groups, d] (slices of one tensor will do), each row of them for
+    rows / groups consecutive rows of r; p, seed, step and row0 as for dropout. Without h there is no block behind: n is that of r. n has
+    h's type (out_dtype without h): r's, or for a float r any of the three. Returns (stream, n), with keep=True
+    (stream, n, kept) with what residual_norm_backward needs; without h the stream is r itself."""
+    return (_native or _ext()).residual_norm(r, h, weight, bias, scale, shift, gate, post, post_weight, _rms(kind), alpha, eps, p, seed,
+                                             step, row0, out_dtype, keep, out, stream_out)
+
+
+def residual_norm_backward(dn, dr, r, h, kept, *, weight=None, bias=None, scale=None, shift=None, gate=None, post: bool = False,
+                           post_weight=None, kind: str = "layer", alpha: float = 1.0, p: float = 0.0, seed: int = 0, step=0,
+                           row0: int = 0, want=(True,) * 8, workspace=None):
+    """sds_residual_norm_backward: (dr, dh, dweight, dbias, dscale, dshift, dgate, dpost_weight) from dn, the stream's own gradient dr
+    (None = zeros) and the forward call's arguments. want: which of the eight to compute; None is returned for the others and
+    for what there was not."""
+    return (_native or _ext()).residual_norm_backward(dn, dr, r, h, kept, weight, bias, scale, shift, gate, post, post_weight, _rms(kind),
+                                                      alpha, 0.0, p, seed, step, row0, want, workspace)
