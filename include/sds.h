@@ -481,8 +481,8 @@ int sds_selftest_gated_ffn_wait(int32_t polls, void* workspace_dev, void* cuda_s
  * row whose step is not in [0, steps) becomes NaN. act one of SDS_ACT_*. Products and all that is added to them are held in
  * float and rounded once, to y_dtype. k and ldx multiples of 8, x_dev and w_dev 16-byte aligned, steps <= 65535 (else
  * SDS_EUNSUPPORTED); n, ldy and ldr are free, and the other arrays aligned to their elements (rows of whole 16-byte pieces are faster).
- * residual_dev may be y_dev (same rows). keep_dev: what the backward pass needs of the forward one (act'(z), rounded to
- * f16), 256-byte aligned, keep_bytes (0 without an activation, where NULL will do); NULL = no backward pass will follow.
+ * residual_dev may be y_dev (same rows). keep_dev: what the backward pass needs of the forward one (act'(z), in
+ * float), 256-byte aligned, keep_bytes (0 without an activation, where NULL will do); NULL = no backward pass will follow.
  * workspace_dev: 256-byte aligned, forward_bytes or backward_bytes. The result of a row may differ in the last bit with
  * the number of rows of the call. */
 #define SDS_ACT_NONE      3     /* g; sds_linear only */

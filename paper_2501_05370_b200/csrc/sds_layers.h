@@ -88,7 +88,7 @@ struct LinearArgs {
   const void* table; const int* step; int steps;
   const void* residual; int64_t ldr;           // of type ty, NULL = none
   void* y; int64_t ldy; int ty;                // SDS_F32 or the operands' type
-  uint16_t* factor;      // act'(z) [rows, n rounded up to 8] f16, or NULL
+  float* factor;         // act'(z) [rows, n rounded up to 8], or NULL
   // backward
   const void* dy; int64_t lddy;                // of type ty
   void* dx; int64_t lddx;                      // any of the four gradients may be NULL
@@ -98,7 +98,7 @@ struct LinearArgs {
 
 struct LinearWorkspace { size_t dz, db, dw, begin, list, table, bytes; };   // offsets of a backward call's parts, and their end
 LinearWorkspace linear_workspace(int64_t rows, int32_t k, int32_t n, int32_t nsteps, bool has_table);
-size_t linear_factor_bytes(int64_t rows, int32_t n);
+size_t linear_factor_bytes(int64_t rows, int32_t n);   // of act'
 cudaError_t launch_linear(const LinearArgs& a, cudaStream_t st);
 cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st);
 cudaError_t linear_gave_up(int* role, cudaStream_t st);

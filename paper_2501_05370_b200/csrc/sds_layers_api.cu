@@ -110,7 +110,7 @@ LinearArgs linear_args(const sds_linear_layer* l, const void* x, int64_t ldx, co
   a.bias = l->bias_dev; a.tbias = l->bias_dtype;
   a.table = l->table_dev; a.step = step; a.steps = l->steps;
   a.ty = y_dtype;
-  a.factor = static_cast<uint16_t*>(const_cast<void*>(keep));
+  a.factor = static_cast<float*>(const_cast<void*>(keep));
   a.err = static_cast<int*>(workspace);
   return a;
 }

@@ -5,10 +5,8 @@
 //
 // The products are those of sds_tiles.cuh: persistent tiles for batches, weights split over clusters for few rows. Bias, table
 // rows, activation and residual are applied to the accumulator, before its one rounding, so y is written once and z never.
-// For the backward pass the forward one keeps act'(z) as f16 (2 bytes per output): its values lie in [-0.2, 1.2], so that
-// the rounding is at most 2^-11 relative, against 2^-8 of dz as a bf16 operand of the products that follow (f16: the same size).
-// Keeping z itself would take as many bytes and the activation again; keeping a float would make a training step of
-// small k wait for memory.
+// For the backward pass the forward one keeps act'(z) as a float: in 16 bits it would add an error to every gradient as large as that
+// gradient's own rounding, and one a thousand times larger to a float db (2e-4 of it, against 2e-7).
 //
 // Backward: one pass over dy writes dz as operand and adds the columns for db (in float, of the unrounded dz); dx and dW
 // are one launch. The table's gradient is a sum over rows in the order of their steps: the rows of each step are listed
@@ -26,7 +24,7 @@ namespace {
 
 struct DzArgs {
   const void* dy;                                 // [rows, n] of tdy, rows lddy elements apart
-  const uint16_t* factor;                         // [rows, ldz] f16, NULL = ones
+  const float* factor;                            // [rows, ldz], NULL = ones
   uint16_t* dz;                                   // [rows, ldz] of the operands' type, NULL = not wanted
   float* part;                                    // [gridDim.y][n] column sums, NULL = not wanted
   void* db;                                       // with a single chunk of rows the sums go here at once
@@ -41,88 +39,101 @@ __device__ __forceinline__ void store_typed(void* p, int type, size_t i, float v
   else static_cast<uint16_t*>(p)[i] = round16(v, type == SDS_F16);
 }
 
-// A lane takes eight columns of every eighth row of its chunk (VEC: neighbours, in 16-byte accesses; else 32 columns apart).
-// Memory bound: 8192 x 2048 bf16 with its factors.
+// eight columns of a row of dy and of its factors, as they lie in memory
+template <bool F32> struct DzRow { uint4 y[F32 ? 2 : 1], f[2]; };
+template <bool F32, class A>
+__device__ __forceinline__ void dz_request(DzRow<F32>& r, const A& a, int64_t row, int c0) {
+  const char* y = static_cast<const char*>(a.dy) + ((size_t)row * a.lddy + c0) * (F32 ? 4 : 2);
+#pragma unroll
+  for (int i = 0; i < (F32 ? 2 : 1); ++i) r.y[i] = __ldg(reinterpret_cast<const uint4*>(y) + i);
+  if (a.factor)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r.f[i] = __ldg(reinterpret_cast<const uint4*>(a.factor + (size_t)row * a.ldz + c0) + i);
+}
+template <bool F32, class A>
+__device__ __forceinline__ void dz_values(const DzRow<F32>& r, const A& a, float (&v)[8]) {
+  if (F32) {
+    const uint32_t w[8] = {r.y[0].x, r.y[0].y, r.y[0].z, r.y[0].w, r.y[F32].x, r.y[F32].y, r.y[F32].z, r.y[F32].w};
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = __uint_as_float(w[u]);
+  } else {
+    const uint32_t w[4] = {r.y[0].x, r.y[0].y, r.y[0].z, r.y[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = unpack16x2(w[i], a.f16);
+      v[2 * i] = t.x; v[2 * i + 1] = t.y;
+    }
+  }
+  if (a.factor) {
+    const uint32_t w[8] = {r.f[0].x, r.f[0].y, r.f[0].z, r.f[0].w, r.f[1].x, r.f[1].y, r.f[1].z, r.f[1].w};
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] *= __uint_as_float(w[u]);
+  }
+}
+// the same for columns 32 apart, one by one
+template <class A>
+__device__ __forceinline__ void dz_scalar(const A& a, int64_t row, int c0, float (&v)[8]) {
+  float f[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int c = c0 + u * 32;
+    v[u] = c < a.n ? load_typed(a.dy, a.tdy, (size_t)row * a.lddy + c) : 0.f;
+    f[u] = a.factor && c < a.n ? a.factor[(size_t)row * a.ldz + c] : 1.f;
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) v[u] *= f[u];
+}
+
+// A lane takes eight columns of every eighth row of its chunk (VEC: neighbours, in 16-byte accesses; else 32 columns apart), four rows
+// requested ahead. Bound by memory.
 template <bool F32, bool VEC>
 __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
   __shared__ float sums[kDzWarps][kDzCols];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c0 = blockIdx.x * kDzCols + (VEC ? lane * 8 : lane);
-  constexpr int kStep = VEC ? 1 : 32;             // between a lane's columns
   float sum[8] = {};
-  const int stride = (int)gridDim.y * kDzWarps;
-  const auto load = [&](int row, float (&v)[8], float (&f)[8]) {
-    if (VEC) {
-      const bool in = c0 < a.n;
-      if (F32) {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.dy) + (size_t)row * a.lddy + c0);
-        const float4 lo = in ? __ldg(p) : make_float4(0.f, 0.f, 0.f, 0.f), hi = in ? __ldg(p + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
-        v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
-      } else {
-        const uint4 w = in ? __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.dy) + (size_t)row * a.lddy + c0))
-                           : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+  const int64_t stride = (int64_t)gridDim.y * kDzWarps, first = (int64_t)blockIdx.y * kDzWarps + warp;
+  if (VEC && c0 < a.n) {
+    constexpr int kAhead = 4;
+    DzRow<F32> ahead[kAhead];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 t = unpack16x2(q[i], a.f16);
-          v[2 * i] = t.x; v[2 * i + 1] = t.y;
-        }
-      }
-      if (a.factor) {
-        const uint4 w = in ? __ldg(reinterpret_cast<const uint4*>(a.factor + (size_t)row * a.ldz + c0)) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+    for (int i = 0; i < kAhead; ++i)
+      if (first + i * stride < a.rows) dz_request(ahead[i], a, first + i * stride, c0);
+    for (int64_t base = first; base < a.rows; base += kAhead * stride) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 t = unpack16x2(q[i], 1);
-          f[2 * i] = t.x; f[2 * i + 1] = t.y;
-        }
+      for (int i = 0; i < kAhead; ++i) {
+        const int64_t row = base + i * stride, next = row + kAhead * stride;
+        if (row >= a.rows) break;
+        float v[8];
+        dz_values(ahead[i], a, v);
+        if (next < a.rows) dz_request(ahead[i], a, next, c0);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum[u] += v[u];
+        if (a.dz)
+          *reinterpret_cast<uint4*>(a.dz + (size_t)row * a.ldz + c0) =
+              make_uint4(pack16(v[0], v[1], a.f16), pack16(v[2], v[3], a.f16), pack16(v[4], v[5], a.f16), pack16(v[6], v[7], a.f16));
       }
-    } else {
+    }
+  } else if (!VEC) {
+#pragma unroll 2
+    for (int64_t row = first; row < a.rows; row += stride) {
+      float v[8];
+      dz_scalar(a, row, c0, v);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int c = c0 + u * kStep;
-        v[u] = c < a.n ? load_typed(a.dy, a.tdy, (size_t)row * a.lddy + c) : 0.f;
-        if (a.factor) f[u] = c < a.n ? unpack16(a.factor[(size_t)row * a.ldz + c], 1) : 0.f;
+        sum[u] += v[u];
+        if (a.dz && c0 + u * 32 < a.n) a.dz[(size_t)row * a.ldz + c0 + u * 32] = round16(v[u], a.f16);
       }
-    }
-  };
-  const auto take = [&](int row, float (&v)[8], const float (&f)[8]) {
-    if (a.factor)
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] *= f[u];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) sum[u] += v[u];
-    if (!a.dz) return;
-    if (VEC) {
-      if (c0 < a.n)
-        *reinterpret_cast<uint4*>(a.dz + (size_t)row * a.ldz + c0) =
-            make_uint4(pack16(v[0], v[1], a.f16), pack16(v[2], v[3], a.f16), pack16(v[4], v[5], a.f16), pack16(v[6], v[7], a.f16));
-    } else {
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (c0 + u * kStep < a.n) a.dz[(size_t)row * a.ldz + c0 + u * kStep] = round16(v[u], a.f16);
-    }
-  };
-  constexpr int kAhead = 4;                       // rows requested before the first is used
-  for (int row = blockIdx.y * kDzWarps + warp; row < a.rows;) {
-    float v[kAhead][8], f[kAhead][8];
-    if (row <= a.rows - 1 - (kAhead - 1) * stride) {
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) load(row + i * stride, v[i], f[i]);
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) take(row + i * stride, v[i], f[i]);
-      if (row > a.rows - 1 - kAhead * stride) break;              // (before the sum below could pass 2^31)
-      row += kAhead * stride;
-    } else {
-      load(row, v[0], f[0]);
-      take(row, v[0], f[0]);
-      if (row > a.rows - 1 - stride) break;
-      row += stride;
     }
   }
   if (!a.part) return;
+  if (VEC) {
+    *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+  } else {
 #pragma unroll
-  for (int u = 0; u < 8; ++u) sums[warp][VEC ? lane * 8 + u : lane + u * 32] = sum[u];
+    for (int u = 0; u < 8; ++u) sums[warp][lane + u * 32] = sum[u];
+  }
   __syncthreads();
   const int c = blockIdx.x * kDzCols + threadIdx.x;
   if (c >= a.n) return;
@@ -151,10 +162,10 @@ __global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks
   }
 }
 
-// Chunks of rows: four rows for every warp, until there are eight CTAs for each SM.
+// Chunks of rows: four rows for every warp, until there are two CTAs for each SM (which hold 96 KB of requests between them).
 int dz_chunks(int64_t rows, int32_t n) {
   const int64_t cols = (n + kDzCols - 1) / kDzCols;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 4 * kDzWarps - 1) / (4 * kDzWarps), (8 * 148 + cols - 1) / cols));
+  return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 4 * kDzWarps - 1) / (4 * kDzWarps), 2 * 148 / cols));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -165,183 +176,174 @@ struct TableArgs {
   const int* step;                                // [rows]
   int* begin;                                     // [steps + 1] where a step's rows begin in the list
   int* list;                                      // [rows] rows in the order of their steps; those outside the table are left out
-  const void* dy; const uint16_t* factor;         // as in DzArgs
+  int* list_step;                                 // [rows] the steps, in the same order
+  const void* dy; const float* factor;            // as in DzArgs
   float* part;                                    // [slices][2][n] sums of runs that cross a slice's begin, its end
   uint16_t* dtable;                               // [steps, n] of the operands' type
   int64_t lddy, ldz;
   int tdy, rows, n, steps, f16;
-  int slice, slices;                              // list entries of a warp; warps' worth of the longest list
 };
 
-constexpr int kListThreads = 256;
+constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
+constexpr int kSlice = 32;                        // list entries of a warp of k_table_sum: one in each lane
 
-// One CTA per step: how many rows have smaller steps, then its own rows in ascending order. Every CTA reads all of `step`,
-// twice, from L2: 250 steps over 8192 rows are 16 MB.
+// One CTA per step: how many rows have smaller steps, then its own rows in ascending order, a warp for every sixteenth of the rows. Every
+// CTA reads all of `step`, twice, from L2 and L1: 250 steps over 8192 rows are 8 MB.
 __global__ void __launch_bounds__(kListThreads) k_table_list(const TableArgs a) {
-  __shared__ int below[kListThreads / 32], counts[kListThreads / 32];
-  __shared__ int base;
+  __shared__ int less[kListWarps], same[kListWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.x;
-  int less = 0;
-  for (int64_t r = threadIdx.x; r < a.rows; r += kListThreads) {
-    const int v = __ldg(a.step + r);
-    less += v >= 0 && v < s;
-  }
+  const int64_t share = ((int64_t)a.rows + kListThreads - 1) / kListThreads * 32;
+  const int64_t r0 = warp * share, r1 = min((int64_t)a.rows, r0 + share);
+  constexpr int kAhead = 8;
+  int nless = 0, nsame = 0;
+  for (int64_t r = r0 + lane; r < r1; r += 32 * kAhead) {
+    int v[kAhead];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) less += __shfl_xor_sync(0xffffffffu, less, o);
-  if (lane == 0) below[warp] = less;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    int t = 0;
-    for (int w = 0; w < kListThreads / 32; ++w) t += below[w];
-    base = t;
-    a.begin[s] = t;
-  }
-  __syncthreads();
-  int at = base;
-  for (int64_t r0 = 0; r0 < a.rows; r0 += kListThreads) {
-    const int64_t r = r0 + threadIdx.x;
-    const bool mine = r < a.rows && __ldg(a.step + r) == s;
-    const uint32_t votes = __ballot_sync(0xffffffffu, mine);
-    if (lane == 0) counts[warp] = __popc(votes);
-    __syncthreads();
-    int before = 0, all = 0;
+    for (int i = 0; i < kAhead; ++i) v[i] = r + 32 * i < r1 ? __ldg(a.step + r + 32 * i) : -1;
 #pragma unroll
-    for (int w = 0; w < kListThreads / 32; ++w) {
-      if (w < warp) before += counts[w];
-      all += counts[w];
+    for (int i = 0; i < kAhead; ++i) {
+      nless += v[i] >= 0 && v[i] < s;
+      nsame += v[i] == s;
     }
-    if (mine) a.list[at + before + __popc(votes & ((1u << lane) - 1u))] = (int)r;
-    at += all;
-    __syncthreads();
   }
-  if (s == a.steps - 1 && threadIdx.x == 0) a.begin[a.steps] = at;
-}
-
-// the last step that begins at or before entry i of the list (i < its length, so that step has rows)
-__device__ __forceinline__ int step_of(const int* begin, int steps, int i) {
-  int lo = 0, hi = steps;                         // begin[lo] <= i < begin[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (begin[mid] <= i) lo = mid; else hi = mid;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    nless += __shfl_xor_sync(0xffffffffu, nless, o);
+    nsame += __shfl_xor_sync(0xffffffffu, nsame, o);
   }
-  return lo;
+  if (lane == 0) { less[warp] = nless; same[warp] = nsame; }
+  __syncthreads();
+  int base = 0, at = 0, all = 0;
+  for (int w = 0; w < kListWarps; ++w) {
+    base += less[w];
+    if (w < warp) at += same[w];
+    all += same[w];
+  }
+  if (threadIdx.x == 0) {
+    a.begin[s] = base;
+    if (s == a.steps - 1) a.begin[a.steps] = base + all;
+  }
+  if (nsame == 0) return;
+  at += base;
+  for (int64_t r = r0; r < r1; r += 32 * kAhead) {
+    int v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) v[i] = r + 32 * i + lane < r1 ? __ldg(a.step + r + 32 * i + lane) : -1;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t votes = __ballot_sync(0xffffffffu, v[i] == s);
+      if (v[i] == s) {
+        const int to = at + __popc(votes & ((1u << lane) - 1u));
+        a.list[to] = (int)(r + 32 * i + lane);
+        a.list_step[to] = s;
+      }
+      at += __popc(votes);
+    }
+  }
 }
 
 constexpr int kTableThreads = 128, kTableWarps = kTableThreads / 32;
 
-// A warp adds `slice` entries of the list over 256 columns (VEC: eight neighbours per lane). A run of one step that lies inside
-// the slice is a finished row of the gradient; the others are parts for k_table_join.
+// A warp adds the rows of a slice of the list over 256 columns (VEC: eight neighbours per lane), four rows requested ahead. A run of one
+// step that begins and ends in the slice is a finished row of the gradient; the others are parts for k_table_join.
 template <bool F32, bool VEC>
 __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) {
   const int lane = threadIdx.x & 31;
   const int64_t sl = (int64_t)blockIdx.y * kTableWarps + (threadIdx.x >> 5);
   const int total = a.begin[a.steps];
-  if (sl * a.slice >= total) return;
-  const int i0 = (int)(sl * a.slice), i1 = (int)min((int64_t)total, (sl + 1) * a.slice);
+  if (sl * kSlice >= total) return;
+  const int i0 = (int)(sl * kSlice), count = min(kSlice, total - i0);
   const int c0 = blockIdx.x * 256 + (VEC ? lane * 8 : lane);
+  const bool live = c0 < a.n;
   constexpr int kStep = VEC ? 1 : 32;
+  const int my_row = lane < count ? __ldg(a.list + i0 + lane) : 0, my_step = lane < count ? __ldg(a.list_step + i0 + lane) : -1;
+  const int step_before = i0 > 0 ? __ldg(a.list_step + i0 - 1) : -1, step_after = i0 + count < total ? __ldg(a.list_step + i0 + count) : -1;
   float sum[8] = {};
-  int s = step_of(a.begin, a.steps, i0);
-  int from = a.begin[s], end = a.begin[s + 1];
-  const auto flush = [&]() {
-    if (from >= i0 && end <= i1) {
-      uint16_t* out = a.dtable + (size_t)s * a.n;
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (c0 + u * kStep < a.n) out[c0 + u * kStep] = round16(sum[u], a.f16);
-    } else {
-      float* out = a.part + ((size_t)sl * 2 + (from >= i0 ? 1 : 0)) * a.n;
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (c0 + u * kStep < a.n) out[c0 + u * kStep] = sum[u];
-    }
-  };
-  constexpr int kAhead = 4;
-  for (int i = i0; i < i1; i += kAhead) {
-    float v[kAhead][8];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (i + k >= i1) break;
-      const int row = __ldg(a.list + i + k);
+  const auto flush = [&](int s, bool whole) {     // the run of step s that ends here
+    if (whole) {
+      uint16_t* out = a.dtable + (size_t)s * a.n + c0;
       if (VEC) {
-        float f[8];
-        const bool in = c0 < a.n;
-        if (F32) {
-          const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.dy) + (size_t)row * a.lddy + c0);
-          const float4 lo = in ? __ldg(p) : make_float4(0.f, 0.f, 0.f, 0.f), hi = in ? __ldg(p + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
-          v[k][0] = lo.x; v[k][1] = lo.y; v[k][2] = lo.z; v[k][3] = lo.w; v[k][4] = hi.x; v[k][5] = hi.y; v[k][6] = hi.z; v[k][7] = hi.w;
-        } else {
-          const uint4 w = in ? __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.dy) + (size_t)row * a.lddy + c0))
-                             : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float2 t = unpack16x2(q[u], a.f16);
-            v[k][2 * u] = t.x; v[k][2 * u + 1] = t.y;
-          }
-        }
-        if (a.factor) {
-          const uint4 w = in ? __ldg(reinterpret_cast<const uint4*>(a.factor + (size_t)row * a.ldz + c0)) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float2 t = unpack16x2(q[u], 1);
-            f[2 * u] = t.x; f[2 * u + 1] = t.y;
-          }
-#pragma unroll
-          for (int u = 0; u < 8; ++u) v[k][u] *= f[u];
-        }
+        if (live)
+          *reinterpret_cast<uint4*>(out) = make_uint4(pack16(sum[0], sum[1], a.f16), pack16(sum[2], sum[3], a.f16),
+                                                      pack16(sum[4], sum[5], a.f16), pack16(sum[6], sum[7], a.f16));
       } else {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int c = c0 + u * kStep;
-          v[k][u] = c < a.n ? load_typed(a.dy, a.tdy, (size_t)row * a.lddy + c) : 0.f;
-          if (a.factor && c < a.n) v[k][u] *= unpack16(a.factor[(size_t)row * a.ldz + c], 1);
-        }
+        for (int u = 0; u < 8; ++u)
+          if (c0 + u * kStep < a.n) out[u * kStep] = round16(sum[u], a.f16);
       }
+    } else {
+      float* out = a.part + ((size_t)sl * 2 + (s == step_before ? 0 : 1)) * a.n + c0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (c0 + u * kStep < a.n) out[u * kStep] = sum[u];
     }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum[u] = 0.f;
+  };
+  constexpr int kAhead = 4;
+  DzRow<F32> ahead[kAhead];
+  int first_row[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) first_row[k] = __shfl_sync(0xffffffffu, my_row, min(k, count - 1));
+  if (VEC && live)
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) dz_request(ahead[k], a, first_row[k], c0);
+  int step = __shfl_sync(0xffffffffu, my_step, 0);
+  for (int i = 0; i < kSlice; i += kAhead) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (i + k >= i1) break;
-      if (i + k >= end) {                         // the next step that has rows
-        flush();
-#pragma unroll
-        for (int u = 0; u < 8; ++u) sum[u] = 0.f;
-        do { ++s; end = a.begin[s + 1]; } while (end <= i + k);
-        from = a.begin[s];
+      if (i + k >= count) break;
+      const int s = __shfl_sync(0xffffffffu, my_step, i + k), row = __shfl_sync(0xffffffffu, my_row, i + k);
+      const int next = __shfl_sync(0xffffffffu, my_row, min(i + k + kAhead, count - 1));
+      if (s != step) {
+        flush(step, step != step_before);
+        step = s;
       }
+      float v[8];
+      if (VEC) {
+        if (live) {
+          dz_values(ahead[k], a, v);
+          if (i + k + kAhead < count) dz_request(ahead[k], a, next, c0);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum[u] += v[k][u];
+          for (int u = 0; u < 8; ++u) sum[u] += v[u];
+        }
+      } else {
+        dz_scalar(a, row, c0, v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum[u] += v[u];
+      }
     }
   }
-  flush();
+  flush(step, step != step_before && step != step_after);
 }
 
-// One CTA per step and 256 columns: zeros for a step without rows, the sums of a run that crosses slices.
+// The sums of a run that crosses slices, and zeros for a step without rows. A CTA takes one step and 256 / W columns, a warp of W for
+// the same columns every W-th slice: W = 1 where there are CTAs enough, else 8 (few steps have long runs).
+template <int W>
 __global__ void __launch_bounds__(256) k_table_join(const TableArgs a) {
-  const int s = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
+  __shared__ float sums[W][256 / W];
+  const int s = blockIdx.y, x = threadIdx.x % (256 / W), w = threadIdx.x / (256 / W), c = blockIdx.x * (256 / W) + x;
   const int from = a.begin[s], end = a.begin[s + 1];
-  if (c >= a.n) return;
+  const int first = from / kSlice, last = (end - 1) / kSlice;
+  if (from < end && first == last) return;        // written by the slice's warp
   float sum = 0.f;
-  if (from < end) {
-    const int first = from / a.slice, last = (end - 1) / a.slice;
-    if (first == last) return;                    // written by the slice's warp
-    sum = a.part[((size_t)first * 2 + 1) * a.n + c];
-#pragma unroll 4
-    for (int i = first + 1; i <= last; ++i) sum += a.part[(size_t)i * 2 * a.n + c];
+  if (from < end && c < a.n) {
+    if (w == 0) sum = a.part[((size_t)first * 2 + 1) * a.n + c];
+#pragma unroll 8
+    for (int i = first + 1 + w; i <= last; i += W) sum += a.part[(size_t)i * 2 * a.n + c];
   }
-  a.dtable[(size_t)s * a.n + c] = round16(sum, a.f16);
+  if (W > 1) {
+    sums[w][x] = sum;
+    __syncthreads();
+    if (w > 0) return;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) sum += sums[i][x];
+  }
+  if (c < a.n) a.dtable[(size_t)s * a.n + c] = round16(sum, a.f16);
 }
 
-// List entries of a warp: 32, or more where that makes over four times as many warps as the machine holds.
-int table_slice(int64_t rows, int32_t n) {
-  const int64_t cols = (n + 255) / 256, most = 4 * 148 * 48;
-  return (int)std::max<int64_t>(32, (rows * cols + most - 1) / most);
-}
-int64_t table_slices(int64_t rows, int32_t n) {
-  const int s = table_slice(rows, n);
-  return (rows + s - 1) / s;
-}
+int64_t table_slices(int64_t rows) { return (rows + kSlice - 1) / kSlice; }
 
 inline size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 inline bool whole(const void* p, int64_t ld, size_t bytes) {      // rows of whole 16-byte pieces
@@ -384,21 +386,43 @@ cudaError_t linear_gave_up(int* role, cudaStream_t st) {
   return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
 }
 
-size_t linear_factor_bytes(int64_t rows, int32_t n) { return (size_t)rows * round_up(n, 8) * 2; }
+size_t linear_factor_bytes(int64_t rows, int32_t n) { return (size_t)rows * round_up(n, 8) * 4; }
 
 LinearWorkspace linear_workspace(int64_t rows, int32_t k, int32_t n, int32_t nsteps, bool has_table) {
   LinearWorkspace w{};
   size_t at = 256;                                // the status word
   const auto take = [&](size_t bytes) { const size_t o = at; at = round_up(at + bytes, 256); return o; };
-  w.dz = take(linear_factor_bytes(rows, n));
+  w.dz = take((size_t)rows * round_up(n, 8) * 2);
   w.db = take(rows > 0 ? (size_t)dz_chunks(rows, n) * n * 4 : 0);
   w.dw = take(rows > 0 ? part_floats(n, k, linear_parts(rows, k, n)) * 4 : 0);
   w.begin = take(has_table ? ((size_t)nsteps + 1) * 4 : 0);
-  w.list = take(has_table ? (size_t)rows * 4 : 0);
-  w.table = take(has_table && rows > 0 ? (size_t)table_slices(rows, n) * 2 * n * 4 : 0);
+  w.list = take(has_table ? (size_t)rows * 8 : 0);
+  w.table = take(has_table ? (size_t)table_slices(rows) * 2 * n * 4 : 0);
   w.bytes = at;
   return w;
 }
+
+namespace {
+
+template <int EPI>
+cudaError_t forward(const LinearArgs& a, const FfnArgs& f, const LinearEpilogue& e, cudaStream_t st) {
+  if (prefer_split<EPI>(a.rows, a.n, steps(a.k))) {
+    SplitSpec s{};
+    s.w[0] = {a.w, a.k}; s.t[0] = {a.x, a.ldx};
+    s.nseg = 1; s.N = a.n; s.K = a.k; s.out = a.y; s.ldo = a.ldy;
+    return launch_split<EPI>(f, s, nullptr, true, st, &e);
+  }
+  ProductSpec s{};
+  s.a[0] = {a.x, a.ldx}; s.b[0] = {a.w, a.k};
+  s.nseg = 1; s.M = a.rows; s.N = a.n; s.K = a.k; s.out = a.y; s.ldo = a.ldy;
+  // The epilogue has more to do than the feed-forward block's, and a tile of few steps ends sooner: eight warps up to 64 steps of K,
+  // four beyond. Four and eight: 8192 x 2048 x 2048 with SiLU, bias and table 75.8 and 68.5 us, with GELU 87.6 and 72.2, 1037 x 1000 x 2731
+  // with GELU 30.9 and 25.6; 16384 x 8192 x 2048 392 and 405, with a float residual 474 and 486.
+  if (steps(a.k) <= 64) return launch_tiles<EPI, false, false, 8>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
+  return launch_tiles<EPI, false>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
+}
+
+}  // namespace
 
 cudaError_t launch_linear(const LinearArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaMemsetAsync(a.err, 0, sizeof(int), st);
@@ -410,20 +434,11 @@ cudaError_t launch_linear(const LinearArgs& a, cudaStream_t st) {
   e.factor = a.act == SDS_ACT_NONE ? nullptr : a.factor;
   e.ldf = (int64_t)round_up(a.n, 8);
   const size_t size = a.ty == SDS_F32 ? 4 : 2;
-  e.wide = (size_t)a.n * size % 16 == 0 && whole(a.y, a.ldy, size) && (!a.residual || whole(a.residual, a.ldr, size));
-  e.table_wide = a.n % 8 == 0 && whole(a.table, a.n, 2);
+  const bool wide = a.n % 8 == 0 && whole(a.y, a.ldy, size) && (!a.residual || whole(a.residual, a.ldr, size)) &&
+                    (!a.table || whole(a.table, a.n, 2));
   FfnArgs f{};
   f.rows = a.rows; f.f16 = a.f16; f.act = a.act; f.err = a.err;
-  if (prefer_split<kLinear>(a.rows, a.n, steps(a.k))) {
-    SplitSpec s{};
-    s.w[0] = {a.w, a.k}; s.t[0] = {a.x, a.ldx};
-    s.nseg = 1; s.N = a.n; s.K = a.k; s.out = a.y; s.ldo = a.ldy;
-    return launch_split<kLinear>(f, s, nullptr, true, st, &e);
-  }
-  ProductSpec s{};
-  s.a[0] = {a.x, a.ldx}; s.b[0] = {a.w, a.k};
-  s.nseg = 1; s.M = a.rows; s.N = a.n; s.K = a.k; s.out = a.y; s.ldo = a.ldy;
-  return launch_tiles<kLinear, false>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
+  return wide ? forward<kLinear>(a, f, e, st) : forward<kLinearNarrow>(a, f, e, st);
 }
 
 namespace {
@@ -458,7 +473,7 @@ cudaError_t launch_join(const float* part, uint16_t* out, int M, int N, int part
 cudaError_t launch_table(const TableArgs& t, bool vec, cudaStream_t st) {
   k_table_list<<<t.steps, kListThreads, 0, st>>>(t);
   const int cols = (t.n + 255) / 256;
-  const dim3 grid(cols, (t.slices + kTableWarps - 1) / kTableWarps);
+  const dim3 grid(cols, (unsigned)((table_slices(t.rows) + kTableWarps - 1) / kTableWarps));
   if (t.tdy == SDS_F32) {
     if (vec) k_table_sum<true, true><<<grid, kTableThreads, 0, st>>>(t);
     else k_table_sum<true, false><<<grid, kTableThreads, 0, st>>>(t);
@@ -466,7 +481,8 @@ cudaError_t launch_table(const TableArgs& t, bool vec, cudaStream_t st) {
     if (vec) k_table_sum<false, true><<<grid, kTableThreads, 0, st>>>(t);
     else k_table_sum<false, false><<<grid, kTableThreads, 0, st>>>(t);
   }
-  k_table_join<<<dim3(cols, t.steps), 256, 0, st>>>(t);
+  if ((int64_t)cols * t.steps >= 4 * 148) k_table_join<1><<<dim3(cols, t.steps), 256, 0, st>>>(t);
+  else k_table_join<8><<<dim3((t.n + 31) / 32, t.steps), 256, 0, st>>>(t);
   return cudaGetLastError();
 }
 
@@ -484,7 +500,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
   }
   char* ws = reinterpret_cast<char*>(a.err);
   const LinearWorkspace at = linear_workspace(a.rows, a.k, a.n, a.steps, a.dtable != nullptr);
-  const uint16_t* factor = a.act == SDS_ACT_NONE ? nullptr : a.factor;
+  const float* factor = a.act == SDS_ACT_NONE ? nullptr : a.factor;
   const int64_t ldz = (int64_t)round_up(a.n, 8);
   const size_t sy = a.ty == SDS_F32 ? 4 : 2;
   const bool vec = a.n % 8 == 0 && whole(a.dy, a.lddy, sy);
@@ -510,11 +526,11 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
     TableArgs t{};
     t.step = a.step;
     t.begin = reinterpret_cast<int*>(ws + at.begin); t.list = reinterpret_cast<int*>(ws + at.list);
+    t.list_step = t.list + a.rows;
     t.part = reinterpret_cast<float*>(ws + at.table);
     t.dy = a.dy; t.lddy = a.lddy; t.tdy = a.ty; t.factor = factor; t.ldz = ldz;
     t.dtable = static_cast<uint16_t*>(a.dtable);
     t.rows = a.rows; t.n = a.n; t.steps = a.steps; t.f16 = a.f16;
-    t.slice = table_slice(a.rows, a.n); t.slices = (int)table_slices(a.rows, a.n);
     if ((e = launch_table(t, vec, st)) != cudaSuccess) return e;
   }
   if (!products) return cudaMemsetAsync(a.err, 0, sizeof(int), st);

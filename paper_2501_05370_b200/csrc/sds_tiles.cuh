@@ -31,7 +31,9 @@ enum FfnEpi : int {
   kFfnAdd = 2,     // out (float) += acc
   kFfnDGlu = 3,    // accumulator holds dH: dG, dU
   kLinear = 4,     // out (16 bit or float) = act(acc + bias + table[step]) + residual, and the kept factor act'
+  kLinearNarrow = 5,  // the same where output, residual or table do not lie in whole 16-byte pieces
 };
+__host__ __device__ constexpr bool is_linear(int epi) { return epi == kLinear || epi == kLinearNarrow; }
 
 constexpr int kBM = 128;                          // rows of one CTA's accumulator
 constexpr int kBK = 64;                           // elements of K per stage: one 128-byte swizzle row
@@ -41,7 +43,7 @@ constexpr int kChunkBytes = 64 * kBK * 2;         // 64 x 64 elements
 // one's products. Measured at 16384 rows, d = 2048, f = 8192 in a long run: forward projections 806 us with 4 warps, 896
 // with 8; dH 550 and 566; second product 430 and 447.
 constexpr int kEpiWarps = 4;
-constexpr int kTileThreads = 64 + 32 * kEpiWarps; // warp 0: TMA, warp 1: MMA and tensor memory, then the epilogue
+constexpr int tile_threads(int epilogue_warps) { return 64 + 32 * epilogue_warps; }   // warp 0: TMA, warp 1: MMA and tensor memory
 constexpr int kWarpStage = 2048;                  // staging bytes of an epilogue warp: 32 rows of 64 bytes
 
 // one product C[M, N] = sum over segments A_s B_s, with every operand K-major ([M or N, K]) or MN-major ([K, M or N])
@@ -62,10 +64,9 @@ struct LinearEpilogue {
   const uint16_t* table;                          // [steps, N] of the operands' type, NULL = none
   const int* step;                                // [M] row of the table; a row whose step is outside the table is NaN
   const void* residual;                           // [M, N] of the output's type, NULL = none
-  uint16_t* factor;                               // [M, ldf] f16, ldf = N rounded up to 8, NULL = not kept
+  float* factor;                                  // [M, ldf], ldf = N rounded up to 8, NULL = not kept
   int64_t ldr, ldf;
   int tbias, ty, steps;                           // ty: output and residual, SDS_F32 or (else) the operands' type
-  int wide, table_wide;                           // output and residual (table) lie in whole 16-byte pieces
 };
 
 constexpr int kMaxProducts = 4;
@@ -156,7 +157,7 @@ __device__ __forceinline__ size_t keep_index(int row, int col, int ncc, int whic
 
 // 32 rows of 64 bytes, one per lane as 16 words, to global memory: turned through shared memory so that four lanes
 // write the 64 bytes of a row. Piece p of row r lies at p ^ (r / 2 % 4): 128-bit accesses free of bank conflicts both ways.
-__device__ __forceinline__ void store_rows64(uint4* stg, const uint32_t (&w)[16], char* out, size_t ld_bytes, int nrows,
+__device__ __forceinline__ void store_rows64(uint4* stg, const uint32_t* w, char* out, size_t ld_bytes, int nrows,
                                              int npieces, int lane) {
 #pragma unroll
   for (int p = 0; p < 4; ++p)
@@ -207,63 +208,83 @@ __device__ __forceinline__ uint16_t round16(float v, int f16) {
   return f16 ? __half_as_ushort(__float2half_rn(v)) : (uint16_t)(pack_bf16x2(v, 0.f) & 0xffffu);
 }
 
-// kLinear: 16 floats of every row (a lane's each) out, with the residual added before the rounding. Turned through shared memory:
-// in whole pieces four lanes write 16 columns of a row, element by element 16 lanes do.
-struct LinearResidual { float4 v[4]; };
-// what such a store will add, requested ahead of it (whole pieces only)
-__device__ __forceinline__ LinearResidual fetch_residual(const LinearEpilogue& e, int row0, int col, int nrows, int N, int f16, int lane) {
-  LinearResidual r;
-  const int c = col + 4 * (lane & 3);
+// kLinear. A warp's 32 rows of 64 bytes change hands through its staging area: in memory's order (four lanes to a row, or, where
+// rows are not whole 16-byte pieces, an element per lane), and one row to a lane, as 16 words.
+struct Rows64 { uint4 v[4]; };
+__device__ __forceinline__ uint4* staged(uint4* stg, int row, int piece) { return stg + row * 4 + (piece ^ ((row >> 1) & 3)); }
+__device__ __forceinline__ uint16_t* staged16(uint4* stg, int row, int c) { return reinterpret_cast<uint16_t*>(staged(stg, row, c >> 3)) + (c & 7); }
+__device__ __forceinline__ uint32_t* staged32(uint4* stg, int row, int c) { return reinterpret_cast<uint32_t*>(staged(stg, row, c >> 2)) + (c & 3); }
+// whole pieces: requested ahead of their use; at(i) is this lane's piece of row 8 i + lane / 4, NULL where there is none
+template <class F>
+__device__ __forceinline__ void fetch_rows(Rows64& r, F at) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int row = 8 * i + (lane >> 2);
-    r.v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row < nrows && c < N) {
-      const size_t at = (size_t)(row0 + row) * e.ldr + c;
-      if (e.ty == SDS_F32) {
-        r.v[i] = *reinterpret_cast<const float4*>(static_cast<const float*>(e.residual) + at);   // (may be the output: no read-only load)
-      } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(e.residual) + at);
-        const float2 a = unpack16x2(w.x, f16), b = unpack16x2(w.y, f16);
-        r.v[i] = make_float4(a.x, a.y, b.x, b.y);
-      }
-    }
+    const uint4* p = at(i);
+    r.v[i] = p ? *p : make_uint4(0u, 0u, 0u, 0u);
   }
-  return r;
 }
-__device__ __forceinline__ void store_linear16(uint4* stg, const uint32_t* w, const LinearEpilogue& e, const LinearResidual& add, void* out,
-                                               int64_t ldo, int row0, int col, int nrows, int N, int f16, int lane) {
-#pragma unroll
-  for (int p = 0; p < 4; ++p)
-    stg[lane * 4 + (p ^ ((lane >> 1) & 3))] = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+__device__ __forceinline__ void take_staged(uint4* stg, uint32_t (&w)[16], int lane) {
   __syncwarp();
-  if (e.wide) {
-    const int pc = lane & 3, c = col + 4 * pc;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 8 * i + (lane >> 2);
-      const uint4 q = stg[r * 4 + (pc ^ ((r >> 1) & 3))];
-      if (r < nrows && c < N) {
-        const float4 v = make_float4(__uint_as_float(q.x) + add.v[i].x, __uint_as_float(q.y) + add.v[i].y,
-                                     __uint_as_float(q.z) + add.v[i].z, __uint_as_float(q.w) + add.v[i].w);
-        const size_t at = (size_t)(row0 + r) * ldo + c;
-        if (e.ty == SDS_F32) *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = v;
-        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack16(v.x, v.y, f16), pack16(v.z, v.w, f16));
-      }
-    }
-  } else {
-    const int cc = lane & 15, c = col + cc;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-      const int r = 2 * i + (lane >> 4);
-      float v = reinterpret_cast<const float*>(stg + r * 4 + ((cc >> 2) ^ ((r >> 1) & 3)))[cc & 3];
-      if (r < nrows && c < N) {
-        if (e.residual) v += load_typed(e.residual, e.ty, (size_t)(row0 + r) * e.ldr + c);
-        const size_t at = (size_t)(row0 + r) * ldo + c;
-        if (e.ty == SDS_F32) static_cast<float*>(out)[at] = v;
-        else static_cast<uint16_t*>(out)[at] = round16(v, f16);
-      }
-    }
+  for (int p = 0; p < 4; ++p) {
+    const uint4 v = *staged(stg, lane, p);
+    w[4 * p] = v.x; w[4 * p + 1] = v.y; w[4 * p + 2] = v.z; w[4 * p + 3] = v.w;
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void rows_to_lanes(uint4* stg, const Rows64& r, uint32_t (&w)[16], int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *staged(stg, 8 * i + (lane >> 2), lane & 3) = r.v[i];
+  take_staged(stg, w, lane);
+}
+// element by element: from(row) points to the first column of a row, NULL = zeros; ncols columns are there
+template <class F>
+__device__ __forceinline__ void narrow16_to_lanes(uint4* stg, F from, int ncols, uint32_t (&w)[16], int lane) {
+  uint16_t v[32];
+#pragma unroll
+  for (int r = 0; r < 32; ++r) {
+    const uint16_t* p = from(r);
+    v[r] = p && lane < ncols ? p[lane] : (uint16_t)0;
+  }
+#pragma unroll
+  for (int r = 0; r < 32; ++r) *staged16(stg, r, lane) = v[r];
+  take_staged(stg, w, lane);
+}
+template <class F>
+__device__ __forceinline__ void narrow32_to_lanes(uint4* stg, F from, int ncols, uint32_t (&w)[16], int lane) {
+  uint32_t v[16];
+  const int c = lane & 15;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t* p = from(2 * i + (lane >> 4));
+    v[i] = p && c < ncols ? p[c] : 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) *staged32(stg, 2 * i + (lane >> 4), c) = v[i];
+  take_staged(stg, w, lane);
+}
+__device__ __forceinline__ void stage_lanes(uint4* stg, const uint32_t* w, int lane) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p) *staged(stg, lane, p) = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+  __syncwarp();
+}
+__device__ __forceinline__ void store_narrow16(uint4* stg, const uint32_t (&w)[16], uint16_t* out, int64_t ld, int nrows, int ncols, int lane) {
+  stage_lanes(stg, w, lane);
+#pragma unroll
+  for (int r = 0; r < 32; ++r) {
+    const uint16_t v = *staged16(stg, r, lane);
+    if (r < nrows && lane < ncols) out[(size_t)r * ld + lane] = v;
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void store_narrow32(uint4* stg, const uint32_t* w, uint32_t* out, int64_t ld, int nrows, int ncols, int lane) {
+  stage_lanes(stg, w, lane);
+  const int c = lane & 15;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = 2 * i + (lane >> 4);
+    const uint32_t v = *staged32(stg, r, c);
+    if (r < nrows && c < ncols) out[(size_t)r * ld + c] = v;
   }
   __syncwarp();
 }
@@ -299,13 +320,13 @@ __device__ __forceinline__ void give_up(int* err, int role) {
 // batches: persistent tiles
 // ---------------------------------------------------------------------------------------------
 
-template <int BN, bool PAIR> struct FfnTile {
+template <int BN, bool PAIR, int EW = kEpiWarps> struct FfnTile {
   static constexpr int kTM = PAIR ? 2 * kBM : kBM;                 // rows of a tile
   static constexpr int kBRows = PAIR ? BN / 2 : BN;                // rows of B that one CTA stages
   static constexpr int kABytes = kBM * kBK * 2;
   static constexpr int kBBytes = kBRows * kBK * 2;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kFixedBytes = 1024 /*align*/ + 256 /*barriers*/ + kEpiWarps * kWarpStage;
+  static constexpr int kFixedBytes = 1024 /*align*/ + 256 /*barriers*/ + EW * kWarpStage;
   static constexpr int kStages = (227 * 1024 - kFixedBytes) / kStageBytes;
   static constexpr int kSmemBytes = kStages * kStageBytes + kFixedBytes;
   static constexpr int kTmemCols = 2 * BN;
@@ -375,9 +396,10 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
 // Bound by the tensor cores: 16384 x 2048 x 8192 forward 1280 us, 1290 TFLOP/s (92 % of the library's rate in a long run, where power
 // sets the clock); 8192 rows forward and backward 2130 us, 1160 TFLOP/s beside the kept factors.
 // CUT: products whose K is cut (FfnProduct::parts); its own kernel, as the others lose up to 5 % to the arithmetic.
-template <int BN, int EPI, bool PAIR, bool MN, bool CUT>
-__global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
-  using C = FfnTile<BN, PAIR>;
+// EW: epilogue warps, four or eight (two for each quarter of the lanes, half of the columns each).
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW>
+__global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
+  using C = FfnTile<BN, PAIR, EW>;
   constexpr int TM = C::kTM, TN = EPI == kFfnGlu ? BN / 2 : BN;    // output columns of a tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -395,7 +417,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   const int nworkers = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar + s, 1); mbar_init(empty_bar + s, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(tfull_bar + s, 1); mbar_init(tempty_bar + s, PAIR ? 2 * kEpiWarps : kEpiWarps); }
+    for (int s = 0; s < 2; ++s) { mbar_init(tfull_bar + s, 1); mbar_init(tempty_bar + s, PAIR ? 2 * EW : EW); }
     *abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -535,7 +557,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
   } else {
     // ---------------- epilogue: a warp reaches the 32 tensor-memory lanes of quarter warp % 4 ----------------
     const int q = warp & 3;
-    constexpr int kChunks = TN / 32;              // chunks of 32 output columns
+    constexpr int kChunks = TN / 32 / (EW / 4);   // chunks of 32 output columns of a warp
+    const int first_chunk = (warp - 2) / 4 * kChunks, last_chunk = first_chunk + kChunks - 1;
     uint4* stg = reinterpret_cast<uint4*>(epi_stage + (warp - 2) * kWarpStage);
     const uint32_t drained0 = (PAIR && rank != 0) ? map_to_cta(smem_u32(tempty_bar), 0u) : 0u;
     const int f16 = g.f16;
@@ -561,35 +584,51 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
         }
       };
       if (EPI == kFfnDGlu) keep_fetch(n0);
-      // so do the lane's row of the table and the bias (kLinear)
-      int64_t table_row = -1;
-      uint4 tab[4];
+      // neither do the bias, the rows of the table and the residual (kLinear): requested a chunk ahead
+      int table_row = -1, piece_row[4];           // of the lane's row; of the rows of which it fetches a piece
+      Rows64 tab, res[2];
       float bias_next = 0.f;
-      auto added_fetch = [&](int col) {
+      const auto added_fetch = [&](int col) {
         const LinearEpilogue& e = g.lin;
+        const int pc = lane & 3;
         if (e.bias) bias_next = col + lane < N ? load_typed(e.bias, e.tbias, (size_t)(col + lane)) : 0.f;
-        if (e.table && e.table_wide)
+        if (EPI == kLinear && e.table)
+          fetch_rows(tab, [&](int i) -> const uint4* {
+            const bool in = piece_row[i] >= 0 && col + 8 * pc < N;
+            return in ? reinterpret_cast<const uint4*>(e.table + (size_t)piece_row[i] * N + col) + pc : nullptr;
+          });
+        if (EPI == kLinear && e.residual) {
+          const int per = e.ty == SDS_F32 ? 4 : 8;              // columns of a piece; 16 or 32 of a row of 64 bytes
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            tab[i] = table_row >= 0 && col + 8 * i < N ? __ldg(reinterpret_cast<const uint4*>(e.table + table_row * N + col) + i)
-                                                       : make_uint4(0u, 0u, 0u, 0u);
-      };
-      if (EPI == kLinear) {
-        if (g.lin.table && lane < nlive) {
-          const int s = __ldg(g.lin.step + row0 + lane);
-          table_row = s >= 0 && s < g.lin.steps ? s : -1;
+          for (int hf = 0; hf < 2; ++hf)
+            if (hf == 0 || per == 4)
+              fetch_rows(res[hf], [&](int i) -> const uint4* {
+                const int r = 8 * i + (lane >> 2), c = col + 16 * hf + per * pc;
+                const char* at = static_cast<const char*>(e.residual) + ((size_t)(row0 + r) * e.ldr + c) * (16 / per);
+                return r < nlive && c < N ? reinterpret_cast<const uint4*>(at) : nullptr;
+              });
         }
-        added_fetch(n0);
+      };
+      if (is_linear(EPI)) {
+        if (g.lin.table) {
+          if (lane < nlive) {
+            const int s = __ldg(g.lin.step + row0 + lane);
+            table_row = s >= 0 && s < g.lin.steps ? s : -1;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) piece_row[i] = __shfl_sync(0xffffffffu, table_row, 8 * i + (lane >> 2));
+        }
+        added_fetch(n0 + first_chunk * 32);
       }
       if (!wait_for_sums(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s, (p.K + kBK - 1) / kBK * p.nseg)) { ok = false; break; }
       tc_fence_after();
 #pragma unroll 1
-      for (int chunk = 0; chunk < kChunks; ++chunk) {
+      for (int chunk = first_chunk; chunk <= last_chunk; ++chunk) {
         const int c = chunk * 32, col = n0 + c;
         uint32_t acc[32], up[EPI == kFfnGlu ? 32 : 1];
         tmem_ld32(tbase + (uint32_t)c, acc);
         if (EPI == kFfnGlu) tmem_ld32(tbase + (uint32_t)(BN / 2 + c), reinterpret_cast<uint32_t(&)[32]>(up));
-        if (chunk == kChunks - 1) {               // accumulator read: hand the buffer back
+        if (chunk == last_chunk) {                // accumulator read: hand the buffer back
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -646,12 +685,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
           for (int i = 0; i < 16; ++i) w[i] = pack16(__uint_as_float(acc[2 * i]), __uint_as_float(acc[2 * i + 1]), f16);
           store_rows64(stg, w, static_cast<char*>(p.out) + ((size_t)row0 * p.ldo + col) * 2, (size_t)p.ldo * 2, nlive,
                        npieces, lane);
-        } else if (EPI == kLinear) {
+        } else if (is_linear(EPI)) {
           const LinearEpilogue& e = g.lin;
-          LinearResidual add[2] = {};
-          if (e.residual && e.wide)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) add[hf] = fetch_residual(e, row0, col + 16 * hf, nlive, N, f16, lane);
+          const int ncols = min(32, N - col);
+          uint32_t w[16];
           if (e.bias) {
             reinterpret_cast<float*>(stg)[lane] = bias_next;
             __syncwarp();
@@ -665,60 +702,77 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
             }
             __syncwarp();
           }
-          if (e.table) {
-            const uint32_t* tw = reinterpret_cast<const uint32_t*>(tab);
+          const auto add16 = [&](float bad) {     // w as 32 16-bit values, plus `bad`
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              float2 t;
-              if (e.table_wide) {
-                t = unpack16x2(tw[i], f16);
-              } else {
-                const uint16_t* from = e.table + table_row * N + col + 2 * i;
-                t.x = table_row >= 0 && col + 2 * i < N ? unpack16(from[0], f16) : 0.f;
-                t.y = table_row >= 0 && col + 2 * i + 1 < N ? unpack16(from[1], f16) : 0.f;
-              }
-              if (table_row < 0) t.x = t.y = __int_as_float(0x7fffffff);
-              acc[2 * i] = __float_as_uint(__uint_as_float(acc[2 * i]) + t.x);
-              acc[2 * i + 1] = __float_as_uint(__uint_as_float(acc[2 * i + 1]) + t.y);
+              const float2 t = unpack16x2(w[i], f16);
+              acc[2 * i] = __float_as_uint(__uint_as_float(acc[2 * i]) + (t.x + bad));
+              acc[2 * i + 1] = __float_as_uint(__uint_as_float(acc[2 * i + 1]) + (t.y + bad));
             }
+          };
+          if (e.table) {
+            if (EPI == kLinear) {
+              rows_to_lanes(stg, tab, w, lane);
+            } else {
+              narrow16_to_lanes(stg, [&](int r) -> const uint16_t* {
+                const int s = __shfl_sync(0xffffffffu, table_row, r);
+                return s >= 0 ? e.table + (size_t)s * N + col : nullptr;
+              }, ncols, w, lane);
+            }
+            add16(table_row < 0 ? __int_as_float(0x7fffffff) : 0.f);
           }
-          if (chunk < kChunks - 1) added_fetch(col + 32);
+          Rows64 res_now[2] = {res[0], res[1]};
+          if (chunk < last_chunk) added_fetch(col + 32);
           if (g.act != SDS_ACT_NONE)
             with_activation(g.act, [&](auto act) {
               constexpr int ACT = decltype(act)::value;
-              if (e.factor) {
-                uint32_t fw[16];
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                uint32_t da[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                  float a0, a1, d0, d1;
-                  activation<ACT>(__uint_as_float(acc[2 * i]), a0, d0);
-                  activation<ACT>(__uint_as_float(acc[2 * i + 1]), a1, d1);
-                  acc[2 * i] = __float_as_uint(a0);
-                  acc[2 * i + 1] = __float_as_uint(a1);
-                  fw[i] = pack16(d0, d1, 1);
-                }
-                store_rows64(stg, fw, reinterpret_cast<char*>(e.factor + (size_t)row0 * e.ldf + col), (size_t)e.ldf * 2, nlive,
-                             min(4, ((int)e.ldf - col) >> 3), lane);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
                   float a0, d0;
-                  activation<ACT>(__uint_as_float(acc[i]), a0, d0);
-                  acc[i] = __float_as_uint(a0);
+                  activation<ACT>(__uint_as_float(acc[16 * hf + i]), a0, d0);
+                  acc[16 * hf + i] = __float_as_uint(a0);
+                  da[i] = __float_as_uint(d0);
                 }
+                if (e.factor && col + 16 * hf < (int)e.ldf)
+                  store_rows64(stg, da, reinterpret_cast<char*>(e.factor + (size_t)row0 * e.ldf + col + 16 * hf), (size_t)e.ldf * 4, nlive,
+                               min(4, ((int)e.ldf - col - 16 * hf) >> 2), lane);
               }
             });
-          if (e.wide && e.ty != SDS_F32 && !e.residual) {
-            uint32_t w[16];
+          if (e.residual && e.ty != SDS_F32) {
+            if (EPI == kLinear) rows_to_lanes(stg, res_now[0], w, lane);
+            else narrow16_to_lanes(stg, [&](int r) -> const uint16_t* {
+              return r < nlive ? static_cast<const uint16_t*>(e.residual) + (size_t)(row0 + r) * e.ldr + col : nullptr;
+            }, ncols, w, lane);
+            add16(0.f);
+          } else if (e.residual) {
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              if (EPI == kLinear) rows_to_lanes(stg, res_now[hf], w, lane);
+              else narrow32_to_lanes(stg, [&](int r) -> const uint32_t* {
+                return r < nlive ? static_cast<const uint32_t*>(e.residual) + (size_t)(row0 + r) * e.ldr + col + 16 * hf : nullptr;
+              }, ncols - 16 * hf, w, lane);
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                acc[16 * hf + i] = __float_as_uint(__uint_as_float(acc[16 * hf + i]) + __uint_as_float(w[i]));
+            }
+          }
+          if (e.ty != SDS_F32) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack16(__uint_as_float(acc[2 * i]), __uint_as_float(acc[2 * i + 1]), f16);
-            store_rows64(stg, w, static_cast<char*>(p.out) + ((size_t)row0 * p.ldo + col) * 2, (size_t)p.ldo * 2, nlive,
-                         npieces, lane);
+            uint16_t* out = static_cast<uint16_t*>(p.out) + (size_t)row0 * p.ldo + col;
+            if (EPI == kLinear) store_rows64(stg, w, reinterpret_cast<char*>(out), (size_t)p.ldo * 2, nlive, npieces, lane);
+            else store_narrow16(stg, w, out, p.ldo, nlive, ncols, lane);
           } else {
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-              if (col + 16 * hf < N)
-                store_linear16(stg, acc + 16 * hf, e, add[hf], p.out, p.ldo, row0, col + 16 * hf, nlive, N, f16, lane);
+            for (int hf = 0; hf < 2; ++hf) {
+              if (16 * hf >= ncols) continue;
+              uint32_t* out = static_cast<uint32_t*>(p.out) + (size_t)row0 * p.ldo + col + 16 * hf;
+              if (EPI == kLinear) store_rows64(stg, acc + 16 * hf, reinterpret_cast<char*>(out), (size_t)p.ldo * 4, nlive, min(4, (ncols - 16 * hf) >> 2), lane);
+              else store_narrow32(stg, acc + 16 * hf, out, p.ldo, nlive, ncols - 16 * hf, lane);
+            }
           }
         } else if (EPI == kFfnAdd) {
 #pragma unroll
@@ -737,7 +791,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_ffn_tile(const __grid_const
             wur[2 * i] = pack16(a0 * kq[i].x, a1 * kq[i].y, f16);
             wur[2 * i + 1] = pack16(a2 * kq[i].z, a3 * kq[i].w, f16);
           }
-          if (chunk < kChunks - 1) keep_fetch(col + 32);
+          if (chunk < last_chunk) keep_fetch(col + 32);
           const size_t off = ((size_t)row0 * p.ldo + col) * 2;
           store_rows64(stg, wgr, static_cast<char*>(p.out) + off, (size_t)p.ldo * 2, nlive, npieces, lane);
           store_rows64(stg, wur, static_cast<char*>(g.out2) + off, (size_t)p.ldo * 2, nlive, npieces, lane);
@@ -1005,7 +1059,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
           *reinterpret_cast<float4*>(g.keep + keep_index(tok, col, ncc, 1)) = a;
         }
       }
-    } else if (EPI == kLinear) {
+    } else if (is_linear(EPI)) {
       const LinearEpilogue& e = g.lin;
       const int col = n0 + 4 * lane, live = min(4, g.N - col);
       if (live > 0) {
@@ -1019,7 +1073,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
           const bool in = at >= 0 && at < e.steps;
           const uint16_t* from = e.table + (int64_t)(in ? at : 0) * g.N + col;
           float t[4] = {0.f, 0.f, 0.f, 0.f};
-          if (e.table_wide) {
+          if (EPI == kLinear) {
             const uint2 w = __ldg(reinterpret_cast<const uint2*>(from));
             const float2 lo = unpack16x2(w.x, g.f16), hi = unpack16x2(w.y, g.f16);
             t[0] = lo.x; t[1] = lo.y; t[2] = hi.x; t[3] = hi.y;
@@ -1037,15 +1091,15 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
           for (int u = 0; u < 4; ++u) activation<ACT>(z[u], z[u], da[u]);
         });
         if (e.factor)                             // (its rows are padded to eight columns)
-          *reinterpret_cast<uint2*>(e.factor + (size_t)tok * e.ldf + col) = make_uint2(pack16(da[0], da[1], 1), pack16(da[2], da[3], 1));
+          *reinterpret_cast<float4*>(e.factor + (size_t)tok * e.ldf + col) = make_float4(da[0], da[1], da[2], da[3]);
         const size_t to = (size_t)tok * g.ldo + col;
         if (e.residual)
 #pragma unroll
           for (int u = 0; u < 4; ++u)
             if (u < live) z[u] += load_typed(e.residual, e.ty, (size_t)tok * e.ldr + col + u);
-        if (e.wide && e.ty == SDS_F32) {
+        if (EPI == kLinear && e.ty == SDS_F32) {
           *reinterpret_cast<float4*>(static_cast<float*>(g.out) + to) = make_float4(z[0], z[1], z[2], z[3]);
-        } else if (e.wide) {
+        } else if (EPI == kLinear) {
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.out) + to) = make_uint2(pack16(z[0], z[1], g.f16), pack16(z[2], z[3], g.f16));
         } else {
 #pragma unroll
@@ -1110,15 +1164,15 @@ struct KernelInfo {
   std::atomic<int> resident[kMaxDevices];         // 0: not looked up; else 1 + resident CTAs (clusters of a pair)
 };
 
-template <int BN, int EPI, bool PAIR, bool MN, bool CUT>
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW>
 cudaError_t tile_resident(int* n) {
   static KernelInfo info;                         // zero-initialised
-  using C = FfnTile<BN, PAIR>;
+  using C = FfnTile<BN, PAIR, EW>;
   const int dev = current_device();
   if (dev < 0) return cudaErrorInvalidDevice;
   int r = info.resident[dev].load(std::memory_order_acquire);
   if (r == 0) {
-    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     int sms = 0, got = 0;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
@@ -1126,14 +1180,14 @@ cudaError_t tile_resident(int* n) {
     if (PAIR) {
       cudaLaunchConfig_t cfg{};
       cfg.gridDim = dim3(sms / 2 * 2);
-      cfg.blockDim = dim3(kTileThreads);
+      cfg.blockDim = dim3(tile_threads(EW));
       cfg.dynamicSmemBytes = C::kSmemBytes;
       cudaLaunchAttribute attr{};
       attr.id = cudaLaunchAttributeClusterDimension;
       attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
-      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN, CUT>, &cfg)) != cudaSuccess) return e;
+      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW>, &cfg)) != cudaSuccess) return e;
       got = std::min(got, sms / 2);
     }
     if (got < 1) return cudaErrorLaunchOutOfResources;
@@ -1144,23 +1198,23 @@ cudaError_t tile_resident(int* n) {
   return cudaSuccess;
 }
 
-template <int BN, int EPI, bool PAIR, bool MN, bool CUT>
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW>
 cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) {
-  using C = FfnTile<BN, PAIR>;
+  using C = FfnTile<BN, PAIR, EW>;
   int resident = 0;
-  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN, CUT>(&resident);
+  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN, CUT, EW>(&resident);
   if (e != cudaSuccess) return e;
   const int workers = (int)std::min<int64_t>(tiles, resident);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(PAIR ? 2 * workers : workers);
-  cfg.blockDim = dim3(kTileThreads);
+  cfg.blockDim = dim3(tile_threads(EW));
   cfg.dynamicSmemBytes = C::kSmemBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   launch_attributes(attr, PAIR ? 2 : 1);
-  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN, CUT>, g);
+  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW>, g);
 }
 
 // where an operand lies: [rows, cols] with rows ld elements apart; K-major if K runs along the columns
@@ -1194,7 +1248,7 @@ inline int ksteps(const ProductSpec& s) { return (steps(s.K) * s.nseg + s.parts 
 // Tile shape: single CTAs on 128 x 128 tiles while these are at most one per SM (each has an SM of its own), pairs on
 // 256 x 256 tiles above that. Several products of one launch: those with the longer tiles come first; there are at most
 // two lengths (specs[0] may differ from the others).
-template <int EPI, bool MN, bool CUT = false>
+template <int EPI, bool MN, bool CUT = false, int EW = kEpiWarps>
 cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first, cudaStream_t st,
                          float* keep = nullptr, void* out2 = nullptr, bool beside = false, const LinearEpilogue* lin = nullptr) {
   constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
@@ -1238,7 +1292,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     }
   }
   if (pair) {
-    const cudaError_t e = launch_tile_t<256, EPI, true, MN, CUT>(g, wide, st);
+    const cudaError_t e = launch_tile_t<256, EPI, true, MN, CUT, EW>(g, wide, st);
     if (e != cudaErrorLaunchOutOfResources) return e;
     // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
     for (int i = 0; EPI == kFfnGlu && i < n; ++i)
@@ -1246,7 +1300,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
         if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, MN, 64))
           return cudaErrorInvalidValue;
   }
-  return launch_tile_t<128, EPI, false, MN, CUT>(g, small, st);
+  return launch_tile_t<128, EPI, false, MN, CUT, EW>(g, small, st);
 }
 
 template <int BN, int EPI>
