@@ -552,8 +552,9 @@ int sds_dropout(const sds_dropout_spec* spec, const void* x_dev, int64_t ldx, in
  * block behind: n is that of r, and out_dev, gate and post are not used. w_dev, b_dev, post_w_dev [d] of w_dtype (NULL = ones,
  * zeros, ones); gate_dev, scale_dev, shift_dev [groups, d] of cond_dtype, rows ld_gate, ld_scale, ld_shift elements apart (NULL = ones,
  * zeros, zeros): rows / groups consecutive rows share one row of them (rows a multiple of groups; groups = 1: one vector for all,
- * groups = rows: one each). d <= 16384 (else SDS_EUNSUPPORTED). eps >= 0 and alpha finite. All is held in float and rounded once; n is that of the
- * unrounded out. keep_dev: [6, rows] floats (keep_bytes) that the backward pass needs, 256-byte aligned (NULL = none will follow).
+ * groups = rows: one each). d <= 16384, rows less than
+ * 2^31 elements apart (else SDS_EUNSUPPORTED). eps >= 0 and alpha finite. All is held in float and rounded once; n is that of the
+ * unrounded out. keep_dev: [rows, 8] floats (keep_bytes) that the backward pass needs, 256-byte aligned (NULL = none will follow).
  * out_dev may be r_dev and n_dev h_dev (same rows) where no backward pass will need them. */
 #define SDS_NORM_LAYER    0
 #define SDS_NORM_RMS      1

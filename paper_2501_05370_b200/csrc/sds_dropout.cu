@@ -16,7 +16,8 @@ constexpr int kDropThreads = 256;
 template <class TX, class TY, bool VEC>
 __global__ void __launch_bounds__(kDropThreads) k_dropout(const DropoutCall a, int64_t nb) {
   start_after_prior_kernel();
-  const uint32_t dstep = a.drop.threshold ? dropout_step(a.drop) : 0u;
+  const bool drops = a.drop.threshold != 0;
+  const uint32_t dstep = drops ? dropout_step(a.drop) : 0u;
   const int64_t stride = (int64_t)gridDim.x * kDropThreads, first = (int64_t)blockIdx.x * kDropThreads + threadIdx.x;
   const int64_t srow = stride / nb, sblock = stride % nb;
   int64_t row = first / nb, block = first % nb;
@@ -28,25 +29,25 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout(const DropoutCall a, i
   constexpr int kAhead = VEC ? 4 : 1;             // blocks requested before the first is used
   while (row < a.rows) {
     int64_t rows[kAhead], blocks[kAhead];
-    float x[kAhead][kE], res[kAhead][kE];
-    Raw<TX, true> xr[kAhead];
-    Raw<TY, true> rr[kAhead];
+    float2 x[kAhead][P], res[kAhead][P];
+    Raw<TX> xr[kAhead];
+    Raw<TY> rr[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       rows[i] = row;
       blocks[i] = block;
       if (row < a.rows) {
-        const TX* px = static_cast<const TX*>(a.x) + (size_t)row * a.ldx + block * kE;
-        const TY* pr = static_cast<const TY*>(a.residual) + (size_t)row * a.ldr + block * kE;
+        const TX* px = static_cast<const TX*>(a.x) + (size_t)row * a.ldx + block * kBlock;
+        const TY* pr = static_cast<const TY*>(a.residual) + (size_t)row * a.ldr + block * kBlock;
         if (VEC) {
           xr[i].load(px);
           if (a.residual) rr[i].load(pr);
         } else {
-          const int live = (int)min((int64_t)kE, a.d - block * kE);
+          const int live = (int)min((int64_t)kBlock, a.d - block * kBlock);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) {
-            x[i][e] = e < live ? Conv<TX>::get(px[e]) : 0.f;
-            res[i][e] = a.residual && e < live ? Conv<TY>::get(pr[e]) : 0.f;
+          for (int e = 0; e < kBlock; ++e) {
+            element(x[i], e) = e < live ? Conv<TX>::get(px[e]) : 0.f;
+            element(res[i], e) = a.residual && e < live ? Conv<TY>::get(pr[e]) : 0.f;
           }
         }
       }
@@ -57,27 +58,28 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout(const DropoutCall a, i
       if (rows[i] >= a.rows) break;
       if (VEC) {
         words_to(xr[i].q, x[i], TX{});
-        if (a.residual) {
-          words_to(rr[i].q, res[i], TY{});
-        } else {
+        if (a.residual) words_to(rr[i].q, res[i], TY{});
+      }
+      Kept kept;
+      if (drops) kept = kept_block(a.drop, dstep, a.drop.row0 + (uint64_t)rows[i], (uint32_t)blocks[i]);
+      const float2 scale = both(drops ? a.drop.scale : 1.0f);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) res[i][e] = 0.f;
+      for (int k = 0; k < P; ++k) {
+        if (a.residual) {
+          add_branch(res[i][k], scale, x[i][k], drops, kept, k);
+          x[i][k] = res[i][k];
+        } else if (drops) {
+          x[i][k] = select_kept(mul2(scale, x[i][k]), kept, k);
         }
       }
-      const uint32_t kept = a.drop.threshold ? kept_block(a.drop, dstep, a.drop.row0 + (uint64_t)rows[i], (uint32_t)blocks[i]) : 0xffu;
-#pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        if (a.residual) x[i][e] = add_branch(res[i][e], 1.0f, x[i][e], kept, e, a.drop);
-        else if (a.drop.threshold) x[i][e] = (kept >> e) & 1u ? x[i][e] * a.drop.scale : 0.f;
-      }
-      TY* py = static_cast<TY*>(a.y) + (size_t)rows[i] * a.ldy + blocks[i] * kE;
+      TY* py = static_cast<TY*>(a.y) + (size_t)rows[i] * a.ldy + blocks[i] * kBlock;
       if (VEC) {
         store_words(py, x[i]);
       } else {
-        const int live = (int)min((int64_t)kE, a.d - blocks[i] * kE);
+        const int live = (int)min((int64_t)kBlock, a.d - blocks[i] * kBlock);
 #pragma unroll
-        for (int e = 0; e < kE; ++e)
-          if (e < live) py[e] = Conv<TY>::put(x[i][e]);
+        for (int e = 0; e < kBlock; ++e)
+          if (e < live) py[e] = Conv<TY>::put(element(x[i], e));
       }
     }
   }
@@ -89,14 +91,14 @@ cudaError_t dropout_k(const DropoutCall& a, cudaStream_t st) {
   int resident = 0;
   const cudaError_t e = row_resident(k_dropout<TX, TY, VEC>, cache, kDropThreads, 0, 1, &resident);
   if (e != cudaSuccess) return e;
-  const int64_t nb = (a.d + kE - 1) / kE, ctas = (a.rows * nb + kDropThreads - 1) / kDropThreads;
+  const int64_t nb = (a.d + kBlock - 1) / kBlock, ctas = (a.rows * nb + kDropThreads - 1) / kDropThreads;
   return row_launch(k_dropout<TX, TY, VEC>, dim3((unsigned)std::min<int64_t>(ctas, resident)), kDropThreads, 0, 1, st, a, nb);
 }
 
 template <class TX, class TY>
 cudaError_t dropout_t(const DropoutCall& a, cudaStream_t st) {
-  const bool vec = a.d % 8 == 0 && pieces16(a.x, a.ldx, a.tx) && pieces16(a.y, a.ldy, a.ty) &&
-                   (!a.residual || pieces16(a.residual, a.ldr, a.ty));
+  const bool vec = a.d % 8 == 0 && pieces8(a.x, a.ldx, a.tx) && pieces8(a.y, a.ldy, a.ty) &&
+                   (!a.residual || pieces8(a.residual, a.ldr, a.ty));
   return vec ? dropout_k<TX, TY, true>(a, st) : dropout_k<TX, TY, false>(a, st);
 }
 

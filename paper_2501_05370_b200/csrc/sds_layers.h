@@ -129,7 +129,7 @@ struct ResidualNormArgs {
   const void* gate; const void* scale; const void* shift; int tc;                  // [groups, d] each, NULL = ones, zeros, zeros
   int64_t ldgate, ldscale, ldshift;
   bool wide_w, wide_c;                           // the vectors (the rows of gate, scale and shift) lie in whole 16-byte pieces
-  float* stats;                                  // [6][rows]: mean, its remainder, 1 / size, and the same of post; forward: may be NULL
+  float4* stats;                                 // [rows][2]: mean, its remainder, 1 / size, and the same of post; forward: may be NULL
   // backward
   const void* dn; int64_t lddn;
   const void* dr; int64_t lddr;                  // NULL = zeros
@@ -138,15 +138,15 @@ struct ResidualNormArgs {
   void* dw; void* db; void* dwp;
   void* dgate; void* dscale; void* dshift;
   int64_t lddgate, lddscale, lddshift;
-  // how the rows are dealt out, and where their sums go (residual_norm_plan)
-  int mode, workers, piece, pieces, total;       // rows of a piece, pieces of a group, pieces in all
+  // how the rows are dealt out, and where their sums go
+  int mode, workers, share;                      // rows of a worker
   float* part;                                   // [workers][3][d]
-  float* piece_part;                             // [groups * pieces][3][d]
+  float* group_part;                             // [workers][2][3][d]: sums of a group that began before the worker's rows, that goes on behind them
 };
 
 constexpr int kResidualMaxD = 16384;
-// how a backward call deals out its rows: sets mode, workers, piece, pieces and total of a; floats of the two workspaces
-void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* piece_floats);
+// how a backward call sums over rows: sets mode and workers (the most) of a; floats of the two workspaces
+void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* group_floats);
 cudaError_t launch_residual_norm(const ResidualNormArgs& a, cudaStream_t st);
 cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_t st);
 // y = D x + residual over [rows, d]

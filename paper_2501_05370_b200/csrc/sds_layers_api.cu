@@ -129,8 +129,13 @@ DropoutArgs dropout_args(const sds_dropout_spec& s) {
   return a;
 }
 
+// rows that the residual norm's kernels reach by one 32-bit multiplication
+int check_near_rows(const void* p, int64_t ld, int32_t dtype, int64_t rows, int32_t d) {
+  const int rc = check_rows(p, ld, dtype, rows, d);
+  return rc != SDS_OK || rows == 0 ? rc : ld < ((int64_t)1 << 31) ? SDS_OK : SDS_EUNSUPPORTED;
+}
 // a vector per group
-int check_cond(const void* p, int64_t ld, int32_t type, int64_t groups, int32_t d) { return p ? check_rows(p, ld, type, groups, d) : SDS_OK; }
+int check_cond(const void* p, int64_t ld, int32_t type, int64_t groups, int32_t d) { return p ? check_near_rows(p, ld, type, groups, d) : SDS_OK; }
 
 int check_residual_norm(const sds_residual_norm_op* op) {
   if (!op || op->rows < 0 || op->rows > kMaxSize || op->d <= 0 || op->groups < 1 || (op->rows > 0 && op->rows % op->groups) ||
@@ -161,7 +166,7 @@ ResidualNormArgs residual_norm_args(const sds_residual_norm_op* op, const void* 
   a.w = op->w_dev; a.b = op->b_dev; a.wp = a.post ? op->post_w_dev : nullptr; a.tw = op->w_dtype;
   a.gate = h ? op->gate_dev : nullptr; a.scale = op->scale_dev; a.shift = op->shift_dev; a.tc = op->cond_dtype;
   a.ldgate = op->ld_gate; a.ldscale = op->ld_scale; a.ldshift = op->ld_shift;
-  a.stats = const_cast<float*>(keep);
+  a.stats = reinterpret_cast<float4*>(const_cast<float*>(keep));
   return a;
 }
 
@@ -172,9 +177,9 @@ size_t residual_norm_bytes(const sds_residual_norm_op* op) {
   for (const bool cond : {false, true}) {
     ResidualNormArgs a = residual_norm_args(op, nullptr, 0, op, 0, nullptr);    // (as if there were an h)
     a.dgate = cond ? &most : nullptr;
-    size_t part = 0, piece = 0;
-    residual_norm_plan(&a, &part, &piece);
-    most = std::max(most, align_up(part * 4) + align_up(piece * 4));
+    size_t part = 0, groups = 0;
+    residual_norm_plan(&a, &part, &groups);
+    most = std::max(most, align_up(part * 4) + align_up(groups * 4));
   }
   return most;
 }
@@ -405,10 +410,10 @@ int sds_residual_norm(const sds_residual_norm_op* op, const void* r_dev, int64_t
                       void* out_dev, int64_t ldo, void* n_dev, int64_t ldn, float* keep_dev, void* cuda_stream) {
   int rc = check_residual_norm(op);
   if (rc != SDS_OK) return rc;
-  if ((rc = check_rows(r_dev, ldr, op->r_dtype, op->rows, op->d)) != SDS_OK) return rc;
-  if (h_dev && (rc = check_rows(h_dev, ldh, op->h_dtype, op->rows, op->d)) != SDS_OK) return rc;
-  if (h_dev && (rc = check_rows(out_dev, ldo, op->r_dtype, op->rows, op->d)) != SDS_OK) return rc;
-  if ((rc = check_rows(n_dev, ldn, op->h_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if ((rc = check_near_rows(r_dev, ldr, op->r_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if (h_dev && (rc = check_near_rows(h_dev, ldh, op->h_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if (h_dev && (rc = check_near_rows(out_dev, ldo, op->r_dtype, op->rows, op->d)) != SDS_OK) return rc;
+  if ((rc = check_near_rows(n_dev, ldn, op->h_dtype, op->rows, op->d)) != SDS_OK) return rc;
   if (!aligned(keep_dev, kAlign)) return SDS_ENOMEM;
   ResidualNormArgs a = residual_norm_args(op, r_dev, ldr, h_dev, ldh, keep_dev);
   a.out = out_dev; a.ldo = ldo;
@@ -420,7 +425,7 @@ int sds_residual_norm_bytes(const sds_residual_norm_op* op, sds_residual_norm_si
   if (!sizes) return SDS_EINVAL;
   const int rc = check_residual_norm(op);
   if (rc != SDS_OK) return rc;
-  sizes->keep_bytes = (size_t)op->rows * 6 * 4;
+  sizes->keep_bytes = (size_t)op->rows * 8 * 4;
   sizes->backward_bytes = residual_norm_bytes(op);
   return SDS_OK;
 }
@@ -437,7 +442,7 @@ int sds_residual_norm_backward(const sds_residual_norm_op* op, const void* dn_de
       {dn_dev, lddn, op->h_dtype, true},         {dout_dev, lddout, op->r_dtype, false}, {r_dev, ldr, op->r_dtype, true},
       {h_dev, ldh, op->h_dtype, false},          {g.dr_dev, g.ld_dr, op->r_dtype, false}, {g.dh_dev, g.ld_dh, op->h_dtype, false}};
   for (const auto& x : arrays)
-    if ((x.needed || x.p) && (rc = check_rows(x.p, x.ld, x.type, op->rows, op->d)) != SDS_OK) return rc;
+    if ((x.needed || x.p) && (rc = check_near_rows(x.p, x.ld, x.type, op->rows, op->d)) != SDS_OK) return rc;
   if (op->rows > 0 && !h_dev && (g.dh_dev || g.dgate_dev || g.dpost_w_dev)) return SDS_EINVAL;
   if (g.dpost_w_dev && !op->post) return SDS_EINVAL;
   for (const void* p : {(const void*)g.dw_dev, (const void*)g.db_dev, (const void*)g.dpost_w_dev})
@@ -458,10 +463,10 @@ int sds_residual_norm_backward(const sds_residual_norm_op* op, const void* dn_de
   a.dgate = g.dgate_dev; a.dscale = g.dscale_dev; a.dshift = g.dshift_dev;
   a.lddgate = g.ld_dgate; a.lddscale = g.ld_dscale; a.lddshift = g.ld_dshift;
   if (op->rows > 0) {
-    size_t part = 0, piece = 0;
-    residual_norm_plan(&a, &part, &piece);
+    size_t part = 0, groups = 0;
+    residual_norm_plan(&a, &part, &groups);
     a.part = static_cast<float*>(workspace_dev);
-    a.piece_part = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align_up(part * 4));
+    a.group_part = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align_up(part * 4));
   }
   return result(launch_residual_norm_backward(a, static_cast<cudaStream_t>(cuda_stream)));
 }

@@ -5,11 +5,8 @@ namespace sds {
 
 namespace {
 
-// groups of threads that run at once in a backward launch: 512 threads per SM (128 registers each)
-int most_workers(int d) {
-  const int tpr = d <= 256 ? 32 : d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : d <= 8192 ? 1024 : 2048;
-  return kRowSms * 512 / tpr;
-}
+// groups of threads that run at once in a backward launch: 512 threads per SM
+int most_workers(int d) { return kRowSms * 512 / residual_threads(d); }
 
 constexpr int kJoinWarps = 32;
 
@@ -52,23 +49,25 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(const Residua
   const float f = 1.0f + (a.scale ? load_any(a.scale, a.tc, c) : 0.f), gate = a.gate ? load_any(a.gate, a.tc, c) : 1.f;
   if (a.dw) store_any(a.dw, a.tw, c, f * A);
   if (a.db) store_any(a.db, a.tw, c, f * B);
-  if (a.dwp) store_any(a.dwp, a.tw, c, a.alpha * gate * C);
+  if (a.dwp) store_any(a.dwp, a.tw, c, gate * C);
   if (a.dshift) store_any(a.dshift, a.tc, c, B);
   if (a.dscale) store_any(a.dscale, a.tc, c, fmaf(w, A, b * B));
-  if (a.dgate) store_any(a.dgate, a.tc, c, a.alpha * wp * C);
+  if (a.dgate) store_any(a.dgate, a.tc, c, wp * C);
 }
 
-// The pieces of each group: a CTA takes 32 columns of one group, a warp every eighth piece.
+// Groups whose rows several workers had: a CTA takes 32 columns of one group, a warp every eighth part.
 __global__ void __launch_bounds__(256) k_residual_join_groups(const ResidualNormArgs a, int strips) {
   __shared__ float sums[3][8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = a.d;
   const int group = (int)(blockIdx.x / strips), c = (int)(blockIdx.x % strips) * 32 + lane;
   start_after_prior_kernel();
+  const int first = (int)((int64_t)group * a.per / a.share), last = (int)(((int64_t)(group + 1) * a.per - 1) / a.share);
+  if (first == last) return;                      // written by its worker
   float s[3] = {0.f, 0.f, 0.f};
   if (c < d) {
 #pragma unroll 4
-    for (int i = warp; i < a.pieces; i += 8) {
-      const float* from = a.piece_part + ((size_t)group * a.pieces + i) * 3 * d + c;
+    for (int i = first + warp; i <= last; i += 8) {
+      const float* from = a.group_part + ((size_t)i * 2 + (i == first ? 1 : 0)) * 3 * d + c;
       s[0] += from[0];
       s[1] += from[d];
       s[2] += from[2 * (size_t)d];
@@ -86,10 +85,10 @@ __global__ void __launch_bounds__(256) k_residual_join_groups(const ResidualNorm
   const float w = a.w ? load_any(a.w, a.tw, c) : 1.f, b = a.b ? load_any(a.b, a.tw, c) : 0.f, wp = a.wp ? load_any(a.wp, a.tw, c) : 1.f;
   if (a.dshift) store_any(a.dshift, a.tc, (size_t)group * a.lddshift + c, t[1]);
   if (a.dscale) store_any(a.dscale, a.tc, (size_t)group * a.lddscale + c, fmaf(w, t[0], b * t[1]));
-  if (a.dgate) store_any(a.dgate, a.tc, (size_t)group * a.lddgate + c, a.alpha * wp * t[2]);
+  if (a.dgate) store_any(a.dgate, a.tc, (size_t)group * a.lddgate + c, wp * t[2]);
 }
 
-cudaError_t launch_rows(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+cudaError_t launch_rows(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
   if (a.tr == SDS_BF16) return residual_bf16(a, vec, backward, st);
   if (a.tr == SDS_F16) return residual_f16(a, vec, backward, st);
   if (a.th == SDS_BF16) return residual_f32_bf16(a, vec, backward, st);
@@ -97,35 +96,16 @@ cudaError_t launch_rows(const ResidualNormArgs& a, bool vec, bool backward, cuda
   return residual_f32(a, vec, backward, st);
 }
 
-bool whole(const void* p, int64_t ld, int type) { return !p || pieces16(p, ld, type); }
+bool whole(const void* p, int64_t ld, int type) { return !p || pieces8(p, ld, type); }
 
 }  // namespace
 
-void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* piece_floats) {
-  const int cap = most_workers(a->d);
+void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* group_floats) {
   const bool wanted = a->dgate || a->dscale || a->dshift, conditioned = wanted || a->gate || a->scale || a->shift;
-  *piece_floats = 0;
-  a->pieces = 1;
-  if (a->groups > 1 && a->per > 1 && wanted) {
-    // Pieces per group: those with the fewest rows for the busiest worker. A piece costs about two rows more (its sums go to
-    // memory), one where it is a whole group and they are the result.
-    a->mode = kSumGroups;
-    int64_t least = INT64_MAX;
-    const int most = (int)std::min<int64_t>(a->per, 8 * (((int64_t)cap + a->groups - 1) / a->groups));
-    for (int p = 1; p <= most; ++p) {
-      const int rows = (a->per + p - 1) / p, n = (a->per + rows - 1) / rows;
-      const int64_t rounds = ((int64_t)a->groups * n + cap - 1) / cap, cost = rounds * (rows + (n > 1 ? 2 : 1));
-      if (cost < least) { least = cost; a->piece = rows; a->pieces = n; }
-    }
-    a->total = a->groups * a->pieces;
-    a->workers = std::min(cap, a->total);
-    if (a->pieces > 1) *piece_floats = (size_t)a->total * 3 * (size_t)a->d;
-  } else {
-    a->mode = conditioned && a->groups > 1 ? kSumWeighted : kSumAll;
-    a->piece = std::max(1, (a->rows + cap - 1) / cap);
-    a->workers = a->total = (a->rows + a->piece - 1) / a->piece;
-  }
+  a->mode = a->groups == 1 || !conditioned ? kSumAll : a->per > 1 && wanted ? kSumGroups : kSumWeighted;
+  a->workers = std::min(a->rows, most_workers(a->d));
   *part_floats = (size_t)a->workers * 3 * (size_t)a->d;
+  *group_floats = a->mode == kSumGroups ? 2 * *part_floats : 0;
 }
 
 cudaError_t launch_residual_norm(const ResidualNormArgs& a, cudaStream_t st) {
@@ -159,7 +139,7 @@ cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_
              whole(a.dgate, a.lddgate, a.tc) && whole(a.dscale, a.lddscale, a.tc) && whole(a.dshift, a.lddshift, a.tc);
   if ((e = launch_rows(g, vec, true, st)) != cudaSuccess) return e;
   const int strips = (a.d + 31) / 32;
-  if (a.mode == kSumGroups && a.pieces > 1 &&
+  if (a.mode == kSumGroups && g.share % g.per != 0 &&     // (else no group crosses workers)
       (e = row_launch(k_residual_join_groups, dim3((unsigned)((int64_t)a.groups * strips)), 256, 0, 1, st, g, strips)) != cudaSuccess)
     return e;
   const bool any = a.dw || a.db || a.dwp || (a.mode == kSumAll && (a.dgate || a.dscale || a.dshift));

@@ -9,13 +9,13 @@
 //   dx  = dn (1 + scale) w
 //   g   = dr + s (dx - <dx> - xhat <dx xhat>)                       (rms: without <dx>); the gradient of r
 //   dq  = alpha gate D g,   dh = dq or, behind post, the same formula with dq wp and post's statistics
-// Sums over the rows of a group: A = sum dn xhat, B = sum dn, C = sum g D q/wp. They give every gradient of a vector:
-//   dshift = B, dscale = w A + b B, dgate = alpha wp C;  dw = sum_groups (1 + scale) A, db = sum_groups (1 + scale) B,
-//   dwp = sum_groups alpha gate C.
+// Sums over the rows of a group: A = sum dn xhat, B = sum dn, C = sum alpha D g q / wp. They give every gradient of a vector:
+//   dshift = B, dscale = w A + b B, dgate = wp C;  dw = sum_groups (1 + scale) A, db = sum_groups (1 + scale) B,
+//   dwp = sum_groups gate C.
 //
 // Bound by memory: r, h in and r', n out; r, h, dn, dr in and the gradients of r and h out. The backward pass makes r' again from r and
 // h, which it needs anyway, so r' need not be kept, and xhat is not that of a rounded r'. A group of threads holds a row in registers,
-// eight columns a thread. Statistics are held in float; layer norm takes them around the rounded mean and takes the mean's
+// eight columns a thread, in pairs (the row kernels would otherwise be bound by issue). Statistics are held in float; layer norm takes them around the rounded mean and takes the mean's
 // remainder back out, so that rows far from zero keep 24 bits of their spread.
 //
 // Sums over rows: a worker (the group of threads) adds its rows in registers, workers' sums are added by a second kernel in a
@@ -34,297 +34,483 @@ namespace sds {
 namespace {
 
 constexpr int kStreamDropout = 3;
-constexpr int kE = 8;                             // columns of a thread: one 16-byte access of 16-bit types, one block of the generator
+constexpr int kBlock = 8;                         // columns of one access of 16-bit types, and of one block of the generator
 
 // how the rows of a backward call are dealt out (ResidualNormArgs::mode)
 enum ResidualMode : int {
   kSumAll = 0,      // one group: a worker's rows, their plain sums A, B, C
   kSumWeighted = 1, // sums weighted with each row's own scale and gate; rows that are groups of their own write their gradients at once
-  kSumGroups = 2,   // pieces of groups: plain sums per piece, and the worker's weighted sums over its pieces
+  kSumGroups = 2,   // plain sums per group, whole ones and parts of those that cross workers, and the worker's weighted sums over them
 };
 
-// eight columns of a thread as they lie in memory
-template <class T, bool VEC> struct Raw;
-template <class T> struct Raw<T, true> {
+// eight neighbouring columns as they lie in memory
+template <class T> struct Raw {
   static constexpr int kUnits = sizeof(T) / 2;
   uint4 q[kUnits];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) q[i] = *(reinterpret_cast<const uint4*>(p) + i);
   }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) q[i] = make_uint4(0u, 0u, 0u, 0u);
-  }
 };
-
-__device__ __forceinline__ void words_to(const uint4 (&q)[2], float (&o)[kE], float) {
-  const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
-#pragma unroll
-  for (int e = 0; e < kE; ++e) o[e] = __uint_as_float(w[e]);
+// as four pairs of floats
+constexpr int P = kBlock / 2;
+__device__ __forceinline__ void words_to(const uint4* q, float2 (&o)[P], float) {
+  o[0] = make_float2(__uint_as_float(q[0].x), __uint_as_float(q[0].y));
+  o[1] = make_float2(__uint_as_float(q[0].z), __uint_as_float(q[0].w));
+  o[2] = make_float2(__uint_as_float(q[1].x), __uint_as_float(q[1].y));
+  o[3] = make_float2(__uint_as_float(q[1].z), __uint_as_float(q[1].w));
 }
-__device__ __forceinline__ void words_to(const uint4 (&q)[1], float (&o)[kE], Bf16) {
-  const uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o[2 * i] = __uint_as_float(w[i] << 16);
-    o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+__device__ __forceinline__ float2 pair_of(uint32_t w, Bf16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 pair_of(uint32_t w, F16) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+template <class T> __device__ __forceinline__ void words_to(const uint4* q, float2 (&o)[P], T t) {
+  o[0] = pair_of(q[0].x, t); o[1] = pair_of(q[0].y, t); o[2] = pair_of(q[0].z, t); o[3] = pair_of(q[0].w, t);
 }
-__device__ __forceinline__ void words_to(const uint4 (&q)[1], float (&o)[kE], F16) {
-  const uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    o[2 * i] = v.x;
-    o[2 * i + 1] = v.y;
-  }
+// (eight floats are one 32-byte store: as two of 16 bytes a warp would write half a sector at a time)
+__device__ __forceinline__ void store_words(float* p, const float2 (&v)[P]) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y),
+               "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y)
+               : "memory");
 }
-__device__ __forceinline__ void store_words(float* p, const float (&v)[kE]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-template <class T> __device__ __forceinline__ void store_words(T* p, const float (&v)[kE]) {
+template <class T> __device__ __forceinline__ void store_words(T* p, const float2 (&v)[P]) {
   Pack<T, 8> o;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) put2(o, i, make_float2(v[2 * i], v[2 * i + 1]));
+  for (int i = 0; i < P; ++i) put2(o, i, v[i]);
   *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&o);
 }
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float& element(float2* v, int e) { return reinterpret_cast<float*>(v)[e]; }
+__device__ __forceinline__ float element(const float2* v, int e) { return reinterpret_cast<const float*>(v)[e]; }
+// (rows lie less than 2^31 elements apart: one multiplication)
+template <class T> __device__ __forceinline__ T* row_of(void* p, int row, int64_t ld) {
+  return static_cast<T*>(p) + (uint64_t)(uint32_t)row * (uint32_t)ld;
+}
+template <class T> __device__ __forceinline__ const T* row_of(const void* p, int row, int64_t ld) {
+  return static_cast<const T*>(p) + (uint64_t)(uint32_t)row * (uint32_t)ld;
+}
 
-// The columns of a group's thread t. VEC: eight neighbours. Else: 32 neighbours for a warp, eight times, each as many columns further as the
-// group has threads in a CTA.
+// A group of TPR threads holds a row, T of them in each of CL CTAs.
+template <int TPR, int CL> struct ResidualShape {
+  static constexpr int T = TPR / CL;
+  static constexpr int kCta = T < 128 ? 128 : T;
+  static constexpr int kRows = kCta / T;                        // rows of a CTA at a time
+  static constexpr int kSlots = 2 * kRows * 4 * (TPR > 32 ? TPR / 32 : 1);
+  static constexpr int kStatSlots = kCta / (T < 32 ? T : 32);   // a row's statistics, for each warp (or each group in a warp)
+};
+
+// The eight columns of a group's thread t. VEC: neighbours; a thread beyond d computes on whatever it holds and is left out of sums and
+// stores. Else: T apart, so that a warp's accesses are neighbours; columns beyond d hold zeros.
 template <int TPR, int CL, bool VEC> struct Columns {
   static constexpr int T = TPR / CL;
-  int c0;
-  __device__ explicit Columns(int t) : c0(VEC ? t * kE : t / T * T * kE + t % T) {}
+  int c0, tid, d;
+  bool live;
+  __device__ Columns(int t, int d_) : c0(VEC ? t * kBlock : t / T * T * kBlock + t % T), tid(t % T), d(d_) { live = c0 < d; }
   __device__ __forceinline__ int at(int e) const { return VEC ? c0 + e : c0 + e * T; }
+  __device__ __forceinline__ bool has(int e) const { return VEC ? live : c0 + e * T < d; }
 };
 
 template <class T, class C>
-__device__ __forceinline__ void load_scalar(const T* row, const C& col, int d, float (&o)[kE]) {
+__device__ __forceinline__ void load_scalar(const T* row, const C& col, float2 (&o)[P]) {
 #pragma unroll
-  for (int e = 0; e < kE; ++e) o[e] = col.at(e) < d ? Conv<T>::get(row[col.at(e)]) : 0.f;
+  for (int e = 0; e < kBlock; ++e) element(o, e) = col.has(e) ? Conv<T>::get(row[col.at(e)]) : 0.f;
 }
-template <class T, bool VEC, class C>
-__device__ __forceinline__ void store_row(T* row, const C& col, int d, const float (&v)[kE]) {
+template <class T, int TPR, int CL, bool VEC>
+__device__ __forceinline__ void store_row(T* row, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
   if (VEC) {
-    if (col.c0 < d) store_words(row + col.c0, v);
+    if (on && col.live) store_words(row + col.c0, v);
   } else {
 #pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (col.at(e) < d) row[col.at(e)] = Conv<T>::put(v[e]);
+    for (int e = 0; e < kBlock; ++e)
+      if (on && col.has(e)) row[col.at(e)] = Conv<T>::put(element(v, e));
   }
 }
 
-// a thread's columns of a vector of any of the three types, `fill` where there is none
-template <bool VEC, class C>
-__device__ __forceinline__ void load_vector8(const void* p, int type, bool wide, size_t off, const C& col, int d, float fill, float (&o)[kE]) {
-  if (!p) {
-#pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = fill;
-  } else if (VEC && wide) {
-    if (col.c0 >= d) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e) o[e] = 0.f;
-    } else if (type == SDS_F32) {
-      Raw<float, true> r;
-      r.load(static_cast<const float*>(p) + off + col.c0);
-      words_to(r.q, o, 0.f);
-    } else if (type == SDS_BF16) {
-      Raw<Bf16, true> r;
-      r.load(static_cast<const Bf16*>(p) + off + col.c0);
-      words_to(r.q, o, Bf16{});
-    } else {
-      Raw<F16, true> r;
-      r.load(static_cast<const F16*>(p) + off + col.c0);
-      words_to(r.q, o, F16{});
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = col.at(e) < d ? load_any(p, type, off + col.at(e)) : 0.f;
-  }
-}
-template <bool VEC, class C>
-__device__ __forceinline__ void store_vector8(void* p, int type, bool wide, size_t off, const C& col, int d, const float (&v)[kE]) {
-  if (VEC && wide) {
-    if (col.c0 >= d) return;
-    if (type == SDS_F32) store_words(static_cast<float*>(p) + off + col.c0, v);
-    else if (type == SDS_BF16) store_words(static_cast<Bf16*>(p) + off + col.c0, v);
-    else store_words(static_cast<F16*>(p) + off + col.c0, v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (col.at(e) < d) store_any(p, type, off + col.at(e), v[e]);
-  }
-}
-
-// One bit for each of the eight columns of a block: kept. 16 of the block's 128 bits decide a column, low half of a word first.
-__device__ __forceinline__ uint32_t kept_block(const DropoutArgs& a, uint32_t step, uint64_t row, uint32_t block) {
-  const uint4 x = philox_block(a.seed, kStreamDropout, row, step, block);
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t kept = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    kept |= ((w[i] & 0xffffu) >= a.threshold ? 1u : 0u) << (2 * i);
-    kept |= ((w[i] >> 16) >= a.threshold ? 1u : 0u) << (2 * i + 1);
-  }
-  return kept;
-}
-// The same for a thread's columns. Where these are not one block, a warp's 256 columns are 32 blocks: a lane draws one, and the
-// bits change hands. (All 32 lanes call it.)
+// A thread's columns of a vector of any of the three types. 16-bit `wide` vectors (whole 16-byte pieces, VEC only) can be requested
+// ahead, as they lie in memory; floats are read where they are used (twice the registers, and they mostly lie in L1).
 template <int TPR, int CL, bool VEC>
-__device__ __forceinline__ uint32_t kept_columns(const DropoutArgs& a, uint32_t step, int row, const Columns<TPR, CL, VEC>& col, int lane) {
-  if (VEC) return kept_block(a, step, a.row0 + (uint32_t)row, (uint32_t)col.c0 >> 3);
-  const uint32_t mine = kept_block(a, step, a.row0 + (uint32_t)row,
-                                   (uint32_t)(col.c0 - lane + (lane >> 2) * Columns<TPR, CL, VEC>::T + (lane & 3) * 8) >> 3);
-  uint32_t kept = 0;
+__device__ __forceinline__ void request_vector(uint4& r, const void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col) {
+  if (VEC && wide && p && type != SDS_F32 && col.live) r = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + off + col.c0));
+}
+// (p is not NULL)
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ void take_vector(const uint4& r, const void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col,
+                                            float2 (&o)[P]) {
+  if (VEC && wide) {
+    if (type == SDS_F32) {
+      const uint4* from = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + off + (col.live ? col.c0 : 0));
+      const uint4 q[2] = {__ldg(from), __ldg(from + 1)};
+      words_to(q, o, 0.f);
+    } else if (type == SDS_BF16) {
+      words_to(&r, o, Bf16{});
+    } else {
+      words_to(&r, o, F16{});
+    }
+  } else if (type == SDS_F32) {
+    load_scalar(static_cast<const float*>(p) + off, col, o);
+  } else if (type == SDS_BF16) {
+    load_scalar(static_cast<const Bf16*>(p) + off, col, o);
+  } else {
+    load_scalar(static_cast<const F16*>(p) + off, col, o);
+  }
+}
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ void load_vector(const void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col, float2 (&o)[P]) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  request_vector(r, p, type, wide, off, col);
+  take_vector(r, p, type, wide, off, col, o);
+}
+template <class T, int TPR, int CL, bool VEC>
+__device__ __forceinline__ void store_typed_vector(T* p, bool wide, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
+  if (VEC && wide) {
+    if (on && col.live) store_words(p + col.c0, v);
+  } else {
 #pragma unroll
-  for (int e = 0; e < kE; ++e) kept |= ((__shfl_sync(kAll, mine, e * 4 + (lane >> 3)) >> (lane & 7)) & 1u) << e;
+    for (int e = 0; e < kBlock; ++e)
+      if (on && col.has(e)) p[col.at(e)] = Conv<T>::put(element(v, e));
+  }
+}
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ void store_vector(void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
+  if (type == SDS_F32) store_typed_vector(static_cast<float*>(p) + off, wide, col, on, v);
+  else if (type == SDS_BF16) store_typed_vector(static_cast<Bf16*>(p) + off, wide, col, on, v);
+  else store_typed_vector(static_cast<F16*>(p) + off, wide, col, on, v);
+}
+// where a group's row of gate, scale or shift begins
+__device__ __forceinline__ uint64_t cond_at(int group, int64_t ld) { return (uint64_t)(uint32_t)group * (uint32_t)ld; }
+
+// Which of a thread's eight columns are kept: 16 of the block's 128 bits decide a column, low half of a word first.
+struct Kept {
+  uint32_t w[4], limit;                                         // limit: the threshold in the upper half
+  __device__ __forceinline__ bool operator()(int e) const { return ((e & 1) ? w[e / 2] : w[e / 2] << 16) >= limit; }
+};
+__device__ __forceinline__ Kept kept_block(const DropoutArgs& a, uint32_t step, uint64_t row, uint32_t block) {
+  const uint4 x = philox_block(a.seed, kStreamDropout, row, step, block);
+  Kept k{{x.x, x.y, x.z, x.w}, a.threshold << 16};
+  if (a.threshold >= 65536u) {                                  // nothing is kept
+    k.w[0] = k.w[1] = k.w[2] = k.w[3] = 0u;
+    k.limit = ~0u;
+  }
+  return k;
+}
+// The same for a thread's columns. Where these are not a block, the blocks of a warp's (or of a smaller group's) columns are drawn one by
+// a lane, and a bit for each column changes hands. (All 32 lanes call it.)
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ Kept kept_columns(const DropoutArgs& a, uint32_t step, int row, const Columns<TPR, CL, VEC>& col, int lane) {
+  constexpr int T = TPR / CL, W = T < 32 ? T : 32, kPer = W / 8;     // W neighbours are kPer blocks
+  const uint64_t r = a.row0 + (uint32_t)row;
+  if (VEC) return kept_block(a, step, r, (uint32_t)col.c0 >> 3);
+  const int in = lane % W;
+  const Kept mine = kept_block(a, step, r, (uint32_t)(col.c0 - in + in / kPer * T + in % kPer * 8) >> 3);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < kBlock; ++e) bits |= (mine(e) ? 1u : 0u) << e;
+  Kept kept{{0u, 0u, 0u, 0u}, 0x80000000u};                     // (a kept column has the top bit of its half)
+#pragma unroll
+  for (int e = 0; e < kBlock; ++e) {
+    const uint32_t bit = (__shfl_sync(kAll, bits, lane - in + e * kPer + (in >> 3)) >> (in & 7)) & 1u;
+    kept.w[e / 2] |= bit << ((e & 1) ? 31 : 15);
+  }
   return kept;
 }
 __device__ __forceinline__ uint32_t dropout_step(const DropoutArgs& a) { return a.step + (a.step_dev ? (uint32_t)*a.step_dev : 0u); }
+
+// r + k q where a column is kept, else r
+__device__ __forceinline__ void add_branch(float2& r, float2 k, float2 q, bool drops, const Kept& kept, int i) {
+  if (!drops) {
+    r = fma2(k, q, r);
+  } else {
+    if (kept(2 * i)) r.x = fmaf(k.x, q.x, r.x);
+    if (kept(2 * i + 1)) r.y = fmaf(k.y, q.y, r.y);
+  }
+}
+// v where a column is kept, else 0
+__device__ __forceinline__ float2 select_kept(float2 v, const Kept& kept, int i) {
+  return make_float2(kept(2 * i) ? v.x : 0.f, kept(2 * i + 1) ? v.y : 0.f);
+}
 
 // Sums over a group, each call in the other half of its slots: a half is written again only after the barrier of the call between.
 template <int TPR, int CL> struct GroupSums {
   static constexpr int NW = TPR > 32 ? TPR / 32 : 1;
   float* slot;
   int t, bar, flip = 0;
-  __device__ GroupSums(float* slots, int sub, int t_) : slot(slots + sub * 8 * NW), t(t_), bar(1 + sub) {}
+  bool live;                                                    // threads beyond d are left out
+  __device__ GroupSums(float* slots, int sub, int t_, bool live_) : slot(slots + sub * 8 * NW), t(t_), bar(1 + sub), live(live_) {}
   template <int N> __device__ __forceinline__ void operator()(float (&v)[N]) {
-    group_sum<TPR, N, CL>(v, slot + flip * 4 * NW, t, bar);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = live ? v[n] : 0.f;
+    float* at = slot + flip * 4 * NW;
     flip ^= 1;
+    if constexpr (NW < 4 || NW > 16 || CL > 1) {
+      group_sum<TPR, N, CL>(v, at, t, bar);
+    } else {                                                    // four warps' sums at a time
+      group_post<TPR, N, 1>(v, at, t);
+      asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(TPR) : "memory");
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < NW; w += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(at + n * NW + w);
+          const float2 two = add2(make_float2(q.x, q.y), make_float2(q.z, q.w));
+          s = w == 0 ? two : add2(s, two);
+        }
+        v[n] = total(s);
+      }
+    }
   }
 };
 
-// r + alpha gate D q, in the forward pass and again in the backward one
-__device__ __forceinline__ float add_branch(float r, float k, float q, uint32_t kept, int e, const DropoutArgs& drop) {
-  return (kept >> e) & 1u ? fmaf(drop.threshold ? k * drop.scale : k, q, r) : r;
+// v - m, and (v - rest) s, where there are columns
+template <class C>
+__device__ __forceinline__ void shift_row(float2 (&v)[P], float m, const C& col, bool vec) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = add2(v[i], both(-m));
+  } else {
+#pragma unroll
+    for (int e = 0; e < kBlock; ++e) element(v, e) = col.has(e) ? element(v, e) - m : 0.f;
+  }
+}
+template <class C>
+__device__ __forceinline__ void scale_row(float2 (&v)[P], float rest, float s, const C& col, bool vec) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = fma2(v[i], both(s), both(-rest * s));
+  } else {
+#pragma unroll
+    for (int e = 0; e < kBlock; ++e) element(v, e) = col.has(e) ? (element(v, e) - rest) * s : 0.f;
+  }
+}
+// sums of a and of a b over the thread's columns
+__device__ __forceinline__ void pair_sums(const float2 (&a)[P], const float2 (&b)[P], float (&s)[2]) {
+  float2 x = a[0], y = mul2(a[0], b[0]);
+#pragma unroll
+  for (int i = 1; i < P; ++i) {
+    x = add2(x, a[i]);
+    y = fma2(a[i], b[i], y);
+  }
+  s[0] = total(x);
+  s[1] = total(y);
 }
 
-struct RowStats { float mean, rest, scale; };
-// Turns the row v into xhat. Columns beyond d hold zeros, and do so afterwards.
-template <int TPR, int CL, class C>
-__device__ __forceinline__ RowStats normalise(float (&v)[kE], GroupSums<TPR, CL>& sums, const C& col, int d, float inv_d, bool rms, float eps) {
-  RowStats st{0.f, 0.f, 0.f};
+// Turns the row v into xhat; mean, remainder, 1 / size.
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ float4 normalise(float2 (&v)[P], GroupSums<TPR, CL>& sums, const Columns<TPR, CL, VEC>& col, float inv_d, bool rms, float eps) {
+  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
   if (rms) {
-    float s[1] = {0.f};
+    float2 x = mul2(v[0], v[0]);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) s[0] = fmaf(v[e], v[e], s[0]);
+    for (int i = 1; i < P; ++i) x = fma2(v[i], v[i], x);
+    float s[1] = {total(x)};
     sums(s);
-    st.scale = rsqrtf(fmaf(s[0], inv_d, eps));
-  } else {
-    float s[1] = {0.f};
+    st.z = rsqrtf(fmaf(s[0], inv_d, eps));
 #pragma unroll
-    for (int e = 0; e < kE; ++e) s[0] += v[e];
-    sums(s);
-    st.mean = s[0] * inv_d;
-    float q[2] = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      v[e] = col.at(e) < d ? v[e] - st.mean : 0.f;
-      q[0] += v[e];
-      q[1] = fmaf(v[e], v[e], q[1]);
-    }
-    sums(q);
-    st.rest = q[0] * inv_d;
-    st.scale = rsqrtf(fmaf(-st.rest, st.rest, q[1] * inv_d) + eps);
-#pragma unroll
-    for (int e = 0; e < kE; ++e) v[e] = col.at(e) < d ? v[e] - st.rest : 0.f;
+    for (int i = 0; i < P; ++i) v[i] = mul2(v[i], both(st.z));
+    return st;
   }
+  float2 x = v[0];
 #pragma unroll
-  for (int e = 0; e < kE; ++e) v[e] *= st.scale;
+  for (int i = 1; i < P; ++i) x = add2(x, v[i]);
+  float s[1] = {total(x)};
+  sums(s);
+  st.x = s[0] * inv_d;
+  shift_row(v, st.x, col, VEC);
+  float q[2];
+  pair_sums(v, v, q);
+  sums(q);
+  st.y = q[0] * inv_d;
+  st.z = rsqrtf(fmaf(-st.y, st.y, q[1] * inv_d) + eps);
+  scale_row(v, st.y, st.z, col, VEC);
   return st;
 }
 
-template <int TPR, int CL> struct ResidualShape {
-  static constexpr int T = TPR / CL;                            // threads of a row in one CTA
-  static constexpr int kCta = T < 128 ? 128 : T;
-  static constexpr int kRows = kCta / T;                        // rows of a CTA at a time
-  static constexpr int kSlots = 2 * kRows * 4 * (TPR > 32 ? TPR / 32 : 1);
-};
+// ---------------------------------------------------------------------------------------------
+// rows to come: a ring in shared memory
+// ---------------------------------------------------------------------------------------------
 
+// VEC: a warp copies and reads its own columns, so there is no barrier, and the copies take no registers. Else the group copies the
+// 16-byte pieces that cover its CTA's part of the row (they may begin up to 15 bytes before it and end as many behind: within
+// pieces of memory that hold some of the row), and reads elements, behind a barrier.
+template <class T, int TPR, int CL, bool VEC> struct RingRow {
+  using S = ResidualShape<TPR, CL>;
+  static constexpr int kUnits = sizeof(T) / 2;                  // 16-byte pieces of eight columns
+  static constexpr int kGroup = S::T * kUnits + 2;              // not VEC: pieces of a group
+  static constexpr int kPieces = VEC ? kUnits * S::kCta : kGroup * S::kRows;
+};
+constexpr int kRingStages = 3;
+// where piece u of a row of floats lies: a lane reads two neighbouring pieces, eight lanes from all banks
+__device__ __forceinline__ int ring_piece(int u) { return u ^ ((u >> 3) & 1); }
+
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kRingStages - 2) : "memory"); }
+
+template <class T, int TPR, int CL, bool VEC>
+__device__ __forceinline__ void ring_copy(uint4* to, const T* row, const Columns<TPR, CL, VEC>& col, int sub) {
+  using R = RingRow<T, TPR, CL, VEC>;
+  using S = ResidualShape<TPR, CL>;
+  if (VEC) {
+    if (R::kUnits == 1) {
+      if (col.live) copy16(to + threadIdx.x, row + col.c0);
+    } else {                                                    // lanes copy neighbouring pieces: whole sectors
+      constexpr int W = S::T < 32 ? S::T : 32;
+      const int in = (int)threadIdx.x % W, u0 = ((int)threadIdx.x - in) * 2 + in, first = col.c0 - in * kBlock;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (first + (in + i * W) * 4 < col.d) copy16(to + ring_piece(u0 + i * W), row + first + (in + i * W) * 4);
+    }
+  } else {
+    const int part = col.c0 - col.tid, n = min(col.d - part, S::T * kBlock);      // the CTA's columns
+    if (n <= 0) return;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(row + part);
+    const char* from = reinterpret_cast<const char*>(first & ~(uintptr_t)15);
+    const int pieces = ((int)(first & 15) + n * (int)sizeof(T) + 15) >> 4;
+#pragma unroll
+    for (int k = 0; k <= R::kUnits; ++k) {                      // (R::kGroup pieces at most: one beyond T kUnits at most where T > 1)
+      const int i = col.tid + k * S::T;
+      if (i < pieces) copy16(to + sub * R::kGroup + i, from + 16 * i);
+    }
+  }
+}
+template <class T, int TPR, int CL, bool VEC>
+__device__ __forceinline__ void ring_take(const uint4* from, const T* row, const Columns<TPR, CL, VEC>& col, int sub, float2 (&o)[P]) {
+  using R = RingRow<T, TPR, CL, VEC>;
+  using S = ResidualShape<TPR, CL>;
+  if (VEC) {
+    uint4 w[R::kUnits];
+#pragma unroll
+    for (int i = 0; i < R::kUnits; ++i) w[i] = from[R::kUnits == 1 ? (int)threadIdx.x : ring_piece(2 * (int)threadIdx.x + i)];
+    words_to(w, o, T{});
+  } else {
+    const char* mine = reinterpret_cast<const char*>(from + sub * R::kGroup) + (reinterpret_cast<uintptr_t>(row + (col.c0 - col.tid)) & 15);
+#pragma unroll
+    for (int e = 0; e < kBlock; ++e)
+      element(o, e) = col.has(e) ? Conv<T>::get(reinterpret_cast<const T*>(mine)[e * S::T + col.tid]) : 0.f;
+  }
+}
+// the group's copies are there for all of its threads
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ void ring_ready(int sub) {
+  copies_wait();
+  constexpr int T = TPR / CL;
+  if (!VEC && T > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "r"(T) : "memory");
+  else __syncwarp();
+}
+
+// A worker's rows are neighbours: `row` up to `end`, `group` the row's group and `left` its rows from here on.
+struct RowWalk {
+  int row, end, group, left;
+  __device__ RowWalk(const ResidualNormArgs& a, int worker) {
+    const int64_t first = (int64_t)worker * a.share;
+    row = (int)min((int64_t)a.rows, first);
+    end = min(a.rows - row, a.share) + row;
+    group = row / a.per;
+    left = a.per - (row - group * a.per);
+  }
+  __device__ __forceinline__ bool on() const { return row < end; }
+  __device__ __forceinline__ void next() { ++row; }
+  __device__ __forceinline__ void next_group(int per) {         // behind next()
+    if (--left == 0) { ++group; left = per; }
+  }
+};
+// whether the worker, or another one of its warp (small groups: the warp's lanes stay together), has a row left
+template <int T> __device__ __forceinline__ bool rows_left(bool on) { return T < 32 ? __any_sync(kAll, on) : on; }
+
+// A group takes neighbouring rows, which mostly share their row of gate, scale and shift. Rows come through the ring, vectors are requested
+// before the sums that they wait for.
 template <class TR, class TH, int TPR, int CL, bool VEC>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;
+  constexpr int kR = RingRow<TR, TPR, CL, VEC>::kPieces, kStage = kR + RingRow<TH, TPR, CL, VEC>::kPieces;
+  extern __shared__ uint4 ring[];
   __shared__ __align__(16) float slots[S::kSlots];
   const int sub = threadIdx.x / S::T, lane = threadIdx.x & 31;
   const int t = (CL > 1 ? (int)(blockIdx.x % CL) * S::T : 0) + (int)threadIdx.x % S::T;
-  const Columns<TPR, CL, VEC> col(t);
-  GroupSums<TPR, CL> sums(slots, sub, t);
+  const Columns<TPR, CL, VEC> col(t, a.d);
+  GroupSums<TPR, CL> sums(slots, sub, t, !VEC || col.live);
   if (CL > 1) {                                                 // the peers' slots are there to be written
     cluster_arrive();
     cluster_wait();
   }
   start_after_prior_kernel();
-  const int d = a.d, step = (int)gridDim.x / CL * S::kRows;
-  const float inv_d = 1.0f / (float)d;
-  const uint32_t dstep = a.drop.threshold ? dropout_step(a.drop) : 0u;
-  const bool live = col.c0 < d;
-  Raw<TR, true> rn;
-  Raw<TH, true> hn;
-  const auto fetch = [&](int row) {
-    if (!VEC) return;
-    rn.zero();
-    hn.zero();
-    if (live && row < a.rows) {
-      rn.load(static_cast<const TR*>(a.r) + (size_t)row * a.ldr + col.c0);
-      if (a.h) hn.load(static_cast<const TH*>(a.h) + (size_t)row * a.ldh + col.c0);
+  const float inv_d = 1.0f / (float)a.d;
+  const bool drops = a.drop.threshold != 0;
+  const uint32_t dstep = drops ? dropout_step(a.drop) : 0u;
+  const float2 alpha = both(drops ? a.alpha * a.drop.scale : a.alpha);
+  RowWalk at(a, (int)blockIdx.x / CL * S::kRows + sub);
+  const auto request = [&](int row, int stage) {
+    if (row < at.end) {
+      uint4* to = ring + stage * kStage;
+      ring_copy(to, row_of<TR>(a.r, row, a.ldr), col, sub);
+      if (a.h) ring_copy(to + kR, row_of<TH>(a.h, row, a.ldh), col, sub);
     }
+    copies_end();
   };
-  int row = (int)blockIdx.x / CL * S::kRows + sub;
-  fetch(row);
-  for (; row < a.rows; row += step) {
-    float v[kE], q[kE];
-    if (VEC) {
-      words_to(rn.q, v, TR{});
-      words_to(hn.q, q, TH{});
-    } else {
-      load_scalar(static_cast<const TR*>(a.r) + (size_t)row * a.ldr, col, d, v);
-      if (a.h) load_scalar(static_cast<const TH*>(a.h) + (size_t)row * a.ldh, col, d, q);
-    }
-    if (row < a.rows - step) fetch(row + step);
-    const int group = a.per == 1 ? row : row / a.per;
+  for (int s = 0; s < kRingStages - 1; ++s) request(at.row + s, s);
+  int stage = 0;
+  while (rows_left<S::T>(at.on())) {
+    const bool on = at.on();
+    const int row = on ? at.row : 0, group = on ? at.group : 0;
+    float2 v[P], q[P], x[P];
+    uint4 gate, scale, shift;
+    if (a.h) request_vector(gate, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col);
+    request_vector(scale, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col);
+    request_vector(shift, a.shift, a.tc, a.wide_c, cond_at(group, a.ldshift), col);
+    ring_ready<TPR, CL, VEC>(sub);
+    const uint4* mine = ring + stage * kStage;
+    ring_take(mine, row_of<TR>(a.r, row, a.ldr), col, sub, v);
     if (a.h) {
+      ring_take(mine + kR, row_of<TH>(a.h, row, a.ldh), col, sub, q);
       if (a.post) {
-        const RowStats st = normalise(q, sums, col, d, inv_d, a.rms, a.eps);
-        float wp[kE];
-        load_vector8<VEC>(a.wp, a.tw, a.wide_w, 0, col, d, 1.f, wp);
+        const float4 st = normalise(q, sums, col, inv_d, a.rms, a.eps);
+        if (a.wp) {
+          load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) q[e] *= wp[e];
-        if (a.stats && t == 0) {
-          a.stats[(size_t)3 * a.rows + row] = st.mean;
-          a.stats[(size_t)4 * a.rows + row] = st.rest;
-          a.stats[(size_t)5 * a.rows + row] = st.scale;
+          for (int i = 0; i < P; ++i) q[i] = mul2(q[i], x[i]);
         }
+        if (a.stats && t == 0 && on) a.stats[2 * (size_t)row + 1] = st;
       }
-      const uint32_t kept = a.drop.threshold ? kept_columns(a.drop, dstep, row, col, lane) : 0xffu;
-      float gate[kE];
-      load_vector8<VEC>(a.gate, a.tc, a.wide_c, (size_t)group * a.ldgate, col, d, 1.f, gate);
+      Kept kept;
+      if (drops) kept = kept_columns(a.drop, dstep, row, col, lane);
+      if (a.gate) {
+        take_vector(gate, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col, x);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) v[e] = add_branch(v[e], a.alpha * gate[e], q[e], kept, e, a.drop);
-      store_row<TR, VEC>(static_cast<TR*>(a.out) + (size_t)row * a.ldo, col, d, v);
-    }
-    const RowStats st = normalise(v, sums, col, d, inv_d, a.rms, a.eps);
-    if (a.stats && t == 0) {
-      a.stats[row] = st.mean;
-      a.stats[(size_t)a.rows + row] = st.rest;
-      a.stats[(size_t)2 * a.rows + row] = st.scale;
-    }
-    if (a.w || a.b) {
-      float w[kE], b[kE];
-      load_vector8<VEC>(a.w, a.tw, a.wide_w, 0, col, d, 1.f, w);
-      load_vector8<VEC>(a.b, a.tw, a.wide_w, 0, col, d, 0.f, b);
+        for (int i = 0; i < P; ++i) add_branch(v[i], mul2(alpha, x[i]), q[i], drops, kept, i);
+      } else {
 #pragma unroll
-      for (int e = 0; e < kE; ++e) v[e] = fmaf(v[e], w[e], b[e]);
+        for (int i = 0; i < P; ++i) add_branch(v[i], alpha, q[i], drops, kept, i);
+      }
+      store_row(row_of<TR>(a.out, row, a.ldo), col, on, v);
     }
-    if (a.scale || a.shift) {
-      float sc[kE], sh[kE];
-      load_vector8<VEC>(a.scale, a.tc, a.wide_c, (size_t)group * a.ldscale, col, d, 0.f, sc);
-      load_vector8<VEC>(a.shift, a.tc, a.wide_c, (size_t)group * a.ldshift, col, d, 0.f, sh);
+    const float4 st = normalise(v, sums, col, inv_d, a.rms, a.eps);
+    // (behind a sum: all threads of the group are done with the row before, whose place this takes)
+    request(at.row + kRingStages - 1, stage == 0 ? kRingStages - 1 : stage - 1);
+    if (a.stats && t == 0 && on) a.stats[2 * (size_t)row] = st;
+    if (a.w) {
+      load_vector(a.w, a.tw, a.wide_w, 0, col, x);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) v[e] = fmaf(v[e], 1.0f + sc[e], sh[e]);
+      for (int i = 0; i < P; ++i) v[i] = mul2(v[i], x[i]);
     }
-    store_row<TH, VEC>(static_cast<TH*>(a.n) + (size_t)row * a.ldn, col, d, v);
+    if (a.b) {
+      load_vector(a.b, a.tw, a.wide_w, 0, col, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
+    }
+    if (a.scale) {
+      take_vector(scale, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = fma2(v[i], x[i], v[i]);
+    }
+    if (a.shift) {
+      take_vector(shift, a.shift, a.tc, a.wide_c, cond_at(group, a.ldshift), col, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
+    }
+    store_row(row_of<TH>(a.n, row, a.ldn), col, on, v);
+    at.next();
+    at.next_group(a.per);
+    stage = stage + 1 == kRingStages ? 0 : stage + 1;
   }
 }
 
@@ -332,52 +518,26 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
 // backward
 // ---------------------------------------------------------------------------------------------
 
-// The rows to come pass through a ring in shared memory, each thread's own columns: it copies and reads them itself, so there is no
-// barrier, and the copies take no registers.
-template <class TR, class TH> struct ResidualRing {
-  static constexpr int kStages = 3;
-  static constexpr int kR = sizeof(TR) / 2, kH = sizeof(TH) / 2;          // 16-byte pieces of a thread's columns
-  static constexpr int kPieces = 2 * kR + 2 * kH;                         // dr, r, dn, h
-};
-
-__device__ __forceinline__ void copy16(void* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-}
-
-// Where a worker stands: its row, the end of its piece, the piece.
-struct RowWalk {
-  int row, end, piece;
-  __device__ __forceinline__ void enter(const ResidualNormArgs& a, int p) {
-    piece = p;
-    if (a.mode == kSumGroups) {
-      const int g = p / a.pieces, j = p - g * a.pieces;
-      row = g * a.per + j * a.piece;
-      end = min(row + a.piece, (g + 1) * a.per);
-    } else {
-      row = p * a.piece;
-      end = min(row + a.piece, a.rows);
-    }
-  }
-  __device__ __forceinline__ bool done(const ResidualNormArgs& a) const { return piece >= a.total; }
-  __device__ __forceinline__ void next(const ResidualNormArgs& a) {
-    if (++row < end) return;
-    const int p = piece + a.workers;
-    if (p < a.total) enter(a, p);
-    else piece = a.total;
-  }
+template <class TR, class TH, int TPR, int CL, bool VEC> struct ResidualBwd {
+  using S = ResidualShape<TPR, CL>;
+  static constexpr int kR = RingRow<TR, TPR, CL, VEC>::kPieces, kH = RingRow<TH, TPR, CL, VEC>::kPieces;
+  static constexpr int kStats = 2 * kR + 2 * kH;                // dr, r, dn, h, then the statistics
+  static constexpr int kStage = kStats + 2 * S::kStatSlots;
+  static constexpr int kSmemBytes = kRingStages * kStage * 16;
+  static constexpr int kMinCtas = 512 / S::kCta;                // 512 threads of 128 registers
 };
 
 template <class TR, class TH, int TPR, int CL, bool VEC>
-__global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualShape<TPR, CL>::kCta <= 256 ? 512 / ResidualShape<TPR, CL>::kCta : 1)
-    k_residual_norm_bwd(const ResidualNormArgs a) {
+__global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, TH, TPR, CL, VEC>::kMinCtas) k_residual_norm_bwd(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;
-  using G = ResidualRing<TR, TH>;
-  extern __shared__ uint4 ring[];                               // [stage][piece][thread] (VEC)
+  using G = ResidualBwd<TR, TH, TPR, CL, VEC>;
+  constexpr int kWarp = S::T < 32 ? S::T : 32;
+  extern __shared__ uint4 ring[];
   __shared__ __align__(16) float slots[S::kSlots];
   const int sub = threadIdx.x / S::T, lane = threadIdx.x & 31;
   const int t = (CL > 1 ? (int)(blockIdx.x % CL) * S::T : 0) + (int)threadIdx.x % S::T;
-  const Columns<TPR, CL, VEC> col(t);
-  GroupSums<TPR, CL> sums(slots, sub, t);
+  const Columns<TPR, CL, VEC> col(t, a.d);
+  GroupSums<TPR, CL> sums(slots, sub, t, !VEC || col.live);
   if (CL > 1) {
     cluster_arrive();
     cluster_wait();
@@ -386,207 +546,230 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualShape<TP
   const int worker = (int)blockIdx.x / CL * S::kRows + sub;
   const int d = a.d;
   const float inv_d = 1.0f / (float)d;
-  const uint32_t dstep = a.drop.threshold ? dropout_step(a.drop) : 0u;
-  const bool live = col.c0 < d;
-  if (worker >= a.workers) return;                              // (a whole group; with clusters there is none)
-  float sa[kE] = {}, sb[kE] = {}, sc_[kE] = {};                 // A, B, C, or their weighted forms
+  const bool drops = a.drop.threshold != 0;
+  const uint32_t dstep = drops ? dropout_step(a.drop) : 0u;
+  const float2 alpha = both(drops ? a.alpha * a.drop.scale : a.alpha);     // of a kept column
+  float2 sa[P], sb[P], sq[P];                                   // A, B, C, or their weighted forms
+#pragma unroll
+  for (int i = 0; i < P; ++i) sa[i] = sb[i] = sq[i] = both(0.f);
   bool first_flush = true;
 
-  RowWalk ahead, at;
-  at.enter(a, worker);
-  ahead = at;
-  const auto request = [&](int stage) {
-    if (VEC && live && !ahead.done(a)) {
-      uint4* to = ring + (size_t)stage * G::kPieces * S::kCta + threadIdx.x;
-      const TR* dr = static_cast<const TR*>(a.dr) + (size_t)ahead.row * a.lddr + col.c0;
-      const TR* r = static_cast<const TR*>(a.r) + (size_t)ahead.row * a.ldr + col.c0;
-      const TH* dn = static_cast<const TH*>(a.dn) + (size_t)ahead.row * a.lddn + col.c0;
-      const TH* h = static_cast<const TH*>(a.h) + (size_t)ahead.row * a.ldh + col.c0;
-#pragma unroll
-      for (int i = 0; i < G::kR; ++i) {
-        if (a.dr) copy16(to + i * S::kCta, dr + i * 4);
-        copy16(to + (G::kR + i) * S::kCta, r + i * 4);
-      }
-#pragma unroll
-      for (int i = 0; i < G::kH; ++i) {
-        copy16(to + (2 * G::kR + i) * S::kCta, dn + i * 4);
-        if (a.h) copy16(to + (2 * G::kR + G::kH + i) * S::kCta, h + i * 4);
+  RowWalk at(a, worker);
+  const int begin = at.row;
+  const auto request = [&](int row, int stage) {
+    if (row < at.end) {
+      uint4* to = ring + stage * G::kStage;
+      if (a.dr) ring_copy(to, row_of<TR>(a.dr, row, a.lddr), col, sub);
+      ring_copy(to + G::kR, row_of<TR>(a.r, row, a.ldr), col, sub);
+      ring_copy(to + 2 * G::kR, row_of<TH>(a.dn, row, a.lddn), col, sub);
+      if (a.h) ring_copy(to + 2 * G::kR + G::kH, row_of<TH>(a.h, row, a.ldh), col, sub);
+      if (threadIdx.x % kWarp == 0) {
+        uint4* st = to + G::kStats + threadIdx.x / kWarp * 2;
+        copy16(st, a.stats + 2 * (size_t)row);
+        if (a.post) copy16(st + 1, a.stats + 2 * (size_t)row + 1);
       }
     }
-    if (!ahead.done(a)) ahead.next(a);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    copies_end();
   };
-  if (VEC)
-    for (int s = 0; s < G::kStages - 1; ++s) request(s);
+  for (int s = 0; s < kRingStages - 1; ++s) request(at.row + s, s);
   int stage = 0;
 
-  for (; !at.done(a);) {
-    const int row = at.row, group = a.per == 1 ? row : row / a.per;
-    float v[kE], q[kE], dx[kE], g[kE];
-    if (VEC) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(G::kStages - 2) : "memory");
-      const uint4* from = ring + (size_t)stage * G::kPieces * S::kCta + threadIdx.x;
-      const auto take = [&](auto type, int piece, float (&o)[kE], bool there) {
-        uint4 w[sizeof(type) / 2];
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(type) / 2; ++i) w[i] = there && live ? from[(piece + i) * S::kCta] : make_uint4(0u, 0u, 0u, 0u);
-        words_to(w, o, type);
-      };
-      take(TR{}, 0, g, a.dr != nullptr);
-      take(TR{}, G::kR, v, true);
-      take(TH{}, 2 * G::kR, dx, true);
-      take(TH{}, 2 * G::kR + G::kH, q, a.h != nullptr);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kE; ++e) g[e] = q[e] = 0.f;
-      if (a.dr) load_scalar(static_cast<const TR*>(a.dr) + (size_t)row * a.lddr, col, d, g);
-      load_scalar(static_cast<const TR*>(a.r) + (size_t)row * a.ldr, col, d, v);
-      load_scalar(static_cast<const TH*>(a.dn) + (size_t)row * a.lddn, col, d, dx);
-      if (a.h) load_scalar(static_cast<const TH*>(a.h) + (size_t)row * a.ldh, col, d, q);
-    }
-    if (VEC) {
-      const int free_stage = stage == 0 ? G::kStages - 1 : stage - 1;     // (its row is done)
-      request(free_stage);
-      stage = stage + 1 == G::kStages ? 0 : stage + 1;
-    }
+  while (rows_left<S::T>(at.on())) {
+    const bool on = at.on();
+    const int row = on ? at.row : 0, group = on ? at.group : 0;
+    uint4 gate_raw, scale_raw;
+    if (a.h) request_vector(gate_raw, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col);
+    request_vector(scale_raw, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col);
+    ring_ready<TPR, CL, VEC>(sub);
+    const uint4* mine = ring + stage * G::kStage;
+    const float4* stats = reinterpret_cast<const float4*>(mine + G::kStats + threadIdx.x / kWarp * 2);
+    float2 v[P], q[P], dx[P], x[P];
+    ring_take(mine + G::kR, row_of<TR>(a.r, row, a.ldr), col, sub, v);
     // r' again, and xhat
-    uint32_t kept = 0xffu;
-    float gate[kE], wp[kE];
+    Kept kept;
     float post_scale = 1.f;
     if (a.h) {
+      ring_take(mine + 2 * G::kR + G::kH, row_of<TH>(a.h, row, a.ldh), col, sub, q);
+      if (drops) kept = kept_columns(a.drop, dstep, row, col, lane);
       if (a.post) {
-        const float pm = a.stats[(size_t)3 * a.rows + row], pr = a.stats[(size_t)4 * a.rows + row];
-        post_scale = a.stats[(size_t)5 * a.rows + row];
-#pragma unroll
-        for (int e = 0; e < kE; ++e) q[e] = col.at(e) < d ? ((q[e] - pm) - pr) * post_scale : 0.f;
+        const float4 st = stats[1];
+        post_scale = st.z;
+        shift_row(q, st.x, col, VEC);
+        scale_row(q, st.y, st.z, col, VEC);
       }
-      load_vector8<VEC>(a.wp, a.tw, a.wide_w, 0, col, d, 1.f, wp);
-      load_vector8<VEC>(a.gate, a.tc, a.wide_c, (size_t)group * a.ldgate, col, d, 1.f, gate);
-      if (a.drop.threshold) kept = kept_columns(a.drop, dstep, row, col, lane);
+      float2 k[P];                                              // alpha gate wp (of a kept column)
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        v[e] = add_branch(v[e], a.alpha * gate[e], a.post ? q[e] * wp[e] : q[e], kept, e, a.drop);
+      for (int i = 0; i < P; ++i) k[i] = q[i];
+      if (a.wp) {
+        load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) k[i] = mul2(k[i], x[i]);
+      }
+      if (a.gate) {
+        take_vector(gate_raw, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) add_branch(v[i], mul2(alpha, x[i]), k[i], drops, kept, i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) add_branch(v[i], alpha, k[i], drops, kept, i);
       }
     }
-    const float m = a.stats[row], rest = a.stats[(size_t)a.rows + row], s = a.stats[(size_t)2 * a.rows + row];
+    const float4 st = stats[0];
+    shift_row(v, st.x, col, VEC);
+    scale_row(v, st.y, st.z, col, VEC);
+    ring_take(mine + 2 * G::kR, row_of<TH>(a.dn, row, a.lddn), col, sub, dx);
+    if (S::T < 32 && !on) {                                     // (nothing of a row that is not there may reach the sums)
 #pragma unroll
-    for (int e = 0; e < kE; ++e) v[e] = col.at(e) < d ? ((v[e] - m) - rest) * s : 0.f;
+      for (int i = 0; i < P; ++i) v[i] = q[i] = dx[i] = both(0.f);
+    }
     // A and B, and dn (1 + scale) w
-    float own_a[kE];                                            // rows that are groups: A of this row
-    {
-      float sc[kE];
-      load_vector8<VEC>(a.scale, a.tc, a.wide_c, (size_t)group * a.ldscale, col, d, 0.f, sc);
+    const bool weighted = a.mode == kSumWeighted, own_rows = weighted && a.per == 1;
+    if (own_rows && a.dshift) store_vector(a.dshift, a.tc, a.wide_c, cond_at(row, a.lddshift), col, on, dx);
+    if (own_rows && a.dscale) {
+      float2 o[P];
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        const float f = 1.0f + sc[e];
-        const float k = a.mode == kSumWeighted ? f : 1.0f;
-        own_a[e] = dx[e] * v[e];
-        sa[e] = fmaf(k, own_a[e], sa[e]);
-        sb[e] = fmaf(k, dx[e], sb[e]);
-      }
-      if (a.mode == kSumWeighted && a.per == 1) {
-        if (a.dshift) store_vector8<VEC>(a.dshift, a.tc, a.wide_c, (size_t)row * a.lddshift, col, d, dx);
-        if (a.dscale) {
-          float w[kE], b[kE];
-          load_vector8<VEC>(a.w, a.tw, a.wide_w, 0, col, d, 1.f, w);
-          load_vector8<VEC>(a.b, a.tw, a.wide_w, 0, col, d, 0.f, b);
-#pragma unroll
-          for (int e = 0; e < kE; ++e) own_a[e] = fmaf(w[e], own_a[e], b[e] * dx[e]);
-          store_vector8<VEC>(a.dscale, a.tc, a.wide_c, (size_t)row * a.lddscale, col, d, own_a);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < kE; ++e) dx[e] *= 1.0f + sc[e];
+      for (int i = 0; i < P; ++i) o[i] = mul2(dx[i], v[i]);
       if (a.w) {
-        float w[kE];
-        load_vector8<VEC>(a.w, a.tw, a.wide_w, 0, col, d, 1.f, w);
+        load_vector(a.w, a.tw, a.wide_w, 0, col, x);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) dx[e] *= w[e];
+        for (int i = 0; i < P; ++i) o[i] = mul2(o[i], x[i]);
       }
-    }
-    float c[2] = {0.f, 0.f};
+      if (a.b) {
+        load_vector(a.b, a.tw, a.wide_w, 0, col, x);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      c[0] += dx[e];
-      c[1] = fmaf(dx[e], v[e], c[1]);
+        for (int i = 0; i < P; ++i) o[i] = fma2(dx[i], x[i], o[i]);
+      }
+      store_vector(a.dscale, a.tc, a.wide_c, cond_at(row, a.lddscale), col, on, o);
     }
+    const auto add_ab = [&]() {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        sa[i] = fma2(dx[i], v[i], sa[i]);
+        sb[i] = add2(sb[i], dx[i]);
+      }
+    };
+    if (!weighted) add_ab();
+    if (a.scale) {
+      take_vector(scale_raw, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) dx[i] = fma2(dx[i], x[i], dx[i]);
+    }
+    if (weighted) add_ab();
+    if (a.w) {
+      load_vector(a.w, a.tw, a.wide_w, 0, col, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) dx[i] = mul2(dx[i], x[i]);
+    }
+    float c[2];
+    pair_sums(dx, v, c);
     sums(c);
-    const float c1 = a.rms ? 0.f : c[0] * inv_d, c2 = c[1] * inv_d;
+    // (behind a sum: all threads of the group are done with the row before, whose place this takes)
+    request(at.row + kRingStages - 1, stage == 0 ? kRingStages - 1 : stage - 1);
+    const float2 c1 = both(a.rms ? 0.f : -c[0] * inv_d), c2 = both(-c[1] * inv_d);
+    float2 g[P];
+    if (a.dr) {
+      ring_take(mine, row_of<TR>(a.dr, row, a.lddr), col, sub, g);
+    } else {
 #pragma unroll
-    for (int e = 0; e < kE; ++e) g[e] = fmaf(s, dx[e] - c1 - v[e] * c2, g[e]);
-    if (a.dr_in) store_row<TR, VEC>(static_cast<TR*>(a.dr_in) + (size_t)row * a.lddr_in, col, d, g);
+      for (int i = 0; i < P; ++i) g[i] = both(0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) g[i] = fma2(both(st.z), fma2(c2, v[i], add2(dx[i], c1)), g[i]);
+    if (a.dr_in) store_row(row_of<TR>(a.dr_in, row, a.lddr_in), col, on, g);
     if (a.h) {
+      // alpha D g; its product with post(h) (or h) is the row's C
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
-        if (a.drop.threshold) g[e] = (kept >> e) & 1u ? g[e] * a.drop.scale : 0.f;
-        const float k = a.alpha * gate[e];
-        const float own = g[e] * q[e];                          // C of this row
-        sc_[e] = fmaf(a.mode == kSumWeighted ? k : 1.0f, own, sc_[e]);
-        v[e] = a.alpha * (a.post ? wp[e] : 1.f) * own;          // the row's dgate
-        g[e] *= k;                                              // dq
+      for (int i = 0; i < P; ++i) {
+        g[i] = mul2(alpha, g[i]);
+        if (drops) g[i] = select_kept(g[i], kept, i);
       }
-      if (a.mode == kSumWeighted && a.per == 1 && a.dgate)
-        store_vector8<VEC>(a.dgate, a.tc, a.wide_c, (size_t)row * a.lddgate, col, d, v);
+      if (own_rows && a.dgate) {
+        float2 o[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) o[i] = mul2(g[i], q[i]);
+        if (a.wp) {
+          load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
+#pragma unroll
+          for (int i = 0; i < P; ++i) o[i] = mul2(o[i], x[i]);
+        }
+        store_vector(a.dgate, a.tc, a.wide_c, cond_at(row, a.lddgate), col, on, o);
+      }
+      const auto add_c = [&]() {
+#pragma unroll
+        for (int i = 0; i < P; ++i) sq[i] = S::T < 32 && !on ? sq[i] : fma2(g[i], q[i], sq[i]);
+      };
+      if (!weighted) add_c();
+      if (a.gate) {
+        take_vector(gate_raw, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) g[i] = mul2(g[i], x[i]);
+      }
+      if (weighted) add_c();
       if (a.dh) {
         if (a.post) {
-          float e2[2] = {0.f, 0.f};
+          if (a.wp) {
+            load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) {
-            g[e] = col.at(e) < d ? g[e] * wp[e] : 0.f;
-            e2[0] += g[e];
-            e2[1] = fmaf(g[e], q[e], e2[1]);
+            for (int i = 0; i < P; ++i) g[i] = mul2(g[i], x[i]);
           }
-          sums(e2);
-          const float p1 = a.rms ? 0.f : e2[0] * inv_d, p2 = e2[1] * inv_d;
+          if (!VEC) {                                           // (beyond d, g holds the mean that it took off)
 #pragma unroll
-          for (int e = 0; e < kE; ++e) g[e] = post_scale * (g[e] - p1 - q[e] * p2);
+            for (int e = 0; e < kBlock; ++e)
+              if (!col.has(e)) element(g, e) = 0.f;
+          }
+          float e2[2];
+          pair_sums(g, q, e2);
+          sums(e2);
+          const float2 p1 = both(a.rms ? 0.f : -e2[0] * inv_d), p2 = both(-e2[1] * inv_d), ps = both(post_scale);
+#pragma unroll
+          for (int i = 0; i < P; ++i) g[i] = mul2(ps, fma2(p2, q[i], add2(g[i], p1)));
         }
-        store_row<TH, VEC>(static_cast<TH*>(a.dh) + (size_t)row * a.lddh, col, d, g);
+        store_row(row_of<TH>(a.dh, row, a.lddh), col, on, g);
       }
     }
-    const bool piece_ends = row + 1 == at.end;
-    const int piece = at.piece;
-    at.next(a);
-    if (a.mode == kSumGroups && piece_ends) {
-      float sc[kE];
-      load_vector8<VEC>(a.scale, a.tc, a.wide_c, (size_t)group * a.ldscale, col, d, 0.f, sc);
-      if (!a.h || !a.gate)
-#pragma unroll
-        for (int e = 0; e < kE; ++e) gate[e] = 1.f;
+    at.next();
+    stage = stage + 1 == kRingStages ? 0 : stage + 1;
+    // a group's rows, or this worker's of them, are done: its sums are the group's, or a part of them
+    if (a.mode == kSumGroups && on && (at.left == 1 || !at.on())) {
+      const bool from_here = row - (a.per - at.left) >= begin, whole = from_here && at.left == 1;
       float* total = a.part + (size_t)worker * 3 * d;
+      float* part = a.group_part + ((size_t)worker * 2 + (from_here ? 1 : 0)) * 3 * d;
 #pragma unroll
-      for (int e = 0; e < kE; ++e) {
+      for (int e = 0; e < kBlock; ++e) {
+        if (!col.has(e)) continue;
         const int cc = col.at(e);
-        if (cc >= d) continue;
-        const float wa = (1.0f + sc[e]) * sa[e], wb = (1.0f + sc[e]) * sb[e], wc = a.alpha * gate[e] * sc_[e];
-        total[cc] = first_flush ? wa : total[cc] + wa;
-        total[d + cc] = first_flush ? wb : total[d + cc] + wb;
-        total[2 * d + cc] = first_flush ? wc : total[2 * d + cc] + wc;
-        if (a.pieces == 1) {
+        const float A = element(sa, e), B = element(sb, e), C = element(sq, e);
+        const float f = 1.0f + (a.scale ? load_any(a.scale, a.tc, cond_at(group, a.ldscale) + cc) : 0.f);
+        const float k = a.h && a.gate ? load_any(a.gate, a.tc, cond_at(group, a.ldgate) + cc) : 1.f;
+        total[cc] = first_flush ? f * A : fmaf(f, A, total[cc]);
+        total[d + cc] = first_flush ? f * B : fmaf(f, B, total[d + cc]);
+        total[2 * d + cc] = first_flush ? k * C : fmaf(k, C, total[2 * d + cc]);
+        if (whole) {
           const float w = a.w ? load_any(a.w, a.tw, cc) : 1.f, b = a.b ? load_any(a.b, a.tw, cc) : 0.f;
-          if (a.dshift) store_any(a.dshift, a.tc, (size_t)group * a.lddshift + cc, sb[e]);
-          if (a.dscale) store_any(a.dscale, a.tc, (size_t)group * a.lddscale + cc, fmaf(w, sa[e], b * sb[e]));
-          if (a.dgate) store_any(a.dgate, a.tc, (size_t)group * a.lddgate + cc, a.alpha * (a.post && a.wp ? load_any(a.wp, a.tw, cc) : 1.f) * sc_[e]);
+          if (a.dshift) store_any(a.dshift, a.tc, cond_at(group, a.lddshift) + cc, B);
+          if (a.dscale) store_any(a.dscale, a.tc, cond_at(group, a.lddscale) + cc, fmaf(w, A, b * B));
+          if (a.dgate) store_any(a.dgate, a.tc, cond_at(group, a.lddgate) + cc, (a.wp ? load_any(a.wp, a.tw, cc) : 1.f) * C);
         } else {
-          float* mine = a.piece_part + (size_t)piece * 3 * d;
-          mine[cc] = sa[e];
-          mine[d + cc] = sb[e];
-          mine[2 * d + cc] = sc_[e];
+          part[cc] = A;
+          part[d + cc] = B;
+          part[2 * d + cc] = C;
         }
-        sa[e] = sb[e] = sc_[e] = 0.f;
       }
+#pragma unroll
+      for (int i = 0; i < P; ++i) sa[i] = sb[i] = sq[i] = both(0.f);
       first_flush = false;
     }
+    at.next_group(a.per);
   }
-  if (a.mode != kSumGroups) {
+  if (a.mode != kSumGroups && worker < a.workers) {
     float* total = a.part + (size_t)worker * 3 * d;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
+    for (int e = 0; e < kBlock; ++e) {
+      if (!col.has(e)) continue;
       const int cc = col.at(e);
-      if (cc >= d) continue;
-      total[cc] = sa[e];
-      total[d + cc] = sb[e];
-      total[2 * d + cc] = sc_[e];
+      total[cc] = element(sa, e);
+      total[d + cc] = element(sb, e);
+      total[2 * d + cc] = element(sq, e);
     }
   }
 }
@@ -652,55 +835,70 @@ cudaError_t row_launch(K kernel, dim3 grid, int threads, int smem, int cluster, 
 template <class TR, class TH, int TPR, int CL, bool VEC>
 cudaError_t residual_fwd_k(const ResidualNormArgs& a, cudaStream_t st) {
   using S = ResidualShape<TPR, CL>;
+  constexpr int smem = kRingStages * (RingRow<TR, TPR, CL, VEC>::kPieces + RingRow<TH, TPR, CL, VEC>::kPieces) * 16;
   static std::atomic<int> cache[kRowDevices];
   int resident = 0;
-  const cudaError_t e = row_resident(k_residual_norm<TR, TH, TPR, CL, VEC>, cache, S::kCta, 0, CL, &resident);
+  const cudaError_t e = row_resident(k_residual_norm<TR, TH, TPR, CL, VEC>, cache, S::kCta, smem, CL, &resident);
   if (e != cudaSuccess) return e;
-  const int grid = std::min((a.rows + S::kRows - 1) / S::kRows, resident);
-  return row_launch(k_residual_norm<TR, TH, TPR, CL, VEC>, dim3((unsigned)(grid * CL)), S::kCta, 0, CL, st, a);
+  ResidualNormArgs g = a;
+  const int64_t most = (int64_t)resident * S::kRows;
+  g.share = (int)((a.rows + most - 1) / most);
+  g.workers = (a.rows + g.share - 1) / g.share;
+  const int grid = (g.workers + S::kRows - 1) / S::kRows;
+  return row_launch(k_residual_norm<TR, TH, TPR, CL, VEC>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
 }
 
 template <class TR, class TH, int TPR, int CL, bool VEC>
-cudaError_t residual_bwd_k(const ResidualNormArgs& a, cudaStream_t st) {
+cudaError_t residual_bwd_k(ResidualNormArgs& g, cudaStream_t st) {
   using S = ResidualShape<TPR, CL>;
-  constexpr int smem = VEC ? ResidualRing<TR, TH>::kStages * ResidualRing<TR, TH>::kPieces * S::kCta * 16 : 0;
+  constexpr int smem = ResidualBwd<TR, TH, TPR, CL, VEC>::kSmemBytes;
   static std::atomic<int> cache[kRowDevices];
   int resident = 0;
   const cudaError_t e = row_resident(k_residual_norm_bwd<TR, TH, TPR, CL, VEC>, cache, S::kCta, smem, CL, &resident);
   if (e != cudaSuccess) return e;
-  const int grid = (a.workers + S::kRows - 1) / S::kRows;       // (workers beyond the resident ones run after them)
-  return row_launch(k_residual_norm_bwd<TR, TH, TPR, CL, VEC>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, a);
+  // no more workers than run at once, nor than the workspace was made for
+  const int64_t most = std::min<int64_t>(g.workers, (int64_t)resident * S::kRows);
+  g.share = (int)((g.rows + most - 1) / most);
+  g.workers = (g.rows + g.share - 1) / g.share;
+  const int grid = (g.workers + S::kRows - 1) / S::kRows;
+  return row_launch(k_residual_norm_bwd<TR, TH, TPR, CL, VEC>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
 }
 
-inline bool pieces16(const void* p, int64_t ld, int type) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (type == SDS_F32 ? 4 : 2) % 16 == 0;
+// rows of whole pieces of eight columns
+inline bool pieces8(const void* p, int64_t ld, int type) {
+  const int bytes = type == SDS_F32 ? 32 : 16;
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * (bytes / 8) % bytes == 0;
 }
 
 template <class TR, class TH, int TPR, int CL>
-cudaError_t residual_t(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+cudaError_t residual_t(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
   if (backward) return vec ? residual_bwd_k<TR, TH, TPR, CL, true>(a, st) : residual_bwd_k<TR, TH, TPR, CL, false>(a, st);
   return vec ? residual_fwd_k<TR, TH, TPR, CL, true>(a, st) : residual_fwd_k<TR, TH, TPR, CL, false>(a, st);
 }
 
-// eight columns per thread: a warp up to 256 columns, one CTA up to 4096, a cluster of two or four beyond
+// threads of a row's group: part of a warp, one CTA, a cluster of two or four beyond 4096 columns
+inline int residual_threads(int d) { return d <= 64 ? 8 : d <= 256 ? 32 : d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : d <= 8192 ? 1024 : 2048; }
 template <class TR, class TH>
-cudaError_t residual_launch(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
-  if (a.d <= 256) return residual_t<TR, TH, 32, 1>(a, vec, backward, st);
-  if (a.d <= 512) return residual_t<TR, TH, 64, 1>(a, vec, backward, st);
-  if (a.d <= 1024) return residual_t<TR, TH, 128, 1>(a, vec, backward, st);
-  if (a.d <= 2048) return residual_t<TR, TH, 256, 1>(a, vec, backward, st);
-  if (a.d <= 4096) return residual_t<TR, TH, 512, 1>(a, vec, backward, st);
-  if (a.d <= 8192) return residual_t<TR, TH, 1024, 2>(a, vec, backward, st);
-  return residual_t<TR, TH, 2048, 4>(a, vec, backward, st);
+cudaError_t residual_launch(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+  switch (residual_threads(a.d)) {
+    case 8: return residual_t<TR, TH, 8, 1>(a, vec, backward, st);
+    case 32: return residual_t<TR, TH, 32, 1>(a, vec, backward, st);
+    case 64: return residual_t<TR, TH, 64, 1>(a, vec, backward, st);
+    case 128: return residual_t<TR, TH, 128, 1>(a, vec, backward, st);
+    case 256: return residual_t<TR, TH, 256, 1>(a, vec, backward, st);
+    case 512: return residual_t<TR, TH, 512, 1>(a, vec, backward, st);
+    case 1024: return residual_t<TR, TH, 1024, 2>(a, vec, backward, st);
+    default: return residual_t<TR, TH, 2048, 4>(a, vec, backward, st);
+  }
 }
 
 }  // namespace
 
-// one source for each pair of types
-cudaError_t residual_f32(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
-cudaError_t residual_f32_bf16(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
-cudaError_t residual_f32_f16(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
-cudaError_t residual_bf16(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
-cudaError_t residual_f16(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
+// one source for each pair of types; backward: a.workers becomes the number of workers launched
+cudaError_t residual_f32(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
+cudaError_t residual_f32_bf16(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
+cudaError_t residual_f32_f16(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
+cudaError_t residual_bf16(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
+cudaError_t residual_f16(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st);
 
 }  // namespace sds

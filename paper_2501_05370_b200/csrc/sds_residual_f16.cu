@@ -3,7 +3,7 @@
 
 namespace sds {
 
-cudaError_t residual_f16(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+cudaError_t residual_f16(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
   return residual_launch<F16, F16>(a, vec, backward, st);
 }
 

@@ -3,7 +3,7 @@
 
 namespace sds {
 
-cudaError_t residual_f32(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+cudaError_t residual_f32(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
   return residual_launch<float, float>(a, vec, backward, st);
 }
 

@@ -3,7 +3,7 @@
 
 namespace sds {
 
-cudaError_t residual_f32_bf16(const ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
+cudaError_t residual_f32_bf16(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
   return residual_launch<float, Bf16>(a, vec, backward, st);
 }
 

@@ -621,7 +621,7 @@ PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::Tensor out, kept;
     if (s.h) out = output(a[19], r, r.scalar_type(), &ldo);
     else require(a[19] == Py_None, "stream_out needs h");
-    if (keep) kept = empty({6, s.r.rows}, at::kFloat, r);
+    if (keep) kept = empty({s.r.rows, 8}, at::kFloat, r);
     check(sds_residual_norm(&s.op, r.data_ptr(), s.r.ld, s.h ? s.h->data_ptr() : nullptr, s.ldh, ptr(out), ldo, y.data_ptr(), ldn,
                             static_cast<float*>(ptr(kept)), c10::cuda::getCurrentCUDAStream(r.get_device()).stream()),
           "sds_residual_norm");
@@ -645,7 +645,7 @@ PyObject* residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       lddout = rows_of(v, "dr").ld;
       dout = v.data_ptr();
     }
-    require(kept.scalar_type() == at::kFloat && kept.is_contiguous() && kept.device() == r.device() && kept.numel() == 6 * s.r.rows,
+    require(kept.scalar_type() == at::kFloat && kept.is_contiguous() && kept.device() == r.device() && kept.numel() == 8 * s.r.rows,
             "kept must be what residual_norm(keep=True) returned for these sizes");
     sds_residual_norm_sizes sizes;
     check(sds_residual_norm_bytes(&s.op, &sizes), "sds_residual_norm_bytes");

@@ -467,7 +467,7 @@ def test_empty_and_shapes():
     cond = torch.ones(3, 64, device="cuda")
     w = torch.ones(64, device="cuda")
     out, n, kept = sds.residual_norm(x, h, gate=cond, scale=cond, shift=cond, weight=w, bias=w, post=True, post_weight=w, keep=True)
-    assert out.shape == n.shape == (0, 64) and kept.shape == (6, 0)
+    assert out.shape == n.shape == (0, 64) and kept.shape == (0, 8)
     got = sds.residual_norm_backward(n, out, x, h, kept, gate=cond, scale=cond, shift=cond, weight=w, bias=w, post=True, post_weight=w)
     assert all((g == 0).all() for g in got) and got[4].shape == (3, 64)
     r = gen(1)
