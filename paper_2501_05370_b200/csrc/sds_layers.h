@@ -128,7 +128,6 @@ struct ResidualNormArgs {
   const void* w; const void* b; const void* wp; int tw;                            // [d] each, NULL = ones, zeros, ones
   const void* gate; const void* scale; const void* shift; int tc;                  // [groups, d] each, NULL = ones, zeros, zeros
   int64_t ldgate, ldscale, ldshift;
-  bool wide_w, wide_c;                           // the vectors (the rows of gate, scale and shift) lie in whole 16-byte pieces
   float4* stats;                                 // [rows][2]: mean, its remainder, 1 / size, and the same of post; forward: may be NULL
   // backward
   const void* dn; int64_t lddn;

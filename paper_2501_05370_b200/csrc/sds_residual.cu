@@ -97,6 +97,10 @@ cudaError_t launch_rows(ResidualNormArgs& a, bool vec, bool backward, cudaStream
 }
 
 bool whole(const void* p, int64_t ld, int type) { return !p || pieces8(p, ld, type); }
+bool whole_vectors(const ResidualNormArgs& a) {
+  return a.d % 8 == 0 && whole(a.w, 0, a.tw) && whole(a.b, 0, a.tw) && whole(a.wp, 0, a.tw) && whole(a.gate, a.ldgate, a.tc) &&
+         whole(a.scale, a.ldscale, a.tc) && whole(a.shift, a.ldshift, a.tc);
+}
 
 }  // namespace
 
@@ -110,11 +114,9 @@ void residual_norm_plan(ResidualNormArgs* a, size_t* part_floats, size_t* group_
 
 cudaError_t launch_residual_norm(const ResidualNormArgs& a, cudaStream_t st) {
   if (a.rows <= 0) return cudaSuccess;
-  const bool vec = a.d % 8 == 0 && whole(a.r, a.ldr, a.tr) && whole(a.h, a.ldh, a.th) && whole(a.n, a.ldn, a.th) &&
+  const bool vec = whole_vectors(a) && whole(a.r, a.ldr, a.tr) && whole(a.h, a.ldh, a.th) && whole(a.n, a.ldn, a.th) &&
                    (!a.h || whole(a.out, a.ldo, a.tr));
   ResidualNormArgs g = a;
-  g.wide_w = whole(a.w, 0, a.tw) && whole(a.b, 0, a.tw) && whole(a.wp, 0, a.tw);
-  g.wide_c = whole(a.gate, a.ldgate, a.tc) && whole(a.scale, a.ldscale, a.tc) && whole(a.shift, a.ldshift, a.tc);
   return launch_rows(g, vec, false, st);
 }
 
@@ -131,12 +133,10 @@ cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_
         return e;
     return cudaSuccess;
   }
-  const bool vec = a.d % 8 == 0 && whole(a.r, a.ldr, a.tr) && whole(a.h, a.ldh, a.th) && whole(a.dn, a.lddn, a.th) &&
-                   whole(a.dr, a.lddr, a.tr) && whole(a.dr_in, a.lddr_in, a.tr) && whole(a.dh, a.lddh, a.th);
+  const bool vec = whole_vectors(a) && whole(a.r, a.ldr, a.tr) && whole(a.h, a.ldh, a.th) && whole(a.dn, a.lddn, a.th) &&
+                   whole(a.dr, a.lddr, a.tr) && whole(a.dr_in, a.lddr_in, a.tr) && whole(a.dh, a.lddh, a.th) &&
+                   whole(a.dgate, a.lddgate, a.tc) && whole(a.dscale, a.lddscale, a.tc) && whole(a.dshift, a.lddshift, a.tc);
   ResidualNormArgs g = a;
-  g.wide_w = whole(a.w, 0, a.tw) && whole(a.b, 0, a.tw) && whole(a.wp, 0, a.tw);
-  g.wide_c = whole(a.gate, a.ldgate, a.tc) && whole(a.scale, a.ldscale, a.tc) && whole(a.shift, a.ldshift, a.tc) &&
-             whole(a.dgate, a.lddgate, a.tc) && whole(a.dscale, a.lddscale, a.tc) && whole(a.dshift, a.lddshift, a.tc);
   if ((e = launch_rows(g, vec, true, st)) != cudaSuccess) return e;
   const int strips = (a.d + 31) / 32;
   if (a.mode == kSumGroups && g.share % g.per != 0 &&     // (else no group crosses workers)

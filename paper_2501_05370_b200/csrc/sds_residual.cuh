@@ -124,17 +124,16 @@ __device__ __forceinline__ void store_row(T* row, const Columns<TPR, CL, VEC>& c
   }
 }
 
-// A thread's columns of a vector of any of the three types. 16-bit `wide` vectors (whole 16-byte pieces, VEC only) can be requested
-// ahead, as they lie in memory; floats are read where they are used (twice the registers, and they mostly lie in L1).
+// A thread's columns of a vector of any of the three types. 16-bit vectors of whole pieces (VEC) can be requested ahead, as they lie in memory; floats are read where they are used (twice the registers, and they mostly lie in L1).
 template <int TPR, int CL, bool VEC>
-__device__ __forceinline__ void request_vector(uint4& r, const void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col) {
-  if (VEC && wide && p && type != SDS_F32 && col.live) r = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + off + col.c0));
+__device__ __forceinline__ void request_vector(uint4& r, const void* p, int type, uint64_t off, const Columns<TPR, CL, VEC>& col) {
+  if (VEC && p && type != SDS_F32 && col.live) r = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + off + col.c0));
 }
 // (p is not NULL)
 template <int TPR, int CL, bool VEC>
-__device__ __forceinline__ void take_vector(const uint4& r, const void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col,
+__device__ __forceinline__ void take_vector(const uint4& r, const void* p, int type, uint64_t off, const Columns<TPR, CL, VEC>& col,
                                             float2 (&o)[P]) {
-  if (VEC && wide) {
+  if (VEC) {
     if (type == SDS_F32) {
       const uint4* from = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + off + (col.live ? col.c0 : 0));
       const uint4 q[2] = {__ldg(from), __ldg(from + 1)};
@@ -153,14 +152,14 @@ __device__ __forceinline__ void take_vector(const uint4& r, const void* p, int t
   }
 }
 template <int TPR, int CL, bool VEC>
-__device__ __forceinline__ void load_vector(const void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col, float2 (&o)[P]) {
+__device__ __forceinline__ void load_vector(const void* p, int type, uint64_t off, const Columns<TPR, CL, VEC>& col, float2 (&o)[P]) {
   uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  request_vector(r, p, type, wide, off, col);
-  take_vector(r, p, type, wide, off, col, o);
+  request_vector(r, p, type, off, col);
+  take_vector(r, p, type, off, col, o);
 }
 template <class T, int TPR, int CL, bool VEC>
-__device__ __forceinline__ void store_typed_vector(T* p, bool wide, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
-  if (VEC && wide) {
+__device__ __forceinline__ void store_typed_vector(T* p, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
+  if (VEC) {
     if (on && col.live) store_words(p + col.c0, v);
   } else {
 #pragma unroll
@@ -169,10 +168,10 @@ __device__ __forceinline__ void store_typed_vector(T* p, bool wide, const Column
   }
 }
 template <int TPR, int CL, bool VEC>
-__device__ __forceinline__ void store_vector(void* p, int type, bool wide, uint64_t off, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
-  if (type == SDS_F32) store_typed_vector(static_cast<float*>(p) + off, wide, col, on, v);
-  else if (type == SDS_BF16) store_typed_vector(static_cast<Bf16*>(p) + off, wide, col, on, v);
-  else store_typed_vector(static_cast<F16*>(p) + off, wide, col, on, v);
+__device__ __forceinline__ void store_vector(void* p, int type, uint64_t off, const Columns<TPR, CL, VEC>& col, bool on, const float2 (&v)[P]) {
+  if (type == SDS_F32) store_typed_vector(static_cast<float*>(p) + off, col, on, v);
+  else if (type == SDS_BF16) store_typed_vector(static_cast<Bf16*>(p) + off, col, on, v);
+  else store_typed_vector(static_cast<F16*>(p) + off, col, on, v);
 }
 // where a group's row of gate, scale or shift begins
 __device__ __forceinline__ uint64_t cond_at(int group, int64_t ld) { return (uint64_t)(uint32_t)group * (uint32_t)ld; }
@@ -417,9 +416,11 @@ struct RowWalk {
 // whether the worker, or another one of its warp (small groups: the warp's lanes stay together), has a row left
 template <int T> __device__ __forceinline__ bool rows_left(bool on) { return T < 32 ? __any_sync(kAll, on) : on; }
 
+// FULL: with post or dropout. Two kernels, as the time of either goes with the length of its code: with vectors of unaligned pieces in the
+// aligned kernels too, these were twice as long and 16384 x 2048 backward took 142 us conditioned (119 without), 177 with all parts (156).
 // A group takes neighbouring rows, which mostly share their row of gate, scale and shift. Rows come through the ring, vectors are requested
 // before the sums that they wait for.
-template <class TR, class TH, int TPR, int CL, bool VEC>
+template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;
   constexpr int kR = RingRow<TR, TPR, CL, VEC>::kPieces, kStage = kR + RingRow<TH, TPR, CL, VEC>::kPieces;
@@ -435,7 +436,7 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
   }
   start_after_prior_kernel();
   const float inv_d = 1.0f / (float)a.d;
-  const bool drops = a.drop.threshold != 0;
+  const bool drops = FULL && a.drop.threshold != 0;
   const uint32_t dstep = drops ? dropout_step(a.drop) : 0u;
   const float2 alpha = both(drops ? a.alpha * a.drop.scale : a.alpha);
   RowWalk at(a, (int)blockIdx.x / CL * S::kRows + sub);
@@ -454,18 +455,18 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
     const int row = on ? at.row : 0, group = on ? at.group : 0;
     float2 v[P], q[P], x[P];
     uint4 gate, scale, shift;
-    if (a.h) request_vector(gate, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col);
-    request_vector(scale, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col);
-    request_vector(shift, a.shift, a.tc, a.wide_c, cond_at(group, a.ldshift), col);
+    if (a.h) request_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col);
+    request_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col);
+    request_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col);
     ring_ready<TPR, CL, VEC>(sub);
     const uint4* mine = ring + stage * kStage;
     ring_take(mine, row_of<TR>(a.r, row, a.ldr), col, sub, v);
     if (a.h) {
       ring_take(mine + kR, row_of<TH>(a.h, row, a.ldh), col, sub, q);
-      if (a.post) {
+      if (FULL && a.post) {
         const float4 st = normalise(q, sums, col, inv_d, a.rms, a.eps);
-        if (a.wp) {
-          load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
+        if (FULL && a.wp) {
+          load_vector(a.wp, a.tw, 0, col, x);
 #pragma unroll
           for (int i = 0; i < P; ++i) q[i] = mul2(q[i], x[i]);
         }
@@ -474,7 +475,7 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
       Kept kept;
       if (drops) kept = kept_columns(a.drop, dstep, row, col, lane);
       if (a.gate) {
-        take_vector(gate, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col, x);
+        take_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
 #pragma unroll
         for (int i = 0; i < P; ++i) add_branch(v[i], mul2(alpha, x[i]), q[i], drops, kept, i);
       } else {
@@ -488,22 +489,22 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
     request(at.row + kRingStages - 1, stage == 0 ? kRingStages - 1 : stage - 1);
     if (a.stats && t == 0 && on) a.stats[2 * (size_t)row] = st;
     if (a.w) {
-      load_vector(a.w, a.tw, a.wide_w, 0, col, x);
+      load_vector(a.w, a.tw, 0, col, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) v[i] = mul2(v[i], x[i]);
     }
     if (a.b) {
-      load_vector(a.b, a.tw, a.wide_w, 0, col, x);
+      load_vector(a.b, a.tw, 0, col, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
     }
     if (a.scale) {
-      take_vector(scale, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col, x);
+      take_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) v[i] = fma2(v[i], x[i], v[i]);
     }
     if (a.shift) {
-      take_vector(shift, a.shift, a.tc, a.wide_c, cond_at(group, a.ldshift), col, x);
+      take_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
     }
@@ -518,6 +519,11 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
 // backward
 // ---------------------------------------------------------------------------------------------
 
+// (the compiler spends more on pairing registers in the backward kernel than pairs save: 16384 x 2048 conditioned 142 us with them, 137 without)
+__device__ __forceinline__ float2 each_fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+__device__ __forceinline__ float2 each_mul2(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ float2 each_add2(float2 a, float2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+
 template <class TR, class TH, int TPR, int CL, bool VEC> struct ResidualBwd {
   using S = ResidualShape<TPR, CL>;
   static constexpr int kR = RingRow<TR, TPR, CL, VEC>::kPieces, kH = RingRow<TH, TPR, CL, VEC>::kPieces;
@@ -527,7 +533,19 @@ template <class TR, class TH, int TPR, int CL, bool VEC> struct ResidualBwd {
   static constexpr int kMinCtas = 512 / S::kCta;                // 512 threads of 128 registers
 };
 
-template <class TR, class TH, int TPR, int CL, bool VEC>
+// total = or += k v
+template <int TPR, int CL, bool VEC>
+__device__ __forceinline__ void add_total(float* total, const float2 (&v)[P], const float2 (&k)[P], const Columns<TPR, CL, VEC>& col, bool first) {
+  float2 o[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) o[i] = both(0.f);
+  if (!first) load_scalar(total, col, o);
+#pragma unroll
+  for (int i = 0; i < P; ++i) o[i] = each_fma2(k[i], v[i], o[i]);
+  store_typed_vector(total, col, true, o);
+}
+
+template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, TH, TPR, CL, VEC>::kMinCtas) k_residual_norm_bwd(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;
   using G = ResidualBwd<TR, TH, TPR, CL, VEC>;
@@ -546,7 +564,7 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
   const int worker = (int)blockIdx.x / CL * S::kRows + sub;
   const int d = a.d;
   const float inv_d = 1.0f / (float)d;
-  const bool drops = a.drop.threshold != 0;
+  const bool drops = FULL && a.drop.threshold != 0;
   const uint32_t dstep = drops ? dropout_step(a.drop) : 0u;
   const float2 alpha = both(drops ? a.alpha * a.drop.scale : a.alpha);     // of a kept column
   float2 sa[P], sb[P], sq[P];                                   // A, B, C, or their weighted forms
@@ -566,7 +584,7 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
       if (threadIdx.x % kWarp == 0) {
         uint4* st = to + G::kStats + threadIdx.x / kWarp * 2;
         copy16(st, a.stats + 2 * (size_t)row);
-        if (a.post) copy16(st + 1, a.stats + 2 * (size_t)row + 1);
+        if (FULL && a.post) copy16(st + 1, a.stats + 2 * (size_t)row + 1);
       }
     }
     copies_end();
@@ -578,8 +596,8 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     const bool on = at.on();
     const int row = on ? at.row : 0, group = on ? at.group : 0;
     uint4 gate_raw, scale_raw;
-    if (a.h) request_vector(gate_raw, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col);
-    request_vector(scale_raw, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col);
+    if (a.h) request_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col);
+    request_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col);
     ring_ready<TPR, CL, VEC>(sub);
     const uint4* mine = ring + stage * G::kStage;
     const float4* stats = reinterpret_cast<const float4*>(mine + G::kStats + threadIdx.x / kWarp * 2);
@@ -591,7 +609,7 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     if (a.h) {
       ring_take(mine + 2 * G::kR + G::kH, row_of<TH>(a.h, row, a.ldh), col, sub, q);
       if (drops) kept = kept_columns(a.drop, dstep, row, col, lane);
-      if (a.post) {
+      if (FULL && a.post) {
         const float4 st = stats[1];
         post_scale = st.z;
         shift_row(q, st.x, col, VEC);
@@ -600,15 +618,15 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
       float2 k[P];                                              // alpha gate wp (of a kept column)
 #pragma unroll
       for (int i = 0; i < P; ++i) k[i] = q[i];
-      if (a.wp) {
-        load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
+      if (FULL && a.wp) {
+        load_vector(a.wp, a.tw, 0, col, x);
 #pragma unroll
-        for (int i = 0; i < P; ++i) k[i] = mul2(k[i], x[i]);
+        for (int i = 0; i < P; ++i) k[i] = each_mul2(k[i], x[i]);
       }
       if (a.gate) {
-        take_vector(gate_raw, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col, x);
+        take_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
 #pragma unroll
-        for (int i = 0; i < P; ++i) add_branch(v[i], mul2(alpha, x[i]), k[i], drops, kept, i);
+        for (int i = 0; i < P; ++i) add_branch(v[i], each_mul2(alpha, x[i]), k[i], drops, kept, i);
       } else {
 #pragma unroll
         for (int i = 0; i < P; ++i) add_branch(v[i], alpha, k[i], drops, kept, i);
@@ -624,41 +642,41 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     }
     // A and B, and dn (1 + scale) w
     const bool weighted = a.mode == kSumWeighted, own_rows = weighted && a.per == 1;
-    if (own_rows && a.dshift) store_vector(a.dshift, a.tc, a.wide_c, cond_at(row, a.lddshift), col, on, dx);
+    if (own_rows && a.dshift) store_vector(a.dshift, a.tc, cond_at(row, a.lddshift), col, on, dx);
     if (own_rows && a.dscale) {
       float2 o[P];
 #pragma unroll
-      for (int i = 0; i < P; ++i) o[i] = mul2(dx[i], v[i]);
+      for (int i = 0; i < P; ++i) o[i] = each_mul2(dx[i], v[i]);
       if (a.w) {
-        load_vector(a.w, a.tw, a.wide_w, 0, col, x);
+        load_vector(a.w, a.tw, 0, col, x);
 #pragma unroll
-        for (int i = 0; i < P; ++i) o[i] = mul2(o[i], x[i]);
+        for (int i = 0; i < P; ++i) o[i] = each_mul2(o[i], x[i]);
       }
       if (a.b) {
-        load_vector(a.b, a.tw, a.wide_w, 0, col, x);
+        load_vector(a.b, a.tw, 0, col, x);
 #pragma unroll
-        for (int i = 0; i < P; ++i) o[i] = fma2(dx[i], x[i], o[i]);
+        for (int i = 0; i < P; ++i) o[i] = each_fma2(dx[i], x[i], o[i]);
       }
-      store_vector(a.dscale, a.tc, a.wide_c, cond_at(row, a.lddscale), col, on, o);
+      store_vector(a.dscale, a.tc, cond_at(row, a.lddscale), col, on, o);
     }
     const auto add_ab = [&]() {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        sa[i] = fma2(dx[i], v[i], sa[i]);
-        sb[i] = add2(sb[i], dx[i]);
+        sa[i] = each_fma2(dx[i], v[i], sa[i]);
+        sb[i] = each_add2(sb[i], dx[i]);
       }
     };
     if (!weighted) add_ab();
     if (a.scale) {
-      take_vector(scale_raw, a.scale, a.tc, a.wide_c, cond_at(group, a.ldscale), col, x);
+      take_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
 #pragma unroll
-      for (int i = 0; i < P; ++i) dx[i] = fma2(dx[i], x[i], dx[i]);
+      for (int i = 0; i < P; ++i) dx[i] = each_fma2(dx[i], x[i], dx[i]);
     }
     if (weighted) add_ab();
     if (a.w) {
-      load_vector(a.w, a.tw, a.wide_w, 0, col, x);
+      load_vector(a.w, a.tw, 0, col, x);
 #pragma unroll
-      for (int i = 0; i < P; ++i) dx[i] = mul2(dx[i], x[i]);
+      for (int i = 0; i < P; ++i) dx[i] = each_mul2(dx[i], x[i]);
     }
     float c[2];
     pair_sums(dx, v, c);
@@ -674,43 +692,43 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
       for (int i = 0; i < P; ++i) g[i] = both(0.f);
     }
 #pragma unroll
-    for (int i = 0; i < P; ++i) g[i] = fma2(both(st.z), fma2(c2, v[i], add2(dx[i], c1)), g[i]);
+    for (int i = 0; i < P; ++i) g[i] = each_fma2(both(st.z), each_fma2(c2, v[i], each_add2(dx[i], c1)), g[i]);
     if (a.dr_in) store_row(row_of<TR>(a.dr_in, row, a.lddr_in), col, on, g);
     if (a.h) {
       // alpha D g; its product with post(h) (or h) is the row's C
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        g[i] = mul2(alpha, g[i]);
+        g[i] = each_mul2(alpha, g[i]);
         if (drops) g[i] = select_kept(g[i], kept, i);
       }
       if (own_rows && a.dgate) {
         float2 o[P];
 #pragma unroll
-        for (int i = 0; i < P; ++i) o[i] = mul2(g[i], q[i]);
-        if (a.wp) {
-          load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
+        for (int i = 0; i < P; ++i) o[i] = each_mul2(g[i], q[i]);
+        if (FULL && a.wp) {
+          load_vector(a.wp, a.tw, 0, col, x);
 #pragma unroll
-          for (int i = 0; i < P; ++i) o[i] = mul2(o[i], x[i]);
+          for (int i = 0; i < P; ++i) o[i] = each_mul2(o[i], x[i]);
         }
-        store_vector(a.dgate, a.tc, a.wide_c, cond_at(row, a.lddgate), col, on, o);
+        store_vector(a.dgate, a.tc, cond_at(row, a.lddgate), col, on, o);
       }
       const auto add_c = [&]() {
 #pragma unroll
-        for (int i = 0; i < P; ++i) sq[i] = S::T < 32 && !on ? sq[i] : fma2(g[i], q[i], sq[i]);
+        for (int i = 0; i < P; ++i) sq[i] = S::T < 32 && !on ? sq[i] : each_fma2(g[i], q[i], sq[i]);
       };
       if (!weighted) add_c();
       if (a.gate) {
-        take_vector(gate_raw, a.gate, a.tc, a.wide_c, cond_at(group, a.ldgate), col, x);
+        take_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
 #pragma unroll
-        for (int i = 0; i < P; ++i) g[i] = mul2(g[i], x[i]);
+        for (int i = 0; i < P; ++i) g[i] = each_mul2(g[i], x[i]);
       }
       if (weighted) add_c();
       if (a.dh) {
-        if (a.post) {
-          if (a.wp) {
-            load_vector(a.wp, a.tw, a.wide_w, 0, col, x);
+        if (FULL && a.post) {
+          if (FULL && a.wp) {
+            load_vector(a.wp, a.tw, 0, col, x);
 #pragma unroll
-            for (int i = 0; i < P; ++i) g[i] = mul2(g[i], x[i]);
+            for (int i = 0; i < P; ++i) g[i] = each_mul2(g[i], x[i]);
           }
           if (!VEC) {                                           // (beyond d, g holds the mean that it took off)
 #pragma unroll
@@ -722,7 +740,7 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
           sums(e2);
           const float2 p1 = both(a.rms ? 0.f : -e2[0] * inv_d), p2 = both(-e2[1] * inv_d), ps = both(post_scale);
 #pragma unroll
-          for (int i = 0; i < P; ++i) g[i] = mul2(ps, fma2(p2, q[i], add2(g[i], p1)));
+          for (int i = 0; i < P; ++i) g[i] = each_mul2(ps, each_fma2(p2, q[i], each_add2(g[i], p1)));
         }
         store_row(row_of<TH>(a.dh, row, a.lddh), col, on, g);
       }
@@ -733,27 +751,47 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     if (a.mode == kSumGroups && on && (at.left == 1 || !at.on())) {
       const bool from_here = row - (a.per - at.left) >= begin, whole = from_here && at.left == 1;
       float* total = a.part + (size_t)worker * 3 * d;
-      float* part = a.group_part + ((size_t)worker * 2 + (from_here ? 1 : 0)) * 3 * d;
+      float2 f[P], k[P];
 #pragma unroll
-      for (int e = 0; e < kBlock; ++e) {
-        if (!col.has(e)) continue;
-        const int cc = col.at(e);
-        const float A = element(sa, e), B = element(sb, e), C = element(sq, e);
-        const float f = 1.0f + (a.scale ? load_any(a.scale, a.tc, cond_at(group, a.ldscale) + cc) : 0.f);
-        const float k = a.h && a.gate ? load_any(a.gate, a.tc, cond_at(group, a.ldgate) + cc) : 1.f;
-        total[cc] = first_flush ? f * A : fmaf(f, A, total[cc]);
-        total[d + cc] = first_flush ? f * B : fmaf(f, B, total[d + cc]);
-        total[2 * d + cc] = first_flush ? k * C : fmaf(k, C, total[2 * d + cc]);
-        if (whole) {
-          const float w = a.w ? load_any(a.w, a.tw, cc) : 1.f, b = a.b ? load_any(a.b, a.tw, cc) : 0.f;
-          if (a.dshift) store_any(a.dshift, a.tc, cond_at(group, a.lddshift) + cc, B);
-          if (a.dscale) store_any(a.dscale, a.tc, cond_at(group, a.lddscale) + cc, fmaf(w, A, b * B));
-          if (a.dgate) store_any(a.dgate, a.tc, cond_at(group, a.lddgate) + cc, (a.wp ? load_any(a.wp, a.tw, cc) : 1.f) * C);
-        } else {
-          part[cc] = A;
-          part[d + cc] = B;
-          part[2 * d + cc] = C;
+      for (int i = 0; i < P; ++i) f[i] = k[i] = both(0.f);
+      if (a.scale) load_vector(a.scale, a.tc, cond_at(group, a.ldscale), col, f);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        f[i].x += 1.0f; f[i].y += 1.0f;
+        k[i] = both(1.0f);
+      }
+      if (a.h && a.gate) load_vector(a.gate, a.tc, cond_at(group, a.ldgate), col, k);
+      add_total(total, sa, f, col, first_flush);
+      add_total(total + d, sb, f, col, first_flush);
+      add_total(total + 2 * d, sq, k, col, first_flush);
+      if (whole) {
+        if (a.dshift) store_vector(a.dshift, a.tc, cond_at(group, a.lddshift), col, true, sb);
+        if (a.dscale) {
+          if (a.w) {
+            load_vector(a.w, a.tw, 0, col, x);
+#pragma unroll
+            for (int i = 0; i < P; ++i) sa[i] = each_mul2(sa[i], x[i]);
+          }
+          if (a.b) {
+            load_vector(a.b, a.tw, 0, col, x);
+#pragma unroll
+            for (int i = 0; i < P; ++i) sa[i] = each_fma2(sb[i], x[i], sa[i]);
+          }
+          store_vector(a.dscale, a.tc, cond_at(group, a.lddscale), col, true, sa);
         }
+        if (a.dgate) {
+          if (FULL && a.wp) {
+            load_vector(a.wp, a.tw, 0, col, x);
+#pragma unroll
+            for (int i = 0; i < P; ++i) sq[i] = each_mul2(sq[i], x[i]);
+          }
+          store_vector(a.dgate, a.tc, cond_at(group, a.lddgate), col, true, sq);
+        }
+      } else {
+        float* part = a.group_part + ((size_t)worker * 2 + (from_here ? 1 : 0)) * 3 * d;
+        store_typed_vector(part, col, true, sa);
+        store_typed_vector(part + d, col, true, sb);
+        store_typed_vector(part + 2 * d, col, true, sq);
       }
 #pragma unroll
       for (int i = 0; i < P; ++i) sa[i] = sb[i] = sq[i] = both(0.f);
@@ -763,14 +801,9 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
   }
   if (a.mode != kSumGroups && worker < a.workers) {
     float* total = a.part + (size_t)worker * 3 * d;
-#pragma unroll
-    for (int e = 0; e < kBlock; ++e) {
-      if (!col.has(e)) continue;
-      const int cc = col.at(e);
-      total[cc] = element(sa, e);
-      total[d + cc] = element(sb, e);
-      total[2 * d + cc] = element(sq, e);
-    }
+    store_typed_vector(total, col, true, sa);
+    store_typed_vector(total + d, col, true, sb);
+    store_typed_vector(total + 2 * d, col, true, sq);
   }
 }
 
@@ -832,36 +865,36 @@ cudaError_t row_launch(K kernel, dim3 grid, int threads, int smem, int cluster, 
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <class TR, class TH, int TPR, int CL, bool VEC>
+template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
 cudaError_t residual_fwd_k(const ResidualNormArgs& a, cudaStream_t st) {
   using S = ResidualShape<TPR, CL>;
   constexpr int smem = kRingStages * (RingRow<TR, TPR, CL, VEC>::kPieces + RingRow<TH, TPR, CL, VEC>::kPieces) * 16;
   static std::atomic<int> cache[kRowDevices];
   int resident = 0;
-  const cudaError_t e = row_resident(k_residual_norm<TR, TH, TPR, CL, VEC>, cache, S::kCta, smem, CL, &resident);
+  const cudaError_t e = row_resident(k_residual_norm<TR, TH, TPR, CL, VEC, FULL>, cache, S::kCta, smem, CL, &resident);
   if (e != cudaSuccess) return e;
   ResidualNormArgs g = a;
   const int64_t most = (int64_t)resident * S::kRows;
   g.share = (int)((a.rows + most - 1) / most);
   g.workers = (a.rows + g.share - 1) / g.share;
   const int grid = (g.workers + S::kRows - 1) / S::kRows;
-  return row_launch(k_residual_norm<TR, TH, TPR, CL, VEC>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
+  return row_launch(k_residual_norm<TR, TH, TPR, CL, VEC, FULL>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
 }
 
-template <class TR, class TH, int TPR, int CL, bool VEC>
+template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
 cudaError_t residual_bwd_k(ResidualNormArgs& g, cudaStream_t st) {
   using S = ResidualShape<TPR, CL>;
   constexpr int smem = ResidualBwd<TR, TH, TPR, CL, VEC>::kSmemBytes;
   static std::atomic<int> cache[kRowDevices];
   int resident = 0;
-  const cudaError_t e = row_resident(k_residual_norm_bwd<TR, TH, TPR, CL, VEC>, cache, S::kCta, smem, CL, &resident);
+  const cudaError_t e = row_resident(k_residual_norm_bwd<TR, TH, TPR, CL, VEC, FULL>, cache, S::kCta, smem, CL, &resident);
   if (e != cudaSuccess) return e;
   // no more workers than run at once, nor than the workspace was made for
   const int64_t most = std::min<int64_t>(g.workers, (int64_t)resident * S::kRows);
   g.share = (int)((g.rows + most - 1) / most);
   g.workers = (g.rows + g.share - 1) / g.share;
   const int grid = (g.workers + S::kRows - 1) / S::kRows;
-  return row_launch(k_residual_norm_bwd<TR, TH, TPR, CL, VEC>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
+  return row_launch(k_residual_norm_bwd<TR, TH, TPR, CL, VEC, FULL>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
 }
 
 // rows of whole pieces of eight columns
@@ -870,10 +903,15 @@ inline bool pieces8(const void* p, int64_t ld, int type) {
   return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * (bytes / 8) % bytes == 0;
 }
 
+template <class TR, class TH, int TPR, int CL, bool VEC>
+cudaError_t residual_t(ResidualNormArgs& a, bool backward, cudaStream_t st) {
+  const bool full = a.post || a.drop.threshold != 0;
+  if (backward) return full ? residual_bwd_k<TR, TH, TPR, CL, VEC, true>(a, st) : residual_bwd_k<TR, TH, TPR, CL, VEC, false>(a, st);
+  return full ? residual_fwd_k<TR, TH, TPR, CL, VEC, true>(a, st) : residual_fwd_k<TR, TH, TPR, CL, VEC, false>(a, st);
+}
 template <class TR, class TH, int TPR, int CL>
 cudaError_t residual_t(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
-  if (backward) return vec ? residual_bwd_k<TR, TH, TPR, CL, true>(a, st) : residual_bwd_k<TR, TH, TPR, CL, false>(a, st);
-  return vec ? residual_fwd_k<TR, TH, TPR, CL, true>(a, st) : residual_fwd_k<TR, TH, TPR, CL, false>(a, st);
+  return vec ? residual_t<TR, TH, TPR, CL, true>(a, backward, st) : residual_t<TR, TH, TPR, CL, false>(a, backward, st);
 }
 
 // threads of a row's group: part of a warp, one CTA, a cluster of two or four beyond 4096 columns
