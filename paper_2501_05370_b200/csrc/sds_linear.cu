@@ -22,14 +22,23 @@ namespace {
 // dz and the bias gradient
 // ---------------------------------------------------------------------------------------------
 
+// Kernels of this file start beside the end of the one in front, and wait for it before they read or write anything. (They let the next
+// one go before that wait: it has to be one that waits in full as well, as every first kernel of a call does.) Their loads are plain
+// ones: the compiler may move read-only loads ahead of the wait.
+__device__ __forceinline__ void start_behind_prior_kernel() {
+  launch_dependents();
+  wait_for_prior_kernel();
+}
+
 struct DzArgs {
   const void* dy;                                 // [rows, n] of tdy, rows lddy elements apart
   const float* factor;                            // [rows, ldz], NULL = ones
   uint16_t* dz;                                   // [rows, ldz] of the operands' type, NULL = not wanted
-  float* part;                                    // [gridDim.y][n] column sums, NULL = not wanted
-  void* db;                                       // with a single chunk of rows the sums go here at once
+  float* part;                                    // [gridDim.y][n] column sums
+  void* db;                                       // NULL = not wanted; where the chunks of rows are one cluster the sums go here at once
   int64_t lddy, ldz;
   int tdy, tdb, rows, n, f16;
+  int cluster;                                    // chunks of rows in a cluster (1: the sums go to part, unless there is but one)
 };
 
 constexpr int kDzThreads = 256, kDzWarps = kDzThreads / 32, kDzCols = 256;
@@ -39,63 +48,77 @@ __device__ __forceinline__ void store_typed(void* p, int type, size_t i, float v
   else static_cast<uint16_t*>(p)[i] = round16(v, type == SDS_F16);
 }
 
-// eight columns of a row of dy and of its factors, as they lie in memory
-template <bool F32> struct DzRow { uint4 y[F32 ? 2 : 1], f[2]; };
-template <bool F32, class A>
-__device__ __forceinline__ void dz_request(DzRow<F32>& r, const A& a, int64_t row, int c0) {
-  const char* y = static_cast<const char*>(a.dy) + ((size_t)row * a.lddy + c0) * (F32 ? 4 : 2);
+// Eight columns of a row of dy and of its factors, as they lie in memory. Where dy's rows are not whole 16-byte pieces (WHOLE = false), the
+// pieces that hold the columns are read, as far as the row goes, and shifted into place: the row's shift is the same for all lanes.
+// (The factors' rows are padded to whole pieces, as dz's are.)
+template <bool F32, bool WHOLE> struct DzRow { uint4 y[(F32 ? 2 : 1) + (WHOLE ? 0 : 1)], f[2]; };
+template <bool F32, bool WHOLE, class A>
+__device__ __forceinline__ void dz_request(DzRow<F32, WHOLE>& r, const A& a, int64_t row, int c0) {
+  constexpr int kSize = F32 ? 4 : 2, kPieces = (F32 ? 2 : 1) + (WHOLE ? 0 : 1);
+  const char* y = static_cast<const char*>(a.dy) + ((size_t)row * a.lddy + c0) * kSize;
+  if (WHOLE) {
 #pragma unroll
-  for (int i = 0; i < (F32 ? 2 : 1); ++i) r.y[i] = __ldg(reinterpret_cast<const uint4*>(y) + i);
+    for (int i = 0; i < kPieces; ++i) r.y[i] = *(reinterpret_cast<const uint4*>(y) + i);
+  } else {
+    const uintptr_t first = reinterpret_cast<uintptr_t>(y) & ~(uintptr_t)15;
+    const uintptr_t last = reinterpret_cast<uintptr_t>(y) + (uintptr_t)(min(8, a.n - c0) * kSize - 1);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      r.y[i] = first + 16 * i <= last ? *(reinterpret_cast<const uint4*>(first) + i) : make_uint4(0u, 0u, 0u, 0u);
+  }
   if (a.factor)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) r.f[i] = __ldg(reinterpret_cast<const uint4*>(a.factor + (size_t)row * a.ldz + c0) + i);
+    for (int i = 0; i < 2; ++i) r.f[i] = *(reinterpret_cast<const uint4*>(a.factor + (size_t)row * a.ldz + c0) + i);
 }
-template <bool F32, class A>
-__device__ __forceinline__ void dz_values(const DzRow<F32>& r, const A& a, float (&v)[8]) {
-  if (F32) {
-    const uint32_t w[8] = {r.y[0].x, r.y[0].y, r.y[0].z, r.y[0].w, r.y[F32].x, r.y[F32].y, r.y[F32].z, r.y[F32].w};
+template <bool F32, bool WHOLE, class A>
+__device__ __forceinline__ void dz_values(const DzRow<F32, WHOLE>& r, const A& a, int64_t row, int c0, float (&v)[8]) {
+  constexpr int kSize = F32 ? 4 : 2, kPieces = (F32 ? 2 : 1) + (WHOLE ? 0 : 1), kWords = F32 ? 8 : 4;
+  uint32_t w[4 * kPieces];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = __uint_as_float(w[u]);
-  } else {
-    const uint32_t w[4] = {r.y[0].x, r.y[0].y, r.y[0].z, r.y[0].w};
+  for (int i = 0; i < kPieces; ++i) { w[4 * i] = r.y[i].x; w[4 * i + 1] = r.y[i].y; w[4 * i + 2] = r.y[i].z; w[4 * i + 3] = r.y[i].w; }
+  if (!WHOLE) {
+    const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(a.dy) + ((size_t)row * a.lddy + c0) * kSize) & 15u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4 * kPieces - 2; ++i) w[i] = shift & 8u ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4 * kPieces - 3; ++i) w[i] = shift & 4u ? w[i + 1] : w[i];
+    if (!F32)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (shift & 2u) * 8u);
+  }
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    if (F32) {
+      v[i] = __uint_as_float(w[i]);
+    } else {
       const float2 t = unpack16x2(w[i], a.f16);
-      v[2 * i] = t.x; v[2 * i + 1] = t.y;
+      v[(2 * i) % 8] = t.x; v[(2 * i + 1) % 8] = t.y;
     }
   }
   if (a.factor) {
-    const uint32_t w[8] = {r.f[0].x, r.f[0].y, r.f[0].z, r.f[0].w, r.f[1].x, r.f[1].y, r.f[1].z, r.f[1].w};
+    const uint32_t f[8] = {r.f[0].x, r.f[0].y, r.f[0].z, r.f[0].w, r.f[1].x, r.f[1].y, r.f[1].z, r.f[1].w};
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] *= __uint_as_float(w[u]);
+    for (int u = 0; u < 8; ++u) v[u] *= __uint_as_float(f[u]);
   }
 }
-// the same for columns 32 apart, one by one
 template <class A>
-__device__ __forceinline__ void dz_scalar(const A& a, int64_t row, int c0, float (&v)[8]) {
-  float f[8];
-#pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const int c = c0 + u * 32;
-    v[u] = c < a.n ? load_typed(a.dy, a.tdy, (size_t)row * a.lddy + c) : 0.f;
-    f[u] = a.factor && c < a.n ? a.factor[(size_t)row * a.ldz + c] : 1.f;
-  }
-#pragma unroll
-  for (int u = 0; u < 8; ++u) v[u] *= f[u];
+__device__ __forceinline__ void dz_store(const A& a, int64_t row, int c0, const float (&v)[8]) {      // (columns beyond n are padding)
+  *reinterpret_cast<uint4*>(a.dz + (size_t)row * a.ldz + c0) =
+      make_uint4(pack16(v[0], v[1], a.f16), pack16(v[2], v[3], a.f16), pack16(v[4], v[5], a.f16), pack16(v[6], v[7], a.f16));
 }
 
-// A lane takes eight columns of every eighth row of its chunk (VEC: neighbours, in 16-byte accesses; else 32 columns apart), four rows
-// requested ahead. Bound by memory.
-template <bool F32, bool VEC>
+// A lane takes eight neighbouring columns of every eighth row of its chunk, four rows requested ahead. Bound by memory.
+template <bool F32, bool WHOLE>
 __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
   __shared__ float sums[kDzWarps][kDzCols];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c0 = blockIdx.x * kDzCols + (VEC ? lane * 8 : lane);
+  const int c0 = blockIdx.x * kDzCols + lane * 8;
   float sum[8] = {};
+  start_behind_prior_kernel();
   const int64_t stride = (int64_t)gridDim.y * kDzWarps, first = (int64_t)blockIdx.y * kDzWarps + warp;
-  if (VEC && c0 < a.n) {
+  if (c0 < a.n) {
     constexpr int kAhead = 4;
-    DzRow<F32> ahead[kAhead];
+    DzRow<F32, WHOLE> ahead[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (first + i * stride < a.rows) dz_request(ahead[i], a, first + i * stride, c0);
@@ -105,42 +128,37 @@ __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
         const int64_t row = base + i * stride, next = row + kAhead * stride;
         if (row >= a.rows) break;
         float v[8];
-        dz_values(ahead[i], a, v);
+        dz_values(ahead[i], a, row, c0, v);
         if (next < a.rows) dz_request(ahead[i], a, next, c0);
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum[u] += v[u];
-        if (a.dz)
-          *reinterpret_cast<uint4*>(a.dz + (size_t)row * a.ldz + c0) =
-              make_uint4(pack16(v[0], v[1], a.f16), pack16(v[2], v[3], a.f16), pack16(v[4], v[5], a.f16), pack16(v[6], v[7], a.f16));
-      }
-    }
-  } else if (!VEC) {
-#pragma unroll 2
-    for (int64_t row = first; row < a.rows; row += stride) {
-      float v[8];
-      dz_scalar(a, row, c0, v);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        sum[u] += v[u];
-        if (a.dz && c0 + u * 32 < a.n) a.dz[(size_t)row * a.ldz + c0 + u * 32] = round16(v[u], a.f16);
+        if (a.dz) dz_store(a, row, c0, v);
       }
     }
   }
-  if (!a.part) return;
-  if (VEC) {
-    *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-    *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
-  } else {
-#pragma unroll
-    for (int u = 0; u < 8; ++u) sums[warp][lane + u * 32] = sum[u];
-  }
+  if (!a.db) return;
+  *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+  *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(sum[4], sum[5], sum[6], sum[7]);
   __syncthreads();
   const int c = blockIdx.x * kDzCols + threadIdx.x;
-  if (c >= a.n) return;
   float s = 0.f;
 #pragma unroll
   for (int w = 0; w < kDzWarps; ++w) s += sums[w][threadIdx.x];
-  if (gridDim.y == 1) store_typed(a.db, a.tdb, c, s);
+  if (a.cluster > 1) {                            // the first CTA of the cluster adds the others' sums
+    sums[0][threadIdx.x] = s;                     // (of this thread's column alone)
+    cluster_sync_all();
+    if (blockIdx.y == 0) {
+      const uint32_t mine = smem_u32(&sums[0][threadIdx.x]);
+      for (int r = 1; r < a.cluster; ++r) {
+        float other;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(other) : "r"(map_to_cta(mine, (uint32_t)r)) : "memory");
+        s += other;
+      }
+    }
+    cluster_sync_all();                           // no CTA leaves while its sums may still be read
+  }
+  if (c >= a.n || (a.cluster > 1 && blockIdx.y > 0)) return;
+  if ((int)gridDim.y == a.cluster) store_typed(a.db, a.tdb, c, s);
   else a.part[(size_t)blockIdx.y * a.n + c] = s;
 }
 
@@ -148,9 +166,10 @@ __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
 __global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks, int n, void* db, int tdb) {
   __shared__ float sums[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  start_behind_prior_kernel();
   float s = 0.f;
   if (c < n)
-#pragma unroll 4
+#pragma unroll 8
     for (int i = warp; i < chunks; i += 8) s += part[(size_t)i * n + c];
   sums[warp][lane] = s;
   __syncthreads();
@@ -175,31 +194,39 @@ int dz_chunks(int64_t rows, int32_t n) {
 struct TableArgs {
   const int* step;                                // [rows]
   int* begin;                                     // [steps + 1] where a step's rows begin in the list
-  int* list;                                      // [rows] rows in the order of their steps; those outside the table are left out
-  int* list_step;                                 // [rows] the steps, in the same order
+  int* list;                                      // [rows] rows in the order of their steps, those outside the table in the end
+  int* list_step;                                 // [rows] the steps, in the same order (`steps` outside the table)
   const void* dy; const float* factor;            // as in DzArgs
+  uint16_t* dz;                                   // as in DzArgs
+  float* db_part;                                 // [gridDim.y][n] column sums, NULL = not wanted
   float* part;                                    // [slices][2][n] sums of runs that cross a slice's begin, its end
   uint16_t* dtable;                               // [steps, n] of the operands' type
   int64_t lddy, ldz;
   int tdy, rows, n, steps, f16;
+  int slice;                                      // list entries of a warp of k_table_sum: 32 (one in each lane) at most
 };
 
 constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
-constexpr int kSlice = 32;                        // list entries of a warp of k_table_sum: one in each lane
 
-// One CTA per step: how many rows have smaller steps, then its own rows in ascending order, a warp for every sixteenth of the rows. Every
-// CTA reads all of `step`, twice, from L2 and L1: 250 steps over 8192 rows are 8 MB.
+// One CTA per step, and one for rows outside the table: how many rows have smaller steps, then its own rows in ascending order, a warp for
+// every sixteenth of the rows. Every CTA reads all of `step`, twice, from L2 and L1: 250 steps over 8192 rows are 8 MB.
 __global__ void __launch_bounds__(kListThreads) k_table_list(const TableArgs a) {
   __shared__ int less[kListWarps], same[kListWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.x;
   const int64_t share = ((int64_t)a.rows + kListThreads - 1) / kListThreads * 32;
   const int64_t r0 = warp * share, r1 = min((int64_t)a.rows, r0 + share);
   constexpr int kAhead = 8;
+  start_behind_prior_kernel();
+  const auto step_at = [&](int64_t r) {           // -1 behind the last row
+    if (r >= r1) return -1;
+    const int v = a.step[r];
+    return v >= 0 && v < a.steps ? v : a.steps;
+  };
   int nless = 0, nsame = 0;
   for (int64_t r = r0 + lane; r < r1; r += 32 * kAhead) {
     int v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) v[i] = r + 32 * i < r1 ? __ldg(a.step + r + 32 * i) : -1;
+    for (int i = 0; i < kAhead; ++i) v[i] = step_at(r + 32 * i);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       nless += v[i] >= 0 && v[i] < s;
@@ -213,22 +240,18 @@ __global__ void __launch_bounds__(kListThreads) k_table_list(const TableArgs a) 
   }
   if (lane == 0) { less[warp] = nless; same[warp] = nsame; }
   __syncthreads();
-  int base = 0, at = 0, all = 0;
+  int base = 0, at = 0;
   for (int w = 0; w < kListWarps; ++w) {
     base += less[w];
     if (w < warp) at += same[w];
-    all += same[w];
   }
-  if (threadIdx.x == 0) {
-    a.begin[s] = base;
-    if (s == a.steps - 1) a.begin[a.steps] = base + all;
-  }
+  if (threadIdx.x == 0) a.begin[s] = base;
   if (nsame == 0) return;
   at += base;
   for (int64_t r = r0; r < r1; r += 32 * kAhead) {
     int v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) v[i] = r + 32 * i + lane < r1 ? __ldg(a.step + r + 32 * i + lane) : -1;
+    for (int i = 0; i < kAhead; ++i) v[i] = step_at(r + 32 * i + lane);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const uint32_t votes = __ballot_sync(0xffffffffu, v[i] == s);
@@ -244,77 +267,84 @@ __global__ void __launch_bounds__(kListThreads) k_table_list(const TableArgs a) 
 
 constexpr int kTableThreads = 128, kTableWarps = kTableThreads / 32;
 
-// A warp adds the rows of a slice of the list over 256 columns (VEC: eight neighbours per lane), four rows requested ahead. A run of one
-// step that begins and ends in the slice is a finished row of the gradient; the others are parts for k_table_join.
-template <bool F32, bool VEC>
+// The same pass as k_linear_dz with the rows in the order of the list (dy and its factors are read once for all three results). A warp
+// adds the rows of a slice over 256 columns, four rows requested ahead. A run of one step that begins and ends in the slice
+// is a finished row of the gradient; the others are parts for k_table_join.
+template <bool F32, bool WHOLE>
 __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t sl = (int64_t)blockIdx.y * kTableWarps + (threadIdx.x >> 5);
-  const int total = a.begin[a.steps];
-  if (sl * kSlice >= total) return;
-  const int i0 = (int)(sl * kSlice), count = min(kSlice, total - i0);
-  const int c0 = blockIdx.x * 256 + (VEC ? lane * 8 : lane);
-  const bool live = c0 < a.n;
-  constexpr int kStep = VEC ? 1 : 32;
-  const int my_row = lane < count ? __ldg(a.list + i0 + lane) : 0, my_step = lane < count ? __ldg(a.list_step + i0 + lane) : -1;
-  const int step_before = i0 > 0 ? __ldg(a.list_step + i0 - 1) : -1, step_after = i0 + count < total ? __ldg(a.list_step + i0 + count) : -1;
-  float sum[8] = {};
+  __shared__ float sums[kTableWarps][256];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t sl = (int64_t)blockIdx.y * kTableWarps + warp;
+  const int total = a.rows, i0 = (int)min((int64_t)total, sl * a.slice), count = min(a.slice, total - i0);   // (0: behind the last row)
+  start_behind_prior_kernel();
+  const int c0 = blockIdx.x * 256 + lane * 8;
+  const bool live = c0 < a.n, whole_out = a.n % 8 == 0;
+  const int my_row = lane < count ? a.list[i0 + lane] : 0, my_step = lane < count ? a.list_step[i0 + lane] : -1;
+  const int step_before = i0 > 0 ? a.list_step[i0 - 1] : -1, step_after = i0 + count < total ? a.list_step[i0 + count] : -1;
+  float sum[8] = {}, all[8] = {};
   const auto flush = [&](int s, bool whole) {     // the run of step s that ends here
-    if (whole) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) all[u] += sum[u];
+    if (s == a.steps || !live) {                  // outside the table
+    } else if (whole) {
       uint16_t* out = a.dtable + (size_t)s * a.n + c0;
-      if (VEC) {
-        if (live)
-          *reinterpret_cast<uint4*>(out) = make_uint4(pack16(sum[0], sum[1], a.f16), pack16(sum[2], sum[3], a.f16),
-                                                      pack16(sum[4], sum[5], a.f16), pack16(sum[6], sum[7], a.f16));
+      if (whole_out) {
+        *reinterpret_cast<uint4*>(out) = make_uint4(pack16(sum[0], sum[1], a.f16), pack16(sum[2], sum[3], a.f16),
+                                                    pack16(sum[4], sum[5], a.f16), pack16(sum[6], sum[7], a.f16));
       } else {
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-          if (c0 + u * kStep < a.n) out[u * kStep] = round16(sum[u], a.f16);
+          if (c0 + u < a.n) out[u] = round16(sum[u], a.f16);
       }
     } else {
-      float* out = a.part + ((size_t)sl * 2 + (s == step_before ? 0 : 1)) * a.n + c0;
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (c0 + u * kStep < a.n) out[u * kStep] = sum[u];
+      float* out = a.part + ((size_t)sl * 2 + (s == step_before ? 0 : 1)) * a.ldz + c0;
+      *reinterpret_cast<float4*>(out) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+      *reinterpret_cast<float4*>(out + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u) sum[u] = 0.f;
   };
   constexpr int kAhead = 4;
-  DzRow<F32> ahead[kAhead];
-  int first_row[kAhead];
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k) first_row[k] = __shfl_sync(0xffffffffu, my_row, min(k, count - 1));
-  if (VEC && live)
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) dz_request(ahead[k], a, first_row[k], c0);
+  DzRow<F32, WHOLE> ahead[kAhead];
   int step = __shfl_sync(0xffffffffu, my_step, 0);
-  for (int i = 0; i < kSlice; i += kAhead) {
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int row = __shfl_sync(0xffffffffu, my_row, k);
+    if (live && k < count) dz_request(ahead[k], a, row, c0);
+  }
+  for (int i = 0; i < count; i += kAhead) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (i + k >= count) break;
       const int s = __shfl_sync(0xffffffffu, my_step, i + k), row = __shfl_sync(0xffffffffu, my_row, i + k);
-      const int next = __shfl_sync(0xffffffffu, my_row, min(i + k + kAhead, count - 1));
+      const int next = __shfl_sync(0xffffffffu, my_row, (i + k + kAhead) & 31);
       if (s != step) {
         flush(step, step != step_before);
         step = s;
       }
-      float v[8];
-      if (VEC) {
-        if (live) {
-          dz_values(ahead[k], a, v);
-          if (i + k + kAhead < count) dz_request(ahead[k], a, next, c0);
-#pragma unroll
-          for (int u = 0; u < 8; ++u) sum[u] += v[u];
-        }
-      } else {
-        dz_scalar(a, row, c0, v);
+      if (live) {
+        float v[8];
+        dz_values(ahead[k], a, row, c0, v);
+        if (i + k + kAhead < count) dz_request(ahead[k], a, next, c0);
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum[u] += v[u];
+        if (a.dz) dz_store(a, row, c0, v);
       }
     }
   }
-  flush(step, step != step_before && step != step_after);
+  if (count > 0) flush(step, step != step_before && step != step_after);
+  if (!a.db_part) return;
+  *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(all[0], all[1], all[2], all[3]);
+  *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(all[4], all[5], all[6], all[7]);
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 256 / kTableThreads; ++u) {
+    const int x = threadIdx.x + u * kTableThreads, c = blockIdx.x * 256 + x;
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kTableWarps; ++w) t += sums[w][x];
+    if (c < a.n) a.db_part[(size_t)blockIdx.y * a.n + c] = t;
+  }
 }
 
 // The sums of a run that crosses slices, and zeros for a step without rows. A CTA takes one step and 256 / W columns, a warp of W for
@@ -323,14 +353,15 @@ template <int W>
 __global__ void __launch_bounds__(256) k_table_join(const TableArgs a) {
   __shared__ float sums[W][256 / W];
   const int s = blockIdx.y, x = threadIdx.x % (256 / W), w = threadIdx.x / (256 / W), c = blockIdx.x * (256 / W) + x;
+  start_behind_prior_kernel();
   const int from = a.begin[s], end = a.begin[s + 1];
-  const int first = from / kSlice, last = (end - 1) / kSlice;
+  const int first = from / a.slice, last = (end - 1) / a.slice;
   if (from < end && first == last) return;        // written by the slice's warp
   float sum = 0.f;
   if (from < end && c < a.n) {
-    if (w == 0) sum = a.part[((size_t)first * 2 + 1) * a.n + c];
+    if (w == 0) sum = a.part[((size_t)first * 2 + 1) * a.ldz + c];
 #pragma unroll 8
-    for (int i = first + 1 + w; i <= last; i += W) sum += a.part[(size_t)i * 2 * a.n + c];
+    for (int i = first + 1 + w; i <= last; i += W) sum += a.part[(size_t)i * 2 * a.ldz + c];
   }
   if (W > 1) {
     sums[w][x] = sum;
@@ -343,7 +374,15 @@ __global__ void __launch_bounds__(256) k_table_join(const TableArgs a) {
   if (c < a.n) a.dtable[(size_t)s * a.n + c] = round16(sum, a.f16);
 }
 
-int64_t table_slices(int64_t rows) { return (rows + kSlice - 1) / kSlice; }
+// Entries of a slice: as many as leave 24 warps for every SM, between 8 and 32 (a warp's rows wait for memory one behind the other).
+int table_slice(int64_t rows, int32_t n) {
+  const int64_t cols = (n + 255) / 256;
+  int s = 32;
+  while (s > 8 && rows * cols < (int64_t)s * 24 * 148) s /= 2;
+  return s;
+}
+int64_t table_slices(int64_t rows, int32_t n) { return (rows + table_slice(rows, n) - 1) / table_slice(rows, n); }
+int64_t table_parts(int64_t rows, int32_t n) { return (table_slices(rows, n) + kTableWarps - 1) / kTableWarps; }
 
 inline size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 inline bool whole(const void* p, int64_t ld, size_t bytes) {      // rows of whole 16-byte pieces
@@ -393,11 +432,11 @@ LinearWorkspace linear_workspace(int64_t rows, int32_t k, int32_t n, int32_t nst
   size_t at = 256;                                // the status word
   const auto take = [&](size_t bytes) { const size_t o = at; at = round_up(at + bytes, 256); return o; };
   w.dz = take((size_t)rows * round_up(n, 8) * 2);
-  w.db = take(rows > 0 ? (size_t)dz_chunks(rows, n) * n * 4 : 0);
+  w.db = take(rows > 0 ? (size_t)std::max<int64_t>(dz_chunks(rows, n), has_table ? table_parts(rows, n) : 0) * n * 4 : 0);
   w.dw = take(rows > 0 ? part_floats(n, k, linear_parts(rows, k, n)) * 4 : 0);
   w.begin = take(has_table ? ((size_t)nsteps + 1) * 4 : 0);
   w.list = take(has_table ? (size_t)rows * 8 : 0);
-  w.table = take(has_table ? (size_t)table_slices(rows) * 2 * n * 4 : 0);
+  w.table = take(has_table ? (size_t)table_slices(rows, n) * 2 * round_up(n, 8) * 4 : 0);
   w.bytes = at;
   return w;
 }
@@ -443,16 +482,25 @@ cudaError_t launch_linear(const LinearArgs& a, cudaStream_t st) {
 
 namespace {
 
-cudaError_t launch_dz(const DzArgs& d, bool vec, int chunks, cudaStream_t st) {
+template <class K, class... Args>
+cudaError_t start(K kernel, dim3 grid, int threads, int cluster_y, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  launch_attributes(attr, 1);
+  attr[0].val.clusterDim.y = (unsigned)cluster_y;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+cudaError_t launch_dz(const DzArgs& d, bool whole_dy, int chunks, cudaStream_t st) {
   const dim3 grid((d.n + kDzCols - 1) / kDzCols, chunks);
-  if (d.tdy == SDS_F32) {
-    if (vec) k_linear_dz<true, true><<<grid, kDzThreads, 0, st>>>(d);
-    else k_linear_dz<true, false><<<grid, kDzThreads, 0, st>>>(d);
-  } else {
-    if (vec) k_linear_dz<false, true><<<grid, kDzThreads, 0, st>>>(d);
-    else k_linear_dz<false, false><<<grid, kDzThreads, 0, st>>>(d);
-  }
-  return cudaGetLastError();
+  const auto go = [&](auto kernel) { return start(kernel, grid, kDzThreads, d.cluster, st, d); };
+  if (d.tdy == SDS_F32) return whole_dy ? go(k_linear_dz<true, true>) : go(k_linear_dz<true, false>);
+  return whole_dy ? go(k_linear_dz<false, true>) : go(k_linear_dz<false, false>);
 }
 
 cudaError_t launch_join(const float* part, uint16_t* out, int M, int N, int parts, int f16, cudaStream_t st) {
@@ -470,20 +518,17 @@ cudaError_t launch_join(const float* part, uint16_t* out, int M, int N, int part
   return cudaLaunchKernelEx(&cfg, k_ffn_join, join);
 }
 
-cudaError_t launch_table(const TableArgs& t, bool vec, cudaStream_t st) {
-  k_table_list<<<t.steps, kListThreads, 0, st>>>(t);
+cudaError_t launch_table(const TableArgs& t, bool whole_dy, cudaStream_t st) {
+  cudaError_t e = start(k_table_list, dim3(t.steps + 1), kListThreads, 1, st, t);
+  if (e != cudaSuccess) return e;
   const int cols = (t.n + 255) / 256;
-  const dim3 grid(cols, (unsigned)((table_slices(t.rows) + kTableWarps - 1) / kTableWarps));
-  if (t.tdy == SDS_F32) {
-    if (vec) k_table_sum<true, true><<<grid, kTableThreads, 0, st>>>(t);
-    else k_table_sum<true, false><<<grid, kTableThreads, 0, st>>>(t);
-  } else {
-    if (vec) k_table_sum<false, true><<<grid, kTableThreads, 0, st>>>(t);
-    else k_table_sum<false, false><<<grid, kTableThreads, 0, st>>>(t);
-  }
-  if ((int64_t)cols * t.steps >= 4 * 148) k_table_join<1><<<dim3(cols, t.steps), 256, 0, st>>>(t);
-  else k_table_join<8><<<dim3((t.n + 31) / 32, t.steps), 256, 0, st>>>(t);
-  return cudaGetLastError();
+  const dim3 grid(cols, (unsigned)table_parts(t.rows, t.n));
+  const auto go = [&](auto kernel) { return start(kernel, grid, kTableThreads, 1, st, t); };
+  if (t.tdy == SDS_F32) e = whole_dy ? go(k_table_sum<true, true>) : go(k_table_sum<true, false>);
+  else e = whole_dy ? go(k_table_sum<false, true>) : go(k_table_sum<false, false>);
+  if (e != cudaSuccess) return e;
+  return (int64_t)cols * t.steps >= 4 * 148 ? start(k_table_join<1>, dim3(cols, t.steps), 256, 1, st, t)
+                                            : start(k_table_join<8>, dim3((t.n + 31) / 32, t.steps), 256, 1, st, t);
 }
 
 }  // namespace
@@ -503,25 +548,13 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
   const float* factor = a.act == SDS_ACT_NONE ? nullptr : a.factor;
   const int64_t ldz = (int64_t)round_up(a.n, 8);
   const size_t sy = a.ty == SDS_F32 ? 4 : 2;
-  const bool vec = a.n % 8 == 0 && whole(a.dy, a.lddy, sy);
+  const bool whole_dy = a.n % 8 == 0 && whole(a.dy, a.lddy, sy);
   const bool products = a.dx || a.dw;
   // without an activation dy itself is the operand, where its rows are ones that the tensor maps take
   const bool direct = !factor && a.ty != SDS_F32 && whole(a.dy, a.lddy, 2);
-  if ((products && !direct) || a.db) {
-    DzArgs d{};
-    d.dy = a.dy; d.lddy = a.lddy; d.tdy = a.ty;
-    d.factor = factor; d.ldz = ldz; d.f16 = a.f16;
-    d.dz = products && !direct ? reinterpret_cast<uint16_t*>(ws + at.dz) : nullptr;
-    d.part = a.db ? reinterpret_cast<float*>(ws + at.db) : nullptr;
-    d.db = a.db; d.tdb = a.tbias;
-    d.rows = a.rows; d.n = a.n;
-    const int chunks = dz_chunks(a.rows, a.n);
-    if ((e = launch_dz(d, vec, chunks, st)) != cudaSuccess) return e;
-    if (a.db && chunks > 1) {
-      k_linear_db<<<(a.n + 31) / 32, 256, 0, st>>>(d.part, chunks, a.n, a.db, a.tbias);
-      if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    }
-  }
+  uint16_t* to_dz = products && !direct ? reinterpret_cast<uint16_t*>(ws + at.dz) : nullptr;
+  float* db_part = reinterpret_cast<float*>(ws + at.db);
+  int64_t db_parts = 0;                           // whose sums are still to be added
   if (a.dtable) {
     TableArgs t{};
     t.step = a.step;
@@ -529,10 +562,27 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
     t.list_step = t.list + a.rows;
     t.part = reinterpret_cast<float*>(ws + at.table);
     t.dy = a.dy; t.lddy = a.lddy; t.tdy = a.ty; t.factor = factor; t.ldz = ldz;
+    t.dz = to_dz; t.db_part = a.db ? db_part : nullptr;
     t.dtable = static_cast<uint16_t*>(a.dtable);
     t.rows = a.rows; t.n = a.n; t.steps = a.steps; t.f16 = a.f16;
-    if ((e = launch_table(t, vec, st)) != cudaSuccess) return e;
+    t.slice = table_slice(a.rows, a.n);
+    if ((e = launch_table(t, whole_dy, st)) != cudaSuccess) return e;
+    db_parts = a.db ? table_parts(a.rows, a.n) : 0;
+  } else if (to_dz || a.db) {
+    DzArgs d{};
+    d.dy = a.dy; d.lddy = a.lddy; d.tdy = a.ty;
+    d.factor = factor; d.ldz = ldz; d.f16 = a.f16;
+    d.dz = to_dz;
+    d.part = db_part; d.db = a.db; d.tdb = a.tbias;
+    d.rows = a.rows; d.n = a.n;
+    const int chunks = dz_chunks(a.rows, a.n);
+    d.cluster = a.db && chunks <= 8 ? chunks : 1;
+    if ((e = launch_dz(d, whole_dy, chunks, st)) != cudaSuccess) return e;
+    db_parts = a.db && chunks > d.cluster ? chunks : 0;
   }
+  if (db_parts > 0 &&
+      (e = start(k_linear_db, dim3((a.n + 31) / 32), 256, 1, st, (const float*)db_part, (int)db_parts, a.n, a.db, a.tbias)) != cudaSuccess)
+    return e;
   if (!products) return cudaMemsetAsync(a.err, 0, sizeof(int), st);
   const Mat dz = direct ? Mat{a.dy, a.lddy} : Mat{ws + at.dz, ldz};
   FfnArgs f{};

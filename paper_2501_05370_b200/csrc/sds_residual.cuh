@@ -124,10 +124,11 @@ __device__ __forceinline__ void store_row(T* row, const Columns<TPR, CL, VEC>& c
   }
 }
 
+// (Loads are plain ones: the compiler may move read-only loads ahead of the wait for the kernel in front.)
 // A thread's columns of a vector of any of the three types. 16-bit vectors of whole pieces (VEC) can be requested ahead, as they lie in memory; floats are read where they are used (twice the registers, and they mostly lie in L1).
 template <int TPR, int CL, bool VEC>
 __device__ __forceinline__ void request_vector(uint4& r, const void* p, int type, uint64_t off, const Columns<TPR, CL, VEC>& col) {
-  if (VEC && p && type != SDS_F32 && col.live) r = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + off + col.c0));
+  if (VEC && p && type != SDS_F32 && col.live) r = *(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + off + col.c0));
 }
 // (p is not NULL)
 template <int TPR, int CL, bool VEC>
@@ -136,7 +137,7 @@ __device__ __forceinline__ void take_vector(const uint4& r, const void* p, int t
   if (VEC) {
     if (type == SDS_F32) {
       const uint4* from = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + off + (col.live ? col.c0 : 0));
-      const uint4 q[2] = {__ldg(from), __ldg(from + 1)};
+      const uint4 q[2] = {from[0], from[1]};
       words_to(q, o, 0.f);
     } else if (type == SDS_BF16) {
       words_to(&r, o, Bf16{});

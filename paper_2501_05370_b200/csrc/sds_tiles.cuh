@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
       };
       if (EPI == kFfnDGlu) keep_fetch(n0);
       // neither do the bias, the rows of the table and the residual (kLinear): requested a chunk ahead
-      int table_row = -1, piece_row[4];           // of the lane's row; of the rows of which it fetches a piece
+      int table_row = -1, piece_row[4] = {-1, -1, -1, -1};   // of the lane's row; of the rows of which it fetches a piece
       Rows64 tab, res[2];
       float bias_next = 0.f;
       const auto added_fetch = [&](int col) {
@@ -612,7 +612,7 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
       if (is_linear(EPI)) {
         if (g.lin.table) {
           if (lane < nlive) {
-            const int s = __ldg(g.lin.step + row0 + lane);
+            const int s = g.lin.step[row0 + lane];
             table_row = s >= 0 && s < g.lin.steps ? s : -1;
           }
 #pragma unroll
@@ -1069,12 +1069,12 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
           for (int u = 0; u < 4; ++u)
             if (u < live) z[u] += load_typed(e.bias, e.tbias, (size_t)(col + u));
         if (e.table) {
-          const int at = __ldg(e.step + tok);
+          const int at = e.step[tok];
           const bool in = at >= 0 && at < e.steps;
           const uint16_t* from = e.table + (int64_t)(in ? at : 0) * g.N + col;
           float t[4] = {0.f, 0.f, 0.f, 0.f};
           if (EPI == kLinear) {
-            const uint2 w = __ldg(reinterpret_cast<const uint2*>(from));
+            const uint2 w = *reinterpret_cast<const uint2*>(from);
             const float2 lo = unpack16x2(w.x, g.f16), hi = unpack16x2(w.y, g.f16);
             t[0] = lo.x; t[1] = lo.y; t[2] = hi.x; t[3] = hi.y;
           } else {
