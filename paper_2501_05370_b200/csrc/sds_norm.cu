@@ -55,7 +55,7 @@ __device__ __forceinline__ void load_vector(const void* p, int type, bool wide, 
   } else if (V > 1 && wide && type == SDS_F32) {
 #pragma unroll
     for (int q = 0; q < V / 4; ++q) {
-      const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + c) + q);
+      const float4 v = reinterpret_cast<const float4*>(static_cast<const float*>(p) + c)[q];
       o[(4 * q) % V] = v.x; o[(4 * q + 1) % V] = v.y; o[(4 * q + 2) % V] = v.z; o[(4 * q + 3) % V] = v.w;
     }
   } else {
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, VEC && TPR <= 128 && !F
     const bool live = row < rows;
     U x[NV][P];
     U s0 = Unit<V>::all(0.f);
-    const uint16_t* te = RES && live && a.temb ? a.temb + (size_t)__ldg(a.rowk + row) * d : nullptr;
+    const uint16_t* te = RES && live && a.temb ? a.temb + (size_t)a.rowk[row] * d : nullptr;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + t) * V;
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(512, 1) k_norm_bwd(const NormArgs a) {
     copies_commit();
   };
   const auto stats_of = [&](int64_t row) {
-    return row < rows ? make_float2(__ldg(a.mean + row), __ldg(a.rstd + row)) : make_float2(0.f, 0.f);
+    return row < rows ? make_float2(a.mean[row], a.rstd[row]) : make_float2(0.f, 0.f);
   };
   int base = (int)blockIdx.x / CL * RPC, flip = 0, at = 0;
   constexpr bool SKEW = CL > 1 && VEC;                          // (see the loop at the end)

@@ -212,7 +212,8 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* slot, int t, int
 // Kernels overlap their starts: the next one may be started once all CTAs of this one have begun (their launch takes about
 // as long as a small call runs), and this one waits here for the end of the kernel in front, and for its writes.
 // Nothing in device memory is read or written before. The next one is let go before this wait: it may begin while what ran
-// in front of this kernel still runs, so it has to wait in full as well before it reads anything.
+// in front of this kernel still runs, so it has to wait in full as well before it reads anything. (Loads behind it are plain ones: the
+// compiler may move read-only loads ahead of the wait.)
 __device__ __forceinline__ void start_after_prior_kernel() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");

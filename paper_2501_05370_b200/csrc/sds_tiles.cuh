@@ -289,6 +289,7 @@ __device__ __forceinline__ void store_narrow32(uint4* stg, const uint32_t* w, ui
   __syncwarp();
 }
 
+// (Loads of what another kernel wrote are plain ones throughout: the compiler may move read-only loads ahead of the wait for it.)
 // Kernels overlap their starts: one may be started when all CTAs of the one in front have said so (or ended), and waits
 // for that kernel's end, and for its writes, here. Two kinds read device memory before that wait: k_ffn_split in a call's later
 // products, the weights, which nothing in the call writes; and a tile launch `beside` (FfnTileArgs), all it needs, as it reads
@@ -579,8 +580,8 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
         const float4* kp0 = reinterpret_cast<const float4*>(g.keep + (in ? keep_index(row0 + lane, col, ncc, 0) : 0));
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          kp[i] = in ? __ldg(kp0 + i * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
-          kq[i] = in ? __ldg(kp0 + (8 + i) * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+          kp[i] = in ? kp0[i * 32] : make_float4(0.f, 0.f, 0.f, 0.f);
+          kq[i] = in ? kp0[(8 + i) * 32] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
       };
       if (EPI == kFfnDGlu) keep_fetch(n0);
