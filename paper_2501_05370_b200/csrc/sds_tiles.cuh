@@ -290,6 +290,86 @@ __device__ __forceinline__ void store_narrow32(uint4* stg, const uint32_t* w, ui
 }
 
 // (Loads of what another kernel wrote are plain ones throughout: the compiler may move read-only loads ahead of the wait for it.)
+// kLinear with a float result, 16 columns of the warp's rows at a time (a lane's each): what the sums of SUMS leave of the registers
+template <int EPI>
+__device__ __forceinline__ void linear_floats(const LinearEpilogue& e, int act, uint4* stg, float (&z)[16], int table_row, float* out, int64_t ldo,
+                                              int row0, int nrows, int col, int N, int f16, int lane) {
+  constexpr bool WHOLE = EPI == kLinear;
+  const int ncols = min(16, N - col);
+  if (e.bias) {
+    reinterpret_cast<float*>(stg)[lane & 15] = (lane & 15) < ncols ? load_typed(e.bias, e.tbias, (size_t)(col + (lane & 15))) : 0.f;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 b = reinterpret_cast<const float4*>(stg)[i];
+      z[4 * i] += b.x; z[4 * i + 1] += b.y; z[4 * i + 2] += b.z; z[4 * i + 3] += b.w;
+    }
+    __syncwarp();
+  }
+  if (e.table) {
+    const uint16_t* from = e.table + (size_t)max(table_row, 0) * N + col;
+    const float bad = table_row < 0 ? __int_as_float(0x7fffffff) : 0.f;
+    if (WHOLE) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint4 t = 8 * k < ncols ? *reinterpret_cast<const uint4*>(from + 8 * k) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 v = unpack16x2(w[i], f16);
+          z[8 * k + 2 * i] += v.x + bad;
+          z[8 * k + 2 * i + 1] += v.y + bad;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] += (i < ncols ? unpack16(from[i], f16) : 0.f) + bad;
+    }
+  }
+  uint32_t w[16];
+  with_activation_or_none(act, [&](auto a) {
+    constexpr int ACT = decltype(a)::value;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float d;
+      activation<ACT>(z[i], z[i], d);
+      w[i] = __float_as_uint(d);
+    }
+  });
+  if (e.factor)
+    store_rows64(stg, w, reinterpret_cast<char*>(e.factor + (size_t)row0 * e.ldf + col), (size_t)e.ldf * 4, nrows, min(4, ((int)e.ldf - col) >> 2), lane);
+  if (e.residual) {
+    const float* res = static_cast<const float*>(e.residual) + (size_t)row0 * e.ldr + col;
+    if (WHOLE) {
+      Rows64 r;
+      fetch_rows(r, [&](int i) -> const uint4* {
+        const int row = 8 * i + (lane >> 2), c = 4 * (lane & 3);
+        return row < nrows && c < ncols ? reinterpret_cast<const uint4*>(res + (size_t)row * e.ldr + c) : nullptr;
+      });
+      rows_to_lanes(stg, r, w, lane);
+    } else {
+      narrow32_to_lanes(stg, [&](int row) -> const uint32_t* {
+        return row < nrows ? reinterpret_cast<const uint32_t*>(res + (size_t)row * e.ldr) : nullptr;
+      }, ncols, w, lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] += __uint_as_float(w[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(z[i]);
+  float* to = out + (size_t)row0 * ldo + col;
+  if (WHOLE) store_rows64(stg, w, reinterpret_cast<char*>(to), (size_t)ldo * 4, nrows, ncols >> 2, lane);
+  else store_narrow32(stg, w, reinterpret_cast<uint32_t*>(to), ldo, nrows, ncols, lane);
+}
+
+// eight columns of the warp's 32 lanes back to tensor memory; they may be loaded again behind tmem_st_wait
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // Kernels overlap their starts: one may be started when all CTAs of the one in front have said so (or ended), and waits
 // for that kernel's end, and for its writes, here. Two kinds read device memory before that wait: k_ffn_split in a call's later
 // products, the weights, which nothing in the call writes; and a tile launch `beside` (FfnTileArgs), all it needs, as it reads
@@ -397,8 +477,12 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
 // Bound by the tensor cores: 16384 x 2048 x 8192 forward 1280 us, 1290 TFLOP/s (92 % of the library's rate in a long run, where power
 // sets the clock); 8192 rows forward and backward 2130 us, 1160 TFLOP/s beside the kept factors.
 // CUT: products whose K is cut (FfnProduct::parts); its own kernel, as the others lose up to 5 % to the arithmetic.
-// EW: epilogue warps, four or eight (two for each quarter of the lanes, half of the columns each).
-template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW>
+// EW: epilogue warps, four, eight (two for each quarter of the lanes, half of the columns each) or sixteen.
+// SUMS: the tensor cores add to their accumulator without rounding to nearest, so a long sum comes out short by about K / 16 times 2^-25 of
+// itself (K = 8192: 6.4e-6, where a float's own rounding is 3e-8). Where the result is a float, every kSumSteps steps of K
+// have an accumulator of their own, and the epilogue's warps add these in registers (sixteen warps hold a tile's), while the next is filled.
+constexpr int kSumSteps = 12;
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW, bool SUMS>
 __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
   using C = FfnTile<BN, PAIR, EW>;
   constexpr int TM = C::kTM, TN = EPI == kFfnGlu ? BN / 2 : BN;    // output columns of a tile
@@ -513,7 +597,7 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
   } else if (warp == 1) {
     // ---------------- MMA issuer ----------------
     if (lane == 0 && rank == 0) {
-      int stage = 0, it = 0;
+      int stage = 0, it = 0, use = 0;             // use: accumulators filled so far
       uint32_t phase = 0;
       bool ok = true;
       bool more = tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, 0), &at);
@@ -521,34 +605,37 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
         const FfnProduct& p = g.p[at.prod];
         const int all = (p.K + kBK - 1) / kBK * p.nseg;
         const int nkb = CUT ? first_step(all, p.parts, at.part + 1) - first_step(all, p.parts, at.part) : all;
-        const int buf = it & 1;
-        if (!mbar_wait(tempty_bar + buf, ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_s)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
-        const auto multiply = [&](auto order) {
-          constexpr bool a_mn = decltype(order)::value;
-          const uint32_t idesc = make_idesc(TM, BN, g.f16 != 0, a_mn, MN);
-          const uint64_t adesc0 = make_sdesc(smem_u32(stages), a_mn ? (uint32_t)kChunkBytes : 0u);
-          const uint64_t bdesc0 = make_sdesc(smem_u32(stages) + C::kABytes, MN ? (uint32_t)kChunkBytes : 0u);
-          constexpr uint64_t a_step = a_mn ? 128u : 2u, b_step = MN ? 128u : 2u;    // 16 elements of K, in 16 bytes
-          for (int kb = 0; kb < nkb; ++kb) {
-            if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
-            tc_fence_after();
-            const uint64_t adesc = adesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
-            const uint64_t bdesc = bdesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
+        const int accumulators = SUMS ? (nkb + kSumSteps - 1) / kSumSteps : 1;
+        for (int part = 0; ok && part < accumulators; ++part, ++use) {
+          const int buf = use & 1, kb0 = SUMS ? part * kSumSteps : 0, kb1 = SUMS ? min(nkb, kb0 + kSumSteps) : nkb;
+          if (!mbar_wait(tempty_bar + buf, ((uint32_t)(use >> 1) & 1u) ^ 1u, abort_s)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
+          const auto multiply = [&](auto order) {
+            constexpr bool a_mn = decltype(order)::value;
+            const uint32_t idesc = make_idesc(TM, BN, g.f16 != 0, a_mn, MN);
+            const uint64_t adesc0 = make_sdesc(smem_u32(stages), a_mn ? (uint32_t)kChunkBytes : 0u);
+            const uint64_t bdesc0 = make_sdesc(smem_u32(stages) + C::kABytes, MN ? (uint32_t)kChunkBytes : 0u);
+            constexpr uint64_t a_step = a_mn ? 128u : 2u, b_step = MN ? 128u : 2u;    // 16 elements of K, in 16 bytes
+            for (int kb = kb0; kb < kb1; ++kb) {
+              if (!mbar_wait(full_bar + stage, phase, abort_s)) { ok = false; break; }
+              tc_fence_after();
+              const uint64_t adesc = adesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
+              const uint64_t bdesc = bdesc0 + (uint64_t)(stage * (C::kStageBytes >> 4));
 #pragma unroll
-            for (int k = 0; k < kBK / 16; ++k) {
-              if (PAIR) umma_f16_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
-              else umma_f16(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb | k) ? 1u : 0u);
+              for (int k = 0; k < kBK / 16; ++k) {
+                if (PAIR) umma_f16_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb > kb0 || k) ? 1u : 0u);
+                else umma_f16(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, (kb > kb0 || k) ? 1u : 0u);
+              }
+              if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
+              if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+              // where the next tile lies takes a few divisions: worked out while this tile's products run
+              if (kb == 0) more = tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
             }
-            if (PAIR) umma_commit_pair(empty_bar + stage); else umma_commit(empty_bar + stage);
-            if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
-            // where the next tile lies takes a few divisions: worked out while this tile's products run
-            if (kb == 0) more = tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, it + 1), &at);
-          }
-        };
-        if (MN && p.a_mn) multiply(Bool<MN>()); else multiply(Bool<false>());
-        if (ok) { if (PAIR) umma_commit_pair(tfull_bar + buf); else umma_commit(tfull_bar + buf); }
+          };
+          if (MN && p.a_mn) multiply(Bool<MN>()); else multiply(Bool<false>());
+          if (ok) { if (PAIR) umma_commit_pair(tfull_bar + buf); else umma_commit(tfull_bar + buf); }
+        }
       }
       if (!ok) {
         raise_abort(abort_s, PAIR);
@@ -563,15 +650,14 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
     uint4* stg = reinterpret_cast<uint4*>(epi_stage + (warp - 2) * kWarpStage);
     const uint32_t drained0 = (PAIR && rank != 0) ? map_to_cta(smem_u32(tempty_bar), 0u) : 0u;
     const int f16 = g.f16;
-    int it = 0;
+    int it = 0, use = 0;
     bool ok = true;
     for (; ok && tile_at<TM, TN, CUT>(g, M0, tile_index(g, worker, nworkers, it), &at); ++it) {
       const FfnProduct& p = g.p[at.prod];
       const int M = at.prod == 0 ? M0 : p.M, N = p.N;
-      const int buf = it & 1;
+      int buf = it & 1;                           // (SUMS: the last one of the tile)
       const int row0 = at.m * TM + (int)rank * kBM + q * 32, n0 = at.n * TN;
       const int nlive = min(32, M - row0);        // (may be negative)
-      const uint32_t tbase = tmem_base + (uint32_t)(buf * BN) + ((uint32_t)(q * 32) << 16);
       const int ncc = (N + 31) >> 5;
       // the kept factors do not depend on this product: requested before its accumulator is waited for
       float4 kp[8], kq[8];
@@ -610,33 +696,83 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
               });
         }
       };
-      if (is_linear(EPI)) {
-        if (g.lin.table) {
-          if (lane < nlive) {
-            const int s = g.lin.step[row0 + lane];
-            table_row = s >= 0 && s < g.lin.steps ? s : -1;
-          }
+      const auto find_table_row = [&]() {
+        if (!g.lin.table || lane >= nlive) return;
+        const int s = g.lin.step[row0 + lane];
+        table_row = s >= 0 && s < g.lin.steps ? s : -1;
+      };
+      if (is_linear(EPI) && !SUMS) {              // (SUMS: the registers hold sums)
+        find_table_row();
+        if (g.lin.table)
 #pragma unroll
           for (int i = 0; i < 4; ++i) piece_row[i] = __shfl_sync(0xffffffffu, table_row, 8 * i + (lane >> 2));
-        }
         added_fetch(n0 + first_chunk * 32);
       }
-      if (!wait_for_sums(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s, (p.K + kBK - 1) / kBK * p.nseg)) { ok = false; break; }
-      tc_fence_after();
+      const auto hand_back = [&](int b) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR && rank != 0) mbar_arrive_cluster(drained0 + (uint32_t)b * 8u);
+          else mbar_arrive(tempty_bar + b);
+        }
+      };
+      if (SUMS) {                                 // the sum of a tile's accumulators goes back to the last one's place
+        float run[SUMS ? kChunks * 32 : 1];
+        const int nkb = (p.K + kBK - 1) / kBK * p.nseg;
+        for (int kb = 0; kb < nkb; kb += kSumSteps, ++use) {
+          if (!wait_for_sums(tfull_bar + (use & 1), (uint32_t)(use >> 1) & 1u, abort_s, kSumSteps)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t from = tmem_base + (uint32_t)((use & 1) * BN + first_chunk * 32) + ((uint32_t)(q * 32) << 16);
+          const bool last = kb + kSumSteps >= nkb;
+#pragma unroll
+          for (int k = 0; k < (SUMS ? kChunks * 32 : 1); k += 8) {
+            uint32_t part[8];
+            tmem_ld8(from + (uint32_t)k, part);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float v = __uint_as_float(part[i]);
+              run[(k + i) % (SUMS ? kChunks * 32 : 1)] = kb == 0 ? v : run[(k + i) % (SUMS ? kChunks * 32 : 1)] + v;
+              part[i] = __float_as_uint(run[(k + i) % (SUMS ? kChunks * 32 : 1)]);
+            }
+            if (last) tmem_st8(from + (uint32_t)k, part);
+          }
+          if (last) {
+            tmem_st_wait();
+            buf = use & 1;
+          } else {
+            hand_back(use & 1);
+          }
+        }
+        if (!ok) break;
+      } else {
+        if (!wait_for_sums(tfull_bar + buf, (uint32_t)(it >> 1) & 1u, abort_s, (p.K + kBK - 1) / kBK * p.nseg)) { ok = false; break; }
+        tc_fence_after();
+      }
+      const uint32_t tbase = tmem_base + (uint32_t)(buf * BN) + ((uint32_t)(q * 32) << 16);
+      if (SUMS) {
+        find_table_row();
 #pragma unroll 1
-      for (int chunk = first_chunk; chunk <= last_chunk; ++chunk) {
+        for (int c = first_chunk * 32; c < (last_chunk + 1) * 32; c += 16) {
+          float z[16];
+          uint32_t part[16];
+          tmem_ld8(tbase + (uint32_t)c, part);
+          tmem_ld8(tbase + (uint32_t)c + 8u, part + 8);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(part[i]);
+          if (c == last_chunk * 32 + 16) hand_back(buf);
+          if (nlive > 0 && n0 + c < N)
+            linear_floats<EPI>(g.lin, g.act, stg, z, table_row, static_cast<float*>(p.out), p.ldo, row0, nlive, n0 + c, N, f16, lane);
+        }
+      }
+#pragma unroll 1
+      for (int chunk = SUMS ? last_chunk + 1 : first_chunk; chunk <= last_chunk; ++chunk) {
         const int c = chunk * 32, col = n0 + c;
         uint32_t acc[32], up[EPI == kFfnGlu ? 32 : 1];
         tmem_ld32(tbase + (uint32_t)c, acc);
         if (EPI == kFfnGlu) tmem_ld32(tbase + (uint32_t)(BN / 2 + c), reinterpret_cast<uint32_t(&)[32]>(up));
-        if (chunk == last_chunk) {                // accumulator read: hand the buffer back
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (PAIR && rank != 0) mbar_arrive_cluster(drained0 + (uint32_t)buf * 8u);
-            else mbar_arrive(tempty_bar + buf);
-          }
-        }
+        if (chunk == last_chunk) hand_back(buf);  // accumulator read
         if (nlive <= 0 || col >= N) continue;     // (uniform over the warp)
         const int npieces = min(4, (N - col) >> 3);               // pieces of eight 16-bit columns
         if (EPI == kFfnGlu) {
@@ -689,6 +825,7 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
         } else if (is_linear(EPI)) {
           const LinearEpilogue& e = g.lin;
           const int ncols = min(32, N - col);
+          const bool float_out = e.ty == SDS_F32;
           uint32_t w[16];
           if (e.bias) {
             reinterpret_cast<float*>(stg)[lane] = bias_next;
@@ -742,7 +879,7 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
                                min(4, ((int)e.ldf - col - 16 * hf) >> 2), lane);
               }
             });
-          if (e.residual && e.ty != SDS_F32) {
+          if (e.residual && !float_out) {
             if (EPI == kLinear) rows_to_lanes(stg, res_now[0], w, lane);
             else narrow16_to_lanes(stg, [&](int r) -> const uint16_t* {
               return r < nlive ? static_cast<const uint16_t*>(e.residual) + (size_t)(row0 + r) * e.ldr + col : nullptr;
@@ -760,7 +897,7 @@ __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_const
                 acc[16 * hf + i] = __float_as_uint(__uint_as_float(acc[16 * hf + i]) + __uint_as_float(w[i]));
             }
           }
-          if (e.ty != SDS_F32) {
+          if (!float_out) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack16(__uint_as_float(acc[2 * i]), __uint_as_float(acc[2 * i + 1]), f16);
             uint16_t* out = static_cast<uint16_t*>(p.out) + (size_t)row0 * p.ldo + col;
@@ -876,14 +1013,17 @@ struct FfnSplitArgs {
 
 constexpr int kSplitThreads = 256;
 
-template <int BN> struct FfnSplit {
+// kLinear with a float result: a CTA's steps of K are dealt to up to so many accumulators (see SUMS), added in order behind them
+__host__ __device__ constexpr int split_accumulators(int bn, int epi) { return !is_linear(epi) ? 1 : bn >= 128 ? 2 : 4; }
+template <int BN, int EPI> struct FfnSplit {
   static constexpr int kABytes = kBM * kBK * 2, kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
   static constexpr int kFixedBytes = 1024 + 256;
   // half of an SM's shared memory, so that two CTAs share an SM: clusters of eight are then all resident at once, and
   // the CTAs of the next product request their weights while the last ones of this product finish
   static constexpr int kStages = (113 * 1024 - kFixedBytes) / kStageBytes;
   static constexpr int kSmemBytes = kStages * kStageBytes + kFixedBytes;
-  static constexpr int kTmemCols = BN < 32 ? 32 : BN;
+  static constexpr int kAccumulators = split_accumulators(BN, EPI);
+  static constexpr int kTmemCols = BN * kAccumulators < 32 ? 32 : BN * kAccumulators;   // (of 256: two CTAs share an SM)
   static_assert(kStages * kStageBytes >= BN * kBM * 4, "the partial sums fit where the stages were");
 };
 
@@ -898,7 +1038,7 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
 // (5.8 TB/s, 88 % of a copy's rate). What is left of a small call is the ramp of the requests and the exchange, once per product.
 template <int BN, int EPI>
 __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_constant__ FfnSplitArgs g) {
-  using C = FfnSplit<BN>;
+  using C = FfnSplit<BN, EPI>;
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;   // output columns of a CTA
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -916,6 +1056,9 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   const int n0 = (int)(blockIdx.x / nsplit) * TN, tok0 = (int)blockIdx.y * BN;
   const int kb_seg = (g.K + kBK - 1) / kBK, nkb = kb_seg * g.nseg;
   const int kb0 = (int)((int64_t)nkb * rank / nsplit), kb1 = (int)((int64_t)nkb * (rank + 1) / nsplit);
+  // steps of an accumulator (of a float result: kSumSteps where there are accumulators enough)
+  const int per = C::kAccumulators == 1 || g.lin.ty != SDS_F32
+                      ? kb1 - kb0 : max(kSumSteps, (kb1 - kb0 + C::kAccumulators - 1) / C::kAccumulators);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar + s, 1); mbar_init(empty_bar + s, 1); }
@@ -987,9 +1130,11 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       tc_fence_after();
       const uint32_t sa = smem_u32(stages + stage * C::kStageBytes);
       const uint64_t adesc = make_sdesc(sa, a_chunk), bdesc = make_sdesc(sa + C::kABytes);
+      const int at = C::kAccumulators == 1 ? 0 : (kb - kb0) / per;
+      const bool begun = C::kAccumulators == 1 ? kb > kb0 : kb - kb0 > at * per;
 #pragma unroll
       for (int k = 0; k < kBK / 16; ++k)
-        umma_f16(tmem_base, adesc + a_step * k, bdesc + (uint64_t)(2 * k), idesc, (kb > kb0 || k) ? 1u : 0u);
+        umma_f16(tmem_base + (uint32_t)(at * BN), adesc + a_step * k, bdesc + (uint64_t)(2 * k), idesc, (begun || k) ? 1u : 0u);
       umma_commit(empty_bar + stage);
       if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
     }
@@ -1015,6 +1160,17 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
     for (int c = 0; c < BN / 2; c += 8)
       tmem_ld8(tmem_base + (uint32_t)(half * (BN / 2) + c) + ((uint32_t)(q * 32) << 16), acc + c);
     tmem_ld_wait();
+    if (C::kAccumulators > 1)
+      for (int b = 1; b * per < kb1 - kb0; ++b) {
+#pragma unroll
+        for (int c = 0; c < BN / 2; c += 8) {
+          uint32_t more[8];
+          tmem_ld8(tmem_base + (uint32_t)(b * BN + half * (BN / 2) + c) + ((uint32_t)(q * 32) << 16), more);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[c + i] = __float_as_uint(__uint_as_float(acc[c + i]) + __uint_as_float(more[i]));
+        }
+      }
 #pragma unroll
     for (int c = 0; c < BN / 2; ++c) part[(half * (BN / 2) + c) * kBM + q * 32 + lane] = __uint_as_float(acc[c]);
   } else if (lane == 0) {
@@ -1165,7 +1321,7 @@ struct KernelInfo {
   std::atomic<int> resident[kMaxDevices];         // 0: not looked up; else 1 + resident CTAs (clusters of a pair)
 };
 
-template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW>
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW, bool SUMS>
 cudaError_t tile_resident(int* n) {
   static KernelInfo info;                         // zero-initialised
   using C = FfnTile<BN, PAIR, EW>;
@@ -1173,7 +1329,7 @@ cudaError_t tile_resident(int* n) {
   if (dev < 0) return cudaErrorInvalidDevice;
   int r = info.resident[dev].load(std::memory_order_acquire);
   if (r == 0) {
-    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW, SUMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     int sms = 0, got = 0;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
@@ -1188,7 +1344,7 @@ cudaError_t tile_resident(int* n) {
       attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
-      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW>, &cfg)) != cudaSuccess) return e;
+      if ((e = cudaOccupancyMaxActiveClusters(&got, k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW, SUMS>, &cfg)) != cudaSuccess) return e;
       got = std::min(got, sms / 2);
     }
     if (got < 1) return cudaErrorLaunchOutOfResources;
@@ -1199,11 +1355,11 @@ cudaError_t tile_resident(int* n) {
   return cudaSuccess;
 }
 
-template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW>
+template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW, bool SUMS>
 cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) {
   using C = FfnTile<BN, PAIR, EW>;
   int resident = 0;
-  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN, CUT, EW>(&resident);
+  const cudaError_t e = tile_resident<BN, EPI, PAIR, MN, CUT, EW, SUMS>(&resident);
   if (e != cudaSuccess) return e;
   const int workers = (int)std::min<int64_t>(tiles, resident);
   cudaLaunchConfig_t cfg{};
@@ -1215,7 +1371,7 @@ cudaError_t launch_tile_t(const FfnTileArgs& g, int64_t tiles, cudaStream_t st) 
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   launch_attributes(attr, PAIR ? 2 : 1);
-  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW>, g);
+  return cudaLaunchKernelEx(&cfg, k_ffn_tile<BN, EPI, PAIR, MN, CUT, EW, SUMS>, g);
 }
 
 // where an operand lies: [rows, cols] with rows ld elements apart; K-major if K runs along the columns
@@ -1249,7 +1405,7 @@ inline int ksteps(const ProductSpec& s) { return (steps(s.K) * s.nseg + s.parts 
 // Tile shape: single CTAs on 128 x 128 tiles while these are at most one per SM (each has an SM of its own), pairs on
 // 256 x 256 tiles above that. Several products of one launch: those with the longer tiles come first; there are at most
 // two lengths (specs[0] may differ from the others).
-template <int EPI, bool MN, bool CUT = false, int EW = kEpiWarps>
+template <int EPI, bool MN, bool CUT = false, int EW = kEpiWarps, bool SUMS = false>
 cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first, cudaStream_t st,
                          float* keep = nullptr, void* out2 = nullptr, bool beside = false, const LinearEpilogue* lin = nullptr) {
   constexpr int kWide = EPI == kFfnGlu ? 128 : 256, kNarrow = EPI == kFfnGlu ? 64 : 128;   // output columns of a tile
@@ -1293,7 +1449,7 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
     }
   }
   if (pair) {
-    const cudaError_t e = launch_tile_t<256, EPI, true, MN, CUT, EW>(g, wide, st);
+    const cudaError_t e = launch_tile_t<256, EPI, true, MN, CUT, EW, SUMS>(g, wide, st);
     if (e != cudaErrorLaunchOutOfResources) return e;
     // no cluster can be resident: single CTAs, whose tile of the fused projections has its own box
     for (int i = 0; EPI == kFfnGlu && i < n; ++i)
@@ -1301,12 +1457,12 @@ cudaError_t launch_tiles(const FfnArgs& a, ProductSpec* specs, int n, bool first
         if (!map_operand(&g.p[i].b[k], specs[i].b[k], a.f16 != 0, specs[i].N, specs[i].K, MN, 64))
           return cudaErrorInvalidValue;
   }
-  return launch_tile_t<128, EPI, false, MN, CUT, EW>(g, small, st);
+  return launch_tile_t<128, EPI, false, MN, CUT, EW, SUMS>(g, small, st);
 }
 
 template <int BN, int EPI>
 cudaError_t launch_split_t(const FfnSplitArgs& g, int tiles, int splits, cudaStream_t st) {
-  using C = FfnSplit<BN>;
+  using C = FfnSplit<BN, EPI>;
   static KernelInfo info;
   const int dev = current_device();
   if (dev < 0) return cudaErrorInvalidDevice;

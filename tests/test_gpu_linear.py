@@ -263,6 +263,20 @@ def test_gradients_over_many_rows(rows, k, n, t):
     assert all(torch.equal(a, b) for a, b in zip(got, check(inputs(rows, k, n, t, 5, steps=10), "silu", t)))
 
 
+@pytest.mark.parametrize("rows,k,n", [(64, 8192, 2048), (100, 8192, 264), (700, 1024, 512), (700, 8192, 512), (3000, 8192, 520), (3000, 2000, 519)])
+def test_long_sums_of_float_results(rows, k, n):
+    """The tensor cores truncate as they add: at most 60 additions (960 products) are left to one accumulator where the result is a float. One
+    loses 2^-24 of the running sum on average, which is two thirds of the final one on average: 60 * 2^-24 * 2 / 3 of it, and float's own
+    roundings. (512 additions at k = 8192 would lose 2e-5.)"""
+    s = inputs(rows, k, n, BF16, 3, ty=F32, residual=True)
+    want = s["x"].double() @ s["w"].double().T
+    y = sds.linear(s["x"], s["w"], out_dtype=F32)
+    assert float((y.double() - want).norm() / want.norm()) <= 60 * 2 * U / 3 + 4 * U
+    y = sds.linear(s["x"], s["w"], residual=s["residual"], out_dtype=F32)
+    want = want + s["residual"].double()
+    assert float((y.double() - want).norm() / want.norm()) <= 60 * 2 * U / 3 + 4 * U
+
+
 def test_gradient_against_differences():
     r = gen(9)
     x, w, b, table = r(40, 24).to(F16), (0.3 * r(48, 24)).to(F16), 0.2 * r(48), (0.4 * r(5, 48)).to(F16)
