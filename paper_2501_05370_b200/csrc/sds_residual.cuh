@@ -52,6 +52,13 @@ template <class T> struct Raw {
     for (int i = 0; i < kUnits; ++i) q[i] = *(reinterpret_cast<const uint4*>(p) + i);
   }
 };
+// (eight floats are one 32-byte load: as two of 16 bytes a warp would ask for half a sector at a time)
+template <> __device__ __forceinline__ void Raw<float>::load(const float* p) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(q[0].x), "=r"(q[0].y), "=r"(q[0].z), "=r"(q[0].w), "=r"(q[1].x), "=r"(q[1].y), "=r"(q[1].z), "=r"(q[1].w)
+               : "l"(p)
+               : "memory");
+}
 // as four pairs of floats
 constexpr int P = kBlock / 2;
 __device__ __forceinline__ void words_to(const uint4* q, float2 (&o)[P], float) {
@@ -136,9 +143,9 @@ __device__ __forceinline__ void take_vector(const uint4& r, const void* p, int t
                                             float2 (&o)[P]) {
   if (VEC) {
     if (type == SDS_F32) {
-      const uint4* from = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + off + (col.live ? col.c0 : 0));
-      const uint4 q[2] = {from[0], from[1]};
-      words_to(q, o, 0.f);
+      Raw<float> f;
+      f.load(static_cast<const float*>(p) + off + (col.live ? col.c0 : 0));
+      words_to(f.q, o, 0.f);
     } else if (type == SDS_BF16) {
       words_to(&r, o, Bf16{});
     } else {
