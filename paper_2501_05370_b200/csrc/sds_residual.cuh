@@ -457,15 +457,18 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
     copies_end();
   };
   for (int s = 0; s < kRingStages - 1; ++s) request(at.row + s, s);
-  int stage = 0;
+  int stage = 0, held = -1;
+  uint4 gate, scale, shift;
   while (rows_left<S::T>(at.on())) {
     const bool on = at.on();
     const int row = on ? at.row : 0, group = on ? at.group : 0;
     float2 v[P], q[P], x[P];
-    uint4 gate, scale, shift;
-    if (a.h) request_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col);
-    request_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col);
-    request_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col);
+    if (group != held) {                                        // (kept while the group lasts)
+      held = group;
+      if (a.h) request_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col);
+      request_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col);
+      request_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col);
+    }
     ring_ready<TPR, CL, VEC>(sub);
     const uint4* mine = ring + stage * kStage;
     ring_take(mine, row_of<TR>(a.r, row, a.ldr), col, sub, v);
@@ -598,14 +601,16 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     copies_end();
   };
   for (int s = 0; s < kRingStages - 1; ++s) request(at.row + s, s);
-  int stage = 0;
-
+  int stage = 0, held = -1;
+  uint4 gate_raw, scale_raw;
   while (rows_left<S::T>(at.on())) {
     const bool on = at.on();
     const int row = on ? at.row : 0, group = on ? at.group : 0;
-    uint4 gate_raw, scale_raw;
-    if (a.h) request_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col);
-    request_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col);
+    if (group != held) {
+      held = group;
+      if (a.h) request_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col);
+      request_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col);
+    }
     ring_ready<TPR, CL, VEC>(sub);
     const uint4* mine = ring + stage * G::kStage;
     const float4* stats = reinterpret_cast<const float4*>(mine + G::kStats + threadIdx.x / kWarp * 2);
