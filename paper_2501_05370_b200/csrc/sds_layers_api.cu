@@ -366,6 +366,7 @@ int sds_linear_backward(const sds_linear_layer* layer, const void* dy_dev, int64
   if ((rc = check_rows(dy_dev, lddy, y_dtype, rows, layer->n)) != SDS_OK) return rc;
   if (dx_dev && (rc = check_ffn_rows(dx_dev, lddx, rows, layer->k)) != SDS_OK) return rc;
   if ((dbias_dev && !layer->bias_dev) || (dtable_dev && !layer->table_dev)) return SDS_EINVAL;
+  if (dtable_dev && rows * layer->steps > ((int64_t)1 << 36)) return SDS_EUNSUPPORTED;     // (every step looks at every row's)
   if (!aligned(dw_dev, 16)) return SDS_EUNSUPPORTED;
   if ((dbias_dev && !aligned(dbias_dev, type_bytes(layer->bias_dtype))) || !aligned(dtable_dev, 2)) return SDS_EINVAL;
   const sds_linear_sizes s = linear_sizes(layer, rows);

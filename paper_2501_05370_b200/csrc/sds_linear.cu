@@ -198,7 +198,7 @@ struct TableArgs {
   int* list_step;                                 // [rows] the steps, in the same order (`steps` outside the table)
   const void* dy; const float* factor;            // as in DzArgs
   uint16_t* dz;                                   // as in DzArgs
-  float* db_part;                                 // [gridDim.y][n] column sums, NULL = not wanted
+  float* db_part;                                 // [table_parts][n] column sums, NULL = not wanted
   float* part;                                    // [slices][2][n] sums of runs that cross a slice's begin, its end
   uint16_t* dtable;                               // [steps, n] of the operands' type
   int64_t lddy, ldz;
@@ -274,10 +274,11 @@ template <bool F32, bool WHOLE>
 __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) {
   __shared__ float sums[kTableWarps][256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t sl = (int64_t)blockIdx.y * kTableWarps + warp;
+  const int cols = (a.n + 255) / 256, strip = (int)(blockIdx.x % cols), part = (int)(blockIdx.x / cols);   // (parts may pass 65535)
+  const int64_t sl = (int64_t)part * kTableWarps + warp;
   const int total = a.rows, i0 = (int)min((int64_t)total, sl * a.slice), count = min(a.slice, total - i0);   // (0: behind the last row)
   start_behind_prior_kernel();
-  const int c0 = blockIdx.x * 256 + lane * 8;
+  const int c0 = strip * 256 + lane * 8;
   const bool live = c0 < a.n, whole_out = a.n % 8 == 0;
   const int my_row = lane < count ? a.list[i0 + lane] : 0, my_step = lane < count ? a.list_step[i0 + lane] : -1;
   const int step_before = i0 > 0 ? a.list_step[i0 - 1] : -1, step_after = i0 + count < total ? a.list_step[i0 + count] : -1;
@@ -339,11 +340,11 @@ __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) 
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < 256 / kTableThreads; ++u) {
-    const int x = threadIdx.x + u * kTableThreads, c = blockIdx.x * 256 + x;
+    const int x = threadIdx.x + u * kTableThreads, c = strip * 256 + x;
     float t = 0.f;
 #pragma unroll
     for (int w = 0; w < kTableWarps; ++w) t += sums[w][x];
-    if (c < a.n) a.db_part[(size_t)blockIdx.y * a.n + c] = t;
+    if (c < a.n) a.db_part[(size_t)part * a.n + c] = t;
   }
 }
 
@@ -523,7 +524,7 @@ cudaError_t launch_table(const TableArgs& t, bool whole_dy, cudaStream_t st) {
   cudaError_t e = start(k_table_list, dim3(t.steps + 1), kListThreads, 1, st, t);
   if (e != cudaSuccess) return e;
   const int cols = (t.n + 255) / 256;
-  const dim3 grid(cols, (unsigned)table_parts(t.rows, t.n));
+  const dim3 grid((unsigned)(cols * table_parts(t.rows, t.n)));
   const auto go = [&](auto kernel) { return start(kernel, grid, kTableThreads, 1, st, t); };
   if (t.tdy == SDS_F32) e = whole_dy ? go(k_table_sum<true, true>) : go(k_table_sum<true, false>);
   else e = whole_dy ? go(k_table_sum<false, true>) : go(k_table_sum<false, false>);

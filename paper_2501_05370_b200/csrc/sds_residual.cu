@@ -55,14 +55,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(const Residua
   if (a.dgate) store_any(a.dgate, a.tc, c, wp * C);
 }
 
-// Groups whose rows several workers had: a CTA takes 32 columns of one group, a warp every eighth part.
+// Groups whose rows several workers had: one for each border between two workers, where it is the first border in its group. A CTA takes
+// 32 columns of it, a warp every eighth part.
 __global__ void __launch_bounds__(256) k_residual_join_groups(const ResidualNormArgs a, int strips) {
   __shared__ float sums[3][8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = a.d;
-  const int group = (int)(blockIdx.x / strips), c = (int)(blockIdx.x % strips) * 32 + lane;
+  const int first = (int)(blockIdx.x / strips), c = (int)(blockIdx.x % strips) * 32 + lane;
+  const int64_t border = (int64_t)(first + 1) * a.share;
+  const int group = (int)(border / a.per);
   start_after_prior_kernel();
-  const int first = (int)((int64_t)group * a.per / a.share), last = (int)(((int64_t)(group + 1) * a.per - 1) / a.share);
-  if (first == last) return;                      // written by its worker
+  if (border % a.per == 0 || (int64_t)group * a.per / a.share != first) return;
+  const int last = (int)(((int64_t)(group + 1) * a.per - 1) / a.share);
   float s[3] = {0.f, 0.f, 0.f};
   if (c < d) {
 #pragma unroll 4
@@ -139,8 +142,8 @@ cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_
   ResidualNormArgs g = a;
   if ((e = launch_rows(g, vec, true, st)) != cudaSuccess) return e;
   const int strips = (a.d + 31) / 32;
-  if (a.mode == kSumGroups && g.share % g.per != 0 &&     // (else no group crosses workers)
-      (e = row_launch(k_residual_join_groups, dim3((unsigned)((int64_t)a.groups * strips)), 256, 0, 1, st, g, strips)) != cudaSuccess)
+  if (a.mode == kSumGroups && g.workers > 1 && g.share % g.per != 0 &&      // (else no group crosses workers)
+      (e = row_launch(k_residual_join_groups, dim3((unsigned)((g.workers - 1) * strips)), 256, 0, 1, st, g, strips)) != cudaSuccess)
     return e;
   const bool any = a.dw || a.db || a.dwp || (a.mode == kSumAll && (a.dgate || a.dscale || a.dshift));
   return any ? row_launch(k_residual_join, dim3((unsigned)strips), kJoinWarps * 32, 0, 1, st, g) : cudaSuccess;

@@ -302,6 +302,26 @@ def test_gradient_against_differences():
             assert abs(got - want) <= 4 * half(F16) * size * 4 + 1e-5 * abs(want)
 
 
+def test_many_rows_with_a_table():
+    """More slices of the list than a grid's second dimension has."""
+    rows, n, steps = 8_500_000, 8, 3
+    s = inputs(rows, 8, n, BF16, 5, steps=steps)
+    kw = dict(table=s["table"], step=s["step"])
+    kept = sds.linear(s["x"], s["w"], s["b"], None, keep=True, **kw)[1]
+    _, _, db, dt = sds.linear_backward(s["dy"], s["x"], s["w"], kept, bias=s["b"], want=(False, False, True, True), **kw)
+    dy = s["dy"].double()
+    want = torch.stack([dy[s["step"] == i].sum(0) for i in range(steps)])
+    size = torch.stack([dy[s["step"] == i].abs().sum(0) for i in range(steps)])
+    # slices of 32 rows, joined eight at a time in one chain of rows / 256, or (bias) parts of 128 in chains of rows / 1024
+    close(dt, want, (rows / 256 + 64) * U * size, "dtable")
+    close(db, dy.sum(0), (rows / 1024 + 64) * U * dy.abs().sum(0), "db")
+    big = torch.empty(1 << 21, 8, device="cuda", dtype=BF16)
+    with pytest.raises(sds.SdsError) as e:
+        sds.linear_backward(big, big, s["w"], sds.linear(big[:1], s["w"], keep=True)[1], table=torch.empty(40000, 8, device="cuda", dtype=BF16),
+                            step=torch.zeros(1 << 21, device="cuda", dtype=torch.int32))
+    assert e.value.code == sb.SDS_EUNSUPPORTED
+
+
 def test_empty_and_shapes():
     w, b, table = torch.randn(16, 8, device="cuda").bfloat16(), torch.randn(16, device="cuda"), torch.randn(3, 16, device="cuda").bfloat16()
     x = torch.empty(2, 0, 8, device="cuda", dtype=BF16)

@@ -344,7 +344,8 @@ def test_every_part_alone_and_together(rows, d, groups, part):
 
 @pytest.mark.parametrize("rows,d,groups", [(5000, 64, 1), (5000, 64, 5000), (5000, 64, 5), (5000, 64, 1250), (3000, 72, 2), (2400, 1001, 3), (2400, 1001, 800),
                                            (1200, 2048, 1), (1200, 2048, 4), (1200, 2048, 600), (640, 4096, 2), (400, 8192, 1), (300, 16384, 3), (300, 8200, 300),
-                                           (4097, 40, 17), (10000, 8, 1)])
+                                           (4097, 40, 17), (10000, 8, 1), (60000, 16, 20000), (60000, 16, 15),
+                                           (6000, 300, 2000)])
 def test_sums_over_many_rows(rows, d, groups):
     """Workers with several rows, pieces of groups, whole groups per worker, rows that are groups; the same bits again."""
     s = make(rows, d, F32, BF16, rows + d, groups=groups, weight=F32, bias=F32, mod=BF16, gate=BF16, post=True, post_weight=F32, p=0.1)
