@@ -1151,6 +1151,26 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   wait_for_prior_kernel();                        // (nothing else in device memory is read or written before)
   launch_dependents();
   if (g.clear_err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
+  // kLinear: what is added to this lane's four columns, and its row of the table for the warp's first token, requested before the sums
+  // are waited for
+  const int lin_col = n0 + 4 * lane, lin_first = tok0 + (int)rank * (BN / (int)nsplit) + warp;
+  float lin_bias[4] = {0.f, 0.f, 0.f, 0.f};
+  uint2 lin_table = make_uint2(0u, 0u);
+  int lin_row = -1;
+  const auto find_row = [&](int tok) {
+    if (!g.lin.table || tok >= g.rows) return;
+    const int at = g.lin.step[tok];
+    lin_row = at >= 0 && at < g.lin.steps ? at : -1;
+    if (EPI == kLinear && lin_row >= 0 && lin_col < g.N)
+      lin_table = *reinterpret_cast<const uint2*>(g.lin.table + (size_t)lin_row * g.N + lin_col);
+  };
+  if (is_linear(EPI)) {
+    if (g.lin.bias)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (lin_col + u < g.N) lin_bias[u] = load_typed(g.lin.bias, g.lin.tbias, (size_t)(lin_col + u));
+    find_row(lin_first);
+  }
   // the accumulator to shared memory, [token][row of the instruction]
   const bool ok = wait_for_sums(tfull_bar, 0u, abort_s, kb1 - kb0);
   if (ok) {
@@ -1219,29 +1239,23 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       }
     } else if (is_linear(EPI)) {
       const LinearEpilogue& e = g.lin;
-      const int col = n0 + 4 * lane, live = min(4, g.N - col);
+      const int col = lin_col, live = min(4, g.N - col);
+      if (tok != lin_first) find_row(tok);
       if (live > 0) {
-        float z[4] = {s.x, s.y, s.z, s.w}, da[4];
-        if (e.bias)
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (u < live) z[u] += load_typed(e.bias, e.tbias, (size_t)(col + u));
+        float z[4] = {s.x + lin_bias[0], s.y + lin_bias[1], s.z + lin_bias[2], s.w + lin_bias[3]}, da[4];
         if (e.table) {
-          const int at = e.step[tok];
-          const bool in = at >= 0 && at < e.steps;
-          const uint16_t* from = e.table + (int64_t)(in ? at : 0) * g.N + col;
           float t[4] = {0.f, 0.f, 0.f, 0.f};
           if (EPI == kLinear) {
-            const uint2 w = *reinterpret_cast<const uint2*>(from);
-            const float2 lo = unpack16x2(w.x, g.f16), hi = unpack16x2(w.y, g.f16);
+            const float2 lo = unpack16x2(lin_table.x, g.f16), hi = unpack16x2(lin_table.y, g.f16);
             t[0] = lo.x; t[1] = lo.y; t[2] = hi.x; t[3] = hi.y;
-          } else {
+          } else if (lin_row >= 0) {
+            const uint16_t* from = e.table + (size_t)lin_row * g.N + col;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
               if (u < live) t[u] = unpack16(from[u], g.f16);
           }
 #pragma unroll
-          for (int u = 0; u < 4; ++u) z[u] += in ? t[u] : __int_as_float(0x7fffffff);
+          for (int u = 0; u < 4; ++u) z[u] += lin_row >= 0 ? t[u] : __int_as_float(0x7fffffff);
         }
         with_activation_or_none(g.act, [&](auto act) {
           constexpr int ACT = decltype(act)::value;
