@@ -1161,25 +1161,61 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   wait_for_prior_kernel();                        // (nothing else in device memory is read or written before)
   launch_dependents();
   if (g.clear_err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
-  // kLinear: what is added to this lane's four columns, and its row of the table for the warp's first token, requested before the sums
-  // are waited for
-  const int lin_col = n0 + 4 * lane, lin_first = tok0 + (int)rank * (BN / (int)nsplit) + warp;
+  // kLinear: what is added to this lane's four columns of a token, requested before the sums are waited for, then a token ahead; a
+  // lane holds the table's row of its own one of the warp's tokens
+  const int share = BN / (int)nsplit, first = tok0 + (int)rank * share + warp, lin_col = n0 + 4 * lane, live = min(4, g.N - lin_col);
   float lin_bias[4] = {0.f, 0.f, 0.f, 0.f};
-  uint2 lin_table = make_uint2(0u, 0u);
-  int lin_row = -1;
-  const auto find_row = [&](int tok) {
-    if (!g.lin.table || tok >= g.rows) return;
-    const int at = g.lin.step[tok];
-    lin_row = at >= 0 && at < g.lin.steps ? at : -1;
-    if (EPI == kLinear && lin_row >= 0 && lin_col < g.N)
-      lin_table = *reinterpret_cast<const uint2*>(g.lin.table + (size_t)lin_row * g.N + lin_col);
+  uint32_t lin_table[4] = {0u, 0u, 0u, 0u}, lin_residual[4] = {0u, 0u, 0u, 0u};
+  int lin_rows = -1, lin_row = -1;
+  const auto request_four = [&](uint32_t (&w)[4], const void* p, bool floats, size_t i) {
+    if (EPI == kLinear) {
+      if (floats) {
+        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+        w[0] = v.x; w[1] = v.y;
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (u < live) w[u] = floats ? static_cast<const uint32_t*>(p)[i + u] : static_cast<const uint16_t*>(p)[i + u];
+    }
+  };
+  const auto four = [&](const uint32_t (&w)[4], bool floats, float (&v)[4]) {
+    if (floats) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = __uint_as_float(w[u]);
+    } else if (EPI == kLinear) {
+      const float2 lo = unpack16x2(w[0], g.f16), hi = unpack16x2(w[1], g.f16);
+      v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = unpack16(w[u], g.f16);
+    }
+  };
+  const auto request_added = [&](int k) {         // for the warp's k-th token
+    if (g.lin.table) {
+      lin_row = __shfl_sync(0xffffffffu, lin_rows, k);
+      if (lin_row >= 0 && live > 0) request_four(lin_table, g.lin.table, false, (size_t)lin_row * g.N + lin_col);
+    }
+    const int tok = first + k * (kSplitThreads / 32);
+    if (g.lin.residual && tok < g.rows && live > 0)
+      request_four(lin_residual, g.lin.residual, g.lin.ty == SDS_F32, (size_t)tok * g.lin.ldr + lin_col);
   };
   if (is_linear(EPI)) {
     if (g.lin.bias)
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (lin_col + u < g.N) lin_bias[u] = load_typed(g.lin.bias, g.lin.tbias, (size_t)(lin_col + u));
-    find_row(lin_first);
+        if (u < live) lin_bias[u] = load_typed(g.lin.bias, g.lin.tbias, (size_t)(lin_col + u));
+    if (g.lin.table) {
+      const int i = lane * (kSplitThreads / 32), tok = first + i;
+      if (warp + i < share && tok < g.rows) {
+        const int at = g.lin.step[tok];
+        lin_rows = at >= 0 && at < g.lin.steps ? at : -1;
+      }
+    }
+    request_added(0);
   }
   // the accumulator to shared memory, [token][row of the instruction]
   const bool ok = wait_for_sums(tfull_bar, 0u, abort_s, kb1 - kb0);
@@ -1212,22 +1248,28 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   if (nsplit > 1) cluster_sync_all(); else __syncthreads();
 
   // this CTA's share of the tokens: partial sums added in the order of K, then the epilogue; a lane holds four columns
-  const int share = BN / (int)nsplit;
   const uint32_t part_a = smem_u32(part);
   const int ncc = (g.N + 31) >> 5;
+  float4 sums[8];                                 // of a token, one for each CTA; requested a token ahead
+  const auto request_sums = [&](int i) {
+    const uint32_t off = (uint32_t)(((int)rank * share + i) * kBM + lane * 4) * 4u;
+#pragma unroll
+    for (uint32_t r = 0; r < 8; ++r)
+      if (r < nsplit) sums[r] = ld_cluster4(map_to_cta(part_a + off, r));
+  };
+  if (warp < share) request_sums(warp);
   for (int i = warp; i < share; i += kSplitThreads / 32) {
-    const int tk = (int)rank * share + i, tok = tok0 + tk;
+    const int tok = first + i - warp;
     if (tok >= g.rows) break;
-    const uint32_t off = (uint32_t)(tk * kBM + lane * 4) * 4u;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (nsplit == 1) {
-      s = *reinterpret_cast<const float4*>(part + tk * kBM + lane * 4);
-    } else {
-      for (uint32_t r = 0; r < nsplit; ++r) {
-        const float4 v = ld_cluster4(map_to_cta(part_a + off, r));
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-      }
+    float4 s = sums[0];
+    if (nsplit > 1) {
+      s.x += 0.f; s.y += 0.f; s.z += 0.f; s.w += 0.f;
+#pragma unroll
+      for (uint32_t r = 1; r < 8; ++r)
+        if (r < nsplit) { s.x += sums[r].x; s.y += sums[r].y; s.z += sums[r].z; s.w += sums[r].w; }
     }
+    const bool more = i + kSplitThreads / 32 < share;
+    if (more) request_sums(i + kSplitThreads / 32);
     if (EPI == kFfnGlu) {
       float4 u;
       u.x = __shfl_down_sync(0xffffffffu, s.x, 16); u.y = __shfl_down_sync(0xffffffffu, s.y, 16);
@@ -1249,23 +1291,17 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
       }
     } else if (is_linear(EPI)) {
       const LinearEpilogue& e = g.lin;
-      const int col = lin_col, live = min(4, g.N - col);
-      if (tok != lin_first) find_row(tok);
+      const int col = lin_col;
+      float t[4], added[4];
+      four(lin_table, false, t);
+      four(lin_residual, e.ty == SDS_F32, added);
+      const bool known = lin_row >= 0;
+      if (more) request_added((i - warp) / (kSplitThreads / 32) + 1);
       if (live > 0) {
         float z[4] = {s.x + lin_bias[0], s.y + lin_bias[1], s.z + lin_bias[2], s.w + lin_bias[3]}, da[4];
         if (e.table) {
-          float t[4] = {0.f, 0.f, 0.f, 0.f};
-          if (EPI == kLinear) {
-            const float2 lo = unpack16x2(lin_table.x, g.f16), hi = unpack16x2(lin_table.y, g.f16);
-            t[0] = lo.x; t[1] = lo.y; t[2] = hi.x; t[3] = hi.y;
-          } else if (lin_row >= 0) {
-            const uint16_t* from = e.table + (size_t)lin_row * g.N + col;
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-              if (u < live) t[u] = unpack16(from[u], g.f16);
-          }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) z[u] += lin_row >= 0 ? t[u] : __int_as_float(0x7fffffff);
+          for (int u = 0; u < 4; ++u) z[u] += known ? t[u] : __int_as_float(0x7fffffff);
         }
         with_activation_or_none(g.act, [&](auto act) {
           constexpr int ACT = decltype(act)::value;
@@ -1277,8 +1313,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
         const size_t to = (size_t)tok * g.ldo + col;
         if (e.residual)
 #pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (u < live) z[u] += load_typed(e.residual, e.ty, (size_t)tok * e.ldr + col + u);
+          for (int u = 0; u < 4; ++u) z[u] += added[u];
         if (EPI == kLinear && e.ty == SDS_F32) {
           *reinterpret_cast<float4*>(static_cast<float*>(g.out) + to) = make_float4(z[0], z[1], z[2], z[3]);
         } else if (EPI == kLinear) {
@@ -1550,7 +1585,7 @@ bool prefer_split(int rows, int N, int nkb) {
 
 template <int EPI>
 cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st,
-                         const LinearEpilogue* lin = nullptr) {
+                         const LinearEpilogue* lin = nullptr, int count = 0) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
   const int bn = split_tokens(a.rows);
   FfnSplitArgs g;
@@ -1568,7 +1603,7 @@ cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool
   for (int k = 0; k < s.nseg; ++k)
     if (!map_operand(&g.t[k], s.t[k], a.f16 != 0, a.rows, s.K, false, bn)) return cudaErrorInvalidValue;
   const int tiles = (s.N + TN - 1) / TN;
-  const int splits = split_count(a.rows, tiles, ksteps(s));
+  const int splits = count > 0 ? count : split_count(a.rows, tiles, ksteps(s));
   switch (bn) {
     case 16: return launch_split_t<16, EPI>(g, tiles, splits, st);
     case 32: return launch_split_t<32, EPI>(g, tiles, splits, st);
