@@ -483,12 +483,11 @@ cudaError_t forward(const LinearArgs& a, const FfnArgs& f, const LinearEpilogue&
   ProductSpec s{};
   s.a[0] = {a.x, a.ldx}; s.b[0] = {a.w, a.k};
   s.nseg = 1; s.M = a.rows; s.N = a.n; s.K = a.k; s.out = a.y; s.ldo = a.ldy;
-  // The epilogue has more to do than the feed-forward block's, and a tile of few steps ends sooner: eight warps up to 64 steps of K,
-  // four beyond. Four and eight: 8192 x 2048 x 2048 with SiLU, bias and table 75.8 and 68.5 us, with GELU 87.6 and 72.2, 1037 x 1000 x 2731
-  // with GELU 30.9 and 25.6; 16384 x 8192 x 2048 392 and 405, with a float residual 474 and 486.
+  // The epilogue has more to do than the feed-forward block's: eight warps. Four and eight: 8192 x 2048 x 2048 with SiLU, bias and table
+  // 59.1 and 56.7 us, with GELU 70.5 and 57.7, 1037 x 1000 x 2731 with GELU 30.2 and 23.9; 16384 x 8192 x 2048 354.9 and 357.7, with
+  // bias and GELU 378.8 and 373.5.
   if (a.ty == SDS_F32 && steps(a.k) > kSumSteps) return launch_tiles<EPI, false, false, 16, true>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
-  if (steps(a.k) <= 64) return launch_tiles<EPI, false, false, 8>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
-  return launch_tiles<EPI, false>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
+  return launch_tiles<EPI, false, false, 8>(f, &s, 1, true, st, nullptr, nullptr, false, &e);
 }
 
 }  // namespace
