@@ -8,18 +8,21 @@ namespace {
 // groups of threads that run at once in a backward launch: 512 threads per SM
 int most_workers(int d) { return kRowSms * 512 / residual_threads(d); }
 
-constexpr int kJoinWarps = 32;
-
-// 32 columns of a CTA; a warp adds every 32nd worker's sums. One group (kSumAll): the plain sums give every gradient; else
-// they are weighted already, and the groups' own gradients were written before.
-__global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(const ResidualNormArgs a) {
-  __shared__ float sums[3][kJoinWarps][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, d = a.d;
+// COLS columns of a CTA, a thread one of them of every PARTS-th worker. Bound by latency: as many parts as leave every SM one CTA of
+// 1024 threads, and short CTAs for wide rows. Backward of 1021 x 1001 float (511 workers): <8, 128> 16.0 us, <16, 64> 16.5, <16, 16> 22.3;
+// 20000 x 64 23.0, 33.2, 116; 64 x 2048 8.4, 7.1, 7.1; 16384 x 2048 126.7, 124.3, 128.5; 300 x 5000 30.0, 27.2, 24.7; 1 x 10056 18.8, 12.9, 8.7.
+// One group (kSumAll): the plain sums give every gradient; else they are weighted already, and the groups' own gradients were written
+// before.
+template <int COLS, int PARTS>
+__global__ void __launch_bounds__(COLS * PARTS) k_residual_join(const ResidualNormArgs a) {
+  __shared__ float sums[3][PARTS * COLS], total[3][COLS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = threadIdx.x % COLS, d = a.d;
+  const int c = blockIdx.x * COLS + col;
   start_after_prior_kernel();
   float s[3] = {0.f, 0.f, 0.f};
   if (c < d) {
 #pragma unroll 4
-    for (int i = warp; i < a.workers; i += kJoinWarps) {
+    for (int64_t i = threadIdx.x / COLS; i < a.workers; i += PARTS) {
       const float* from = a.part + (size_t)i * 3 * d + c;
       s[0] += from[0];
       s[1] += from[d];
@@ -27,18 +30,19 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(const Residua
     }
   }
 #pragma unroll
-  for (int k = 0; k < 3; ++k) sums[k][warp][lane] = s[k];
+  for (int k = 0; k < 3; ++k) sums[k][threadIdx.x] = s[k];
   __syncthreads();
   if (warp < 3) {
     float v = 0.f;
 #pragma unroll 8
-    for (int i = 0; i < kJoinWarps; ++i) v += sums[warp][i][lane];
-    __syncwarp();
-    sums[warp][0][lane] = v;
+    for (int i = 0; i < PARTS * COLS / 32; ++i) v += sums[warp][i * 32 + lane];
+#pragma unroll
+    for (int at = COLS; at < 32; at *= 2) v += __shfl_xor_sync(0xffffffffu, v, at);
+    if (lane < COLS) total[warp][lane] = v;
   }
   __syncthreads();
-  if (warp != 0 || c >= d) return;
-  const float A = sums[0][0][lane], B = sums[1][0][lane], C = sums[2][0][lane];
+  if (threadIdx.x >= COLS || c >= d) return;
+  const float A = total[0][col], B = total[1][col], C = total[2][col];
   if (a.mode != kSumAll) {
     if (a.dw) store_any(a.dw, a.tw, c, A);
     if (a.db) store_any(a.db, a.tw, c, B);
@@ -146,7 +150,12 @@ cudaError_t launch_residual_norm_backward(const ResidualNormArgs& a, cudaStream_
       (e = row_launch(k_residual_join_groups, dim3((unsigned)((g.workers - 1) * strips)), 256, 0, 1, st, g, strips)) != cudaSuccess)
     return e;
   const bool any = a.dw || a.db || a.dwp || (a.mode == kSumAll && (a.dgate || a.dscale || a.dshift));
-  return any ? row_launch(k_residual_join, dim3((unsigned)strips), kJoinWarps * 32, 0, 1, st, g) : cudaSuccess;
+  if (!any) return cudaSuccess;
+  const auto join = [&](auto kernel, int cols, int parts) {
+    return row_launch(kernel, dim3((unsigned)((a.d + cols - 1) / cols)), cols * parts, 0, 1, st, g);
+  };
+  if (a.d <= 8 * kRowSms) return join(k_residual_join<8, 128>, 8, 128);
+  return a.d <= 16 * kRowSms ? join(k_residual_join<16, 64>, 16, 64) : join(k_residual_join<16, 16>, 16, 16);
 }
 
 }  // namespace sds
