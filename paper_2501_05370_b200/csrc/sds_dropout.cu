@@ -12,7 +12,8 @@ namespace {
 
 constexpr int kDropThreads = 256;
 
-// A thread takes blocks of eight columns of the whole array, in steps of the grid, two requested at a time.
+// A thread takes blocks of eight columns of the whole array, in steps of the grid, two requested at a time. Bound by memory: 16384 x 2048
+// bf16 onto a float residual 50 us (336 MB, 6.7 TB/s), its gradient from float to bf16 36 (201 MB, 5.6 TB/s).
 template <class TX, class TY>
 __global__ void __launch_bounds__(kDropThreads, 3) k_dropout(const DropoutCall a, int64_t nb) {
   start_after_prior_kernel();
@@ -60,6 +61,7 @@ __global__ void __launch_bounds__(kDropThreads, 3) k_dropout(const DropoutCall a
 }
 
 // Rows that are not whole pieces: a warp takes 256 columns of a row, a lane every 32nd of them, so that accesses are neighbours.
+// 33500 x 1001 bf16 49 us (134 MB, 2.7 TB/s): 16-bit loads and stores, and issue.
 template <class TX, class TY>
 __global__ void __launch_bounds__(kDropThreads) k_dropout_narrow(const DropoutCall a, int64_t groups) {
   start_after_prior_kernel();

@@ -107,7 +107,8 @@ __device__ __forceinline__ void dz_store(const A& a, int64_t row, int c0, const 
       make_uint4(pack16(v[0], v[1], a.f16), pack16(v[2], v[3], a.f16), pack16(v[4], v[5], a.f16), pack16(v[6], v[7], a.f16));
 }
 
-// A lane takes eight neighbouring columns of every eighth row of its chunk, four rows requested ahead. Bound by memory.
+// A lane takes eight neighbouring columns of every eighth row of its chunk, four rows requested ahead. Bound by memory: db alone of
+// 8192 x 2048 bf16 behind SiLU 16.5 us (101 MB of dy and act', 6.1 TB/s); 256 x 4096 6.4 us, a launch and the exchange of its sums.
 template <bool F32, bool WHOLE>
 __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
   __shared__ float sums[kDzWarps][kDzCols];
@@ -162,7 +163,8 @@ __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
   else a.part[(size_t)blockIdx.y * a.n + c] = s;
 }
 
-// The chunks' column sums, added in order: 32 columns of a CTA, a warp every eighth chunk.
+// The chunks' column sums, added in order: 32 columns of a CTA, a warp every eighth chunk. Latency: 128 chunks of 2048 columns 5.7 us
+// alone, about 1.5 beside the end of the kernel in front.
 __global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks, int n, void* db, int tdb) {
   __shared__ float sums[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
@@ -209,7 +211,8 @@ struct TableArgs {
 constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
 
 // One CTA per step, and one for rows outside the table: how many rows have smaller steps, then its own rows in ascending order, a warp for
-// every sixteenth of the rows. Every CTA reads all of `step`, twice, from L2 and L1: 250 steps over 8192 rows are 8 MB.
+// every sixteenth of the rows. Every CTA reads all of `step`, twice, from L2 and L1: 250 steps over 8192 rows are 8 MB (8.6 us alone: a
+// few waits for memory one behind the other).
 __global__ void __launch_bounds__(kListThreads) k_table_list(const TableArgs a) {
   __shared__ int less[kListWarps], same[kListWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.x;
@@ -269,7 +272,8 @@ constexpr int kTableThreads = 128, kTableWarps = kTableThreads / 32;
 
 // The same pass as k_linear_dz with the rows in the order of the list (dy and its factors are read once for all three results). A warp
 // adds the rows of a slice over 256 columns, four rows requested ahead. A run of one step that begins and ends in the slice
-// is a finished row of the gradient; the others are parts for k_table_join.
+// is a finished row of the gradient; the others are parts for k_table_join. 8192 x 2048 bf16, 250 steps: 30 us alone (101 MB read, 34
+// written, 4.5 TB/s: rows in the list's order are short requests), against 16.5 and a pass of its own over dz.
 template <bool F32, bool WHOLE>
 __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) {
   __shared__ float sums[kTableWarps][256];

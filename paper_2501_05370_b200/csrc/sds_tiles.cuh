@@ -41,7 +41,8 @@ constexpr int kChunkBytes = 64 * kBK * 2;         // 64 x 64 elements
 // Epilogue warps: one per quarter of the lanes. The main loop takes up shared memory (operand tiles written and read:
 // 128 bytes per cycle), and every warp that stages and polls beside it costs; four finish a tile well within the next
 // one's products. Measured at 16384 rows, d = 2048, f = 8192 in a long run: forward projections 806 us with 4 warps, 896
-// with 8; dH 550 and 566; second product 430 and 447.
+// with 8; dH 550 and 566; second product 430 and 447. Since the feeding lanes are elected (elect_one), 16384 rows forward 1197 and 1209 us,
+// 8192 rows forward and backward 2152 and 2172; short sums gain by 8 (16384 x 512 x 2048 forward 101 and 96).
 constexpr int kEpiWarps = 4;
 constexpr int tile_threads(int epilogue_warps) { return 64 + 32 * epilogue_warps; }   // warp 0: TMA, warp 1: MMA and tensor memory
 constexpr int kWarpStage = 2048;                  // staging bytes of an epilogue warp: 32 rows of 64 bytes
@@ -484,14 +485,16 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
 // MN: B is MN-major and A either (the gradients); else both are K-major. The loops of the two single threads that feed the
 // tensor cores are written out per order: with the order looked up in every step they took 735 cycles per step of K where
 // the products take 512 (16384 x 2048 x 8192, forward projections: 676 -> 611 us at full clocks).
-// Bound by the tensor cores: 16384 x 2048 x 8192 forward 1280 us, 1290 TFLOP/s (92 % of the library's rate in a long run, where power
-// sets the clock); 8192 rows forward and backward 2130 us, 1160 TFLOP/s beside the kept factors.
+// Bound by the tensor cores: 16384 x 2048 x 8192 forward 1147 to 1254 us, 1310 to 1440 TFLOP/s (power sets the clock of a long run); 8192 rows
+// forward and backward 2110 to 2190 us beside the kept factors. kLinear, pairs: 16384 x 2048 x 2048 95 us, 1447 TFLOP/s, with bias, table and
+// SiLU 105, GELU 110, with a float residual 124.
 // CUT: products whose K is cut (FfnProduct::parts); its own kernel, as the others lose up to 5 % to the arithmetic.
 // EW: epilogue warps, four, eight (two for each quarter of the lanes, half of the columns each) or sixteen.
 // SUMS: the tensor cores add to their accumulator without rounding to nearest, so a long sum comes out short by about K / 16 times 2^-25 of
 // itself (K = 8192: 6.4e-6, where a float's own rounding is 3e-8). Where the result is a float, every kSumSteps steps of K
 // have an accumulator of their own, and the epilogue's warps add these in registers (sixteen warps hold a tile's), while the next is filled:
-// a result is then short by at most a millionth. 16384 x 8192 x 2048 with a float residual, at length: 12 steps 593 us, 15 572, 24 546, 64 522.
+// a result is then short by at most a millionth. 16384 x 8192 x 2048 with a float residual, at length: 12 steps 593 us, 15 572, 24 546, 64 522
+// (before the feeding lanes were elected; now 15 steps 431 in short runs, 502 at length, against 424 in one accumulator).
 constexpr int kSumSteps = 15;
 template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW, bool SUMS>
 __global__ void __launch_bounds__(64 + 32 * EW, 1) k_ffn_tile(const __grid_constant__ FfnTileArgs g) {
@@ -1045,8 +1048,8 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   return v;
 }
 
-// 2048 x 8192 bf16, both products: 1 row 24.9 us (4.0 TB/s of weights), 64 rows 31, 128 rows 34; 8 rows of 4096 x 14336 60.8 us
-// (5.8 TB/s, 88 % of a copy's rate). What is left of a small call is the ramp of the requests and the exchange, once per product.
+// 2048 x 8192 bf16, both products: 1 row 24.1 us (4.2 TB/s of weights), 64 rows 30; 8 rows of 4096 x 14336 60.6 us
+// (5.8 TB/s, 89 % of a copy's rate). kLinear: 1 row of 2048 x 2048 5.0 us in a graph, of 8192 x 2048 7.9. What is left of a small call is the ramp of the requests and the exchange, once per product.
 template <int BN, int EPI>
 __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_constant__ FfnSplitArgs g) {
   using C = FfnSplit<BN, EPI>;
@@ -1564,9 +1567,9 @@ inline int split_count(int rows, int tiles, int nkb) {
   return s;
 }
 
-// Which form a product of `rows` tokens with N output columns takes: the shorter estimated time, in steps of K of one
-// CTA (about 0.35 us where few CTAs run, 0.3 us for those of a full launch of pairs) plus what a launch and its
-// epilogue cost. Beyond 2048 rows the few-row form has to be clearly ahead, as it is for few columns and a long K
+// Which form a product of the feed-forward block takes (linear layers: linear_form), for `rows` tokens and N output columns: the shorter
+// estimated time, in steps of K of one CTA (0.35 us where few CTAs run, 0.3 us for those of a full launch of pairs: the times before the
+// feeding lanes were elected, kept so that a block's sums keep their order) plus what a launch and its epilogue cost. Beyond 2048 rows the few-row form has to be clearly ahead, as it is for few columns and a long K
 // (3000 x 64 x 8192 forward 80 -> 53 us, 2100 x 512 x 12288 112 -> 85); close calls there went the other way
 // (4096 x 128 x 512 forward 13.8 -> 17.4).
 template <int EPI>
