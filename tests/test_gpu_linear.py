@@ -3,7 +3,7 @@
 Tolerances, derived from the arithmetic. A rounding to type t is off by at most eps_t / 2 relative (half). On the tensor
 cores a product of 16 terms is added to the accumulator at a time, with at most one truncation (2 u, u = 2^-24) per
 step: (k / 16 + 16) 2 u times the sum of the terms' sizes. Activations are within 2^-19 of themselves and follow the error of their
-argument (|act'| < 1.2, |act''| < 2). The kept derivative is rounded to f16, and dz to the operands' type before the products.
+argument (|act'| < 1.2, |act''| < 2). The kept derivative is a float; dz is rounded to the operands' type before the products.
 Sums over rows in float: at most rows / 8 terms one after the other, then a tree.
 """
 import math
@@ -84,7 +84,7 @@ class Linear64:
         # the derivative as it is kept
         self.eda = 2 * ez + ap * (self.da.abs() + 1) if act else torch.zeros_like(z)
         if act:
-            self.eda = self.eda + half(F16) * (self.da.abs() + self.eda) + tiny(F16)
+            self.eda = self.eda + U * (self.da.abs() + self.eda)
         self.steps = 0 if table is None else table.shape[0]
 
     def backward(self, dy):
@@ -157,6 +157,13 @@ def test_sizes(rows, k, n, t):
     ty = t if which % 3 else F32
     bias = (F32, t, None)[(which + rows) % 3]
     check(inputs(rows, k, n, t, which, steps=7 if rows % 2 else 0, ty=ty, bias=bias, residual=which % 2 == 0), act, ty)
+
+
+@pytest.mark.parametrize("rows,k,n", [(70, 512, 130), (128, 2048, 2048), (256, 2048, 2048), (250, 8192, 640), (500, 4096, 1024), (384, 8192, 2056), (1000, 1024, 1024)])
+def test_forms_of_middle_sizes(rows, k, n):
+    """Between few rows and many: tiles, and the few-row form with one to eight CTAs along K."""
+    check(inputs(rows, k, n, BF16, rows + k, steps=7, residual=True), "silu", BF16)
+    check(inputs(rows, k, n, BF16, rows + n, ty=F32, residual=True), None, F32)
 
 
 @pytest.mark.parametrize("act", [None, "silu", "gelu", "gelu_tanh"])
