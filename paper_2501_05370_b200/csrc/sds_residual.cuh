@@ -557,9 +557,10 @@ __device__ __forceinline__ void add_total(float* total, const float2 (&v)[P], co
   store_typed_vector(total, col, true, o);
 }
 
-// 512 threads of 128 registers an SM: a row's values, the sums over rows and the vectors of its columns are all in registers or shared
-// memory. 16384 x 2048, float stream and bf16 branch: conditioned 114 us (604 MB, 5.3 TB/s), with post, gate and dropout 145 (4.2 TB/s;
-// DRAM busy 47 % of the time: three rounds of sums a row, each a wait of the group).
+// 512 threads of 128 registers an SM: a row's values, the sums over rows and the products of a group's vectors are in registers, and issue is
+// what bounds the parts beside the plain norm: with gate, post weight and weight read and multiplied row by row, 16384 x 2048 with all parts
+// took 145 us (764 instructions of a warp for a row, 64 % of the issue slots), now 125 (604 MB, 4.8 TB/s; a bf16 stream 144 -> 117);
+// conditioned, float stream and bf16 branch, 114 (5.3 TB/s).
 template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, TH, TPR, CL, VEC>::kMinCtas) k_residual_norm_bwd(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;
@@ -606,16 +607,48 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
   };
   for (int s = 0; s < kRingStages - 1; ++s) request(at.row + s, s);
   int stage = 0, held = -1;
-  uint4 gate_raw, scale_raw;
+  // while their group lasts: alpha gate wp, and (1 + scale) w where the sums over rows do not need 1 + scale by itself
+  float2 branch[P], norm[P];
+  const bool weighted = a.mode == kSumWeighted, own_rows = weighted && a.per == 1;
   while (rows_left<S::T>(at.on())) {
     const bool on = at.on();
     const int row = on ? at.row : 0, group = on ? at.group : 0;
-    if (group != held) {
+    uint4 gate_raw, scale_raw;
+    const bool other = group != held;
+    if (other || weighted) {
       held = group;
       if (a.h) request_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col);
       request_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col);
     }
     ring_ready<TPR, CL, VEC>(sub);
+    if (other) {
+      float2 x[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        branch[i] = alpha;
+        norm[i] = both(1.f);
+      }
+      if (a.h && a.gate) {
+        take_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) branch[i] = each_mul2(branch[i], x[i]);
+      }
+      if (FULL && a.wp) {
+        load_vector(a.wp, a.tw, 0, col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) branch[i] = each_mul2(branch[i], x[i]);
+      }
+      if (!weighted && a.scale) {
+        take_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) norm[i] = each_add2(norm[i], x[i]);
+      }
+      if (a.w) {
+        load_vector(a.w, a.tw, 0, col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) norm[i] = each_mul2(norm[i], x[i]);
+      }
+    }
     const uint4* mine = ring + stage * G::kStage;
     const float4* stats = reinterpret_cast<const float4*>(mine + G::kStats + threadIdx.x / kWarp * 2);
     float2 v[P], q[P], dx[P], x[P];
@@ -632,22 +665,8 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
         shift_row(q, st.x, col, VEC);
         scale_row(q, st.y, st.z, col, VEC);
       }
-      float2 k[P];                                              // alpha gate wp (of a kept column)
 #pragma unroll
-      for (int i = 0; i < P; ++i) k[i] = q[i];
-      if (FULL && a.wp) {
-        load_vector(a.wp, a.tw, 0, col, x);
-#pragma unroll
-        for (int i = 0; i < P; ++i) k[i] = each_mul2(k[i], x[i]);
-      }
-      if (a.gate) {
-        take_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
-#pragma unroll
-        for (int i = 0; i < P; ++i) add_branch(v[i], each_mul2(alpha, x[i]), k[i], drops, kept, i);
-      } else {
-#pragma unroll
-        for (int i = 0; i < P; ++i) add_branch(v[i], alpha, k[i], drops, kept, i);
-      }
+      for (int i = 0; i < P; ++i) add_branch(v[i], branch[i], q[i], drops, kept, i);
     }
     const float4 st = stats[0];
     shift_row(v, st.x, col, VEC);
@@ -658,7 +677,6 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
       for (int i = 0; i < P; ++i) v[i] = q[i] = dx[i] = both(0.f);
     }
     // A and B, and dn (1 + scale) w
-    const bool weighted = a.mode == kSumWeighted, own_rows = weighted && a.per == 1;
     if (own_rows && a.dshift) store_vector(a.dshift, a.tc, cond_at(row, a.lddshift), col, on, dx);
     if (own_rows && a.dscale) {
       float2 o[P];
@@ -684,16 +702,15 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
       }
     };
     if (!weighted) add_ab();
-    if (a.scale) {
+    if (weighted && a.scale) {
       take_vector(scale_raw, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) dx[i] = each_fma2(dx[i], x[i], dx[i]);
     }
     if (weighted) add_ab();
-    if (a.w) {
-      load_vector(a.w, a.tw, 0, col, x);
+    if (a.w || (!weighted && a.scale)) {
 #pragma unroll
-      for (int i = 0; i < P; ++i) dx[i] = each_mul2(dx[i], x[i]);
+      for (int i = 0; i < P; ++i) dx[i] = each_mul2(dx[i], norm[i]);
     }
     float c[2];
     pair_sums(dx, v, c);
@@ -712,16 +729,15 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     for (int i = 0; i < P; ++i) g[i] = each_fma2(both(st.z), each_fma2(c2, v[i], each_add2(dx[i], c1)), g[i]);
     if (a.dr_in) store_row(row_of<TR>(a.dr_in, row, a.lddr_in), col, on, g);
     if (a.h) {
-      // alpha D g; its product with post(h) (or h) is the row's C
+      // D g; alpha times its product with post(h) (or h) is the row's C
+      if (drops) {
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        g[i] = each_mul2(alpha, g[i]);
-        if (drops) g[i] = select_kept(g[i], kept, i);
+        for (int i = 0; i < P; ++i) g[i] = select_kept(g[i], kept, i);
       }
       if (own_rows && a.dgate) {
         float2 o[P];
 #pragma unroll
-        for (int i = 0; i < P; ++i) o[i] = each_mul2(g[i], q[i]);
+        for (int i = 0; i < P; ++i) o[i] = each_mul2(alpha, each_mul2(g[i], q[i]));
         if (FULL && a.wp) {
           load_vector(a.wp, a.tw, 0, col, x);
 #pragma unroll
@@ -729,24 +745,18 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
         }
         store_vector(a.dgate, a.tc, cond_at(row, a.lddgate), col, on, o);
       }
-      const auto add_c = [&]() {
-#pragma unroll
-        for (int i = 0; i < P; ++i) sq[i] = S::T < 32 && !on ? sq[i] : each_fma2(g[i], q[i], sq[i]);
-      };
-      if (!weighted) add_c();
-      if (a.gate) {
+      if (weighted && a.gate) {
         take_vector(gate_raw, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
 #pragma unroll
-        for (int i = 0; i < P; ++i) g[i] = each_mul2(g[i], x[i]);
-      }
-      if (weighted) add_c();
-      if (a.dh) {
-        if (FULL && a.post) {
-          if (FULL && a.wp) {
-            load_vector(a.wp, a.tw, 0, col, x);
+        for (int i = 0; i < P; ++i) sq[i] = S::T < 32 && !on ? sq[i] : each_fma2(each_mul2(g[i], x[i]), q[i], sq[i]);
+      } else {
 #pragma unroll
-            for (int i = 0; i < P; ++i) g[i] = each_mul2(g[i], x[i]);
-          }
+        for (int i = 0; i < P; ++i) sq[i] = S::T < 32 && !on ? sq[i] : each_fma2(g[i], q[i], sq[i]);
+      }
+      if (a.dh) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) g[i] = each_mul2(branch[i], g[i]);
+        if (FULL && a.post) {
           if (!VEC) {                                           // (beyond d, g holds the mean that it took off)
 #pragma unroll
             for (int e = 0; e < kBlock; ++e)
@@ -767,6 +777,8 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     // a group's rows, or this worker's of them, are done: its sums are the group's, or a part of them
     if (a.mode == kSumGroups && on && (at.left == 1 || !at.on())) {
       const bool from_here = row - (a.per - at.left) >= begin, whole = from_here && at.left == 1;
+#pragma unroll
+      for (int i = 0; i < P; ++i) sq[i] = each_mul2(alpha, sq[i]);
       float* total = a.part + (size_t)worker * 3 * d;
       float2 f[P], k[P];
 #pragma unroll
@@ -820,6 +832,8 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
     float* total = a.part + (size_t)worker * 3 * d;
     store_typed_vector(total, col, true, sa);
     store_typed_vector(total + d, col, true, sb);
+#pragma unroll
+    for (int i = 0; i < P; ++i) sq[i] = each_mul2(alpha, sq[i]);
     store_typed_vector(total + 2 * d, col, true, sq);
   }
 }
