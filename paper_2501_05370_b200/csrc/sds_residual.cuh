@@ -24,6 +24,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "sds_device.cuh"
 #include "sds_layers.h"
@@ -427,9 +428,12 @@ template <int T> __device__ __forceinline__ bool rows_left(bool on) { return T <
 // FULL: with post or dropout. Two kernels, as the time of either goes with the length of its code: with vectors of unaligned pieces in the
 // aligned kernels too, these were twice as long and 16384 x 2048 backward took 142 us conditioned (119 without), 177 with all parts (156).
 // A group takes neighbouring rows, which mostly share their row of gate, scale and shift. Rows come through the ring, vectors are requested
-// before the sums that they wait for. 16384 x 2048, float stream and bf16 branch: conditioned 75 us (403 MB, 5.4 TB/s, 82 % of a copy's
-// rate), with post, gate and dropout 90 (two rounds of sums, and the generator's integer products).
-template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
+// before the sums that they wait for.
+// HELD: the products of a group's vectors (alpha gate wp, w (1 + scale), b (1 + scale) + shift) stay in registers while the group lasts, at
+// fewer CTAs of an SM. 16384 x 2048 float stream with post, gate, weights and dropout 81.7 -> 71.6 us, with scale, shift and bias too 88.5 ->
+// 73, 65536 x 512 88.7 -> 74; without vectors 70.4 -> 78.6 (layer norm), every row its own 96 -> 113, bf16 stream 89.7 -> 99.6, clusters 127 -> 164.
+// 16384 x 2048, float stream and bf16 branch: conditioned 75 us (403 MB, 5.4 TB/s, 82 % of a copy's rate).
+template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL, bool HELD>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;
   constexpr int kR = RingRow<TR, TPR, CL, VEC>::kPieces, kStage = kR + RingRow<TH, TPR, CL, VEC>::kPieces;
@@ -460,24 +464,64 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
   for (int s = 0; s < kRingStages - 1; ++s) request(at.row + s, s);
   int stage = 0, held = -1;
   uint4 gate, scale, shift;
+  float2 branch[P], norm[P], off[P];                            // HELD
   while (rows_left<S::T>(at.on())) {
     const bool on = at.on();
     const int row = on ? at.row : 0, group = on ? at.group : 0;
     float2 v[P], q[P], x[P];
-    if (group != held) {                                        // (kept while the group lasts)
+    const bool other = group != held;
+    if (other) {                                                // (kept while the group lasts)
       held = group;
       if (a.h) request_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col);
       request_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col);
       request_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col);
     }
     ring_ready<TPR, CL, VEC>(sub);
+    if (HELD && other) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        branch[i] = alpha;
+        norm[i] = both(1.f);
+        off[i] = both(0.f);
+      }
+      if (a.h && a.gate) {
+        take_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) branch[i] = mul2(branch[i], x[i]);
+      }
+      if (a.wp) {
+        load_vector(a.wp, a.tw, 0, col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) branch[i] = mul2(branch[i], x[i]);
+      }
+      if (a.scale) {
+        take_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) norm[i] = add2(norm[i], x[i]);
+      }
+      if (a.b) {
+        load_vector(a.b, a.tw, 0, col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) off[i] = mul2(norm[i], x[i]);
+      }
+      if (a.shift) {
+        take_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) off[i] = add2(off[i], x[i]);
+      }
+      if (a.w) {
+        load_vector(a.w, a.tw, 0, col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) norm[i] = mul2(norm[i], x[i]);
+      }
+    }
     const uint4* mine = ring + stage * kStage;
     ring_take(mine, row_of<TR>(a.r, row, a.ldr), col, sub, v);
     if (a.h) {
       ring_take(mine + kR, row_of<TH>(a.h, row, a.ldh), col, sub, q);
       if (FULL && a.post) {
         const float4 st = normalise(q, sums, col, inv_d, a.rms, a.eps);
-        if (FULL && a.wp) {
+        if (!HELD && a.wp) {
           load_vector(a.wp, a.tw, 0, col, x);
 #pragma unroll
           for (int i = 0; i < P; ++i) q[i] = mul2(q[i], x[i]);
@@ -486,7 +530,10 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
       }
       Kept kept;
       if (drops) kept = kept_columns(a.drop, dstep, row, col, lane);
-      if (a.gate) {
+      if (HELD) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) add_branch(v[i], branch[i], q[i], drops, kept, i);
+      } else if (a.gate) {
         take_vector(gate, a.gate, a.tc, cond_at(group, a.ldgate), col, x);
 #pragma unroll
         for (int i = 0; i < P; ++i) add_branch(v[i], mul2(alpha, x[i]), q[i], drops, kept, i);
@@ -500,25 +547,30 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(
     // (behind a sum: all threads of the group are done with the row before, whose place this takes)
     request(at.row + kRingStages - 1, stage == 0 ? kRingStages - 1 : stage - 1);
     if (a.stats && t == 0 && on) a.stats[2 * (size_t)row] = st;
-    if (a.w) {
-      load_vector(a.w, a.tw, 0, col, x);
+    if (HELD) {
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = mul2(v[i], x[i]);
-    }
-    if (a.b) {
-      load_vector(a.b, a.tw, 0, col, x);
+      for (int i = 0; i < P; ++i) v[i] = fma2(v[i], norm[i], off[i]);
+    } else {
+      if (a.w) {
+        load_vector(a.w, a.tw, 0, col, x);
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
-    }
-    if (a.scale) {
-      take_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
+        for (int i = 0; i < P; ++i) v[i] = mul2(v[i], x[i]);
+      }
+      if (a.b) {
+        load_vector(a.b, a.tw, 0, col, x);
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = fma2(v[i], x[i], v[i]);
-    }
-    if (a.shift) {
-      take_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col, x);
+        for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
+      }
+      if (a.scale) {
+        take_vector(scale, a.scale, a.tc, cond_at(group, a.ldscale), col, x);
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
+        for (int i = 0; i < P; ++i) v[i] = fma2(v[i], x[i], v[i]);
+      }
+      if (a.shift) {
+        take_vector(shift, a.shift, a.tc, cond_at(group, a.ldshift), col, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i] = add2(v[i], x[i]);
+      }
     }
     store_row(row_of<TH>(a.n, row, a.ldn), col, on, v);
     at.next();
@@ -896,20 +948,20 @@ cudaError_t row_launch(K kernel, dim3 grid, int threads, int smem, int cluster, 
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
+template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL, bool HELD>
 cudaError_t residual_fwd_k(const ResidualNormArgs& a, cudaStream_t st) {
   using S = ResidualShape<TPR, CL>;
   constexpr int smem = kRingStages * (RingRow<TR, TPR, CL, VEC>::kPieces + RingRow<TH, TPR, CL, VEC>::kPieces) * 16;
   static std::atomic<int> cache[kRowDevices];
   int resident = 0;
-  const cudaError_t e = row_resident(k_residual_norm<TR, TH, TPR, CL, VEC, FULL>, cache, S::kCta, smem, CL, &resident);
+  const cudaError_t e = row_resident(k_residual_norm<TR, TH, TPR, CL, VEC, FULL, HELD>, cache, S::kCta, smem, CL, &resident);
   if (e != cudaSuccess) return e;
   ResidualNormArgs g = a;
   const int64_t most = (int64_t)resident * S::kRows;
   g.share = (int)((a.rows + most - 1) / most);
   g.workers = (a.rows + g.share - 1) / g.share;
   const int grid = (g.workers + S::kRows - 1) / S::kRows;
-  return row_launch(k_residual_norm<TR, TH, TPR, CL, VEC, FULL>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
+  return row_launch(k_residual_norm<TR, TH, TPR, CL, VEC, FULL, HELD>, dim3((unsigned)(grid * CL)), S::kCta, smem, CL, st, g);
 }
 
 template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
@@ -938,7 +990,12 @@ template <class TR, class TH, int TPR, int CL, bool VEC>
 cudaError_t residual_t(ResidualNormArgs& a, bool backward, cudaStream_t st) {
   const bool full = a.post || a.drop.threshold != 0;
   if (backward) return full ? residual_bwd_k<TR, TH, TPR, CL, VEC, true>(a, st) : residual_bwd_k<TR, TH, TPR, CL, VEC, false>(a, st);
-  return full ? residual_fwd_k<TR, TH, TPR, CL, VEC, true>(a, st) : residual_fwd_k<TR, TH, TPR, CL, VEC, false>(a, st);
+  // (see HELD)
+  if constexpr (VEC && CL == 1 && std::is_same<TR, float>::value) {
+    const int vectors = (a.gate != nullptr) + (a.wp != nullptr) + (a.w != nullptr) + (a.b != nullptr) + (a.scale != nullptr) + (a.shift != nullptr);
+    if (full && a.h && vectors >= 2 && a.per >= 8) return residual_fwd_k<TR, TH, TPR, CL, VEC, true, true>(a, st);
+  }
+  return full ? residual_fwd_k<TR, TH, TPR, CL, VEC, true, false>(a, st) : residual_fwd_k<TR, TH, TPR, CL, VEC, false, false>(a, st);
 }
 template <class TR, class TH, int TPR, int CL>
 cudaError_t residual_t(ResidualNormArgs& a, bool vec, bool backward, cudaStream_t st) {
