@@ -206,6 +206,7 @@ struct TableArgs {
   int64_t lddy, ldz;
   int tdy, rows, n, steps, f16;
   int slice;                                      // list entries of a warp of k_table_sum: 32 (one in each lane) at most
+  int whole_out;                                  // rows of dtable are whole 16-byte pieces
 };
 
 constexpr int kListThreads = 512, kListWarps = kListThreads / 32;
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) 
   const int total = a.rows, i0 = (int)min((int64_t)total, sl * a.slice), count = min(a.slice, total - i0);   // (0: behind the last row)
   start_behind_prior_kernel();
   const int c0 = strip * 256 + lane * 8;
-  const bool live = c0 < a.n, whole_out = a.n % 8 == 0;
+  const bool live = c0 < a.n;
   const int my_row = lane < count ? a.list[i0 + lane] : 0, my_step = lane < count ? a.list_step[i0 + lane] : -1;
   const int step_before = i0 > 0 ? a.list_step[i0 - 1] : -1, step_after = i0 + count < total ? a.list_step[i0 + count] : -1;
   float sum[8] = {}, all[8] = {};
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) 
     if (s == a.steps || !live) {                  // outside the table
     } else if (whole) {
       uint16_t* out = a.dtable + (size_t)s * a.n + c0;
-      if (whole_out) {
+      if (a.whole_out) {
         *reinterpret_cast<uint4*>(out) = make_uint4(pack16(sum[0], sum[1], a.f16), pack16(sum[2], sum[3], a.f16),
                                                     pack16(sum[4], sum[5], a.f16), pack16(sum[6], sum[7], a.f16));
       } else {
@@ -599,6 +600,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
     t.dtable = static_cast<uint16_t*>(a.dtable);
     t.rows = a.rows; t.n = a.n; t.steps = a.steps; t.f16 = a.f16;
     t.slice = table_slice(a.rows, a.n);
+    t.whole_out = a.n % 8 == 0 && whole(a.dtable, a.n, 2);
     if ((e = launch_table(t, whole_dy, st)) != cudaSuccess) return e;
     db_parts = a.db ? table_parts(a.rows, a.n) : 0;
   } else if (to_dz || a.db) {
