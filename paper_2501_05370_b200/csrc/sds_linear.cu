@@ -402,30 +402,47 @@ double tiles_time(int64_t small, int64_t wide, int nkb) {
   return 7.5 + (double)((wide + 73) / 74) * nkb * 0.27;
 }
 
-// The form of a product of `rows` tokens and N output columns: 0 for tiles, else the few-row form's CTAs along K. Up to 64 tokens half
-// a tile of rows would be empty: always the few-row form. Above, the shorter estimate: a step of K takes the few-row form 0.27 us while
-// each CTA has an SM of its own (three stages of its half of the SM's memory are in flight), 0.39 and a later start where two share one;
-// clusters of eight fill no more than 96 SMs singly. 256 x 2048 x 2048: tiles 10.0 us, four CTAs along K 8.8, eight 12.4;
+// The form of a product of `rows` tokens and N output columns: the few-row form's CTAs along K and tokens of a block, or tiles (splits = 0).
+// Up to 64 tokens half a tile of rows would be empty: always the few-row form. Above, the shorter estimate: a step of K takes the few-row
+// form 0.27 us while each CTA has an SM of its own (three stages of its half of the SM's memory are in flight), 0.39 and a later start where
+// two share one; clusters of eight fill no more than 96 SMs singly. 256 x 2048 x 2048: tiles 10.0 us, four CTAs along K 8.8, eight 12.4;
 // 512 x 1024 x 4096 tiles 8.2, one CTA 13.0; 256 x 8192 x 640 tiles 23.5, eight 11.2; 512 x 8192 x 2048 24.3, two 24.6, four 22.4.
-int linear_form(int64_t rows, int N, int nkb) {
-  const int64_t tiles = (N + 127) / 128, tok = (rows + 127) / 128;
-  if (rows <= 64) return split_count((int)rows, (int)tiles, nkb);
-  if (tok > 65535) return 0;                      // (blocks of tokens are the grid's second dimension)
-  double least = tiles_time(tok * tiles, tiles_of(rows, N, 256, 256), nkb);
-  int best = 0;
-  for (int s = 1; s <= 8; s *= 2) {
-    if (s > 1 && nkb / s < 4) break;
-    const int64_t ctas = tiles * tok * s;
-    const int len = (nkb + s - 1) / s;
-    const double time = ctas > (s == 8 ? 96 : 148) ? 9.5 + (double)((ctas + 295) / 296) * len * 0.39 : 6.5 + len * 0.27;
-    if (time < least) { least = time; best = s; }
+// `floats`: a float result, whose sums may not be longer than a CTA's accumulators take (kFewRowSteps each): more CTAs along K, or smaller
+// blocks of tokens, which have more accumulators (128 x 65536 x 512: blocks of 32 48 us,
+// tiles 238), or tiles.
+struct LinearForm { int splits, tokens; };
+LinearForm linear_form(int64_t rows, int N, int nkb, bool floats = false) {
+  const int64_t tiles = (N + 127) / 128, small = (rows + 127) / 128 * tiles;
+  const auto fits = [&](int s, int bn) { return !floats || (nkb + s - 1) / s <= split_accumulators(bn, kLinear) * kFewRowSteps; };
+  if (rows <= 64) {
+    for (int bn = split_tokens((int)rows); bn >= 16; bn /= 2) {
+      int s = split_count((int)rows, (int)tiles, nkb);
+      while (s < 8 && !fits(s, bn)) s *= 2;
+      if (fits(s, bn)) return {s, bn};
+    }
+    return {0, 0};
+  }
+  double least = tiles_time(small, tiles_of(rows, N, 256, 256), nkb);
+  LinearForm best{0, 0};
+  for (int bn = 128; bn >= 16; bn /= 2) {
+    const int64_t tok = (rows + bn - 1) / bn;
+    if (tok > 65535) break;                       // (blocks of tokens are the grid's second dimension)
+    for (int s = 1; s <= 8; s *= 2) {
+      if (s > 1 && nkb / s < 4) break;
+      if (!fits(s, bn)) continue;
+      const int64_t ctas = tiles * tok * s;
+      const int len = (nkb + s - 1) / s;
+      const double time = ctas > (s == 8 ? 96 : 148) ? 9.5 + (double)((ctas + 295) / 296) * len * 0.39 : 6.5 + len * 0.27;
+      if (time < least) { least = time; best = {s, bn}; }
+    }
+    if (fits(8, bn)) break;                       // (smaller blocks read the weights more often)
   }
   return best;
 }
 
 // Parts into which dW's contraction over the rows is cut (see gradient_parts of the feed-forward block).
 int linear_parts(int64_t rows, int32_t k, int32_t n) {
-  const bool dx_tiles = linear_form(rows, k, steps(n)) == 0;
+  const bool dx_tiles = linear_form(rows, k, steps(n)).splits == 0;
   const int kr = steps((int)rows), kx = dx_tiles ? steps(n) : 0;
   const int64_t small = tiles_of(n, k, 128, 128), wide = tiles_of(n, k, 256, 256);
   const int64_t xs = dx_tiles ? tiles_of(rows, k, 128, 128) : 0, xw = dx_tiles ? tiles_of(rows, k, 256, 256) : 0;
@@ -479,11 +496,12 @@ namespace {
 
 template <int EPI>
 cudaError_t forward(const LinearArgs& a, const FfnArgs& f, const LinearEpilogue& e, cudaStream_t st) {
-  if (const int splits = linear_form(a.rows, a.n, steps(a.k))) {
+  const LinearForm form = linear_form(a.rows, a.n, steps(a.k), a.ty == SDS_F32);
+  if (form.splits > 0) {
     SplitSpec s{};
     s.w[0] = {a.w, a.k}; s.t[0] = {a.x, a.ldx};
     s.nseg = 1; s.N = a.n; s.K = a.k; s.out = a.y; s.ldo = a.ldy;
-    return launch_split<EPI>(f, s, nullptr, true, st, &e, splits);
+    return launch_split<EPI>(f, s, nullptr, true, st, &e, form.splits, form.tokens);
   }
   ProductSpec s{};
   s.a[0] = {a.x, a.ldx}; s.b[0] = {a.w, a.k};
@@ -625,12 +643,12 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
   ProductSpec w[2];
   int n = 0;
   bool first = true, beside = false;
-  const int dx_splits = a.dx ? linear_form(a.rows, a.k, steps(a.n)) : 0;
-  if (dx_splits > 0) {
+  const LinearForm dx_form = a.dx ? linear_form(a.rows, a.k, steps(a.n)) : LinearForm{0, 0};
+  if (dx_form.splits > 0) {
     SplitSpec s{};
     s.w[0] = {a.w, a.k}; s.t[0] = dz;
     s.nseg = 1; s.w_mn = true; s.N = a.k; s.K = a.n; s.out = a.dx; s.ldo = a.lddx;
-    if ((e = launch_split<kFfnOut>(f, s, nullptr, first, st, nullptr, dx_splits)) != cudaSuccess) return e;
+    if ((e = launch_split<kFfnOut>(f, s, nullptr, first, st, nullptr, dx_form.splits, dx_form.tokens)) != cudaSuccess) return e;
     first = false;
     beside = true;                                // (dW does not read dx)
   } else if (a.dx) {

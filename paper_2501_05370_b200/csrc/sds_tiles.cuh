@@ -1027,8 +1027,10 @@ struct FfnSplitArgs {
 
 constexpr int kSplitThreads = 256;
 
-// kLinear with a float result: a CTA's steps of K are dealt to up to so many accumulators (see SUMS), added in order behind them
-__host__ __device__ constexpr int split_accumulators(int bn, int epi) { return !is_linear(epi) ? 1 : bn >= 128 ? 2 : 4; }
+// kLinear with a float result: a CTA's steps of K are dealt to up to so many accumulators (see SUMS), added in order behind them: as many
+// as fit half of the tensor memory (two CTAs share an SM). None takes more than kFewRowSteps: no form is chosen that would ask for more.
+__host__ __device__ constexpr int split_accumulators(int bn, int epi) { return is_linear(epi) ? 256 / bn : 1; }
+constexpr int kFewRowSteps = 16;
 template <int BN, int EPI> struct FfnSplit {
   static constexpr int kABytes = kBM * kBK * 2, kBBytes = BN * kBK * 2, kStageBytes = kABytes + kBBytes;
   static constexpr int kFixedBytes = 1024 + 256;
@@ -1037,7 +1039,7 @@ template <int BN, int EPI> struct FfnSplit {
   static constexpr int kStages = (113 * 1024 - kFixedBytes) / kStageBytes;
   static constexpr int kSmemBytes = kStages * kStageBytes + kFixedBytes;
   static constexpr int kAccumulators = split_accumulators(BN, EPI);
-  static constexpr int kTmemCols = BN * kAccumulators < 32 ? 32 : BN * kAccumulators;   // (of 256: two CTAs share an SM)
+  static constexpr int kTmemCols = BN * kAccumulators < 32 ? 32 : BN * kAccumulators;
   static_assert(kStages * kStageBytes >= BN * kBM * 4, "the partial sums fit where the stages were");
 };
 
@@ -1070,7 +1072,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) k_ffn_split(const __grid_con
   const int n0 = (int)(blockIdx.x / nsplit) * TN, tok0 = (int)blockIdx.y * BN;
   const int kb_seg = (g.K + kBK - 1) / kBK, nkb = kb_seg * g.nseg;
   const int kb0 = (int)((int64_t)nkb * rank / nsplit), kb1 = (int)((int64_t)nkb * (rank + 1) / nsplit);
-  // steps of an accumulator (of a float result: kSumSteps where there are accumulators enough)
+  // steps of an accumulator (of a float result: kSumSteps where there are accumulators enough, never more than kFewRowSteps)
   const int per = C::kAccumulators == 1 || g.lin.ty != SDS_F32
                       ? kb1 - kb0 : max(kSumSteps, (kb1 - kb0 + C::kAccumulators - 1) / C::kAccumulators);
 
@@ -1588,9 +1590,9 @@ bool prefer_split(int rows, int N, int nkb) {
 
 template <int EPI>
 cudaError_t launch_split(const FfnArgs& a, const SplitSpec& s, float* keep, bool first, cudaStream_t st,
-                         const LinearEpilogue* lin = nullptr, int count = 0) {
+                         const LinearEpilogue* lin = nullptr, int count = 0, int tokens = 0) {
   constexpr int TN = EPI == kFfnGlu ? 64 : 128;
-  const int bn = split_tokens(a.rows);
+  const int bn = tokens > 0 ? tokens : split_tokens(a.rows);
   FfnSplitArgs g;
   g.rows = a.rows; g.N = s.N; g.K = s.K;
   g.nseg = s.nseg; g.w_mn = s.w_mn;
