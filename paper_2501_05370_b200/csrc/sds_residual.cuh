@@ -326,7 +326,7 @@ __device__ __forceinline__ float4 normalise(float2 (&v)[P], GroupSums<TPR, CL>& 
   pair_sums(v, v, q);
   sums(q);
   st.y = q[0] * inv_d;
-  st.z = rsqrtf(fmaf(-st.y, st.y, q[1] * inv_d) + eps);
+  st.z = rsqrtf(fmaxf(fmaf(-st.y, st.y, q[1] * inv_d), 0.f) + eps);   // (of a constant row, the two may differ by their roundings either way)
   scale_row(v, st.y, st.z, col, VEC);
   return st;
 }
