@@ -554,7 +554,7 @@ int sds_dropout(const sds_dropout_spec* spec, const void* x_dev, int64_t ldx, in
  * zeros, zeros): rows / groups consecutive rows share one row of them (rows a multiple of groups; groups = 1: one vector for all,
  * groups = rows: one each). d <= 16384, rows less than
  * 2^31 elements apart (else SDS_EUNSUPPORTED). eps >= 0 and alpha finite. All is held in float and rounded once; n is that of the
- * unrounded out. keep_dev: [rows, 8] floats (keep_bytes) that the backward pass needs, 256-byte aligned (NULL = none will follow).
+ * unrounded out. A dropped element of h adds nothing, whatever it is, here and to the gradients (behind post it is part of its row's norm). keep_dev: [rows, 8] floats (keep_bytes) that the backward pass needs, 256-byte aligned (NULL = none will follow).
  * out_dev may be r_dev and n_dev h_dev (same rows) where no backward pass will need them. */
 #define SDS_NORM_LAYER    0
 #define SDS_NORM_RMS      1

@@ -719,6 +719,10 @@ __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, 
       }
 #pragma unroll
       for (int i = 0; i < P; ++i) add_branch(v[i], branch[i], q[i], drops, kept, i);
+      if (drops && !a.post) {                                   // (0 times what was dropped is not always 0; behind post, all of its row is NaN then)
+#pragma unroll
+        for (int i = 0; i < P; ++i) q[i] = select_kept(q[i], kept, i);
+      }
     }
     const float4 st = stats[0];
     shift_row(v, st.x, col, VEC);

@@ -41,3 +41,27 @@ def test_constant_rows_far_from_zero(d, eps):
             assert torch.equal(out, x) and (n.double().abs() <= bound).all()
         grads = sds.residual_norm_backward(dn, None, r, h, kept, post=post, weight=w)
         assert all(g is None or torch.isfinite(g).all() for g in grads)
+
+
+@pytest.mark.parametrize("tr,th", [(F32, F32), (F32, BF16), (F16, F16)])
+@pytest.mark.parametrize("rows,d,groups", [(24, 40, 1), (24, 40, 24), (24, 40, 4), (300, 1000, 1), (300, 1000, 300), (300, 1000, 6), (40, 131, 8), (40, 131, 40),
+                                           (20, 6000, 5), (20, 16384, 1)])
+@pytest.mark.parametrize("cond", ["gate", "gate scale shift", ""])
+def test_what_is_dropped_may_be_anything(rows, d, groups, cond, tr, th):
+    """A dropped element of h adds nothing, whatever it is: every result and gradient is that of zeros in its place."""
+    g = gen(rows + d)
+    r, h = g(rows, d).to(tr), g(rows, d).to(th)
+    kw = {name: (0.5 * g(groups, d)).to(th) for name in cond.split()}
+    kw.update(weight=1.0 + 0.1 * g(d), p=0.3, seed=11, step=2)
+    dropped = sds.dropout(torch.ones(rows, d, device="cuda"), 0.3, 11, 2) == 0
+    zeros, bad = h.clone(), h.clone()
+    zeros[dropped] = 0.0
+    values = torch.tensor([float("inf"), float("-inf"), float("nan")], device="cuda", dtype=th)
+    bad[dropped] = values[torch.arange(int(dropped.sum()), device="cuda") % 3]
+    dn, dr = g(rows, d).to(th), g(rows, d).to(tr)
+    results = []
+    for v in (zeros, bad):
+        out, n, kept = sds.residual_norm(r, v, keep=True, **kw)
+        results.append((out, n) + sds.residual_norm_backward(dn, dr, r, v, kept, **kw))
+    for i, (a, b) in enumerate(zip(*results)):
+        assert a is None and b is None or torch.equal(a, b) and torch.isfinite(b).all(), i
