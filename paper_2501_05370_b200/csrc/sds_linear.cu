@@ -2,6 +2,7 @@
 //
 //   forward   z = x W^T + b + table[step], y = act(z) + residual          (x [rows, k], W [n, k])
 //   backward  dz = dy act'(z), dx = dz W, dW = dz^T x, db = sum_rows dz, dtable[s] = sum_{rows with step s} dz
+//   (a row whose step is outside the table is NaN forward, and zeros in dz)
 //
 // The products are those of sds_tiles.cuh: persistent tiles for batches, weights split over clusters for few rows. Bias, table
 // rows, activation and residual are applied to the accumulator, before its one rounding, so y is written once and z never.
@@ -36,8 +37,9 @@ struct DzArgs {
   uint16_t* dz;                                   // [rows, ldz] of the operands' type, NULL = not wanted
   float* part;                                    // [gridDim.y][n] column sums
   void* db;                                       // NULL = not wanted; where the chunks of rows are one cluster the sums go here at once
+  const int* step;                                // [rows], NULL = no table: rows whose step is outside it count as zeros
   int64_t lddy, ldz;
-  int tdy, tdb, rows, n, f16;
+  int tdy, tdb, rows, n, steps, f16;
   int cluster;                                    // chunks of rows in a cluster (1: the sums go to part, unless there is but one)
 };
 
@@ -101,6 +103,11 @@ __device__ __forceinline__ void dz_values(const DzRow<F32, WHOLE>& r, const A& a
     for (int u = 0; u < 8; ++u) v[u] *= __uint_as_float(f[u]);
   }
 }
+// a row whose step is outside the table: neither its dy nor its act' (NaN) counts
+__device__ __forceinline__ void no_row(float (&v)[8]) {
+#pragma unroll
+  for (int u = 0; u < 8; ++u) v[u] = 0.f;
+}
 template <class A>
 __device__ __forceinline__ void dz_store(const A& a, int64_t row, int c0, const float (&v)[8]) {      // (columns beyond n are padding)
   *reinterpret_cast<uint4*>(a.dz + (size_t)row * a.ldz + c0) =
@@ -120,9 +127,14 @@ __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
   if (c0 < a.n) {
     constexpr int kAhead = 4;
     DzRow<F32, WHOLE> ahead[kAhead];
+    int steps_ahead[kAhead] = {};
+    const auto request = [&](int i, int64_t row) {
+      dz_request(ahead[i], a, row, c0);
+      if (a.step) steps_ahead[i] = a.step[row];
+    };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (first + i * stride < a.rows) dz_request(ahead[i], a, first + i * stride, c0);
+      if (first + i * stride < a.rows) request(i, first + i * stride);
     for (int64_t base = first; base < a.rows; base += kAhead * stride) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
@@ -130,7 +142,8 @@ __global__ void __launch_bounds__(kDzThreads) k_linear_dz(const DzArgs a) {
         if (row >= a.rows) break;
         float v[8];
         dz_values(ahead[i], a, row, c0, v);
-        if (next < a.rows) dz_request(ahead[i], a, next, c0);
+        if (a.step && (steps_ahead[i] < 0 || steps_ahead[i] >= a.steps)) no_row(v);
+        if (next < a.rows) request(i, next);
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum[u] += v[u];
         if (a.dz) dz_store(a, row, c0, v);
@@ -331,6 +344,7 @@ __global__ void __launch_bounds__(kTableThreads) k_table_sum(const TableArgs a) 
       if (live) {
         float v[8];
         dz_values(ahead[k], a, row, c0, v);
+        if (s == a.steps) no_row(v);
         if (i + k + kAhead < count) dz_request(ahead[k], a, next, c0);
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum[u] += v[u];
@@ -602,8 +616,8 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
   const size_t sy = a.ty == SDS_F32 ? 4 : 2;
   const bool whole_dy = a.n % 8 == 0 && whole(a.dy, a.lddy, sy);
   const bool products = a.dx || a.dw;
-  // without an activation dy itself is the operand, where its rows are ones that the tensor maps take
-  const bool direct = !factor && a.ty != SDS_F32 && whole(a.dy, a.lddy, 2);
+  // without an activation dy itself is the operand, where its rows are ones that the tensor maps take (and none may have to be left out)
+  const bool direct = !factor && !a.table && a.ty != SDS_F32 && whole(a.dy, a.lddy, 2);
   uint16_t* to_dz = products && !direct ? reinterpret_cast<uint16_t*>(ws + at.dz) : nullptr;
   float* db_part = reinterpret_cast<float*>(ws + at.db);
   int64_t db_parts = 0;                           // whose sums are still to be added
@@ -626,6 +640,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t st) {
     d.dy = a.dy; d.lddy = a.lddy; d.tdy = a.ty;
     d.factor = factor; d.ldz = ldz; d.f16 = a.f16;
     d.dz = to_dz;
+    d.step = a.table ? a.step : nullptr; d.steps = a.steps;
     d.part = db_part; d.db = a.db; d.tdb = a.tbias;
     d.rows = a.rows; d.n = a.n;
     const int chunks = dz_chunks(a.rows, a.n);

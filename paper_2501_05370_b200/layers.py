@@ -129,7 +129,8 @@ def linear(x, weight, bias=None, activation=None, *, table=None, step=None, resi
 def linear_backward(dy, x, weight, kept, *, bias=None, table=None, step=None, want=(True, True, True, True), workspace=None):
     """sds_linear_backward: (dx, dweight, dbias, dtable) from dy (of the forward output's type) and the forward call's x,
     weight, kept, bias, table and step (of bias and table only size and type count). want: which of the four to compute; None
-    is returned for the others, and for the bias and the table where there was none. The residual's gradient is dy."""
+    is returned for the others, and for the bias and the table where there was none. The residual's gradient is dy. A row whose step is
+    outside the table takes no part: zeros in dx, nothing in the others."""
     return (_native or _ext()).linear_backward(dy, x, weight, kept, bias, table, step, want, workspace)
 
 
