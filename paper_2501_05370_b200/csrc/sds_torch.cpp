@@ -117,9 +117,16 @@ bool has_shape(const at::Tensor& y, const at::Tensor& x, int64_t n) {
   return y.dim() == x.dim() && y.size(-1) == n && y.sizes().slice(0, y.dim() - 1) == x.sizes().slice(0, x.dim() - 1);
 }
 
-int64_t integer(PyObject* o) {
+// what Python says of a number that is none, or too large, is a bad argument here
+[[noreturn]] void bad_number(const char* what) {
+  if (!PyErr_ExceptionMatches(PyExc_TypeError) && !PyErr_ExceptionMatches(PyExc_OverflowError) && !PyErr_ExceptionMatches(PyExc_ValueError))
+    throw PythonError{};
+  PyErr_Clear();
+  throw BadArgument(what);
+}
+int64_t integer(PyObject* o, const char* what) {
   const long long v = PyLong_AsLongLong(o);
-  if (v == -1 && PyErr_Occurred()) throw PythonError{};
+  if (v == -1 && PyErr_Occurred()) bad_number(what);
   return v;
 }
 
@@ -404,7 +411,7 @@ int64_t kept_size(const sds_linear_sizes& sizes) { return sizes.keep_bytes ? (in
 PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> PyObject* {
     const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "weight");
-    const Linear s = linear_of(x, w, a[2], a[4], a[5], (int)integer(a[3]));
+    const Linear s = linear_of(x, w, a[2], a[4], a[5], (int)integer(a[3], "activation must be a number"));
     const at::ScalarType yt = dtype_or(a[7], x.scalar_type());
     const int ty = type_code(yt);
     const void* residual = nullptr;
@@ -474,33 +481,31 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // dropout
 // ---------------------------------------------------------------------------------------------
 
-double real(PyObject* o) {
+double real(PyObject* o, const char* what) {
   const double v = PyFloat_AsDouble(o);
-  if (v == -1.0 && PyErr_Occurred()) throw PythonError{};
+  if (v == -1.0 && PyErr_Occurred()) bad_number(what);
   return v;
 }
 
 // a[0..3] = p, seed, step (a number, or an int32 tensor of one element on x's device), row0
 sds_dropout_spec dropout_of(PyObject* const* a, const at::Tensor& x) {
   sds_dropout_spec s{};
-  s.p = real(a[0]);
-  s.seed = PyLong_AsUnsignedLongLong(a[1]);
-  if (s.seed == (uint64_t)-1 && PyErr_Occurred()) {
-    if (PyErr_ExceptionMatches(PyExc_TypeError)) throw PythonError{};
-    PyErr_Clear();
-    throw BadArgument("seed must be in [0, 2^64)");
-  }
+  s.p = real(a[0], "p must be a number");
+  PyObject* seed = PyNumber_Index(a[1]);
+  s.seed = seed ? PyLong_AsUnsignedLongLong(seed) : (uint64_t)-1;
+  Py_XDECREF(seed);
+  if (s.seed == (uint64_t)-1 && PyErr_Occurred()) bad_number("seed must be an integer in [0, 2^64)");
   if (THPVariable_Check(a[2])) {
     const at::Tensor& t = THPVariable_Unpack(a[2]);
     require(t.scalar_type() == at::kInt && t.numel() == 1 && t.device() == x.device(),
             "step must be a number or an int32 tensor of one element on x's device");
     s.step_dev = t.data_ptr<int32_t>();
   } else {
-    const int64_t step = integer(a[2]);
+    const int64_t step = integer(a[2], "step must be in [0, 2^31), or an int32 tensor of one element on x's device");
     require(step >= 0 && step <= INT32_MAX, "step must be in [0, 2^31)");
     s.step = (int32_t)step;
   }
-  s.row0 = integer(a[3]);
+  s.row0 = integer(a[3], "row0 must be an integer below 2^56");
   require(s.p >= 0.0 && s.p <= 1.0, "p must be in [0, 1]");
   require(s.row0 >= 0, "row0 must not be negative");
   return s;
@@ -597,8 +602,8 @@ ResidualNorm residual_norm_of(const at::Tensor& r, PyObject* h, at::ScalarType n
   require(s.h || (!s.cond[0] && !op.post), "gate and post need h");
   op.cond_dtype = type_code(s.c_type);
   op.kind = truth(a[7]) ? SDS_NORM_RMS : SDS_NORM_LAYER;
-  op.alpha = (float)real(a[8]);
-  op.eps = (float)real(a[9]);
+  op.alpha = (float)real(a[8], "alpha must be a number");
+  op.eps = (float)real(a[9], "eps must be a number");
   op.drop = dropout_of(a + 10, r);
   require(s.h || op.drop.p == 0.0, "dropout needs h");
   return s;
