@@ -510,7 +510,7 @@ int sds_linear(const sds_linear_layer* layer, const void* x_dev, int64_t ldx, co
  *   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  dbias = sum_rows dz,  dtable[s] = sum of dz over the rows with step s
  * (that of the residual is dy itself). dx_dev [rows, k] (rows lddx apart, lddx a multiple of 8), dw_dev [n, k], both 16-byte
  * aligned, and dtable_dev [steps, n] of dtype, dbias_dev [n] of bias_dtype; any may be NULL. dz is rounded to dtype as an operand of
- * the two products; the sums take it unrounded, are held in float and added in a fixed order: same bits on every run. Rows
+ * the two products (whatever y_dtype is: with SDS_F16 a dz beyond 65504 becomes infinite there, and one below 2^-25 zero); the sums take it unrounded, are held in float and added in a fixed order: same bits on every run. Rows
  * whose step is outside the table take no part, whatever dy holds there: their rows of dx are zeros, and they add nothing to the other
  * gradients. For dtable, rows * steps is at most 2^36 (else SDS_EUNSUPPORTED). With rows = 0 the parameters' gradients are zeros. */
 int sds_linear_backward(const sds_linear_layer* layer, const void* dy_dev, int64_t lddy, int32_t y_dtype,

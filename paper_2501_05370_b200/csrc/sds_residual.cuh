@@ -432,6 +432,9 @@ template <int T> __device__ __forceinline__ bool rows_left(bool on) { return T <
 // HELD: the products of a group's vectors (alpha gate wp, w (1 + scale), b (1 + scale) + shift) stay in registers while the group lasts, at
 // fewer CTAs of an SM. 16384 x 2048 float stream with post, gate, weights and dropout 81.7 -> 71.6 us, with scale, shift and bias too 88.5 ->
 // 73, 65536 x 512 88.7 -> 74; without vectors 70.4 -> 78.6 (layer norm), every row its own 96 -> 113, bf16 stream 89.7 -> 99.6, clusters 127 -> 164.
+// From eight rows a group on (16384 x 2048 with gate and weight, not held and held: 2 rows 86 and 92, 4 82 and 85, 6 82 and 82, 8 82 and 80, 16 82
+// and 79; with gate, scale, shift and weight 94 and 99, 88 and 88, 88 and 84, 86 and 82, 85 and 80; 65536 x 512 107 and 107, 98 and 92, 94 and 88,
+// 92 and 84, 92 and 82).
 // 16384 x 2048, float stream and bf16 branch: conditioned 75 us (403 MB, 5.4 TB/s, 82 % of a copy's rate).
 template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL, bool HELD>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta) k_residual_norm(const ResidualNormArgs a) {
@@ -612,7 +615,8 @@ __device__ __forceinline__ void add_total(float* total, const float2 (&v)[P], co
 // 512 threads of 128 registers an SM: a row's values, the sums over rows and the products of a group's vectors are in registers, and issue is
 // what bounds the parts beside the plain norm: with gate, post weight and weight read and multiplied row by row, 16384 x 2048 with all parts
 // took 145 us (764 instructions of a warp for a row, 64 % of the issue slots), now 125 (604 MB, 4.8 TB/s; a bf16 stream 144 -> 117);
-// conditioned, float stream and bf16 branch, 114 (5.3 TB/s).
+// conditioned, float stream and bf16 branch, 114 (5.3 TB/s). Held products cost where there is but one vector: a float stream with a weight
+// alone 102 -> 106.
 template <class TR, class TH, int TPR, int CL, bool VEC, bool FULL>
 __global__ void __launch_bounds__(ResidualShape<TPR, CL>::kCta, ResidualBwd<TR, TH, TPR, CL, VEC>::kMinCtas) k_residual_norm_bwd(const ResidualNormArgs a) {
   using S = ResidualShape<TPR, CL>;

@@ -90,8 +90,8 @@ struct FfnTileArgs {
 // the epilogues' arithmetic
 // ---------------------------------------------------------------------------------------------
 
-// a = act(g), da = act'(g). The fast exponential and division are accurate to a few units of the 24-bit
-// significand, far inside the 16-bit operands' rounding.
+// a = act(g), da = act'(g). The fast exponential and division are accurate to a few units of the 24-bit significand per unit of the
+// exponent: far inside the rounding of a 16-bit result; a float one (or a kept derivative) is within 2^-18 of itself up to |g| = 30.
 // GELU: with z = |g| / sqrt(2), Phi(-|g|) = erfcx(z) exp(-z^2) / 2, and the exponential is that of the density. The scaled
 // function is smooth in t = 1 / (1 + 0.33 z): t times a polynomial of degree 7, fitted (least squares, reweighted towards the
 // smallest largest relative error) to 8.2e-8 for z up to 9.6. In floats Phi(-|g|) is off by at most 6e-7 of
@@ -490,10 +490,11 @@ __device__ __forceinline__ int tile_index(const FfnTileArgs& g, int worker, int 
 // SiLU 105, GELU 110, with a float residual 124.
 // CUT: products whose K is cut (FfnProduct::parts); its own kernel, as the others lose up to 5 % to the arithmetic.
 // EW: epilogue warps, four, eight (two for each quarter of the lanes, half of the columns each) or sixteen.
-// SUMS: the tensor cores add to their accumulator without rounding to nearest, so a long sum comes out short by about K / 16 times 2^-25 of
-// itself (K = 8192: 6.4e-6, where a float's own rounding is 3e-8). Where the result is a float, every kSumSteps steps of K
+// SUMS: the tensor cores add to their accumulator without rounding to nearest, so a long sum comes out short. Measured, of itself: terms of
+// either sign lose 0.25 to 0.3 times 2^-24 an addition of 16 products (60 additions 0.9e-6 to 1.0e-6, 384 6.7e-6), terms of one sign 0.5 at 60
+// (2.0e-6) and 1.0 at 384 (2.4e-5); a float's own rounding is 6e-8 at most. Where the result is a float, every kSumSteps steps of K
 // have an accumulator of their own, and the epilogue's warps add these in registers (sixteen warps hold a tile's), while the next is filled:
-// a result is then short by at most a millionth. 16384 x 8192 x 2048 with a float residual, at length: 12 steps 593 us, 15 572, 24 546, 64 522
+// a result is then short by one or two millionths, however long the sum. 16384 x 8192 x 2048 with a float residual, at length: 12 steps 593 us, 15 572, 24 546, 64 522
 // (before the feeding lanes were elected; now 15 steps 431 in short runs, 502 at length, against 424 in one accumulator).
 constexpr int kSumSteps = 15;
 template <int BN, int EPI, bool PAIR, bool MN, bool CUT, int EW, bool SUMS>
