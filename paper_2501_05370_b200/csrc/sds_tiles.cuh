@@ -91,7 +91,7 @@ struct FfnTileArgs {
 // ---------------------------------------------------------------------------------------------
 
 // a = act(g), da = act'(g). The fast exponential and division are accurate to a few units of the 24-bit significand per unit of the
-// exponent: far inside the rounding of a 16-bit result; a float one (or a kept derivative) is within 2^-18 of itself up to |g| = 30.
+// exponent: far inside the rounding of a 16-bit result; a float one is within 2^-18 of itself up to |g| = 30.
 // GELU: with z = |g| / sqrt(2), Phi(-|g|) = erfcx(z) exp(-z^2) / 2, and the exponential is that of the density. The scaled
 // function is smooth in t = 1 / (1 + 0.33 z): t times a polynomial of degree 7, fitted (least squares, reweighted towards the
 // smallest largest relative error) to 8.2e-8 for z up to 9.6. In floats Phi(-|g|) is off by at most 6e-7 of
