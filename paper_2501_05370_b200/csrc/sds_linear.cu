@@ -422,8 +422,7 @@ double tiles_time(int64_t small, int64_t wide, int nkb) {
 // two share one; clusters of eight fill no more than 96 SMs singly. 256 x 2048 x 2048: tiles 10.0 us, four CTAs along K 8.8, eight 12.4;
 // 512 x 1024 x 4096 tiles 8.2, one CTA 13.0; 256 x 8192 x 640 tiles 23.5, eight 11.2; 512 x 8192 x 2048 24.3, two 24.6, four 22.4.
 // `floats`: a float result, whose sums may not be longer than a CTA's accumulators take (kFewRowSteps each): more CTAs along K, or smaller
-// blocks of tokens, which have more accumulators (128 x 65536 x 512: blocks of 32 48 us,
-// tiles 238), or tiles.
+// blocks of tokens, which have more accumulators (128 x 65536 x 512: 48 us in blocks of 32, 238 as tiles), or tiles.
 struct LinearForm { int splits, tokens; };
 LinearForm linear_form(int64_t rows, int N, int nkb, bool floats = false) {
   const int64_t tiles = (N + 127) / 128, small = (rows + 127) / 128 * tiles;
